@@ -306,6 +306,136 @@ int soap_kl_factors_f32(int64_t m, int64_t n, const float *G, float *L, float *R
                         const float *Q_L, const float *Q_R, float beta_kron, float eps,
                         float *lam_L, float *lam_R, void *workspace, size_t workspace_bytes,
                         hipStream_t stream);
+/* ---- operators of the layer around an expert bank ----
+ * What a trainer runs next to soap_step_batched: the layer norm and the router
+ * in front of a bank of experts, and the experts' products in microscaled 4-bit
+ * floating point, up to the [batch][m][n] gradient that the batched steps read.
+ * Streams, errors and ownership as above, with these differences:
+ *  - Activations, logits and their gradients are fp32 or bfloat16 (soap_dtype),
+ *    with a row stride ld* in elements (>= the number of columns), and need only
+ *    the alignment of an element: 16-byte aligned rows are read and written 16
+ *    bytes at a time, others an element at a time.  Parameters, their gradients,
+ *    statistics, gates and losses are fp32, indices int32.  Other buffers are
+ *    16-byte aligned where they are the library's own formats (packed matrices,
+ *    workspaces) and element-aligned otherwise.
+ *  - The token axis may be empty (rows = 0, tokens = 0: sums and counts are then
+ *    zero) and goes up to SOAP_MAX_ROWS.
+ *  - No output may overlap an input or another output; the range of a strided
+ *    matrix is that from its first to its last element.
+ *  - Results do not vary between runs: no floating-point sum depends on the order
+ *    of atomics. */
+typedef enum { SOAP_F32 = 0, SOAP_BF16 = 1 } soap_dtype;
+#define SOAP_MAX_ROWS (1 << 24)
+
+/* Layer norm of each row of x (rows x cols, 1 <= cols <= SOAP_MAX_DIM):
+ *   mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
+ *   y = weight (x - mean) rstd + bias
+ * weight and bias hold cols floats (NULL: ones, zeros); mean and rstd receive
+ * rows floats for the backward pass (NULL: not wanted); eps is finite and > 0.
+ * The backward pass gives, with h = (x - mean) rstd and g = weight dy,
+ *   dx = rstd (g - mean(g) - h mean(g h)),  dweight = sum_rows dy h,  dbias = sum_rows dy
+ * (each NULL where it is not wanted, dx too); the workspace holds the partial
+ * sums of dweight and dbias (it may be NULL if neither is wanted). */
+int soap_layer_norm_forward(int64_t rows, int64_t cols, int dtype, const void *x, int64_t ldx,
+                            const float *weight, const float *bias, float eps, void *y, int64_t ldy,
+                            float *mean, float *rstd, hipStream_t stream);
+size_t soap_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+int soap_layer_norm_backward(int64_t rows, int64_t cols, int dtype, const void *dy, int64_t lddy,
+                             const void *x, int64_t ldx, const float *weight, const float *mean,
+                             const float *rstd, void *dx, int64_t lddx, float *dweight, float *dbias,
+                             void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Router of `tokens` rows of `experts` logits (1 .. SOAP_ROUTER_MAX_EXPERTS).
+ * A token routes unless token_mask (tokens bytes, NULL: none) is 0 for it or it
+ * has no logit above -inf.  It takes its top_k largest logits (1 ..
+ * min(experts, SOAP_ROUTER_MAX_TOP_K)), equal ones by the lowest index, -inf and
+ * NaN never:
+ *   index[t][j]  the j-th largest's expert, or -1 where there is none
+ *   gate[t][j]   p of that expert, p = softmax of the token's logits, divided by
+ *                the sum of the token's chosen p under SOAP_ROUTER_RENORMALIZE
+ *                (0 where index is -1)
+ *   counts[e]    tokens that chose e; counts[experts] = N, the tokens that route
+ *   loss         balance experts sum_e f_e P_e, f_e = counts[e] / (sum of counts),
+ *                P_e = sum over those tokens of p_e / N  (0 if N = 0; may be NULL)
+ * and the dispatch plan (offsets, position and row_token, all or none NULL): the
+ * tokens of expert e have the rows offsets[e] + 0, 1, ... in ascending order, and
+ * offsets[e + 1] is the next multiple of 32 (experts + 1 values); position[t][j]
+ * is the row of index[t][j] (or -1), row_token[r] the token of row r, -1 where it
+ * has none, over all soap_router_rows(tokens, experts, top_k) rows.  tokens top_k
+ * is at most 2^30.  A NaN logit makes its token's gates and the loss NaN.
+ *
+ * The backward pass takes index and counts as the forward pass left them (the
+ * experts of a token distinct) and writes dlogits from the gradient of the gates
+ * (dgate, tokens x top_k, NULL: zero; not read where index is -1) and of the loss
+ * (dloss, one device float, NULL: 1), f_e being constants:
+ *   b_e = dloss balance experts f_e / N
+ *   gates as p:    dlogits = p (d - sum p d), d = b + dgate at the chosen experts
+ *   renormalised:  dlogits = p (b - sum p b) + gate (dgate - sum gate dgate)
+ * and zeros for tokens that do not route. */
+enum { SOAP_ROUTER_RENORMALIZE = 1u << 0 };
+#define SOAP_ROUTER_MAX_EXPERTS 1024
+#define SOAP_ROUTER_MAX_TOP_K 32
+int64_t soap_router_rows(int64_t tokens, int64_t experts, int64_t top_k);
+size_t soap_router_workspace_bytes(int64_t tokens, int64_t experts);
+int soap_router_forward(int64_t tokens, int64_t experts, int64_t top_k, int dtype, const void *logits,
+                        int64_t ld, const uint8_t *token_mask, uint32_t flags, float balance,
+                        int32_t *index, float *gate, int32_t *counts, float *loss, int32_t *offsets,
+                        int32_t *position, int32_t *row_token, void *workspace, size_t workspace_bytes,
+                        hipStream_t stream);
+int soap_router_backward(int64_t tokens, int64_t experts, int64_t top_k, int dtype, const void *logits,
+                         int64_t ld, const uint8_t *token_mask, uint32_t flags, float balance,
+                         const int32_t *index, const int32_t *counts, const float *dgate,
+                         const float *dloss, void *dlogits, int64_t ldd, hipStream_t stream);
+
+/* Microscaled 4-bit floating point (MXFP4).  A packed matrix of `rows` rows of k
+ * values holds, per row, P / 2 bytes of data and P / 32 bytes of scales, P = k
+ * padded to a multiple of 256 (zeros): value i is the lower (i even) or upper
+ * half of byte i / 2, one bit of sign and three that stand for 0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6, times 2^(s - 127), s the scale byte of its block of 32.  Quantising takes
+ * 2^(s - 127) = 2^(floor(log2 max|x|) - 2), at least 2^-127, and rounds x over it to
+ * the nearest value, ties to the even code, 6 at most; a block that holds an
+ * infinity or a NaN gets s = 255, which makes all its values NaN.
+ *
+ * soap_mx4_quantize packs `batch` matrices of rows x cols (matrix b at x + b rows
+ * ldx) along the columns (data, scale: rows x cols), along the rows (data_t,
+ * scale_t: the transposed cols x rows), or both in one pass over x; an unwanted
+ * pair is NULL.  With row_index (batch = 1; `rows` int32), row r is row
+ * row_index[r] of x, or zeros where that is outside [0, x_rows); without it x_rows
+ * is ignored.  Packed matrices of a batch follow each other. */
+size_t soap_mx4_data_bytes(int64_t rows, int64_t k);
+size_t soap_mx4_scale_bytes(int64_t rows, int64_t k);
+int soap_mx4_quantize(int64_t batch, int64_t rows, int64_t cols, int dtype, const void *x, int64_t ldx,
+                      const int32_t *row_index, int64_t x_rows, uint8_t *data, uint8_t *scale,
+                      uint8_t *data_t, uint8_t *scale_t, hipStream_t stream);
+/* The values of a packed matrix, rounded once to a bfloat16 output. */
+int soap_mx4_dequantize(int64_t rows, int64_t k, const uint8_t *data, const uint8_t *scale, int dtype,
+                        void *out, int64_t ldo, hipStream_t stream);
+
+/* Rows of a packed matrix along the columns and the k of one along the rows may be
+ * as many as a dispatch plan has (2^31 - 1); cols, N and K otherwise go up to
+ * SOAP_MAX_ROWS. */
+
+/* Products of packed matrices, C = A B^T summed over k in fp32 and rounded once to
+ * a bfloat16 output.
+ *   soap_mx4_gemm            A M x K, B N x K, C M x N with row stride ldc.
+ *   soap_mx4_gemm_rows       B is `groups` packed N x K matrices; rows offsets[g] ..
+ *                            offsets[g + 1] of C are those of A with B[g], the rows
+ *                            from offsets[groups] on are zeros.
+ *   soap_mx4_gemm_k          C[g] (M x N, groups of them contiguous) sums over the k
+ *                            from offsets[g] to offsets[g + 1] only (zeros if none).
+ * offsets: groups + 1 device int32 (groups <= SOAP_MAX_DIM), 0 first, ascending,
+ * for soap_mx4_gemm_k multiples of 32, as the router's plan has them; values outside
+ * the matrix are taken as its ends. */
+int soap_mx4_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *a_data, const uint8_t *a_scale,
+                  const uint8_t *b_data, const uint8_t *b_scale, int dtype, void *C, int64_t ldc,
+                  hipStream_t stream);
+int soap_mx4_gemm_rows(int64_t groups, int64_t M, int64_t N, int64_t K, const int32_t *offsets,
+                       const uint8_t *a_data, const uint8_t *a_scale, const uint8_t *b_data,
+                       const uint8_t *b_scale, int dtype, void *C, int64_t ldc, hipStream_t stream);
+int soap_mx4_gemm_k(int64_t groups, int64_t M, int64_t N, int64_t K, const int32_t *offsets,
+                    const uint8_t *a_data, const uint8_t *a_scale, const uint8_t *b_data,
+                    const uint8_t *b_scale, int dtype, void *C, hipStream_t stream);
+
 /* ---- measurement ---- */
 
 /* When enabled, every stage of soap_step / soap_step_batched records a pair

@@ -33,6 +33,12 @@ SOAP_FLAG_SKIP_REFRESH = 2
 SOAP_FLAG_STALE_REFRESH = 4
 SOAP_MUON_BF16 = 1
 SOAP_MAX_DIM = 16384
+SOAP_F32 = 0
+SOAP_BF16 = 1
+SOAP_MAX_ROWS = 1 << 24
+SOAP_ROUTER_RENORMALIZE = 1
+SOAP_ROUTER_MAX_EXPERTS = 1024
+SOAP_ROUTER_MAX_TOP_K = 32
 
 EXPORTED = [
     "soap_workspace_bytes", "soap_init_state", "soap_step", "soap_step_batched",
@@ -44,6 +50,10 @@ EXPORTED = [
     "soap_muon_step", "soap_muon_step_batched", "soap_workspace_status",
     "soap_workspace_update_offset", "soap_test_force_qr_give_up", "soap_step_noalloc",
     "soap_test_qr_panel_path",
+    "soap_layer_norm_forward", "soap_layer_norm_workspace_bytes", "soap_layer_norm_backward",
+    "soap_router_rows", "soap_router_workspace_bytes", "soap_router_forward",
+    "soap_router_backward", "soap_mx4_data_bytes", "soap_mx4_scale_bytes", "soap_mx4_quantize",
+    "soap_mx4_dequantize", "soap_mx4_gemm", "soap_mx4_gemm_rows", "soap_mx4_gemm_k",
 ]
 
 
@@ -111,6 +121,26 @@ def lib() -> ctypes.CDLL:
         "soap_timing_get": (_INT, [_INT, ctypes.POINTER(ctypes.c_double),
                                    ctypes.POINTER(ctypes.c_int64),
                                    ctypes.POINTER(ctypes.c_double)]),
+        "soap_layer_norm_forward": (_INT, [_I64, _I64, _INT, _P, _I64, _P, _P, _F, _P, _I64, _P,
+                                           _P, _P]),
+        "soap_layer_norm_workspace_bytes": (_SZ, [_I64, _I64]),
+        "soap_layer_norm_backward": (_INT, [_I64, _I64, _INT, _P, _I64, _P, _I64, _P, _P, _P, _P,
+                                            _I64, _P, _P, _P, _SZ, _P]),
+        "soap_router_rows": (_I64, [_I64, _I64, _I64]),
+        "soap_router_workspace_bytes": (_SZ, [_I64, _I64]),
+        "soap_router_forward": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _U32, _F, _P, _P, _P,
+                                       _P, _P, _P, _P, _P, _SZ, _P]),
+        "soap_router_backward": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _U32, _F, _P, _P,
+                                        _P, _P, _P, _I64, _P]),
+        "soap_mx4_data_bytes": (_SZ, [_I64, _I64]),
+        "soap_mx4_scale_bytes": (_SZ, [_I64, _I64]),
+        "soap_mx4_quantize": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _I64, _P, _P, _P, _P,
+                                     _P]),
+        "soap_mx4_dequantize": (_INT, [_I64, _I64, _P, _P, _INT, _P, _I64, _P]),
+        "soap_mx4_gemm": (_INT, [_I64, _I64, _I64, _P, _P, _P, _P, _INT, _P, _I64, _P]),
+        "soap_mx4_gemm_rows": (_INT, [_I64, _I64, _I64, _I64, _P, _P, _P, _P, _P, _INT, _P, _I64,
+                                      _P]),
+        "soap_mx4_gemm_k": (_INT, [_I64, _I64, _I64, _I64, _P, _P, _P, _P, _P, _INT, _P, _P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -424,3 +454,425 @@ class MuonState:
             soap_muon_step_batched(self.batch, param, grad, self.M, self.m, self.n, beta1, lr,
                                    weight_decay, eps, flat, n_iters, flags, self.workspace,
                                    self.ws_bytes, stream)
+
+
+# ------------------------------------------------------------------------------
+# Operators of the layer around an expert bank.  The functions of the C names take
+# raw device pointers (ints) or tensors, whose element type and strides are the
+# caller's to get right; the classes below check them.
+def _raw(x) -> Optional[int]:
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    return x.data_ptr()
+
+
+def soap_layer_norm_forward(rows, cols, dtype, x, ldx, weight, bias, eps, y, ldy, mean, rstd,
+                            stream=None) -> None:
+    _check(lib().soap_layer_norm_forward(rows, cols, dtype, _raw(x), ldx, _raw(weight), _raw(bias),
+                                         eps, _raw(y), ldy, _raw(mean), _raw(rstd),
+                                         _stream(stream)))
+
+
+def soap_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().soap_layer_norm_workspace_bytes(rows, cols))
+
+
+def soap_layer_norm_backward(rows, cols, dtype, dy, lddy, x, ldx, weight, mean, rstd, dx, lddx,
+                             dweight, dbias, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().soap_layer_norm_backward(rows, cols, dtype, _raw(dy), lddy, _raw(x), ldx,
+                                          _raw(weight), _raw(mean), _raw(rstd), _raw(dx), lddx,
+                                          _raw(dweight), _raw(dbias), _raw(workspace),
+                                          workspace_bytes, _stream(stream)))
+
+
+def soap_router_rows(tokens: int, experts: int, top_k: int) -> int:
+    return int(lib().soap_router_rows(tokens, experts, top_k))
+
+
+def soap_router_workspace_bytes(tokens: int, experts: int) -> int:
+    return int(lib().soap_router_workspace_bytes(tokens, experts))
+
+
+def soap_router_forward(tokens, experts, top_k, dtype, logits, ld, token_mask, flags, balance, index,
+                        gate, counts, loss, offsets, position, row_token, workspace, workspace_bytes,
+                        stream=None) -> None:
+    _check(lib().soap_router_forward(tokens, experts, top_k, dtype, _raw(logits), ld,
+                                     _raw(token_mask), flags, balance, _raw(index), _raw(gate),
+                                     _raw(counts), _raw(loss), _raw(offsets), _raw(position),
+                                     _raw(row_token), _raw(workspace), workspace_bytes,
+                                     _stream(stream)))
+
+
+def soap_router_backward(tokens, experts, top_k, dtype, logits, ld, token_mask, flags, balance,
+                         index, counts, dgate, dloss, dlogits, ldd, stream=None) -> None:
+    _check(lib().soap_router_backward(tokens, experts, top_k, dtype, _raw(logits), ld,
+                                      _raw(token_mask), flags, balance, _raw(index), _raw(counts),
+                                      _raw(dgate), _raw(dloss), _raw(dlogits), ldd,
+                                      _stream(stream)))
+
+
+def soap_mx4_data_bytes(rows: int, k: int) -> int:
+    return int(lib().soap_mx4_data_bytes(rows, k))
+
+
+def soap_mx4_scale_bytes(rows: int, k: int) -> int:
+    return int(lib().soap_mx4_scale_bytes(rows, k))
+
+
+def soap_mx4_quantize(batch, rows, cols, dtype, x, ldx, row_index, x_rows, data, scale, data_t,
+                      scale_t, stream=None) -> None:
+    _check(lib().soap_mx4_quantize(batch, rows, cols, dtype, _raw(x), ldx, _raw(row_index), x_rows,
+                                   _raw(data), _raw(scale), _raw(data_t), _raw(scale_t),
+                                   _stream(stream)))
+
+
+def soap_mx4_dequantize(rows, k, data, scale, dtype, out, ldo, stream=None) -> None:
+    _check(lib().soap_mx4_dequantize(rows, k, _raw(data), _raw(scale), dtype, _raw(out), ldo,
+                                     _stream(stream)))
+
+
+def soap_mx4_gemm(M, N, K, a_data, a_scale, b_data, b_scale, dtype, C, ldc, stream=None) -> None:
+    _check(lib().soap_mx4_gemm(M, N, K, _raw(a_data), _raw(a_scale), _raw(b_data), _raw(b_scale),
+                               dtype, _raw(C), ldc, _stream(stream)))
+
+
+def soap_mx4_gemm_rows(groups, M, N, K, offsets, a_data, a_scale, b_data, b_scale, dtype, C, ldc,
+                       stream=None) -> None:
+    _check(lib().soap_mx4_gemm_rows(groups, M, N, K, _raw(offsets), _raw(a_data), _raw(a_scale),
+                                    _raw(b_data), _raw(b_scale), dtype, _raw(C), ldc,
+                                    _stream(stream)))
+
+
+def soap_mx4_gemm_k(groups, M, N, K, offsets, a_data, a_scale, b_data, b_scale, dtype, C,
+                    stream=None) -> None:
+    _check(lib().soap_mx4_gemm_k(groups, M, N, K, _raw(offsets), _raw(a_data), _raw(a_scale),
+                                 _raw(b_data), _raw(b_scale), dtype, _raw(C), _stream(stream)))
+
+
+def _floats(t, name):
+    """SOAP_F32 or SOAP_BF16 of a GPU tensor of activations whose rows are contiguous."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t)}")
+    _here(t, name)
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    if t.dtype == torch.bfloat16:
+        return SOAP_BF16
+    if t.dtype == torch.float32:
+        return SOAP_F32
+    raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _here(t, name):
+    import torch
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def _exactly(t, name, dtype, shape):
+    """Checks a contiguous tensor of a given type and shape on the current device."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    _here(t, name)
+    return t
+
+
+def _ld(t):
+    """Row stride of a two-dimensional tensor (its width where it has at most one row)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _on_stream(stream, inputs):
+    """(context to allocate outputs in, raw stream).  With a stream of one's own the
+    outputs belong to it and the inputs are kept from reuse until it has read them."""
+    import contextlib
+
+    import torch
+    if stream is None:
+        return contextlib.nullcontext(), torch.cuda.current_stream().cuda_stream
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream)
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    return torch.cuda.stream(stream), stream.cuda_stream
+
+
+class LayerNorm:
+    """Layer norm of rows of `cols` values with fp32 ``weight`` and ``bias`` (either may
+    be None): soap_layer_norm_forward / _backward with outputs and workspace allocated
+    by torch.  Inputs are float32 or bfloat16 [rows, cols] with contiguous rows."""
+
+    def __init__(self, weight=None, bias=None, eps: float = 1e-5, cols: Optional[int] = None):
+        import torch
+        given = [t for t in (weight, bias) if t is not None]
+        if cols is None:
+            if not given:
+                raise ValueError("a layer norm without weight and bias needs cols")
+            cols = given[0].numel()
+        for t, name in ((weight, "weight"), (bias, "bias")):
+            if t is not None:
+                _exactly(t, name, torch.float32, (cols,))
+        self.weight, self.bias, self.eps, self.cols = weight, bias, eps, cols
+
+    def _matrix(self, t, name):
+        kind = _floats(t, name)
+        if t.dim() != 2 or t.shape[1] != self.cols:
+            raise ValueError(f"{name} must be [rows, {self.cols}], got {tuple(t.shape)}")
+        return kind
+
+    def forward(self, x, stream=None):
+        """(y, mean, rstd): y of x's type, the statistics float32 [rows]."""
+        import torch
+        kind = self._matrix(x, "x")
+        rows = x.shape[0]
+        ctx, raw = _on_stream(stream, (x, self.weight, self.bias))
+        with ctx:
+            y = torch.empty((rows, self.cols), dtype=x.dtype, device=x.device)
+            mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+        _check(lib().soap_layer_norm_forward(rows, self.cols, kind, x.data_ptr(), _ld(x),
+                                             _raw(self.weight), _raw(self.bias), self.eps,
+                                             y.data_ptr(), self.cols, mean.data_ptr(),
+                                             rstd.data_ptr(), raw))
+        return y, mean, rstd
+
+    def backward(self, dy, x, mean, rstd, stream=None):
+        """(dx, dweight, dbias); dweight and dbias are None without a weight and a bias."""
+        import torch
+        kind = self._matrix(x, "x")
+        if self._matrix(dy, "dy") != kind or dy.shape != x.shape:
+            raise ValueError("dy must have x's type and shape")
+        rows = x.shape[0]
+        _exactly(mean, "mean", torch.float32, (rows,))
+        _exactly(rstd, "rstd", torch.float32, (rows,))
+        ctx, raw = _on_stream(stream, (dy, x, mean, rstd, self.weight))
+        L = lib()
+        with ctx:
+            dx = torch.empty((rows, self.cols), dtype=x.dtype, device=x.device)
+            dweight = torch.empty_like(self.weight) if self.weight is not None else None
+            dbias = torch.empty_like(self.bias) if self.bias is not None else None
+            need = L.soap_layer_norm_workspace_bytes(rows, self.cols)
+            work = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
+        _check(L.soap_layer_norm_backward(rows, self.cols, kind, dy.data_ptr(), _ld(dy),
+                                          x.data_ptr(), _ld(x), _raw(self.weight), mean.data_ptr(),
+                                          rstd.data_ptr(), dx.data_ptr(), self.cols, _raw(dweight),
+                                          _raw(dbias), work.data_ptr(), need, raw))
+        return dx, dweight, dbias
+
+
+class Routing:
+    """What Router.forward found: index, gate [tokens, top_k], counts [experts + 1],
+    loss [1] and the dispatch plan offsets [experts + 1], position [tokens, top_k],
+    row_token [rows] (as soap_router_forward describes them)."""
+
+    __slots__ = ("index", "gate", "counts", "loss", "offsets", "position", "row_token")
+
+
+class Router:
+    """Top-k routing over `experts` with balance loss, counts and dispatch plan
+    (soap_router_forward / _backward).  Logits are float32 or bfloat16
+    [tokens, experts] with contiguous rows, mask a bool [tokens] (False: the token
+    does not route) or None."""
+
+    def __init__(self, experts: int, top_k: int, renormalize: bool = True, balance: float = 0.01):
+        self.experts, self.top_k, self.balance = experts, top_k, balance
+        self.flags = SOAP_ROUTER_RENORMALIZE if renormalize else 0
+
+    def _args(self, logits, mask):
+        import torch
+        kind = _floats(logits, "logits")
+        if logits.dim() != 2 or logits.shape[1] != self.experts:
+            raise ValueError(f"logits must be [tokens, {self.experts}], got {tuple(logits.shape)}")
+        if mask is not None:
+            _exactly(mask, "mask", torch.bool, (logits.shape[0],))
+        return kind
+
+    def forward(self, logits, mask=None, stream=None) -> Routing:
+        import torch
+        kind = self._args(logits, mask)
+        tokens, k, E = logits.shape[0], self.top_k, self.experts
+        L = lib()
+        ctx, raw = _on_stream(stream, (logits, mask))
+        n, rows = tokens * k, L.soap_router_rows(tokens, E, k)
+        need = L.soap_router_workspace_bytes(tokens, E)
+        r = Routing()
+        with ctx:
+            ints = torch.empty(2 * n + 2 * (E + 1) + rows, dtype=torch.int32, device=logits.device)
+            floats = torch.empty(n + 1, dtype=torch.float32, device=logits.device)
+            work = torch.empty(max(need, 16), dtype=torch.uint8, device=logits.device)
+        index, position, r.counts, r.offsets, r.row_token = ints.split([n, n, E + 1, E + 1, rows])
+        gate, r.loss = floats.split([n, 1])
+        r.index, r.position, r.gate = index.view(tokens, k), position.view(tokens, k), gate.view(tokens, k)
+        at, ft = ints.data_ptr(), floats.data_ptr()
+        _check(L.soap_router_forward(tokens, E, k, kind, logits.data_ptr(), _ld(logits), _raw(mask),
+                                     self.flags, self.balance, at, ft, at + 8 * n, ft + 4 * n,
+                                     at + 8 * n + 4 * (E + 1), at + 4 * n, at + 8 * n + 8 * (E + 1),
+                                     work.data_ptr(), need, raw))
+        return r
+
+    def backward(self, logits, index, counts, dgate=None, dloss=None, mask=None, stream=None):
+        """dlogits, of the logits' type, from the gradients of gate (float32
+        [tokens, top_k]) and loss (float32 [1], None: 1)."""
+        import torch
+        kind = self._args(logits, mask)
+        tokens, k, E = logits.shape[0], self.top_k, self.experts
+        _exactly(index, "index", torch.int32, (tokens, k))
+        _exactly(counts, "counts", torch.int32, (E + 1,))
+        if dgate is not None:
+            _exactly(dgate, "dgate", torch.float32, (tokens, k))
+        if dloss is not None:
+            _exactly(dloss, "dloss", torch.float32, (1,))
+        ctx, raw = _on_stream(stream, (logits, mask, index, counts, dgate, dloss))
+        with ctx:
+            out = torch.empty((tokens, E), dtype=logits.dtype, device=logits.device)
+        _check(lib().soap_router_backward(tokens, E, k, kind, logits.data_ptr(), _ld(logits),
+                                          _raw(mask), self.flags, self.balance, index.data_ptr(),
+                                          counts.data_ptr(), _raw(dgate), _raw(dloss),
+                                          out.data_ptr(), E, raw))
+        return out
+
+
+class Mx4:
+    """A matrix, or a batch of them, in packed MXFP4 along its last axis of `k` values:
+    ``data`` and ``scale`` uint8 [.., rows, bytes of a row]."""
+
+    def __init__(self, data, scale, k: int):
+        import torch
+        padded = (k + 255) // 256 * 256
+        _exactly(data, "data", torch.uint8, (*data.shape[:-1], padded // 2))
+        _exactly(scale, "scale", torch.uint8, (*data.shape[:-1], padded // 32))
+        if data.dim() not in (2, 3):
+            raise ValueError("data must be [rows, bytes] or [batch, rows, bytes]")
+        self.data, self.scale, self.k = data, scale, k
+
+    @property
+    def rows(self) -> int:
+        return self.data.shape[-2]
+
+    def values(self, dtype=None, stream=None):
+        """What the packed values stand for, as float32 (default) or bfloat16 [.., rows, k]."""
+        import torch
+        dtype = dtype or torch.float32
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"values are float32 or bfloat16, not {dtype}")
+        ctx, raw = _on_stream(stream, (self.data, self.scale))
+        with ctx:
+            out = torch.empty((*self.data.shape[:-1], self.k), dtype=dtype, device=self.data.device)
+        rows = out.numel() // self.k
+        _check(lib().soap_mx4_dequantize(rows, self.k, self.data.data_ptr(), self.scale.data_ptr(),
+                                         SOAP_BF16 if dtype == torch.bfloat16 else SOAP_F32,
+                                         out.data_ptr(), self.k, raw))
+        return out
+
+
+def _mx4_empty(batch, rows, k, device):
+    import torch
+    padded = (k + 255) // 256 * 256
+    lead = (rows,) if batch is None else (batch, rows)
+    m = Mx4.__new__(Mx4)
+    m.data = torch.empty((*lead, padded // 2), dtype=torch.uint8, device=device)
+    m.scale = torch.empty((*lead, padded // 32), dtype=torch.uint8, device=device)
+    m.k = k
+    return m
+
+
+def mx4_quantize(x, along: str = "cols", row_index=None, stream=None):
+    """x (float32 or bfloat16 [rows, cols], or contiguous [batch, rows, cols]) in MXFP4
+    with blocks along its columns ("cols"), along its rows ("rows": the transposed
+    matrix, [cols, rows]) or both (a pair, x read once).  row_index (int32 [n]) takes
+    the rows row_index[i] of x, zeros where that is not a row of x."""
+    import torch
+    if along not in ("cols", "rows", "both"):
+        raise ValueError(f'along must be "cols", "rows" or "both", got {along!r}')
+    kind = _floats(x, "x")
+    if x.dim() not in (2, 3) or (x.dim() == 3 and not x.is_contiguous()):
+        raise ValueError("x must be [rows, cols] or contiguous [batch, rows, cols]")
+    batch = x.shape[0] if x.dim() == 3 else None
+    if row_index is not None:
+        if batch is not None:
+            raise ValueError("row_index takes a single matrix")
+        _exactly(row_index, "row_index", torch.int32, (row_index.numel(),))
+    cols, x_rows = x.shape[-1], x.shape[-2]
+    rows = x_rows if row_index is None else row_index.numel()
+    ctx, raw = _on_stream(stream, (x, row_index))
+    with ctx:
+        a = _mx4_empty(batch, rows, cols, x.device) if along != "rows" else None
+        b = _mx4_empty(batch, cols, rows, x.device) if along != "cols" else None
+    ld = _ld(x) if batch is None else cols
+    _check(lib().soap_mx4_quantize(batch or 1, rows, cols, kind, x.data_ptr(), ld, _raw(row_index),
+                                   x_rows, *((a.data.data_ptr(), a.scale.data_ptr()) if a else (None, None)),
+                                   *((b.data.data_ptr(), b.scale.data_ptr()) if b else (None, None)),
+                                   raw))
+    return (a, b) if along == "both" else a or b
+
+
+def _mx4_args(a, b, dtype, dims_b):
+    import torch
+    if a.data.dim() != 2 or b.data.dim() != dims_b:
+        raise ValueError(f"a must be one matrix and b {'a batch' if dims_b == 3 else 'one matrix'}")
+    if a.k != b.k:
+        raise ValueError(f"a and b are summed over one axis: {a.k} and {b.k} values")
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"products are float32 or bfloat16, not {dtype}")
+    return SOAP_BF16 if dtype == torch.bfloat16 else SOAP_F32
+
+
+def mx4_product(a: Mx4, b: Mx4, dtype=None, stream=None):
+    """a b^T, float32 (default) or bfloat16 [a.rows, b.rows] (soap_mx4_gemm)."""
+    import torch
+    dtype = dtype or torch.float32
+    kind = _mx4_args(a, b, dtype, 2)
+    ctx, raw = _on_stream(stream, (a.data, a.scale, b.data, b.scale))
+    with ctx:
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.data.device)
+    _check(lib().soap_mx4_gemm(a.rows, b.rows, a.k, a.data.data_ptr(), a.scale.data_ptr(),
+                               b.data.data_ptr(), b.scale.data_ptr(), kind, out.data_ptr(), b.rows,
+                               raw))
+    return out
+
+
+def mx4_product_rows(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
+    """Rows offsets[g] .. offsets[g + 1] of a times b[g]^T, [a.rows, b.rows]; zeros past the
+    last group (soap_mx4_gemm_rows).  offsets: int32 [groups + 1] on the GPU."""
+    import torch
+    dtype = dtype or torch.float32
+    kind = _mx4_args(a, b, dtype, 3)
+    groups = b.data.shape[0]
+    _exactly(offsets, "offsets", torch.int32, (groups + 1,))
+    ctx, raw = _on_stream(stream, (a.data, a.scale, b.data, b.scale, offsets))
+    with ctx:
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.data.device)
+    _check(lib().soap_mx4_gemm_rows(groups, a.rows, b.rows, a.k, offsets.data_ptr(),
+                                    a.data.data_ptr(), a.scale.data_ptr(), b.data.data_ptr(),
+                                    b.scale.data_ptr(), kind, out.data_ptr(), b.rows, raw))
+    return out
+
+
+def mx4_product_k(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
+    """a b^T summed over k = offsets[g] .. offsets[g + 1] for every g, [groups, a.rows, b.rows]:
+    the layout of the batched steps' gradients (soap_mx4_gemm_k)."""
+    import torch
+    dtype = dtype or torch.float32
+    kind = _mx4_args(a, b, dtype, 2)
+    _exactly(offsets, "offsets", torch.int32, (offsets.numel(),))
+    groups = offsets.numel() - 1
+    ctx, raw = _on_stream(stream, (a.data, a.scale, b.data, b.scale, offsets))
+    with ctx:
+        out = torch.empty((groups, a.rows, b.rows), dtype=dtype, device=a.data.device)
+    _check(lib().soap_mx4_gemm_k(groups, a.rows, b.rows, a.k, offsets.data_ptr(), a.data.data_ptr(),
+                                 a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
+                                 out.data_ptr(), raw))
+    return out

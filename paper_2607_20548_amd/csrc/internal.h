@@ -222,4 +222,78 @@ hipError_t qr_factor_and_form_q(float *At, float *Q, float *Rf, int64_t batch, i
 // dst = src^T for one n x n row-major matrix.
 hipError_t launch_transpose(float *dst, const float *src, int64_t n, hipStream_t s);
 
+// ------------------------------------------------------------- layer norm
+// Row strides ld* in elements; weight, bias, dweight, dbias, mean (forward)
+// and rstd (forward) may be null, and out (dx) backward.
+struct LayerNormDesc {
+  int64_t rows = 0, cols = 0;
+  bool bf16 = false;
+  const void *x = nullptr, *dy = nullptr;
+  int64_t ldx = 0, lddy = 0, ldo = 0;
+  const float *weight = nullptr, *bias = nullptr;
+  float eps = 0.f;
+  void *out = nullptr;               // y or dx
+  float *mean = nullptr, *rstd = nullptr;
+  float *dweight = nullptr, *dbias = nullptr, *part = nullptr;
+};
+size_t layer_norm_part_bytes(int64_t rows, int64_t cols);
+hipError_t launch_layer_norm_fwd(const LayerNormDesc &d, hipStream_t s);
+hipError_t launch_layer_norm_bwd(const LayerNormDesc &d, hipStream_t s);
+
+// ----------------------------------------------------------------- router
+struct RouterDesc {
+  int64_t tokens = 0, experts = 0, top_k = 0, ld = 0, ldd = 0, rows = 0;
+  bool bf16 = false;
+  int renorm = 0;
+  float balance = 0.f;
+  const void *logits = nullptr;
+  const uint8_t *mask = nullptr;
+  int *index = nullptr;              // read by the backward pass
+  float *gate = nullptr;
+  int *counts = nullptr;             // [experts + 1]; read by the backward pass
+  float *loss = nullptr;
+  int *offsets = nullptr, *position = nullptr, *row_token = nullptr;   // all or none
+  const float *dgate = nullptr, *dloss = nullptr;
+  void *dlogits = nullptr;
+  void *scratch = nullptr;
+};
+size_t router_scratch_bytes(int64_t tokens, int64_t experts);
+hipError_t launch_router_fwd(const RouterDesc &d, hipStream_t s);
+hipError_t launch_router_bwd(const RouterDesc &d, hipStream_t s);
+
+// ------------------------------------------------------------------ MXFP4
+// A packed matrix of `rows` rows of k values: rows of mx4_padded(k) / 2 bytes of
+// data and mx4_padded(k) / 32 bytes of scales.
+inline int64_t mx4_padded(int64_t k) { return (k + 255) / 256 * 256; }
+struct Mx4Mat {
+  const uint8_t *data = nullptr, *scale = nullptr;
+};
+struct Mx4QuantDesc {
+  int64_t batch = 1, rows = 0, cols = 0, ldx = 0, x_rows = 0;
+  bool bf16 = false;
+  const void *x = nullptr;
+  const int *row_index = nullptr;
+  uint8_t *data = nullptr, *scale = nullptr;       // along the columns, or null
+  uint8_t *data_t = nullptr, *scale_t = nullptr;   // along the rows, or null
+};
+hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s);
+hipError_t launch_mx4_dequantize(const Mx4Mat &a, int64_t rows, int64_t cols, bool bf16, void *out,
+                                 int64_t ldo, hipStream_t s);
+// C = A B^T over k.  offsets (groups + 1 device ints, multiples of 32) null: one
+// product.  by_k: C[g] = A[:, k of g] B[:, k of g]^T (C contiguous); otherwise
+// C's rows of group g = A's rows of g B[g]^T, rows past the last group zero.
+struct Mx4GemmDesc {
+  int64_t groups = 1, M = 0, N = 0, K = 0, ldc = 0;
+  bool by_k = false, bf16 = false;
+  const int *offsets = nullptr;
+  Mx4Mat A, B;
+  void *C = nullptr;
+};
+hipError_t launch_mx4_gemm(const Mx4GemmDesc &d, hipStream_t s);
+
+// ------------------------------------------------- errors of the C ABI
+// The calling thread's error string (soap_last_error) and status.
+int api_fail(int code, const char *fmt, ...);
+int api_ok();
+
 }  // namespace soap

@@ -1043,6 +1043,20 @@ hipError_t scratch_address(void **out) {
 
 }  // namespace
 
+namespace soap {
+
+int api_fail(int code, const char *fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof(g_err), fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+int api_ok() { return ok(); }
+
+}  // namespace soap
+
 extern "C" {
 
 int soap_step_noalloc(float *param, const float *grad, float *L, float *R, float *Q_L, float *Q_R,
