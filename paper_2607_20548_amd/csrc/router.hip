@@ -62,10 +62,10 @@ struct RtParams {
   void *dlogits;
 };
 
-// Ordered as the floats are; 0 for -inf and NaN.
+// Ordered as the floats are (both zeros alike); 0 for -inf and NaN.
 __device__ __forceinline__ uint32_t rt_key(float f) {
   if (!(f > -INFINITY)) return 0u;
-  const uint32_t u = __float_as_uint(f);
+  const uint32_t u = __float_as_uint(f + 0.f);
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float rt_unkey(uint32_t k) {
