@@ -412,8 +412,8 @@ int soap_mx4_dequantize(int64_t rows, int64_t k, const uint8_t *data, const uint
                         void *out, int64_t ldo, hipStream_t stream);
 
 /* Rows of a packed matrix along the columns and the k of one along the rows may be
- * as many as a dispatch plan has (2^31 - 1); cols, N and K otherwise go up to
- * SOAP_MAX_ROWS. */
+ * as many as a dispatch plan has (2^31 - 1 rows, 2 SOAP_MAX_ROWS k); cols, N and K
+ * otherwise go up to SOAP_MAX_ROWS. */
 
 /* Products of packed matrices, C = A B^T summed over k in fp32 and rounded once to
  * a bfloat16 output.

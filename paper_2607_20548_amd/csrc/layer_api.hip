@@ -104,7 +104,7 @@ int check_product(int64_t groups, int64_t M, int64_t N, int64_t K, bool grouped,
                   const uint8_t *ad, const uint8_t *as, int64_t b_rows, const uint8_t *bd,
                   const uint8_t *bs, int dtype, void *C, size_t c_bytes) {
   SOAP_TRY(check_dtype(dtype));
-  SOAP_TRY(check_range("tiles of 32 x 128", (M / 32 + groups + 2) * ((N + 127) / 128), 0, INT32_MAX));
+  SOAP_TRY(check_range("tiles of 128 x 128", (M / 128 + groups + 2) * ((N + 127) / 128), 0, INT32_MAX));
   return check_bufs({{offsets, grouped ? 4 * (size_t)(groups + 1) : 0, "offsets", false, true, 4},
                      {ad, soap_mx4_data_bytes(M, K), "a_data", false, true, 16},
                      {as, soap_mx4_scale_bytes(M, K), "a_scale", false, true, 16},
@@ -340,7 +340,7 @@ int soap_mx4_gemm_k(int64_t groups, int64_t M, int64_t N, int64_t K, const int32
   SOAP_TRY(check_range("groups", groups, 1, SOAP_MAX_DIM));
   SOAP_TRY(check_range("M", M, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_range("N", N, 1, SOAP_MAX_ROWS));
-  SOAP_TRY(check_range("K", K, 0, INT32_MAX));
+  SOAP_TRY(check_range("K", K, 0, 2 * SOAP_MAX_ROWS));
   SOAP_TRY(check_product(groups, M, N, K, true, offsets, a_data, a_scale, N, b_data, b_scale, dtype, C,
                          elem(dtype) * (size_t)groups * (size_t)M * (size_t)N));
   soap::Mx4GemmDesc d;

@@ -18,6 +18,9 @@ namespace {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v8i __attribute__((ext_vector_type(8)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v8u __attribute__((ext_vector_type(8)));
 
 // --------------------------------------------------------- quantisation
 __device__ __forceinline__ uint32_t mx_abs(float f) { return __float_as_uint(f) & 0x7fffffffu; }
@@ -44,63 +47,153 @@ struct QuantParams {
   int vec;
 };
 
-// A workgroup takes 128 rows x 256 columns, a wave 32 rows of them and a lane
-// four columns: every value is read once and both directions are formed in
-// registers.  A block along the columns is eight lanes of one row, a block along
-// the rows one column of a lane.
-template <typename T, bool ROWS, bool COLS>
-__global__ __launch_bounds__(256) void mx4_quantize(QuantParams p) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Along the columns only: eight values per lane, a block is four lanes of a row, so
+// that a wave's loads and stores are contiguous.  A row has LPR lanes, which walk
+// along it in QC_UNITS independent loads at a time.
+constexpr int QC_UNITS = 4;
+template <typename T, int LPR>
+__global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
+  constexpr int ROWS = 256 / LPR;
   const int64_t b = blockIdx.y;
-  const int64_t ct = p.kp / 256, rt = blockIdx.x / ct;
-  const int64_t r0 = (rt * 4 + wave) * 32;
-  const int64_t c0 = (blockIdx.x - rt * ct) * 256 + 4 * lane;
   const T *x = static_cast<const T *>(p.x) + b * p.sx;
-  if (r0 >= (COLS ? p.rp : p.rows)) return;
-  float v[32][4];
-  const bool in4 = c0 + 3 < p.cols;
+  uint8_t *data = p.data + b * p.rows * (p.kp / 2), *scale = p.scale + b * p.rows * (p.kp / 32);
+  typedef typename std::conditional<sizeof(T) == 4, v8u, v4u>::type Raw;
+  const int lane = threadIdx.x % LPR;
+  for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; r < p.rows; r += (int64_t)gridDim.x * ROWS) {
+    int64_t src = r;
+    if (p.row_index) {
+      src = p.row_index[r];
+      if (src >= p.x_rows) src = -1;
+    }
+    const T *xr = x + src * p.ldx;
+    uint8_t *dr = data + r * (p.kp / 2), *sr = scale + r * (p.kp / 32);
+    for (int64_t c0 = 8 * lane; c0 < p.kp; c0 += QC_UNITS * LPR * 8) {
+      Raw raw[QC_UNITS];
+#pragma unroll
+      for (int u = 0; u < QC_UNITS; ++u) {
+        const int64_t c = c0 + u * LPR * 8;
+        raw[u] = Raw(0u);
+        if (src < 0 || c >= p.cols) continue;
+        if (p.vec && c + 8 <= p.cols) {
+          if constexpr (sizeof(T) == 4) {
+            const v4u lo = *reinterpret_cast<const v4u *>(xr + c), hi = *reinterpret_cast<const v4u *>(xr + c + 4);
+            raw[u] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          } else {
+            raw[u] = *reinterpret_cast<const v4u *>(xr + c);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c + j < p.cols) {
+              if constexpr (sizeof(T) == 4) raw[u][j] = __float_as_uint(xr[c + j]);
+              else raw[u][j / 2] |= (uint32_t)xr[c + j] << (16 * (j & 1));
+            }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < QC_UNITS; ++u) {
+        const int64_t c = c0 + u * LPR * 8;
+        auto bits = [&](int j) -> uint32_t {
+          if constexpr (sizeof(T) == 4) return raw[u][j];
+          else return (j & 1) ? raw[u][j / 2] & 0xffff0000u : raw[u][j / 2] << 16;
+        };
+        auto val = [&](int j) { return __uint_as_float(bits(j)); };
+        uint32_t a = 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) a = max(a, bits(j) & 0x7fffffffu);
+        a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xB1, 0xF, 0xF, true));   // lane ^ 1
+        a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xF, 0xF, true));   // lane ^ 2
+        const uint32_t byte = mx_byte(a);
+        const float s = mx_scale(byte);
+        uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, val(0), val(1), s, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(2), val(3), s, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(4), val(5), s, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(6), val(7), s, 3);
+        if (c < p.kp) {
+          *reinterpret_cast<uint32_t *>(dr + c / 2) = q;
+          if ((lane & 3) == 0) sr[c / 32] = (uint8_t)byte;
+        }
+      }
+    }
+  }
+}
+
+// Along the rows, or both ways: a workgroup takes 128 rows x 256 columns, a wave 32
+// rows of them and a lane four columns: every value is read once and both
+// directions are formed in registers.  A block along the columns is eight lanes of
+// one row, a block along the rows one column of a lane; those go through LDS, so
+// that a column's 64 bytes (four blocks) are written together.  Workgroups of
+// consecutive rows run on one XCD, whose L2 joins what they write of a line.
+template <typename T, bool ROWS>
+__global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
+  // column x's block of wave w: 16 bytes at x * 64 + 16 * (w ^ (x / 4 % 4))
+  __shared__ __attribute__((aligned(16))) uint8_t lds[256 * 64 + 256 * 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t b = blockIdx.y;
+  const int64_t rt = (p.rp + 127) / 128;
+  int64_t t = blockIdx.x;
+  {
+    const int nt = gridDim.x, x = blockIdx.x & 7, per = nt >> 3, more = nt & 7;
+    t = x * per + min(x, more) + (blockIdx.x >> 3);
+  }
+  const int64_t ct = t / rt, r0 = ((t - ct * rt) * 4 + wave) * 32;
+  const int64_t cw = ct * 256, c0 = cw + 4 * lane;
+  const T *x = static_cast<const T *>(p.x) + b * p.sx;
+  const bool all = cw + 256 <= p.cols && p.vec;
+  typedef typename std::conditional<sizeof(T) == 4, v4u, v2u>::type Raw;
+  Raw raw[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
     const int64_t r = r0 + i;
     int64_t src = -1;
     if (r < p.rows) src = p.row_index ? (int64_t)p.row_index[r] : r;
     if (src >= p.x_rows) src = -1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[i][j] = 0.f;
+    raw[i] = Raw(0u);
     if (src < 0) continue;
-    const T *xr = x + src * p.ldx + c0;
-    if (p.vec && in4) {
-      if constexpr (sizeof(T) == 4) {
-        const float4 q = *reinterpret_cast<const float4 *>(xr);
-        v[i][0] = q.x; v[i][1] = q.y; v[i][2] = q.z; v[i][3] = q.w;
-      } else {
-        const uint2 q = *reinterpret_cast<const uint2 *>(xr);
-        v[i][0] = __uint_as_float(q.x << 16); v[i][1] = __uint_as_float(q.x & 0xffff0000u);
-        v[i][2] = __uint_as_float(q.y << 16); v[i][3] = __uint_as_float(q.y & 0xffff0000u);
-      }
+    const T *xr = x + src * p.ldx + cw;
+    if (all) {
+      raw[i] = __builtin_nontemporal_load(reinterpret_cast<const Raw *>(xr) + lane);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (c0 + j < p.cols) {
-          if constexpr (sizeof(T) == 4) v[i][j] = xr[j];
-          else v[i][j] = __uint_as_float((uint32_t)xr[j] << 16);
+          if constexpr (sizeof(T) == 4) raw[i][j] = __float_as_uint(xr[4 * lane + j]);
+          else raw[i][j / 2] |= (uint32_t)xr[4 * lane + j] << (16 * (j & 1));
         }
     }
   }
+  auto bits = [&](int i, int j) -> uint32_t {
+    if constexpr (sizeof(T) == 4) return raw[i][j];
+    else return (j & 1) ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16;
+  };
+  auto val = [&](int i, int j) { return __uint_as_float(bits(i, j)); };
   if constexpr (ROWS) {
     uint8_t *data = p.data + b * p.rows * (p.kp / 2), *scale = p.scale + b * p.rows * (p.kp / 32);
     uint32_t keep[4];          // the byte of row 8 i + lane % 8 of the lane's block
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const uint32_t a = max(max(mx_abs(v[i][0]), mx_abs(v[i][1])), max(mx_abs(v[i][2]), mx_abs(v[i][3])));
-      const uint32_t byte = mx_byte(mx_max8(a));
-      const float s = mx_scale(byte);
-      uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[i][0], v[i][1], s, 0);
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[i][2], v[i][3], s, 1);
+    for (int i = 0; i < 32; i += 2) {
+      uint32_t q = 0u;         // row i's four values, then row i + 1's
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t a = 0u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a = max(a, bits(i + k, j) & 0x7fffffffu);
+        const uint32_t byte = mx_byte(mx_max8(a));
+        const float s = mx_scale(byte);
+        if (k == 0) {
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i, 0), val(i, 1), s, 0);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i, 2), val(i, 3), s, 1);
+        } else {
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i + 1, 0), val(i + 1, 1), s, 2);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i + 1, 2), val(i + 1, 3), s, 3);
+        }
+        if (((i + k) & 7) == (lane & 7)) keep[i >> 3] = byte;
+      }
+      // even lanes write row i, odd ones row i + 1: their own values and the other's
       const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)q, 0xB1, 0xF, 0xF, true);
-      if (r0 + i < p.rows && (lane & 1) == 0)
-        *reinterpret_cast<uint32_t *>(data + (r0 + i) * (p.kp / 2) + c0 / 2) = q | (other << 16);
-      if ((i & 7) == (lane & 7)) keep[i >> 3] = byte;
+      const uint32_t out = lane & 1 ? (other >> 16) | (q & 0xffff0000u) : (q & 0xffffu) | (other << 16);
+      const int64_t r = r0 + i + (lane & 1);
+      if (r < p.rows) *reinterpret_cast<uint32_t *>(data + r * (p.kp / 2) + cw / 2 + 4 * (lane >> 1)) = out;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -108,29 +201,38 @@ __global__ __launch_bounds__(256) void mx4_quantize(QuantParams p) {
       if (r < p.rows) scale[r * (p.kp / 32) + c0 / 32] = (uint8_t)keep[i];
     }
   }
-  if constexpr (COLS) {
-    uint8_t *data = p.data_t + b * p.cols * (p.rp / 2), *scale = p.scale_t + b * p.cols * (p.rp / 32);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t a = 0u;
+  for (int j = 0; j < 4; ++j) {
+    uint32_t a = 0u;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) a = max(a, mx_abs(v[i][j]));
-      const uint32_t byte = mx_byte(a);
-      const float s = mx_scale(byte);
-      uint32_t w[4];
+    for (int i = 0; i < 32; ++i) a = max(a, bits(i, j) & 0x7fffffffu);
+    const uint32_t byte = mx_byte(a);
+    const float s = mx_scale(byte);
+    v4u w;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        w[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[8 * k][j], v[8 * k + 1][j], s, 0);
-        w[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[k], v[8 * k + 2][j], v[8 * k + 3][j], s, 1);
-        w[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[k], v[8 * k + 4][j], v[8 * k + 5][j], s, 2);
-        w[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w[k], v[8 * k + 6][j], v[8 * k + 7][j], s, 3);
-      }
-      if (c0 + j < p.cols) {
-        *reinterpret_cast<uint4 *>(data + (c0 + j) * (p.rp / 2) + r0 / 2) = make_uint4(w[0], w[1], w[2], w[3]);
-        scale[(c0 + j) * (p.rp / 32) + r0 / 32] = (uint8_t)byte;
-      }
+    for (int k = 0; k < 4; ++k) {
+      uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, val(8 * k, j), val(8 * k + 1, j), s, 0);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(8 * k + 2, j), val(8 * k + 3, j), s, 1);
+      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(8 * k + 4, j), val(8 * k + 5, j), s, 2);
+      w[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(8 * k + 6, j), val(8 * k + 7, j), s, 3);
     }
+    const int c = 4 * lane + j;
+    *reinterpret_cast<v4u *>(lds + c * 64 + 16 * (wave ^ (lane & 3))) = w;
+    lds[256 * 64 + 4 * c + wave] = (uint8_t)byte;
   }
+  __syncthreads();
+  uint8_t *data = p.data_t + b * p.cols * (p.rp / 2), *scale = p.scale_t + b * p.cols * (p.rp / 32);
+  const int64_t rw = r0 - 32 * wave;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int c = 64 * u + (threadIdx.x >> 2), k = threadIdx.x & 3;
+    if (cw + c < p.cols)
+      *reinterpret_cast<v4u *>(data + (cw + c) * (p.rp / 2) + rw / 2 + 16 * k) =
+          *reinterpret_cast<const v4u *>(lds + c * 64 + 16 * (k ^ ((c >> 2) & 3)));
+  }
+  if (cw + threadIdx.x < p.cols)
+    *reinterpret_cast<uint32_t *>(scale + (cw + threadIdx.x) * (p.rp / 32) + rw / 32) =
+        *reinterpret_cast<const uint32_t *>(lds + 256 * 64 + 4 * threadIdx.x);
 }
 
 // The values of a packed matrix: eight per thread.
@@ -153,15 +255,16 @@ __global__ __launch_bounds__(256) void mx4_dequantize(Mx4Mat a, int64_t rows, in
     T *o = out + r * ldo + c;
     if (vec && c + 8 <= cols) {
       if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4 *>(o) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4 *>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        typedef float v4f __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f *>(o));
+        __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<v4f *>(o + 4));
       } else {
-        uint32_t w[4];
+        v4u w;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) |
                  ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16);
-        *reinterpret_cast<uint4 *>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+        __builtin_nontemporal_store(w, reinterpret_cast<v4u *>(o));
       }
     } else {
 #pragma unroll
@@ -181,6 +284,7 @@ struct MxParams {
   int64_t bytes;              // data bytes of a packed row (16 a block); scales: bytes / 16
   int groups, tiles_m, tiles_n;
   int wide;                   // C can be written 16 bytes at a time
+  int stream;                 // and is too large for the L2s: kept out of them
   const int *offsets;
   const uint8_t *A, *As, *B, *Bs;
   void *C;
@@ -245,252 +349,32 @@ __device__ __forceinline__ bool mx_tile(const MxParams &p, int64_t t, int g, MxT
   return true;
 }
 
-template <typename T>
-__device__ __forceinline__ void mx_put(T *c, float v) {
-  if constexpr (sizeof(T) == 4) *c = v;
-  else *c = __builtin_bit_cast(uint16_t, (__bf16)v);
-}
-
-// 32 x 128 of C per workgroup, 32 x 32 per wave, operands straight from memory:
-// a lane of a matrix instruction takes a whole block (16 bytes) and its scale.
-template <int MODE, typename T>
-__global__ __launch_bounds__(256) void mx4_gemm(MxParams p) {
-  MxTile o;
-  const int64_t tm = blockIdx.x / p.tiles_n, tn = blockIdx.x - tm * p.tiles_n;
-  if (!mx_tile<MODE, 32>(p, tm, blockIdx.y, o)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, xl = lane & 31, h = lane >> 5;
-  const int64_t n0 = tn * 128 + 32 * wave;
-  if (o.m0 >= o.m1 || n0 >= p.N) return;
-  const int64_t ra = min(o.m0 + xl, o.m1 - 1), rb = o.b0 + min(n0 + xl, p.N - 1);
-  const uint8_t *a = p.A + ra * p.bytes, *b = p.B + rb * p.bytes;
-  const uint8_t *as = p.As + ra * (p.bytes / 16), *bs = p.Bs + rb * (p.bytes / 16);
-  v16f acc;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  for (int k = o.kb0; k < o.kb1; k += 2) {
-    const bool live = k + h < o.kb1;
-    const int kk = live ? k + h : k;
-    uint4 x = *reinterpret_cast<const uint4 *>(a + 16 * (int64_t)kk);
-    uint4 y = *reinterpret_cast<const uint4 *>(b + 16 * (int64_t)kk);
-    int sx = as[kk], sy = bs[kk];
-    if (!live) {
-      x = y = make_uint4(0u, 0u, 0u, 0u);
-      sx = sy = 127;
-    }
-    const v8i va = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
-    const v8i vb = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
-    acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va, vb, acc, 4, 4, 0, sx, 0, sy);
-  }
-  T *C = static_cast<T *>(p.C) + o.c0;
-  if (n0 + xl >= p.N) return;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int64_t row = o.m0 + 8 * (r >> 2) + 4 * h + (r & 3);
-    if (row < o.m1) mx_put<T>(C + row * p.ldc + n0 + xl, acc[r]);
-  }
-}
-
-// The same product by tiles of TM x TN through LDS: four waves (2 x 2), each
-// (TM / 2) x (TN / 2) in blocks of 32 x 32.  K advances in slabs of 256 values (128
-// bytes of a row, eight blocks), two in LDS, written there by the loads
-// themselves (16 bytes a lane, no registers): unit g of row x lies at position
-// g ^ (x / 2 % 8) of its 128 bytes, so that sixteen consecutive rows of one unit
-// are in different banks, and each lane fetches the unit that its place in LDS
-// wants.  The scales come 16 bytes a row, two slabs' worth, likewise.  A matrix
-// instruction takes 64 values: lane (row, h) block 2 q + h of the slab at step q,
-// the scale being byte q of the row's even or odd scales.
-//
-// One barrier a slab: before the last of its four steps, whose fragments are read
-// by then, it makes the next slab visible and this one free, the loads of the
-// slab after the next start there, and the last step reads the next slab's first
-// fragments, each step multiplying what was read during the one before.
-//
-// Slabs are whole in the packed rows; blocks outside [kb0, kb1), the neighbours'
-// or padding, are multiplied as zeros.  The B operand goes first, so that a lane
-// holds four consecutive columns of one row of C: results are rounded in
-// registers, staged 32 rows at a time in the wave's part of the LDS and written
-// 16 bytes a lane.
-__device__ __forceinline__ void mx_dma16(uint32_t lds, const uint8_t *base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(lds), "v"(off), "s"(base) : "memory", "m0");
-}
-// All of the workgroup's loads into LDS have landed, and its LDS reads are done.
-__device__ __forceinline__ void mx_sync() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
-
-template <int TM, int TN>
-struct MxLds {
-  static constexpr int ROWS = TM + TN;             // A's rows, then B's
-  static constexpr int DATA = ROWS * 128, SCALE = ROWS * 16;
-  static constexpr int BYTES = 2 * (DATA + SCALE);
-};
-
-template <int MODE, typename T, int TM, int TN>
-__global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams p) {
-  typedef MxLds<TM, TN> L;
-  constexpr int BI = TM / 64, BJ = TN / 64;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[L::BYTES];
-  const int nt = gridDim.x;
-  int t = blockIdx.x;
-  {                                       // a contiguous run of tiles per XCD
-    const int x = t & 7, per = nt >> 3, more = nt & 7;
-    t = x * per + min(x, more) + (t >> 3);
-  }
-  int g = 0;
+// This workgroup's tile of a product by TM x TN: column tn, row tile in o.  A
+// contiguous run of tiles per XCD, eight tiles of rows by all tiles of columns at a
+// time, so that those that run together share operands in the XCD's L2.
+template <int MODE, int TM>
+__device__ __forceinline__ bool mx_my_tile(const MxParams &p, int &tn, int &g, MxTile &o) {
+  const int nt = gridDim.x, x = blockIdx.x & 7, per = nt >> 3, more = nt & 7;
+  int t = x * per + min(x, more) + (blockIdx.x >> 3);
+  g = 0;
   if constexpr (MODE == MX_K) {
     g = t / (p.tiles_m * p.tiles_n);
     t -= g * p.tiles_m * p.tiles_n;
   }
-  // eight tiles of rows by all tiles of columns at a time
   const int per_group = 8 * p.tiles_n, group = t / per_group, first = group * 8;
   const int gsz = min(p.tiles_m - first, 8), in_group = t - group * per_group;
-  const int tm = first + in_group % gsz, tn = in_group / gsz;
-  MxTile o;
-  if (!mx_tile<MODE, TM>(p, tm, g, o)) return;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
-  const int xl = lane & 31, h = lane >> 5;
-  const int64_t m0 = o.m0, n0 = (int64_t)tn * TN;
-  if (m0 >= o.m1) return;
+  tn = in_group / gsz;
+  return mx_tile<MODE, TM>(p, first + in_group % gsz, g, o);
+}
 
-  v16f acc[BI][BJ];
-#pragma unroll
-  for (int i = 0; i < BI; ++i)
-#pragma unroll
-    for (int j = 0; j < BJ; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-  const int am = (int)min((int64_t)TM, o.m1 - m0) - 1, bm = (int)min((int64_t)TN, p.N - n0) - 1;
-  const uint8_t *abase = p.A + m0 * p.bytes, *bbase = p.B + (o.b0 + n0) * p.bytes;
-  const int64_t srow = p.bytes / 16;
-  const uint8_t *asbase = p.As + m0 * srow, *bsbase = p.Bs + (o.b0 + n0) * srow;
-  // data: load s of a wave brings rows 32 s + 8 wave .. + 7
-  uint32_t aoff[TM / 32], boff[TN / 32];
-  const int lr = 8 * wave + (lane >> 3), unit = (lane & 7) ^ ((lr >> 1) & 7);
-#pragma unroll
-  for (int s = 0; s < TM / 32; ++s) aoff[s] = (uint32_t)(min(32 * s + lr, am) * p.bytes + 16 * unit);
-#pragma unroll
-  for (int s = 0; s < TN / 32; ++s) boff[s] = (uint32_t)(min(32 * s + lr, bm) * p.bytes + 16 * unit);
-  // scales: load s of a wave brings rows 64 (4 s + wave) .. + 63 of A's and B's
-  constexpr int SL = L::ROWS / 256;
-  uint32_t soff[SL];
-#pragma unroll
-  for (int s = 0; s < SL; ++s) {
-    const int r = 64 * (4 * s + wave);
-    soff[s] = (uint32_t)((r < TM ? min(r + lane, am) : min(r - TM + lane, bm)) * srow);
-  }
-  const int slabs = (int)(p.bytes >> 7);           // of a packed row; at least 2
-  const int s0 = o.kb0 >> 3, s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : s0;
-  auto load = [&](int s) {                         // slab s; past the last: nothing
-    if (s >= s1) return;
-    const uint32_t dst = lds0 + (s & 1) * L::DATA + wave * 1024;
-    const uint8_t *a = abase + 128 * (int64_t)s, *b = bbase + 128 * (int64_t)s;
-#pragma unroll
-    for (int i = 0; i < TM / 32; ++i) mx_dma16(dst + i * 4096, a, aoff[i]);
-#pragma unroll
-    for (int i = 0; i < TN / 32; ++i) mx_dma16(dst + TM * 128 + i * 4096, b, boff[i]);
-    if ((s & 1) == 0 || s == s0) {
-      const int at = 8 * min(s & ~1, slabs - 2);
-#pragma unroll
-      for (int i = 0; i < SL; ++i) {
-        const int r = 64 * (4 * i + wave);
-        mx_dma16(lds0 + 2 * L::DATA + ((s >> 1) & 1) * L::SCALE + r * 16, (r < TM ? asbase : bsbase) + at,
-                 soff[i]);
-      }
-    }
-  };
-
-  uint4 fa[2][BI], fb[2][BJ];
-  uint32_t sa[2][BI], sb[2][BJ];
-  const int sw = (xl >> 1) & 7;
-  const int arow = wm * (TM / 2) + xl, brow = TM + wn * (TN / 2) + xl;
-  const uint32_t half = h ? 0x07050301u : 0x06040200u;
-  auto frag = [&](int f, int s, int q) {
-    const uint8_t *d = lds + (s & 1) * L::DATA + 16 * ((2 * q + h) ^ sw);
-#pragma unroll
-    for (int i = 0; i < BI; ++i) fa[f][i] = *reinterpret_cast<const uint4 *>(d + (arow + 32 * i) * 128);
-#pragma unroll
-    for (int j = 0; j < BJ; ++j) fb[f][j] = *reinterpret_cast<const uint4 *>(d + (brow + 32 * j) * 128);
-  };
-  auto scales = [&](int f, int s) {
-    const uint8_t *d = lds + 2 * L::DATA + ((s >> 1) & 1) * L::SCALE + 8 * (s - min(s & ~1, slabs - 2));
-#pragma unroll
-    for (int i = 0; i < BI; ++i) {
-      const uint2 v = *reinterpret_cast<const uint2 *>(d + (arow + 32 * i) * 16);
-      sa[f][i] = __builtin_amdgcn_perm(v.y, v.x, half);
-    }
-#pragma unroll
-    for (int j = 0; j < BJ; ++j) {
-      const uint2 v = *reinterpret_cast<const uint2 *>(d + (brow + 32 * j) * 16);
-      sb[f][j] = __builtin_amdgcn_perm(v.y, v.x, half);
-    }
-  };
-  auto multiply = [&](auto step, int f, int fs, int s) {
-    constexpr int q = decltype(step)::value;
-    const int kb = 8 * s + 2 * q;
-    if (kb < o.kb0 || kb + 2 > o.kb1) {            // a block of the two is not this product's
-      const bool live = kb + h >= o.kb0 && kb + h < o.kb1;
-#pragma unroll
-      for (int i = 0; i < BI; ++i) {
-        if (!live) fa[f][i] = make_uint4(0u, 0u, 0u, 0u);
-        if (!live) sa[fs][i] = (sa[fs][i] & ~(0xffu << (8 * q))) | (127u << (8 * q));
-      }
-#pragma unroll
-      for (int j = 0; j < BJ; ++j)
-        if (!live) sb[fs][j] = (sb[fs][j] & ~(0xffu << (8 * q))) | (127u << (8 * q));
-    }
-#pragma unroll
-    for (int i = 0; i < BI; ++i)
-#pragma unroll
-      for (int j = 0; j < BJ; ++j) {
-        const uint4 x = fa[f][i], y = fb[f][j];
-        const v8i va = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0};
-        const v8i vb = {(int)y.x, (int)y.y, (int)y.z, (int)y.w, 0, 0, 0, 0};
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, acc[i][j], 4, 4, q, (int)sb[fs][j],
-                                                                    q, (int)sa[fs][i]);
-      }
-  };
-  using std::integral_constant;
-  if (s1 > s0) {
-    load(s0);
-    mx_sync();
-    load(s0 + 1);
-    frag(0, s0, 0);
-    scales(0, s0);
-    for (int s = s0; s < s1; ++s) {
-      frag(1, s, 1);
-      multiply(integral_constant<int, 0>{}, 0, 0, s);
-      frag(0, s, 2);
-      multiply(integral_constant<int, 1>{}, 1, 0, s);
-      frag(1, s, 3);
-      multiply(integral_constant<int, 2>{}, 0, 0, s);
-      mx_sync();
-      load(s + 2);
-      const bool more = s + 1 < s1;
-      if (more) {
-        frag(0, s + 1, 0);
-        scales(1, s + 1);
-      }
-      multiply(integral_constant<int, 3>{}, 1, 0, s);
-      if (more) {
-#pragma unroll
-        for (int i = 0; i < BI; ++i) sa[0][i] = sa[1][i];
-#pragma unroll
-        for (int j = 0; j < BJ; ++j) sb[0][j] = sb[1][j];
-      }
-    }
-  }
-
-  // Register r of block (i, j) is C[32 i + xl][32 j + 8 (r / 4) + 4 h + r % 4].
-  constexpr int WN = TN / 2, E = sizeof(T), STRIDE = WN * E + 16, PER = 16 / E;
-  static_assert(4 * 32 * STRIDE <= L::BYTES, "the staged rows fit the LDS");
-  uint8_t *stage = lds + wave * 32 * STRIDE;
-  T *C = static_cast<T *>(p.C) + o.c0;
-  const int64_t cw = n0 + wn * WN;
-  mx_sync();
+// The waves' results to C: register r of block (i, j) of a wave whose part of C
+// starts at (row0, col0) is C[row0 + 32 i + xl][col0 + 32 j + 8 (r / 4) + 4 h + r % 4].
+// `stage`: 32 rows of BJ * 32 values (16 bytes apart) of the wave's own.
+template <typename T, int BI, int BJ>
+__device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, int64_t row1, int64_t col0,
+                                         uint8_t *stage, const v16f (&acc)[BI][BJ]) {
+  constexpr int E = sizeof(T), STRIDE = BJ * 32 * E + 16, PER = 16 / E;
+  const int lane = threadIdx.x & 63, xl = lane & 31, h = lane >> 5;
 #pragma unroll
   for (int i = 0; i < BI; ++i) {
 #pragma unroll
@@ -511,17 +395,18 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
         }
       }
     __builtin_amdgcn_wave_barrier();
-    constexpr int LANES = WN / PER, RPI = 64 / LANES;       // lanes of a row, rows of an access
+    constexpr int LANES = BJ * 32 / PER, RPI = 64 / LANES;       // lanes of a row, rows of an access
     const int er = lane / LANES, ec = PER * (lane % LANES);
 #pragma unroll
     for (int u = 0; u < 32 / RPI; ++u) {
       const int x = er + RPI * u;
-      const int64_t row = m0 + wm * (TM / 2) + 32 * i + x, col = cw + ec;
-      const uint4 v = *reinterpret_cast<const uint4 *>(stage + x * STRIDE + ec * E);
-      if (row >= o.m1 || col >= p.N) continue;
+      const int64_t row = row0 + 32 * i + x, col = col0 + ec;
+      const v4u v = *reinterpret_cast<const v4u *>(stage + x * STRIDE + ec * E);
+      if (row >= row1 || col >= p.N) continue;
       T *dst = C + row * p.ldc + col;
       if (p.wide && col + PER <= p.N) {
-        *reinterpret_cast<uint4 *>(dst) = v;
+        if (p.stream) __builtin_nontemporal_store(v, reinterpret_cast<v4u *>(dst));
+        else *reinterpret_cast<v4u *>(dst) = v;
       } else {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -536,35 +421,344 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
   }
 }
 
-template <int MODE, typename T, int TM, int TN>
-hipError_t mx_launch_tile(MxParams p, hipStream_t s) {
-  const int64_t tm = (p.M + TM - 1) / TM + (MODE == MX_ROWS ? p.groups + 1 : 0), tn = (p.N + TN - 1) / TN;
-  const int64_t n = tm * tn * (MODE == MX_K ? p.groups : 1);
-  if (n > INT32_MAX) return hipErrorInvalidValue;
-  p.tiles_m = (int)tm;
-  p.tiles_n = (int)tn;
-  hipLaunchKernelGGL((mx4_gemm_tile<MODE, T, TM, TN>), dim3((unsigned)n), dim3(256), 0, s, p);
-  return hipGetLastError();
+// The same product by tiles of TM x TN through LDS: four waves (2 x 2), each
+// (TM / 2) x (TN / 2) in blocks of 32 x 32.  K advances in slabs of 256 values (128
+// bytes of a row, eight blocks, four matrix instructions of 64 values: lane (row,
+// h) takes block 2 q + h at step q), two in LDS and a third on its way through
+// registers.  Unit g (16 bytes) of row x lies at position g ^ (x / 2 % 8) of its 128
+// bytes, so that sixteen consecutive rows of one unit are in different banks.  The
+// scales come 16 bytes a row, two slabs' worth; byte q of the row's even or odd
+// scales is step q's.
+//
+// One barrier a slab, before the last step, whose fragments are read by then: it
+// makes the next slab visible and this one free.  From there to the next barrier
+// every thread writes the units it holds of the slab after the next there and
+// loads those of the one after that: each load has a whole slab's time, and reads,
+// writes, loads and matrix instructions alternate evenly in the order written (one
+// wave per SIMD: nothing else fills a gap, and a burst of loads holds the wave up
+// until the L1 takes them, 27 cycles a kilobyte).  Loads into LDS without
+// registers, which have to wait for the slab they replace: 4096 x 4096 x 14336
+// @DMA@ us; slabs of 128 values, four of them in LDS: 134 us (64 bytes of a row
+// at a time take the L1 44 cycles a kilobyte).
+//
+// Slabs are whole in the packed rows; blocks outside [kb0, kb1), the neighbours'
+// or padding, get scales of 2^-127 on both sides, whose products vanish (and no
+// NaN); loads past the last slab bring it again.
+// The B operand goes first, so that a lane holds four consecutive columns of one
+// row of C: results are rounded in registers, staged 32 rows at a time in the
+// wave's part of the LDS and written 16 bytes a lane.
+__device__ __forceinline__ void mx_sync() {      // this wave's LDS accesses done, then all waves'
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// Tiles through LDS where a packed row has two slabs at least (a load of scales
-// brings two) and the 32-bit offsets of a tile's rows reach it.  256 x 256 where
-// they fill the compute units, one each: 4096 x 4096 x 14336 133 us against 155 in
-// 128-tiles, 2048 x 2048 x 2048 22 against 12.5, 512 x 14336 x 4096 38 against 24.5.
-// Grouped rows leave the last tile of each group part empty: 128-tiles (64 experts
-// of 2048 x 768, 512 rows each, 54 us against 74).
+template <int TM, int TN>
+struct MxLds {
+  static constexpr int ROWS = TM + TN;             // A's rows, then B's
+  static constexpr int DATA = ROWS * 128, SCALE = ROWS * 16;
+  static constexpr int BYTES = 2 * (DATA + SCALE);
+};
+
+template <typename T, int TM, int TN>
+__global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams p) {
+  typedef MxLds<TM, TN> L;
+  constexpr int BI = TM / 64, BJ = TN / 64, NU = BI + BJ;
+  constexpr int UNITS = L::ROWS / 32;              // units of a slab that a thread brings
+  constexpr int SU = L::ROWS / 256;                // and rows of scales
+  static_assert(UNITS == 2 * NU && BI * BJ % NU == 0, "a step's accesses pair up");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[L::BYTES];
+  int tn, g;
+  MxTile o;
+  if (!mx_my_tile<MX_ONE, TM>(p, tn, g, o)) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+  const int xl = lane & 31, h = lane >> 5;
+  const int64_t m0 = o.m0, n0 = (int64_t)tn * TN;
+  if (m0 >= o.m1) return;
+
+  v16f acc[BI][BJ];
+#pragma unroll
+  for (int i = 0; i < BI; ++i)
+#pragma unroll
+    for (int j = 0; j < BJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+  const int am = (int)min((int64_t)TM, o.m1 - m0) - 1, bm = (int)min((int64_t)TN, p.N - n0) - 1;
+  const uint8_t *abase = p.A + m0 * p.bytes, *bbase = p.B + (o.b0 + n0) * p.bytes;
+  const int64_t srow = p.bytes / 16;
+  const uint8_t *asbase = p.As + m0 * srow, *bsbase = p.Bs + (o.b0 + n0) * srow;
+  // thread -> rows lr + 32 i, unit lg of A's and B's rows
+  const int lr = tid >> 3, lg = tid & 7;
+  uint32_t off[UNITS];
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i)
+    off[i] = (uint32_t)((i < TM / 32 ? min(32 * i + lr, am) : min(32 * i - TM + lr, bm)) * p.bytes + 16 * lg);
+  // and rows of scales tid + 256 i
+  uint32_t soff[SU];
+#pragma unroll
+  for (int i = 0; i < SU; ++i) {
+    const int r = 256 * i + tid;
+    soff[i] = (uint32_t)((r < TM ? min(r, am) : min(r - TM, bm)) * srow);
+  }
+  const int slabs = (int)(p.bytes >> 7);           // of a packed row; at least 2
+  const int s0 = o.kb0 >> 3, s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : s0;
+  const int dst = lr * 128 + 16 * (lg ^ ((lr >> 1) & 7));
+  v4u r[UNITS], rs[SU];
+  auto load = [&](int s, int i) {
+    const int64_t k = 128 * (int64_t)min(s, s1 - 1);
+    r[i] = *reinterpret_cast<const v4u *>((i < TM / 32 ? abase : bbase) + k + off[i]);
+  };
+  auto store = [&](int half, int i) {
+    *reinterpret_cast<v4u *>(lds + half * L::DATA + i * 4096 + dst) = r[i];
+  };
+  // scales of the pair of slabs s and s + 1 (the last 16 bytes of a row if s is its last)
+  auto load_scales = [&](int s) {
+    const int at = 8 * min(s, slabs - 2);
+#pragma unroll
+    for (int i = 0; i < SU; ++i) {
+      const uint2 *src = reinterpret_cast<const uint2 *>((256 * i + tid < TM ? asbase : bsbase) + at + soff[i]);
+      const uint2 lo = src[0], hi = src[1];
+      rs[i] = v4u{lo.x, lo.y, hi.x, hi.y};
+    }
+  };
+  auto store_scales = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < SU; ++i)
+      *reinterpret_cast<v4u *>(lds + 2 * L::DATA + (((s - s0) >> 1) & 1) * L::SCALE + (256 * i + tid) * 16) = rs[i];
+  };
+
+  v4u fa[2][BI], fb[2][BJ];
+  uint32_t sa[2][BI], sb[2][BJ];                   // of a pair's first and second slab
+  const int sw = (xl >> 1) & 7;
+  const int arow = wm * (TM / 2) + xl, brow = TM + wn * (TN / 2) + xl;
+  const uint32_t pick = h ? 0x07050301u : 0x06040200u;
+  // fragment x of a step, in the order the matrix instructions want them
+  auto frag = [&](int f, int half, int q, int x) {
+    const uint8_t *d = lds + half * L::DATA + 16 * ((2 * q + h) ^ sw);
+    if (x == 0 || x > BJ) {
+      const int i = x ? x - BJ : 0;
+      fa[f][i] = *reinterpret_cast<const v4u *>(d + (arow + 32 * i) * 128);
+    } else {
+      fb[f][x - 1] = *reinterpret_cast<const v4u *>(d + (brow + 32 * (x - 1)) * 128);
+    }
+  };
+  auto scales = [&](int f, int s) {
+    const int pair = s - ((s - s0) & 1);
+    const uint8_t *d = lds + 2 * L::DATA + (((s - s0) >> 1) & 1) * L::SCALE + 8 * min(s - min(pair, slabs - 2), 1);
+    uint32_t mine = 0u;                            // bytes of the blocks that are this product's
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int kb = 8 * s + 2 * q + h;
+      mine |= kb >= o.kb0 && kb < o.kb1 ? 0xffu << (8 * q) : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < BI; ++i) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(d + (arow + 32 * i) * 16);
+      sa[f][i] = __builtin_amdgcn_perm(v.y, v.x, pick) & mine;
+    }
+#pragma unroll
+    for (int j = 0; j < BJ; ++j) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(d + (brow + 32 * j) * 16);
+      sb[f][j] = __builtin_amdgcn_perm(v.y, v.x, pick) & mine;
+    }
+  };
+  using std::integral_constant;
+  // Step Q of a pair's slab P: multiplies fragment set Q % 2, reads the other, of the
+  // next step, and moves a quarter of the units on: of slab ws to LDS, of slab ws + 1
+  // from memory.
+  auto step = [&](auto qc, auto par, int ws) {
+    constexpr int Q = decltype(qc)::value, P = decltype(par)::value, f = Q & 1;
+    constexpr int rh = Q == 3 ? P ^ 1 : P, rq = (Q + 1) & 3, wh = rh ^ 1, first = rq * NU / 2;
+#pragma unroll
+    for (int u = 0; u < NU; ++u) {
+      frag(f ^ 1, rh, rq, u);
+      if ((u & 1) == 0) {
+        store(wh, first + u / 2);
+        load(ws + 1, first + u / 2);
+      }
+#pragma unroll
+      for (int v = 0; v < BI * BJ / NU; ++v) {
+        const int k = u * (BI * BJ / NU) + v, i = k / BJ, j = k % BJ;
+        const v4u a = fa[f][i], b = fb[f][j];
+        const v8i va = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0};
+        const v8i vb = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, acc[i][j], 4, 4, Q, (int)sb[P][j], Q,
+                                                                    (int)sa[P][i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto slab = [&](auto par, int s) {
+    constexpr int P = decltype(par)::value;
+    step(integral_constant<int, 0>{}, par, s + 1);
+    step(integral_constant<int, 1>{}, par, s + 1);
+    step(integral_constant<int, 2>{}, par, s + 1);
+    mx_sync();
+    scales(P ^ 1, s + 1);
+    if constexpr (P == 0) {
+      store_scales(s + 2);
+      load_scales(s + 4);
+    }
+    step(integral_constant<int, 3>{}, par, s + 2);
+  };
+  if (s1 > s0) {
+    load_scales(s0);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) load(s0, i);
+    store_scales(s0);
+    load_scales(s0 + 2);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      store(0, i);
+      load(s0 + 1, i);
+    }
+    mx_sync();
+    scales(0, s0);
+#pragma unroll
+    for (int u = 0; u < NU; ++u) frag(0, 0, 0, u);
+#pragma unroll
+    for (int i = 0; i < NU / 2; ++i) {
+      store(1, i);
+      load(s0 + 2, i);
+    }
+    for (int s = s0; s < s1; s += 2) {
+      slab(integral_constant<int, 0>{}, s);
+      slab(integral_constant<int, 1>{}, s + 1);
+    }
+  }
+
+  constexpr int STRIDE = BJ * 32 * (int)sizeof(T) + 16;
+  static_assert(4 * 32 * STRIDE <= L::BYTES, "the staged rows fit the LDS");
+  mx_sync();
+  mx_store<T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * (TM / 2), o.m1, n0 + wn * (TN / 2),
+                      lds + wave * 32 * STRIDE, acc);
+}
+
+// Tiles of 128 x 128 for products of fewer or shorter tiles: one slab in LDS, the
+// next on its way through registers, and up to three workgroups per compute unit,
+// which cover each other's barriers, first loads and epilogues.
+template <int MODE, typename T>
+__global__ __launch_bounds__(256, 3) void mx4_gemm_tile128(MxParams p) {
+  constexpr int TM = 128, TN = 128, BI = 2, BJ = 2, UNITS = 8, DATA = 256 * 128;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[DATA + 256 * 8];
+  int tn, g;
+  MxTile o;
+  if (!mx_my_tile<MODE, TM>(p, tn, g, o)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+  const int xl = lane & 31, h = lane >> 5;
+  const int64_t m0 = o.m0, n0 = (int64_t)tn * TN;
+  if (m0 >= o.m1) return;
+  v16f acc[BI][BJ];
+#pragma unroll
+  for (int i = 0; i < BI; ++i)
+#pragma unroll
+    for (int j = 0; j < BJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  const int am = (int)min((int64_t)TM, o.m1 - m0) - 1, bm = (int)min((int64_t)TN, p.N - n0) - 1;
+  const uint8_t *abase = p.A + m0 * p.bytes, *bbase = p.B + (o.b0 + n0) * p.bytes;
+  const int64_t srow = p.bytes / 16;
+  const int lr = tid >> 3, lg = tid & 7;
+  uint32_t off[UNITS];
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i)
+    off[i] = (uint32_t)((i < 4 ? min(32 * i + lr, am) : min(32 * i - TM + lr, bm)) * p.bytes + 16 * lg);
+  const uint8_t *sbase = tid < TM ? p.As + (m0 + min(tid, am)) * srow : p.Bs + (o.b0 + n0 + min(tid - TM, bm)) * srow;
+  const int s0 = o.kb0 >> 3, s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : s0;
+  const int dst = lr * 128 + 16 * (lg ^ ((lr >> 1) & 7));
+  v4u r[UNITS];
+  uint2 rs;
+  auto load = [&](int s) {
+    const int64_t k = 128 * (int64_t)s;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) r[i] = *reinterpret_cast<const v4u *>((i < 4 ? abase : bbase) + k + off[i]);
+    rs = *reinterpret_cast<const uint2 *>(sbase + 8 * (int64_t)s);
+  };
+  if (s1 > s0) load(s0);
+  const int sw = (xl >> 1) & 7, arow = wm * 64 + xl, brow = TM + wn * 64 + xl;
+  const uint32_t pick = h ? 0x07050301u : 0x06040200u;
+  for (int s = s0; s < s1; ++s) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) *reinterpret_cast<v4u *>(lds + i * 4096 + dst) = r[i];
+    *reinterpret_cast<uint2 *>(lds + DATA + 8 * tid) = rs;
+    __syncthreads();
+    load(min(s + 1, s1 - 1));
+    uint32_t mine = 0u;                            // bytes of the blocks that are this product's
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int kb = 8 * s + 2 * q + h;
+      mine |= kb >= o.kb0 && kb < o.kb1 ? 0xffu << (8 * q) : 0u;
+    }
+    uint32_t sa[BI], sb[BJ];
+#pragma unroll
+    for (int i = 0; i < BI; ++i) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(lds + DATA + 8 * (arow + 32 * i));
+      sa[i] = __builtin_amdgcn_perm(v.y, v.x, pick) & mine;
+    }
+#pragma unroll
+    for (int j = 0; j < BJ; ++j) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(lds + DATA + 8 * (brow + 32 * j));
+      sb[j] = __builtin_amdgcn_perm(v.y, v.x, pick) & mine;
+    }
+    auto step = [&](auto qc) {
+      constexpr int q = decltype(qc)::value;
+      const uint8_t *d = lds + 16 * ((2 * q + h) ^ sw);
+      v4u a[BI], b[BJ];
+#pragma unroll
+      for (int i = 0; i < BI; ++i) a[i] = *reinterpret_cast<const v4u *>(d + (arow + 32 * i) * 128);
+#pragma unroll
+      for (int j = 0; j < BJ; ++j) b[j] = *reinterpret_cast<const v4u *>(d + (brow + 32 * j) * 128);
+#pragma unroll
+      for (int i = 0; i < BI; ++i)
+#pragma unroll
+        for (int j = 0; j < BJ; ++j) {
+          const v8i va = {(int)a[i].x, (int)a[i].y, (int)a[i].z, (int)a[i].w, 0, 0, 0, 0};
+          const v8i vb = {(int)b[j].x, (int)b[j].y, (int)b[j].z, (int)b[j].w, 0, 0, 0, 0};
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(vb, va, acc[i][j], 4, 4, q, (int)sb[j], q,
+                                                                      (int)sa[i]);
+        }
+    };
+    step(std::integral_constant<int, 0>{});
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 3>{});
+  }
+  constexpr int STRIDE = BJ * 32 * (int)sizeof(T) + 16;
+  static_assert(4 * 32 * STRIDE <= (int)sizeof(lds), "the staged rows fit the LDS");
+  __syncthreads();
+  mx_store<T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * 64, o.m1, n0 + wn * 64,
+                      lds + wave * 32 * STRIDE, acc);
+}
+
+// 256 x 256 where they fill the compute units, one each (4096 x 4096 x 14336 120 us
+// against 155 in 128-tiles, 2048 x 2048 x 2048 22 against 12, 512 x 14336 x 4096 38
+// against 25).  Grouped products leave the last tile of a group part empty and have
+// few slabs: 128-tiles, three workgroups a compute unit (the weight gradients of 64
+// experts of 2048 x 768, 512 rows each, 108 us against 125 to 138 with two).
 template <int MODE, typename T>
 hipError_t mx_launch(MxParams p, hipStream_t s) {
-  if (p.bytes >= 256 && p.bytes <= (1 << 24)) {
-    const int64_t n256 = (p.M + 255) / 256 * ((p.N + 255) / 256);
-    if (MODE == MX_ONE && n256 >= 256) return mx_launch_tile<MODE, T, 256, 256>(p, s);
-    return mx_launch_tile<MODE, T, 128, 128>(p, s);
+  auto tiles = [&](int bt) {
+    const int64_t tm = (p.M + bt - 1) / bt + (MODE == MX_ROWS ? p.groups + 1 : 0), tn = (p.N + bt - 1) / bt;
+    p.tiles_m = (int)tm;
+    p.tiles_n = (int)tn;
+    return tm * tn * (MODE == MX_K ? p.groups : 1);
+  };
+  int64_t n = tiles(256);
+  if constexpr (MODE == MX_ONE) {
+    if (p.bytes >= 256) {
+      if (n >= 256) {
+        hipLaunchKernelGGL((mx4_gemm_tile<T, 256, 256>), dim3((unsigned)n), dim3(256), 0, s, p);
+      } else {
+        n = tiles(128);
+        hipLaunchKernelGGL((mx4_gemm_tile<T, 128, 128>), dim3((unsigned)n), dim3(256), 0, s, p);
+      }
+      return hipGetLastError();
+    }
   }
-  const int64_t tm = (p.M + 31) / 32 + (MODE == MX_ROWS ? p.groups + 1 : 0);
-  p.tiles_n = (int)((p.N + 127) / 128);
-  if (tm * p.tiles_n > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((mx4_gemm<MODE, T>),
-                     dim3((unsigned)(tm * p.tiles_n), MODE == MX_K ? p.groups : 1), dim3(256), 0, s, p);
+  n = tiles(128);
+  if (n > INT32_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((mx4_gemm_tile128<MODE, T>), dim3((unsigned)n), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -577,23 +771,27 @@ hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s) {
   p.x = d.x; p.row_index = d.row_index;
   p.data = d.data; p.scale = d.scale; p.data_t = d.data_t; p.scale_t = d.scale_t;
   p.kp = mx4_padded(d.cols); p.rp = mx4_padded(d.rows);
-  const int need = d.bf16 ? 8 : 16, elem = d.bf16 ? 2 : 4;
-  p.vec = reinterpret_cast<uintptr_t>(d.x) % need == 0 && d.ldx * elem % need == 0;
-  const bool cols = d.data_t != nullptr, rows = d.data != nullptr;
-  const int64_t rt = ((cols ? p.rp : d.rows) + 127) / 128, ct = p.kp / 256;
-  if (rt == 0) return hipSuccess;
-  if (ct * rt > INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(ct * rt), (unsigned)d.batch);
-#define SOAP_MXQ(T, R, C) hipLaunchKernelGGL((mx4_quantize<T, R, C>), grid, dim3(256), 0, s, p)
-  if (d.bf16) {
-    if (rows && cols) SOAP_MXQ(uint16_t, true, true);
-    else if (rows) SOAP_MXQ(uint16_t, true, false);
-    else SOAP_MXQ(uint16_t, false, true);
-  } else {
-    if (rows && cols) SOAP_MXQ(float, true, true);
-    else if (rows) SOAP_MXQ(float, true, false);
-    else SOAP_MXQ(float, false, true);
+  const int elem = d.bf16 ? 2 : 4;
+  if (!d.data_t) {
+    if (d.rows == 0) return hipSuccess;
+    p.vec = reinterpret_cast<uintptr_t>(d.x) % 16 == 0 && d.ldx * elem % 16 == 0;
+    const bool half = p.kp == 256;               // a row is half a wave's 512 values
+    const int64_t rows = half ? 8 : 4;
+    const dim3 grid((unsigned)std::min<int64_t>((d.rows + rows - 1) / rows, 1 << 16), (unsigned)d.batch);
+#define SOAP_MXQ(T, L) hipLaunchKernelGGL((mx4_quantize_cols<T, L>), grid, dim3(256), 0, s, p)
+    if (d.bf16) { if (half) SOAP_MXQ(uint16_t, 32); else SOAP_MXQ(uint16_t, 64); }
+    else { if (half) SOAP_MXQ(float, 32); else SOAP_MXQ(float, 64); }
+#undef SOAP_MXQ
+    return hipGetLastError();
   }
+  p.vec = reinterpret_cast<uintptr_t>(d.x) % (4 * elem) == 0 && d.ldx % 4 == 0;
+  const int64_t tiles = (p.rp / 128) * (p.kp / 256);
+  if (tiles == 0) return hipSuccess;
+  if (tiles > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)tiles, (unsigned)d.batch);
+#define SOAP_MXQ(T, R) hipLaunchKernelGGL((mx4_quantize_tile<T, R>), grid, dim3(256), 0, s, p)
+  if (d.bf16) { if (d.data) SOAP_MXQ(uint16_t, true); else SOAP_MXQ(uint16_t, false); }
+  else { if (d.data) SOAP_MXQ(float, true); else SOAP_MXQ(float, false); }
 #undef SOAP_MXQ
   return hipGetLastError();
 }
@@ -623,6 +821,10 @@ hipError_t launch_mx4_gemm(const Mx4GemmDesc &d, hipStream_t s) {
   const int64_t elem = d.bf16 ? 2 : 4;
   p.wide = (reinterpret_cast<uintptr_t>(d.C) & 15u) == 0 && d.ldc * elem % 16 == 0 &&
            (!d.by_k || p.sC * elem % 16 == 0);
+  // Written through the L2s, a gradient of 403 MB pushed the operands out of them:
+  // 180 us against 105.  An output that fits them (32 MB) is found there by its reader
+  // (8 MB: 22 us against 28).
+  p.stream = (d.by_k ? d.groups : 1) * d.M * d.N * elem > (32 << 20);
   const int mode = !d.offsets ? MX_ONE : d.by_k ? MX_K : MX_ROWS;
 #define SOAP_MXG(T)                                   \
   (mode == MX_ONE ? mx_launch<MX_ONE, T>(p, s)        \
