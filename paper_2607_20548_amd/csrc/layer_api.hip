@@ -99,12 +99,14 @@ int check_router(int64_t tokens, int64_t experts, int64_t top_k, int dtype, int6
   return SOAP_OK;
 }
 
-// Shared by the products; c_bytes: the range of C.
-int check_product(int64_t groups, int64_t M, int64_t N, int64_t K, bool grouped, const int32_t *offsets,
+// Shared by the products; tile_groups: groups that have all M rows each; c_bytes: the
+// range of C.
+int check_product(int64_t groups, int64_t tile_groups, int64_t M, int64_t N, int64_t K, bool grouped,
+                  const int32_t *offsets,
                   const uint8_t *ad, const uint8_t *as, int64_t b_rows, const uint8_t *bd,
                   const uint8_t *bs, int dtype, void *C, size_t c_bytes) {
   SOAP_TRY(check_dtype(dtype));
-  SOAP_TRY(check_range("tiles of 128 x 128", (M / 128 + groups + 2) * ((N + 127) / 128), 0, INT32_MAX));
+  SOAP_TRY(check_range("tiles of 128 x 128", (M / 128 * tile_groups + 4 * groups + 64) * ((N + 127) / 128), 0, INT32_MAX));
   return check_bufs({{offsets, grouped ? 4 * (size_t)(groups + 1) : 0, "offsets", false, true, 4},
                      {ad, soap_mx4_data_bytes(M, K), "a_data", false, true, 16},
                      {as, soap_mx4_scale_bytes(M, K), "a_scale", false, true, 16},
@@ -310,7 +312,7 @@ int soap_mx4_gemm(int64_t M, int64_t N, int64_t K, const uint8_t *a_data, const 
   SOAP_TRY(check_range("N", N, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_range("K", K, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_ld("ldc", ldc, N));
-  SOAP_TRY(check_product(1, M, N, K, false, nullptr, a_data, a_scale, N, b_data, b_scale, dtype, C,
+  SOAP_TRY(check_product(1, 1, M, N, K, false, nullptr, a_data, a_scale, N, b_data, b_scale, dtype, C,
                          span(M, N, ldc, elem(dtype))));
   soap::Mx4GemmDesc d;
   d.M = M; d.N = N; d.K = K; d.ldc = ldc; d.bf16 = dtype == SOAP_BF16;
@@ -326,7 +328,7 @@ int soap_mx4_gemm_rows(int64_t groups, int64_t M, int64_t N, int64_t K, const in
   SOAP_TRY(check_range("N", N, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_range("K", K, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_ld("ldc", ldc, N));
-  SOAP_TRY(check_product(groups, M, N, K, true, offsets, a_data, a_scale, groups * N, b_data, b_scale,
+  SOAP_TRY(check_product(groups, 1, M, N, K, true, offsets, a_data, a_scale, groups * N, b_data, b_scale,
                          dtype, C, span(M, N, ldc, elem(dtype))));
   soap::Mx4GemmDesc d;
   d.groups = groups; d.M = M; d.N = N; d.K = K; d.ldc = ldc; d.bf16 = dtype == SOAP_BF16;
@@ -341,7 +343,7 @@ int soap_mx4_gemm_k(int64_t groups, int64_t M, int64_t N, int64_t K, const int32
   SOAP_TRY(check_range("M", M, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_range("N", N, 1, SOAP_MAX_ROWS));
   SOAP_TRY(check_range("K", K, 0, 2 * SOAP_MAX_ROWS));
-  SOAP_TRY(check_product(groups, M, N, K, true, offsets, a_data, a_scale, N, b_data, b_scale, dtype, C,
+  SOAP_TRY(check_product(groups, groups, M, N, K, true, offsets, a_data, a_scale, N, b_data, b_scale, dtype, C,
                          elem(dtype) * (size_t)groups * (size_t)M * (size_t)N));
   soap::Mx4GemmDesc d;
   d.groups = groups; d.M = M; d.N = N; d.K = K; d.ldc = N; d.by_k = true; d.bf16 = dtype == SOAP_BF16;

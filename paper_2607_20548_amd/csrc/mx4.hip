@@ -284,13 +284,13 @@ struct MxParams {
   int64_t bytes;              // data bytes of a packed row (16 a block); scales: bytes / 16
   int groups, tiles_m, tiles_n;
   int wide;                   // C can be written 16 bytes at a time
-  int stream;                 // and is too large for the L2s: kept out of them
   const int *offsets;
   const uint8_t *A, *As, *B, *Bs;
   void *C;
 };
 
 enum { MX_ONE = 0, MX_ROWS = 1, MX_K = 2 };
+constexpr int MX_DEAL = 4;    // tiles of rows that grouped products deal to an XCD at a time
 
 // A tile's part of the problem: rows [m0, m1) of A and C, B's first row, blocks
 // [kb0, kb1), C's first element.  Offsets are clamped into the matrix.
@@ -349,28 +349,38 @@ __device__ __forceinline__ bool mx_tile(const MxParams &p, int64_t t, int g, MxT
   return true;
 }
 
-// This workgroup's tile of a product by TM x TN: column tn, row tile in o.  A
-// contiguous run of tiles per XCD, eight tiles of rows by all tiles of columns at a
-// time, so that those that run together share operands in the XCD's L2.
+// This workgroup's tile of a product by TM x TN: column tn, row tile in o.  Tiles
+// that run together share operands in their XCD's L2: one product gives every XCD a
+// contiguous run of tiles, eight tiles of rows by all tiles of columns at a time;
+// groups, whose sizes differ (and whose last tiles may be none), are dealt to the
+// XCDs in turn, four tiles of rows by all of columns.
 template <int MODE, int TM>
 __device__ __forceinline__ bool mx_my_tile(const MxParams &p, int &tn, int &g, MxTile &o) {
-  const int nt = gridDim.x, x = blockIdx.x & 7, per = nt >> 3, more = nt & 7;
-  int t = x * per + min(x, more) + (blockIdx.x >> 3);
+  const int x = blockIdx.x & 7, i = blockIdx.x >> 3;
   g = 0;
-  if constexpr (MODE == MX_K) {
-    g = t / (p.tiles_m * p.tiles_n);
-    t -= g * p.tiles_m * p.tiles_n;
+  int tm;
+  if constexpr (MODE == MX_ONE) {
+    const int nt = gridDim.x, per = nt >> 3, more = nt & 7, t = x * per + min(x, more) + i;
+    const int per_group = 8 * p.tiles_n, group = t / per_group, first = group * 8;
+    const int gsz = min(p.tiles_m - first, 8), in_group = t - group * per_group;
+    tn = in_group / gsz;
+    tm = first + in_group % gsz;
+  } else {
+    const int per = MX_DEAL * p.tiles_n, in = i % per, c = (i / per) * 8 + x;
+    const int deals = (p.tiles_m + MX_DEAL - 1) / MX_DEAL;
+    g = c / deals;
+    tm = (c - g * deals) * MX_DEAL + in % MX_DEAL;
+    tn = in / MX_DEAL;
+    if (g >= (MODE == MX_K ? p.groups : 1) || tm >= p.tiles_m) return false;
   }
-  const int per_group = 8 * p.tiles_n, group = t / per_group, first = group * 8;
-  const int gsz = min(p.tiles_m - first, 8), in_group = t - group * per_group;
-  tn = in_group / gsz;
-  return mx_tile<MODE, TM>(p, first + in_group % gsz, g, o);
+  return mx_tile<MODE, TM>(p, tm, g, o);
 }
 
 // The waves' results to C: register r of block (i, j) of a wave whose part of C
 // starts at (row0, col0) is C[row0 + 32 i + xl][col0 + 32 j + 8 (r / 4) + 4 h + r % 4].
-// `stage`: 32 rows of BJ * 32 values (16 bytes apart) of the wave's own.
-template <typename T, int BI, int BJ>
+// `stage`: 32 rows of BJ * 32 values (16 bytes apart) of the wave's own.  STREAM: C is
+// kept out of the L2s.
+template <bool STREAM, typename T, int BI, int BJ>
 __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, int64_t row1, int64_t col0,
                                          uint8_t *stage, const v16f (&acc)[BI][BJ]) {
   constexpr int E = sizeof(T), STRIDE = BJ * 32 * E + 16, PER = 16 / E;
@@ -405,7 +415,7 @@ __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, 
       if (row >= row1 || col >= p.N) continue;
       T *dst = C + row * p.ldc + col;
       if (p.wide && col + PER <= p.N) {
-        if (p.stream) __builtin_nontemporal_store(v, reinterpret_cast<v4u *>(dst));
+        if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<v4u *>(dst));
         else *reinterpret_cast<v4u *>(dst) = v;
       } else {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -630,14 +640,14 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
   constexpr int STRIDE = BJ * 32 * (int)sizeof(T) + 16;
   static_assert(4 * 32 * STRIDE <= L::BYTES, "the staged rows fit the LDS");
   mx_sync();
-  mx_store<T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * (TM / 2), o.m1, n0 + wn * (TN / 2),
+  mx_store<TM == 256, T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * (TM / 2), o.m1, n0 + wn * (TN / 2),
                       lds + wave * 32 * STRIDE, acc);
 }
 
 // Tiles of 128 x 128 for products of fewer or shorter tiles: one slab in LDS, the
 // next on its way through registers, and up to three workgroups per compute unit,
 // which cover each other's barriers, first loads and epilogues.
-template <int MODE, typename T>
+template <int MODE, typename T, bool STREAM>
 __global__ __launch_bounds__(256, 3) void mx4_gemm_tile128(MxParams p) {
   constexpr int TM = 128, TN = 128, BI = 2, BJ = 2, UNITS = 8, DATA = 256 * 128;
   __shared__ __attribute__((aligned(16))) uint8_t lds[DATA + 256 * 8];
@@ -727,9 +737,14 @@ __global__ __launch_bounds__(256, 3) void mx4_gemm_tile128(MxParams p) {
   constexpr int STRIDE = BJ * 32 * (int)sizeof(T) + 16;
   static_assert(4 * 32 * STRIDE <= (int)sizeof(lds), "the staged rows fit the LDS");
   __syncthreads();
-  mx_store<T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * 64, o.m1, n0 + wn * 64,
+  mx_store<STREAM, T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * 64, o.m1, n0 + wn * 64,
                       lds + wave * 32 * STRIDE, acc);
 }
+
+// Gradients larger than the L2s (32 MB) are written past them: through them, one of
+// 403 MB pushed its operands out, 180 us against 105; one that fits is found there by
+// its reader.  The outputs of 256-tiles are at least as large.
+constexpr int64_t MX_L2 = 32 << 20;
 
 // 256 x 256 where they fill the compute units, one each (4096 x 4096 x 14336 120 us
 // against 155 in 128-tiles, 2048 x 2048 x 2048 22 against 12, 512 x 14336 x 4096 38
@@ -742,7 +757,9 @@ hipError_t mx_launch(MxParams p, hipStream_t s) {
     const int64_t tm = (p.M + bt - 1) / bt + (MODE == MX_ROWS ? p.groups + 1 : 0), tn = (p.N + bt - 1) / bt;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
-    return tm * tn * (MODE == MX_K ? p.groups : 1);
+    if constexpr (MODE == MX_ONE) return tm * tn;
+    const int64_t deals = (tm + MX_DEAL - 1) / MX_DEAL * (MODE == MX_K ? p.groups : 1);
+    return (deals + 7) / 8 * 8 * MX_DEAL * tn;
   };
   int64_t n = tiles(256);
   if constexpr (MODE == MX_ONE) {
@@ -758,7 +775,13 @@ hipError_t mx_launch(MxParams p, hipStream_t s) {
   }
   n = tiles(128);
   if (n > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((mx4_gemm_tile128<MODE, T>), dim3((unsigned)n), dim3(256), 0, s, p);
+  if constexpr (MODE == MX_K) {
+    if (p.groups * p.sC * (int64_t)sizeof(T) > MX_L2) {
+      hipLaunchKernelGGL((mx4_gemm_tile128<MODE, T, true>), dim3((unsigned)n), dim3(256), 0, s, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((mx4_gemm_tile128<MODE, T, false>), dim3((unsigned)n), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -821,10 +844,6 @@ hipError_t launch_mx4_gemm(const Mx4GemmDesc &d, hipStream_t s) {
   const int64_t elem = d.bf16 ? 2 : 4;
   p.wide = (reinterpret_cast<uintptr_t>(d.C) & 15u) == 0 && d.ldc * elem % 16 == 0 &&
            (!d.by_k || p.sC * elem % 16 == 0);
-  // Written through the L2s, a gradient of 403 MB pushed the operands out of them:
-  // 180 us against 105.  An output that fits them (32 MB) is found there by its reader
-  // (8 MB: 22 us against 28).
-  p.stream = (d.by_k ? d.groups : 1) * d.M * d.N * elem > (32 << 20);
   const int mode = !d.offsets ? MX_ONE : d.by_k ? MX_K : MX_ROWS;
 #define SOAP_MXG(T)                                   \
   (mode == MX_ONE ? mx_launch<MX_ONE, T>(p, s)        \
