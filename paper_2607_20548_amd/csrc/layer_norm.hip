@@ -7,27 +7,44 @@
 // All statistics and sums are fp32; a bfloat16 output is rounded once.
 //
 // Both are bound by HBM (2 and 3 values moved per element), so a row is read
-// once: a group of GROUP threads (8 lanes to a workgroup) holds it in
-// registers, V values per thread, and takes the mean, the centred sum of
-// squares and, backward, the two dot products from there.  Unit u of a thread
-// covers the VEC consecutive columns from (u GROUP + thread) VEC on, VEC values
-// being 16 bytes where the operands allow it and one otherwise.  Workgroups
-// walk over the rows and keep the weight (and the sums of dw, db over their
-// rows) in registers.
+// once: a group of GROUP threads (8 lanes to a workgroup) holds it in registers, V
+// values per thread, and takes the mean, the centred sum of squares and,
+// backward, the two dot products from there.  Unit u of a thread covers the VEC
+// consecutive columns from (u GROUP + thread) VEC on, 16 bytes, read and written at
+// once wherever the whole unit is inside the row (rows need no alignment past that
+// of an element) and value by value in the unit that crosses its end.  Workgroups
+// walk over the rows, keep the weight (and the sums of dw, db over their rows) in
+// registers and load their next row before they reduce the present one.
+//
+// Groups of a whole workgroup meet once per row: the variance is put together from
+// the waves' own means and squares about them.  Measured: 16384 x 4096 bfloat16 53 us
+// forward and 77 backward (5.1 and 5.2 TB/s; a copy of 1 GiB reaches 5.2), without the
+// row ahead and with two meetings 76 and 103.
 //
 // dw and db: every workgroup writes the sums over its rows, a second kernel
 // adds these partial sums in a fixed order, so results do not vary between
 // runs.
 #include "internal.h"
+#include "lanes.h"
 
 #include <algorithm>
 
 namespace soap {
 namespace {
 
-constexpr int64_t LN_BLOCKS_FWD = 2048;  // workgroups of a forward launch at most
-constexpr int64_t LN_BLOCKS_BWD = 512;   // of a backward launch: rows of partial sums
-constexpr int LN_FIN = 1024;             // threads of the second kernel: 64 columns x 16 slices
+// Workgroups of a launch at most.  Backward they are the rows of partial sums: two
+// for every compute unit where more than one fits it (16384 x 4096 bfloat16 77 us;
+// 256 workgroups 93, 768 79, 1024 90), one past 4096 columns (8192 x 8192 fp32 146 us
+// against 156 with 512, 4096 x 16384 bfloat16 92 against 102).
+constexpr int64_t LN_BLOCKS_FWD = 1024;
+int64_t ln_blocks_bwd(int64_t cols) { return cols <= 4096 ? 512 : 256; }
+constexpr int LN_FIN = 1024;             // threads of the second kernel,
+constexpr int LN_FIN_COLS = 32;          // 32 columns x 32 slices
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
 
 struct LnParams {
   int64_t rows;
@@ -42,80 +59,97 @@ struct LnParams {
   float *part;   // [workgroup][2][cols]: dw, db
 };
 
-__device__ __forceinline__ float ln_bf16(uint32_t h) { return __uint_as_float(h << 16); }
+// Values of a unit of 16 bytes.
+template <typename T>
+constexpr int ln_vec() { return 16 / (int)sizeof(T); }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void ln_load(const T *p, float *v) {
-  if constexpr (sizeof(T) == 4 && VEC == 4) {
-    const float4 q = *reinterpret_cast<const float4 *>(p);
-    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
-  } else if constexpr (sizeof(T) == 2 && VEC == 8) {
-    const uint4 q = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+// The unit at column col of a row, zeros past its end.
+template <typename T>
+__device__ __forceinline__ v4u ln_load(const T *row, int col, int cols) {
+  if (col + ln_vec<T>() <= cols) return *reinterpret_cast<const v4u_any *>(row + col);
+  v4u q = v4u(0u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = ln_bf16(w[i] & 0xffffu);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  for (int i = 0; i < ln_vec<T>(); ++i)
+    if (col + i < cols) {
+      if constexpr (sizeof(T) == 4) q[i] = __float_as_uint(row[col + i]);
+      else q[i / 2] |= (uint32_t)row[col + i] << (16 * (i & 1));
     }
-  } else if constexpr (sizeof(T) == 2) {
-    v[0] = ln_bf16(*reinterpret_cast<const uint16_t *>(p));
-  } else {
-    v[0] = *reinterpret_cast<const float *>(p);
-  }
+  return q;
 }
 
-template <typename T, int VEC>
-__device__ __forceinline__ void ln_store(T *p, const float *v) {
-  if constexpr (sizeof(T) == 4 && VEC == 4) {
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  } else if constexpr (sizeof(T) == 2 && VEC == 8) {
-    uint32_t w[4];
+template <typename T>
+__device__ __forceinline__ float ln_value(const v4u &q, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(q[i]);
+  else return __uint_as_float((i & 1) ? q[i / 2] & 0xffff0000u : q[i / 2] << 16);
+}
+
+template <typename T>
+__device__ __forceinline__ void ln_store(T *row, int col, int cols, const float *v) {
+  v4u q;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = __float_as_uint(v[i]);
+  } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
+      q[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
              ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i + 1]) << 16);
-    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<uint16_t *>(p) = __builtin_bit_cast(uint16_t, (__bf16)v[0]);
-  } else {
-    *reinterpret_cast<float *>(p) = v[0];
   }
+  if (col + ln_vec<T>() <= cols) {
+    *reinterpret_cast<v4u_any *>(row + col) = q;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < ln_vec<T>(); ++i)
+    if (col + i < cols) {
+      if constexpr (sizeof(T) == 4) row[col + i] = v[i];
+      else row[col + i] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
+    }
 }
 
 template <int VEC>
 __device__ __forceinline__ void ln_param(const float *p, int col, int cols, float dflt, float *v) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) v[i] = p && col + i < cols ? p[col + i] : dflt;
-}
-
-// Sum over the GROUP threads of a row, in a fixed tree; every one of them gets
-// it.  `red` has a slot for each wave and is used by one call between barriers.
-template <int GROUP>
-__device__ __forceinline__ float ln_sum(float v, float *red) {
-  constexpr int W = GROUP < 64 ? GROUP : 64;
+  for (int i = 0; i < VEC; ++i) v[i] = dflt;
+  if (!p) return;
+  if (col + VEC <= cols) {
 #pragma unroll
-  for (int m = W / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m);
-  if constexpr (GROUP > 64) {
-    const int wave = threadIdx.x >> 6;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[wave] = v;
-    __syncthreads();
-    v = 0.f;
+    for (int i = 0; i < VEC; i += 4) {
+      const v4f q = *reinterpret_cast<const v4f_any *>(p + col + i);
 #pragma unroll
-    for (int i = 0; i < GROUP / 64; ++i) v += red[i];
+      for (int j = 0; j < 4; ++j) v[i + j] = q[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (col + i < cols) v[i] = p[col + i];
   }
-  return v;
 }
 
 template <int GROUP>
 constexpr int ln_threads() { return GROUP < 256 ? 256 : GROUP; }
+template <int GROUP>
+constexpr int ln_lanes() { return GROUP < 64 ? GROUP : 64; }
 
-template <typename T, int VEC, int GROUP, int V>
+// Columns that the 64 threads of a wave (or the GROUP < 64 of a row) hold.
+template <int VEC, int GROUP, int U>
+__device__ __forceinline__ int ln_count(int cols, int first_thread) {
+  constexpr int L = ln_lanes<GROUP>();
+  int n = 0;
+#pragma unroll
+  for (int u = 0; u < U; ++u) n += min(max(cols - (u * GROUP + first_thread) * VEC, 0), L * VEC);
+  return n;
+}
+
+template <typename T, int GROUP, int V>
 __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_fwd(LnParams p) {
-  constexpr int NT = ln_threads<GROUP>(), ROWS = NT / GROUP, U = V / VEC;
-  __shared__ float red[NT / 64];
+  constexpr int VEC = ln_vec<T>(), NT = ln_threads<GROUP>(), ROWS = NT / GROUP, U = V / VEC;
+  constexpr int L = ln_lanes<GROUP>(), W = GROUP / L;   // waves of a row
+  __shared__ float2 red[2][NT / 64];
   const int lane = threadIdx.x % GROUP, g = threadIdx.x / GROUP;
+  const int wave = W > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
   const float inv = 1.f / (float)p.cols;
+  const float mine = (float)ln_count<VEC, GROUP, U>(p.cols, wave * 64);
   float w[U][VEC], b[U][VEC];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -124,35 +158,60 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_fwd(LnParams p
     ln_param<VEC>(p.b, col, p.cols, 0.f, b[u]);
   }
   const int64_t step = (int64_t)gridDim.x * ROWS;
-  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < p.rows; r0 += step) {
-    const int64_t row = r0 + g;
-    const bool live = row < p.rows;
-    const T *x = static_cast<const T *>(p.x) + (live ? row : p.rows - 1) * p.ldx;
+  int64_t row = (int64_t)blockIdx.x * ROWS + g;
+  v4u next[U];
+  auto load = [&](int64_t r) {
+    const T *x = static_cast<const T *>(p.x) + min(r, p.rows - 1) * p.ldx;
+#pragma unroll
+    for (int u = 0; u < U; ++u) next[u] = ln_load<T>(x, (u * GROUP + lane) * VEC, p.cols);
+  };
+  load(row);
+  for (int k = 0; row - g < p.rows; row += step, k ^= 1) {
     float v[U][VEC];
     float s = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int col = (u * GROUP + lane) * VEC;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[u][i] = 0.f;
-      if (col < p.cols) ln_load<T, VEC>(x + col, v[u]);
+      for (int i = 0; i < VEC; ++i) {
+        v[u][i] = ln_value<T>(next[u], i);
+        s += v[u][i];
+      }
+    load(row + step);
+    s = lane_sum<L>(s);
+    float mu = W > 1 ? s / mine : s * inv;              // of the wave's columns, or the row's
+    if (W > 1 && mine == 0.f) mu = 0.f;
+    float q = 0.f;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) s += v[u][i];
-    }
-    const float mu = ln_sum<GROUP>(s, red) * inv;
-    s = 0.f;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if ((u * GROUP + lane) * VEC < p.cols) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          v[u][i] -= mu;
-          s = fmaf(v[u][i], v[u][i], s);
+      for (int i = 0; i < VEC; ++i)
+        if ((u * GROUP + lane) * VEC + i < p.cols) {
+          const float d = v[u][i] - mu;
+          q = fmaf(d, d, q);
         }
+    q = lane_sum<L>(q);
+    if constexpr (W > 1) {
+      // sum over waves of (squares about their mean + count (their mean - mean)^2)
+      if ((threadIdx.x & 63) == 0) red[k][wave] = make_float2(s, q);
+      __syncthreads();
+      float2 o[W];
+      s = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        o[i] = red[k][i];
+        s += o[i].x;
+      }
+      mu = s * inv;
+      q = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float n = (float)ln_count<VEC, GROUP, U>(p.cols, 64 * i);
+        const float d = n > 0.f ? o[i].x / n - mu : 0.f;
+        q += o[i].y + n * d * d;
       }
     }
-    const float r = 1.f / sqrtf(ln_sum<GROUP>(s, red) * inv + p.eps);
-    if (!live) continue;
+    const float r = 1.f / sqrtf(q * inv + p.eps);
+    if (row >= p.rows) continue;
     T *y = static_cast<T *>(p.out) + row * p.ldo;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -160,8 +219,8 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_fwd(LnParams p
       if (col >= p.cols) continue;
       float o[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) o[i] = fmaf(v[u][i] * r, w[u][i], b[u][i]);
-      ln_store<T, VEC>(y + col, o);
+      for (int i = 0; i < VEC; ++i) o[i] = fmaf((v[u][i] - mu) * r, w[u][i], b[u][i]);
+      ln_store<T>(y, col, p.cols, o);
     }
     if (lane == 0) {
       if (p.mean) p.mean[row] = mu;
@@ -172,10 +231,11 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_fwd(LnParams p
 
 // out = dx (none if null); part = the sums of dy h and dy over the workgroup's
 // rows (none if null).
-template <typename T, int VEC, int GROUP, int V>
+template <typename T, int GROUP, int V>
 __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_bwd(LnParams p) {
-  constexpr int NT = ln_threads<GROUP>(), ROWS = NT / GROUP, U = V / VEC;
-  __shared__ float red[NT / 64];
+  constexpr int VEC = ln_vec<T>(), NT = ln_threads<GROUP>(), ROWS = NT / GROUP, U = V / VEC;
+  constexpr int L = ln_lanes<GROUP>(), W = GROUP / L;
+  __shared__ float2 red[2][NT / 64];
   const int lane = threadIdx.x % GROUP, g = threadIdx.x / GROUP;
   const float inv = 1.f / (float)p.cols;
   float w[U][VEC], dw[U][VEC], db[U][VEC];
@@ -186,27 +246,38 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_bwd(LnParams p
     for (int i = 0; i < VEC; ++i) dw[u][i] = db[u][i] = 0.f;
   }
   const int64_t step = (int64_t)gridDim.x * ROWS;
-  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < p.rows; r0 += step) {
-    const int64_t row = r0 + g;
+  int64_t row = (int64_t)blockIdx.x * ROWS + g;
+  v4u nx[U], nd[U];
+  float nmu, nr;
+  auto load = [&](int64_t r) {
+    const int64_t at = min(r, p.rows - 1);
+    const T *x = static_cast<const T *>(p.x) + at * p.ldx, *dy = static_cast<const T *>(p.dy) + at * p.lddy;
+    nmu = p.mean_in[at];
+    nr = p.rstd_in[at];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      nx[u] = ln_load<T>(x, (u * GROUP + lane) * VEC, p.cols);
+      nd[u] = ln_load<T>(dy, (u * GROUP + lane) * VEC, p.cols);
+    }
+  };
+  // past 8192 columns the next row does not fit the registers
+  constexpr bool AHEAD = GROUP < 512;
+  if (AHEAD) load(row);
+  for (int k = 0; row - g < p.rows; row += step, k ^= 1) {
+    if (!AHEAD) load(row);
     const bool live = row < p.rows;
-    const int64_t at = live ? row : p.rows - 1;
-    const T *x = static_cast<const T *>(p.x) + at * p.ldx;
-    const T *dy = static_cast<const T *>(p.dy) + at * p.lddy;
-    const float mu = p.mean_in[at], r = p.rstd_in[at];
+    const float mu = nmu, r = nr;
     float h[U][VEC], d[U][VEC];
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int col = (u * GROUP + lane) * VEC;
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) h[u][i] = d[u][i] = 0.f;
-      if (col < p.cols && live) {
-        ln_load<T, VEC>(x + col, h[u]);
-        ln_load<T, VEC>(dy + col, d[u]);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) h[u][i] = (h[u][i] - mu) * r;
+      for (int i = 0; i < VEC; ++i) {
+        const bool in = live && (u * GROUP + lane) * VEC + i < p.cols;
+        h[u][i] = in ? (ln_value<T>(nx[u], i) - mu) * r : 0.f;
+        d[u][i] = in ? ln_value<T>(nd[u], i) : 0.f;
       }
-    }
+    if (AHEAD) load(row + step);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -218,9 +289,21 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_bwd(LnParams p
         s2 = fmaf(d[u][i], h[u][i], s2);
       }
     if (!p.out) continue;
-    s1 = ln_sum<GROUP>(s1, red) * inv;
-    s2 = ln_sum<GROUP>(s2, red) * inv;
+    s1 = lane_sum<L>(s1);
+    s2 = lane_sum<L>(s2);
+    if constexpr (W > 1) {
+      if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = make_float2(s1, s2);
+      __syncthreads();
+      s1 = s2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        s1 += red[k][i].x;
+        s2 += red[k][i].y;
+      }
+    }
     if (!live) continue;
+    s1 *= inv;
+    s2 *= inv;
     T *dx = static_cast<T *>(p.out) + row * p.ldo;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -229,7 +312,7 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_bwd(LnParams p
       float o[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) o[i] = r * (d[u][i] - s1 - h[u][i] * s2);
-      ln_store<T, VEC>(dx + col, o);
+      ln_store<T>(dx, col, p.cols, o);
     }
   }
   if (!p.part) return;
@@ -268,43 +351,50 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_bwd(LnParams p
     }
   } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      const int c = (u * GROUP + lane) * VEC;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int c = (u * GROUP + lane) * VEC + i;
-        if (c >= p.cols) continue;
-        part[c] = dw[u][i];
-        part[p.cols + c] = db[u][i];
+      for (int i = 0; i < VEC; i += 4) {
+        if (c + i + 4 <= p.cols) {
+          *reinterpret_cast<v4f_any *>(part + c + i) = v4f{dw[u][i], dw[u][i + 1], dw[u][i + 2], dw[u][i + 3]};
+          *reinterpret_cast<v4f_any *>(part + p.cols + c + i) =
+              v4f{db[u][i], db[u][i + 1], db[u][i + 2], db[u][i + 3]};
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (c + i + j < p.cols) {
+              part[c + i + j] = dw[u][i + j];
+              part[p.cols + c + i + j] = db[u][i + j];
+            }
+        }
       }
+    }
   }
 }
 
-// dw[c] or db[c] (by blockIdx.y) = sum over the workgroups' partial sums:
-// slice s of 16 adds workgroups s, s + 16, ... in order, then the slices in
-// order.
+// dw[c] or db[c] (by blockIdx.y) = sum over the workgroups' partial sums: slice s of
+// 32 adds workgroups s, s + 32, ... in order, then the slices in order.
 __global__ __launch_bounds__(LN_FIN) void layer_norm_bwd_finish(const float *__restrict__ part,
                                                                int nb, int cols,
                                                                float *__restrict__ dw,
                                                                float *__restrict__ db) {
+  constexpr int C = LN_FIN_COLS, S = LN_FIN / C;
   __shared__ float red[LN_FIN];
   float *out = blockIdx.y == 0 ? dw : db;
   if (!out) return;
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), s = threadIdx.x >> 6;
+  const int c = blockIdx.x * C + threadIdx.x % C, s = threadIdx.x / C;
   float v = 0.f;
   if (c < cols) {
     const float *src = part + (int64_t)blockIdx.y * cols + c;
 #pragma unroll 8
-    for (int k = s; k < nb; k += LN_FIN / 64) v += src[(int64_t)k * 2 * cols];
+    for (int k = s; k < nb; k += S) v += src[(int64_t)k * 2 * cols];
   }
   red[threadIdx.x] = v;
   __syncthreads();
   if (s != 0 || c >= cols) return;
-  for (int k = 1; k < LN_FIN / 64; ++k) v += red[k * 64 + threadIdx.x];
+#pragma unroll
+  for (int k = 1; k < S; ++k) v += red[k * C + threadIdx.x];
   out[c] = v;
-}
-
-bool ln_aligned(const void *p, int64_t ld, int elem) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld * elem % 16 == 0;
 }
 
 // Threads per row and values per thread: the fewest threads of a wave that
@@ -325,17 +415,17 @@ int64_t ln_blocks(int64_t rows, int64_t cols, int64_t most) {
   return std::min((rows + per - 1) / per, most);
 }
 
-template <bool BWD, typename T, int VEC>
+template <bool BWD, typename T>
 hipError_t ln_launch(const LnParams &p, hipStream_t s) {
   const LnShape sh = ln_shape(p.cols);
-  const dim3 grid((unsigned)ln_blocks(p.rows, p.cols, BWD ? LN_BLOCKS_BWD : LN_BLOCKS_FWD));
-#define SOAP_LN(G, N)                                                                             \
-  if (sh.group == G && sh.v == N) {                                                               \
-    if constexpr (BWD)                                                                            \
-      hipLaunchKernelGGL((layer_norm_bwd<T, VEC, G, N>), grid, dim3(ln_threads<G>()), 0, s, p);   \
-    else                                                                                          \
-      hipLaunchKernelGGL((layer_norm_fwd<T, VEC, G, N>), grid, dim3(ln_threads<G>()), 0, s, p);   \
-    return hipGetLastError();                                                                     \
+  const dim3 grid((unsigned)ln_blocks(p.rows, p.cols, BWD ? ln_blocks_bwd(p.cols) : LN_BLOCKS_FWD));
+#define SOAP_LN(G, N)                                                                        \
+  if (sh.group == G && sh.v == N) {                                                          \
+    if constexpr (BWD)                                                                       \
+      hipLaunchKernelGGL((layer_norm_bwd<T, G, N>), grid, dim3(ln_threads<G>()), 0, s, p);   \
+    else                                                                                     \
+      hipLaunchKernelGGL((layer_norm_fwd<T, G, N>), grid, dim3(ln_threads<G>()), 0, s, p);   \
+    return hipGetLastError();                                                                \
   }
   SOAP_LN(8, 8) SOAP_LN(8, 16) SOAP_LN(8, 32)
   SOAP_LN(64, 8) SOAP_LN(64, 16) SOAP_LN(64, 32)
@@ -344,16 +434,10 @@ hipError_t ln_launch(const LnParams &p, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
-template <bool BWD>
-hipError_t ln_dispatch(const LnParams &p, bool bf16, bool wide, hipStream_t s) {
-  if (bf16) return wide ? ln_launch<BWD, uint16_t, 8>(p, s) : ln_launch<BWD, uint16_t, 1>(p, s);
-  return wide ? ln_launch<BWD, float, 4>(p, s) : ln_launch<BWD, float, 1>(p, s);
-}
-
 }  // namespace
 
 size_t layer_norm_part_bytes(int64_t rows, int64_t cols) {
-  return sizeof(float) * 2 * cols * ln_blocks(rows, cols, LN_BLOCKS_BWD);
+  return sizeof(float) * 2 * cols * ln_blocks(rows, cols, ln_blocks_bwd(cols));
 }
 
 hipError_t launch_layer_norm_fwd(const LayerNormDesc &d, hipStream_t s) {
@@ -362,10 +446,7 @@ hipError_t launch_layer_norm_fwd(const LayerNormDesc &d, hipStream_t s) {
   p.rows = d.rows; p.cols = (int)d.cols;
   p.x = d.x; p.ldx = d.ldx; p.w = d.weight; p.b = d.bias; p.eps = d.eps;
   p.out = d.out; p.ldo = d.ldo; p.mean = d.mean; p.rstd = d.rstd;
-  const int elem = d.bf16 ? 2 : 4;
-  const bool wide = d.cols * elem % 16 == 0 && ln_aligned(d.x, d.ldx, elem) &&
-                    ln_aligned(d.out, d.ldo, elem);
-  return ln_dispatch<false>(p, d.bf16, wide, s);
+  return d.bf16 ? ln_launch<false, uint16_t>(p, s) : ln_launch<false, float>(p, s);
 }
 
 hipError_t launch_layer_norm_bwd(const LayerNormDesc &d, hipStream_t s) {
@@ -374,14 +455,12 @@ hipError_t launch_layer_norm_bwd(const LayerNormDesc &d, hipStream_t s) {
   p.x = d.x; p.ldx = d.ldx; p.dy = d.dy; p.lddy = d.lddy; p.w = d.weight;
   p.mean_in = d.mean; p.rstd_in = d.rstd; p.out = d.out; p.ldo = d.ldo;
   p.part = d.dweight || d.dbias ? d.part : nullptr;
-  const int elem = d.bf16 ? 2 : 4;
-  const bool wide = d.cols * elem % 16 == 0 && ln_aligned(d.x, d.ldx, elem) &&
-                    ln_aligned(d.dy, d.lddy, elem) && (!d.out || ln_aligned(d.out, d.ldo, elem));
   hipError_t e = hipSuccess;
-  if (d.rows > 0 && (e = ln_dispatch<true>(p, d.bf16, wide, s)) != hipSuccess) return e;
-  if (!p.part) return hipSuccess;
-  hipLaunchKernelGGL(layer_norm_bwd_finish, dim3((unsigned)((d.cols + 63) / 64), 2), dim3(LN_FIN),
-                     0, s, p.part, (int)ln_blocks(d.rows, d.cols, LN_BLOCKS_BWD), p.cols, d.dweight,
+  if (d.rows > 0)
+    e = d.bf16 ? ln_launch<true, uint16_t>(p, s) : ln_launch<true, float>(p, s);
+  if (e != hipSuccess || !p.part) return e;
+  hipLaunchKernelGGL(layer_norm_bwd_finish, dim3((unsigned)((d.cols + LN_FIN_COLS - 1) / LN_FIN_COLS), 2), dim3(LN_FIN),
+                     0, s, p.part, (int)ln_blocks(d.rows, d.cols, ln_blocks_bwd(d.cols)), p.cols, d.dweight,
                      d.dbias);
   return hipGetLastError();
 }
