@@ -15,8 +15,8 @@
 // A token takes LPR lanes of a wave (8 to 64) with V = 8 or 16 consecutive
 // experts each, so its logits are read once, 16 bytes per lane, and maximum and
 // sum are a few lane exchanges.  A round of the top-k is a maximum over the
-// lane's own values and over the lanes, and the first lane that holds it has
-// the lowest index.
+// lane's own values and over the lanes, then the lowest index that has it; lane j
+// keeps the j-th choice.  Waves need nothing of each other on the way.
 //
 // The plan numbers the tokens of each expert in order.  Workgroups take chunks
 // of consecutive tokens; the first launch also counts its chunk's tokens of
@@ -27,6 +27,7 @@
 // of p go through per-chunk partial sums added in a fixed order.  A single
 // chunk takes one launch.
 #include "internal.h"
+#include "lanes.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -35,16 +36,16 @@ namespace soap {
 namespace {
 
 constexpr int RT_NT = 256;
-constexpr int RT_CHUNK = 128;      // tokens of a chunk at least
-constexpr int RT_CHUNKS = 512;     // chunks at most
+constexpr int RT_ONE = 64;         // tokens of the single chunk of a small batch at most
+constexpr int RT_CHUNK = 32;       // tokens of a chunk of a larger one at least
+constexpr int RT_CHUNKS = 1024;    // chunks at most: four per thread of the second launch
 constexpr int RT_MAX_E = 1024;
 constexpr int RT_MAX_K = 32;
-constexpr int RT_SCAN_E = 16;      // experts of a workgroup of the second launch
 
 struct RtParams {
   int64_t tokens, ld, ldd, rows;
   int experts, top_k, chunk, chunks;
-  int vec;                           // logits can be read 16 bytes at a time
+  int vec, vec_out;                  // logits (dlogits) can be read (written) 16 bytes at a time
   int renorm;
   float balance;
   const void *logits;
@@ -54,8 +55,8 @@ struct RtParams {
   int *counts;
   float *loss;
   int *offsets, *position, *row_token;
-  int *hist;                         // [chunks][experts + 1]: the last is the tokens that route
-  float *psum;                       // [chunks][experts]
+  int *hist;                         // [experts + 1][RT_CHUNKS]: the last is the tokens that route
+  float *psum;                       // [experts][RT_CHUNKS]
   float *ptot;                       // [experts]
   const int *index_in, *counts_in;
   const float *dgate, *dloss;
@@ -70,19 +71,6 @@ __device__ __forceinline__ uint32_t rt_key(float f) {
 }
 __device__ __forceinline__ float rt_unkey(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
-}
-
-template <int LPR>
-__device__ __forceinline__ uint32_t rt_max(uint32_t v) {
-#pragma unroll
-  for (int m = LPR / 2; m >= 1; m >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, m));
-  return v;
-}
-template <int LPR>
-__device__ __forceinline__ float rt_sum(float v) {
-#pragma unroll
-  for (int m = LPR / 2; m >= 1; m >>= 1) v += __shfl_xor(v, m);
-  return v;
 }
 
 // The lane's logits e0 .. e0 + V - 1 of a row; -inf past the last expert.
@@ -119,6 +107,36 @@ __device__ __forceinline__ void rt_load(const T *row, int e0, int experts, int v
   }
 }
 
+template <typename T, int V>
+__device__ __forceinline__ void rt_store(T *row, int e0, int experts, int vec, const float *v) {
+  if constexpr (sizeof(T) == 4) {
+    if (vec && e0 + V <= experts) {
+#pragma unroll
+      for (int i = 0; i < V; i += 4)
+        *reinterpret_cast<float4 *>(row + e0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (e0 + i < experts) row[e0 + i] = v[i];
+  } else {
+    uint32_t w[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i)
+      w[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
+             ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i + 1]) << 16);
+    if (vec && e0 + V <= experts) {
+#pragma unroll
+      for (int i = 0; i < V / 2; i += 4)
+        *reinterpret_cast<uint4 *>(row + e0 + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (e0 + i < experts) row[e0 + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+  }
+}
+
 // exp(l - max) of the lane's values and their sum over the row's lanes; `top`
 // is the key of the row's maximum.
 template <int LPR, int V>
@@ -130,29 +148,41 @@ __device__ __forceinline__ float rt_softmax(const float *l, int e0, int experts,
     p[i] = e0 + i < experts ? expf(l[i] - mx) : 0.f;
     s += p[i];
   }
-  return rt_sum<LPR>(s);
+  return lane_sum<LPR>(s);
 }
 
-// Offsets of the experts' rows (each expert's padded to a multiple of 32) from
-// their counts: an inclusive scan in LDS.  Every thread of the workgroup calls it.
-__device__ void rt_offsets(const int *counts, int experts, int *scan) {
-  for (int e = threadIdx.x; e < experts; e += RT_NT) scan[e] = (counts[e] + 31) & ~31;
-  __syncthreads();
-  for (int d = 1; d < experts; d <<= 1) {
-    int v[RT_MAX_E / RT_NT];
+// base[e] <- first row of expert e (each expert's rows padded to a multiple of 32),
+// from the counts; offsets, if not null, gets them and the end.  Four consecutive
+// experts a thread, a scan over the lanes, then over the waves.  Every thread of the
+// workgroup calls it; it ends with a barrier.
+__device__ void rt_offsets(const int *counts, int experts, int *base, int *offsets) {
+  static_assert(RT_MAX_E == 4 * RT_NT, "four experts a thread");
+  __shared__ int waves[RT_NT / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e0 = 4 * threadIdx.x;
+  int n[4], sum = 0;
 #pragma unroll
-    for (int i = 0; i < RT_MAX_E / RT_NT; ++i) {
-      const int e = threadIdx.x + i * RT_NT;
-      v[i] = e < experts && e >= d ? scan[e - d] : 0;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < RT_MAX_E / RT_NT; ++i) {
-      const int e = threadIdx.x + i * RT_NT;
-      if (e < experts) scan[e] += v[i];
-    }
-    __syncthreads();
+  for (int i = 0; i < 4; ++i) {
+    n[i] = sum;
+    if (e0 + i < experts) sum += (counts[e0 + i] + 31) & ~31;
   }
+  int before = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(before, d);
+    if (lane >= d) before += u;
+  }
+  if (lane == 63) waves[wave] = before;
+  __syncthreads();
+  before -= sum;
+  for (int w = 0; w < wave; ++w) before += waves[w];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (e0 + i < experts) {
+      base[e0 + i] = before + n[i];
+      if (offsets) offsets[e0 + i] = before + n[i];
+    }
+  if (offsets && threadIdx.x == (experts - 1) / 4) offsets[experts] = before + sum;
+  __syncthreads();
 }
 
 // The rows of one chunk's tokens.  base[e] = first row of the chunk's tokens of
@@ -184,19 +214,31 @@ __device__ void rt_assign(const RtParams &p, int64_t t0, int64_t t1, int *base,
   }
 }
 
+// balance E sum_e counts_e psum_e / (sum of counts, tokens that route): one wave.
+template <typename C, typename P>
+__device__ void rt_loss(const RtParams &p, C counts, P psum) {
+  float f = 0.f;
+  int all = 0;
+  for (int e = threadIdx.x & 63; e < p.experts; e += 64) {
+    f += (float)counts[e] * psum[e];
+    all += counts[e];
+  }
+  f = lane_sum<64>(f);
+  all = lane_reduce<64>(all, [](int a, int b) { return a + b; });
+  if ((threadIdx.x & 63) == 0)
+    p.loss[0] = all ? p.balance * (float)p.experts * f / ((float)all * (float)counts[p.experts]) : 0.f;
+}
+
 // ONE: the whole batch is one chunk and everything is done here.
 template <typename T, int LPR, int V, bool ONE>
 __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
-  constexpr int ROWS = RT_NT / LPR;          // tokens of a pass
+  constexpr int ROWS = RT_NT / LPR;                  // tokens of a pass
+  constexpr int SLOTS = (RT_MAX_K + LPR - 1) / LPR;  // choices of a lane
   __shared__ int hist[RT_MAX_E + 1];
   __shared__ float psum[RT_NT / 64][LPR * V];
-  __shared__ float denom[ROWS], rowmax[ROWS];
-  __shared__ int pick[ROWS * RT_MAX_K];
-  __shared__ float val[ROWS * RT_MAX_K];
   const int tid = threadIdx.x, lane = tid % LPR, g = tid / LPR, wave = tid >> 6;
   const int e0 = lane * V, k = p.top_k;
   const int64_t t0 = (int64_t)blockIdx.x * p.chunk, t1 = min(p.tokens, t0 + p.chunk);
-  const uint64_t mine = (LPR == 64 ? ~0ull : ((1ull << LPR) - 1ull)) << ((tid & 63) / LPR * LPR);
   for (int e = tid; e <= p.experts; e += RT_NT) hist[e] = 0;
   if (p.row_token)                            // rows that no token takes
     for (int64_t i = (int64_t)blockIdx.x * RT_NT + tid; i < p.rows; i += (int64_t)gridDim.x * RT_NT)
@@ -216,52 +258,55 @@ __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
       key[i] = on ? rt_key(l[i]) : 0u;
       best = max(best, key[i]);
     }
-    const uint32_t top = rt_max<LPR>(best);
-    const bool routes = top != 0u;
+    const uint32_t top = lane_max<LPR>(best);
+    const float mx = rt_unkey(top);
     const float s = rt_softmax<LPR, V>(l, e0, p.experts, top, pr);
-    if (routes) {
+    if (top != 0u) {
       const float inv = 1.f / s;
 #pragma unroll
       for (int i = 0; i < V; ++i) acc[i] += pr[i] * inv;
       if (lane == 0) atomicAdd(&hist[p.experts], 1);
     }
-    float chosen = 0.f;
+    int pick[SLOTS];
+    float e[SLOTS], chosen = 0.f;
     uint32_t now = top;
-    for (int j = 0; j < k; ++j) {
-      if (j) {
-        best = 0u;
 #pragma unroll
-        for (int i = 0; i < V; ++i) best = max(best, key[i]);
-        now = rt_max<LPR>(best);
+    for (int slot = 0; slot < SLOTS; ++slot) {
+      pick[slot] = -1;
+      uint32_t mine = 0u;
+      const int n = min(k - slot * LPR, LPR);
+      for (int j = 0; j < n; ++j) {
+        if (slot + j) {
+          best = 0u;
+#pragma unroll
+          for (int i = 0; i < V; ++i) best = max(best, key[i]);
+          now = lane_max<LPR>(best);
+        }
+        uint32_t at = 0x7fffffffu;               // the lowest expert that has it
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i) at = key[i] == now ? (uint32_t)(e0 + i) : at;
+        at = lane_reduce<LPR>(at, [](uint32_t a, uint32_t b) { return min(a, b); });
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = (uint32_t)(e0 + i) == at ? 0u : key[i];
+        if (lane == j && now != 0u) {
+          pick[slot] = (int)at;
+          mine = now;
+        }
       }
-      const uint64_t who = __ballot(best == now && now != 0u) & mine;
-      const bool winner = who && (int)(__ffsll((unsigned long long)who) - 1) == (tid & 63);
-      if (winner) {
-        int at = 0;
+      e[slot] = pick[slot] >= 0 ? expf(rt_unkey(mine) - mx) : 0.f;
+      chosen += e[slot];
+    }
+    // a NaN of the row stays one
+    const float denom = p.renorm ? (s - s) + lane_sum<LPR>(chosen) : s;
 #pragma unroll
-        for (int i = V - 1; i >= 0; --i) at = key[i] == now ? i : at;
-#pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = i == at ? 0u : key[i];
-        pick[g * RT_MAX_K + j] = e0 + at;
-        val[g * RT_MAX_K + j] = rt_unkey(now);
-        atomicAdd(&hist[e0 + at], 1);
-      } else if (!who && lane == 0) {
-        pick[g * RT_MAX_K + j] = -1;
+    for (int slot = 0; slot < SLOTS; ++slot) {
+      const int j = slot * LPR + lane;
+      if (in && j < k) {
+        p.index[t * k + j] = pick[slot];
+        p.gate[t * k + j] = pick[slot] >= 0 ? e[slot] / denom : 0.f;
+        if (pick[slot] >= 0) atomicAdd(&hist[pick[slot]], 1);
       }
-      if (now) chosen += expf(rt_unkey(now) - rt_unkey(top));
     }
-    if (lane == 0) {
-      rowmax[g] = rt_unkey(top);
-      denom[g] = p.renorm ? (s - s) + chosen : s;      // a NaN of the row stays one
-    }
-    __syncthreads();
-    const int n = (int)min((int64_t)ROWS, t1 - s0);
-    for (int i = tid; i < n * k; i += RT_NT) {
-      const int r = i / k, e = pick[r * RT_MAX_K + i - r * k];
-      p.index[s0 * k + i] = e;
-      p.gate[s0 * k + i] = e >= 0 ? expf(val[r * RT_MAX_K + i - r * k] - rowmax[r]) / denom[r] : 0.f;
-    }
-    __syncthreads();
   }
   // the chunk's sums of p: the groups of a wave, then the waves, in order
 #pragma unroll
@@ -277,78 +322,64 @@ __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
 #pragma unroll
     for (int w = 0; w < RT_NT / 64; ++w) v += psum[w][e];
     if (ONE) psum[0][e] = v;
-    else p.psum[(int64_t)blockIdx.x * p.experts + e] = v;
+    else p.psum[(int64_t)e * RT_CHUNKS + blockIdx.x] = v;
   }
   if constexpr (!ONE) {
-    for (int e = tid; e <= p.experts; e += RT_NT)
-      p.hist[(int64_t)blockIdx.x * (p.experts + 1) + e] = hist[e];
+    for (int e = tid; e <= p.experts; e += RT_NT) p.hist[(int64_t)e * RT_CHUNKS + blockIdx.x] = hist[e];
   } else {
     __shared__ int base[RT_MAX_E];
     __shared__ unsigned long long bits[RT_MAX_E];
     for (int e = tid; e <= p.experts; e += RT_NT) p.counts[e] = hist[e];
-    __threadfence_block();
     __syncthreads();
-    if (p.loss && wave == 0) {
-      float f = 0.f;
-      int all = 0;
-      for (int e = tid; e < p.experts; e += 64) {
-        f += (float)hist[e] * psum[0][e];
-        all += hist[e];
-      }
-      f = rt_sum<64>(f);
-#pragma unroll
-      for (int m = 32; m >= 1; m >>= 1) all += __shfl_xor(all, m);
-      if (tid == 0)
-        p.loss[0] = all ? p.balance * (float)p.experts * f / ((float)all * (float)hist[p.experts]) : 0.f;
-    }
+    if (p.loss && wave == 0) rt_loss(p, hist, psum[0]);
     if (!p.row_token) return;
-    rt_offsets(hist, p.experts, base);
-    for (int e = tid; e <= p.experts; e += RT_NT) p.offsets[e] = e ? base[e - 1] : 0;
-    __syncthreads();
-    // base[e] <- first row of expert e
-    for (int e = tid; e < p.experts; e += RT_NT) base[e] -= (hist[e] + 31) & ~31;
-    __syncthreads();
+    rt_offsets(hist, p.experts, base, p.offsets);
     rt_assign(p, t0, t1, base, bits);
   }
 }
 
-// For RT_SCAN_E experts (column `experts` of hist is the tokens that route):
-// counts, the exclusive scan of the chunks' counts in place, the sums of p.
-// 16 slices of consecutive chunks per expert.
+// One expert (or, last, the tokens that route): its count, the exclusive scan of the
+// chunks' counts in place, the sum of p.  Four consecutive chunks a thread.
 __global__ __launch_bounds__(RT_NT) void router_scan(RtParams p) {
-  constexpr int S = RT_NT / RT_SCAN_E;
-  __shared__ int tot[S][RT_SCAN_E];
-  __shared__ float ps[S][RT_SCAN_E];
-  const int x = threadIdx.x % RT_SCAN_E, s = threadIdx.x / RT_SCAN_E;
-  const int e = blockIdx.x * RT_SCAN_E + x, E1 = p.experts + 1;
-  const int per = (p.chunks + S - 1) / S;
-  const int c0 = min(p.chunks, s * per), c1 = min(p.chunks, c0 + per);
-  int n = 0;
+  static_assert(RT_CHUNKS == 4 * RT_NT, "four chunks a thread");
+  __shared__ int waves[RT_NT / 64];
+  __shared__ float sums[RT_NT / 64];
+  const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c0 = 4 * threadIdx.x;
+  int *hist = p.hist + (int64_t)e * RT_CHUNKS;
+  const float *psum = p.psum + (int64_t)e * RT_CHUNKS;
+  const bool prob = e < p.experts;
+  int n[4], sum = 0;
   float f = 0.f;
-  if (e <= p.experts) {
-#pragma unroll 8
-    for (int c = c0; c < c1; ++c) n += p.hist[(int64_t)c * E1 + e];
-    if (e < p.experts) {
-#pragma unroll 8
-      for (int c = c0; c < c1; ++c) f += p.psum[(int64_t)c * p.experts + e];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n[i] = sum;
+    if (c0 + i < p.chunks) {
+      sum += hist[c0 + i];
+      if (prob) f += psum[c0 + i];
     }
   }
-  tot[s][x] = n;
-  ps[s][x] = f;
-  __syncthreads();
-  if (e > p.experts) return;
-  int before = 0;
-  for (int i = 0; i < s; ++i) before += tot[i][x];
-  if (s == S - 1) p.counts[e] = before + n;
-  if (s == 0 && e < p.experts) {
-    f = 0.f;
-    for (int i = 0; i < S; ++i) f += ps[i][x];
-    p.ptot[e] = f;
+  int before = sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(before, d);
+    if (lane >= d) before += u;
   }
-  for (int c = c0; c < c1; ++c) {
-    const int v = p.hist[(int64_t)c * E1 + e];
-    p.hist[(int64_t)c * E1 + e] = before;
-    before += v;
+  f = lane_sum<64>(f);
+  if (lane == 63) {
+    waves[wave] = before;
+    sums[wave] = f;
+  }
+  __syncthreads();
+  before -= sum;
+  for (int w = 0; w < wave; ++w) before += waves[w];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c0 + i < p.chunks) hist[c0 + i] = before + n[i];
+  if (threadIdx.x == RT_NT - 1) p.counts[e] = before + sum;
+  if (threadIdx.x == 0 && prob) {
+    f = 0.f;
+    for (int w = 0; w < RT_NT / 64; ++w) f += sums[w];
+    p.ptot[e] = f;
   }
 }
 
@@ -356,141 +387,110 @@ __global__ __launch_bounds__(RT_NT) void router_scan(RtParams p) {
 __global__ __launch_bounds__(RT_NT) void router_plan(RtParams p) {
   __shared__ int base[RT_MAX_E];
   __shared__ unsigned long long bits[RT_MAX_E];
-  __shared__ float red[RT_NT];
-  __shared__ int redn[RT_NT];
-  const int tid = threadIdx.x;
-  if (blockIdx.x == 0 && p.loss) {
-    float f = 0.f;
-    int all = 0;
-    for (int e = tid; e < p.experts; e += RT_NT) {
-      f += (float)p.counts[e] * p.ptot[e];
-      all += p.counts[e];
-    }
-    red[tid] = f;
-    redn[tid] = all;
-    __syncthreads();
-    for (int d = RT_NT / 2; d >= 1; d >>= 1) {
-      if (tid < d) { red[tid] += red[tid + d]; redn[tid] += redn[tid + d]; }
-      __syncthreads();
-    }
-    if (tid == 0)
-      p.loss[0] = redn[0] ? p.balance * (float)p.experts * red[0] /
-                                ((float)redn[0] * (float)p.counts[p.experts])
-                          : 0.f;
-  }
+  if (blockIdx.x == 0 && p.loss && threadIdx.x < 64) rt_loss(p, p.counts, p.ptot);
   if (!p.row_token) return;
-  rt_offsets(p.counts, p.experts, base);
-  if (blockIdx.x == 0)
-    for (int e = tid; e <= p.experts; e += RT_NT) p.offsets[e] = e ? base[e - 1] : 0;
-  __syncthreads();
-  for (int e = tid; e < p.experts; e += RT_NT)
-    base[e] += p.hist[(int64_t)blockIdx.x * (p.experts + 1) + e] - ((p.counts[e] + 31) & ~31);
+  rt_offsets(p.counts, p.experts, base, blockIdx.x == 0 ? p.offsets : nullptr);
+  for (int e = threadIdx.x; e < p.experts; e += RT_NT) base[e] += p.hist[(int64_t)e * RT_CHUNKS + blockIdx.x];
   __syncthreads();
   const int64_t t0 = (int64_t)blockIdx.x * p.chunk, t1 = min(p.tokens, t0 + p.chunk);
   rt_assign(p, t0, t1, base, bits);
 }
 
+// A token's choices and their gradients reach the lanes that hold the experts
+// through the token's own LDS, which only its lanes (of one wave) touch.
 template <typename T, int LPR, int V>
 __global__ __launch_bounds__(RT_NT) void router_bwd(RtParams p) {
   constexpr int ROWS = RT_NT / LPR;
-  __shared__ float dg[ROWS][LPR * V];        // dgate at the chosen experts, 0 elsewhere
-  __shared__ float share[LPR * V];           // b_e
-  __shared__ int total;
+  __shared__ __attribute__((aligned(16))) float dg[ROWS][LPR * V];   // dgate at the chosen experts, 0 elsewhere
+  __shared__ uint32_t chosen[ROWS][LPR];     // bit i: expert lane V + i
+  __shared__ int totals[RT_NT / 64];
   const int tid = threadIdx.x, lane = tid % LPR, g = tid / LPR, e0 = lane * V, k = p.top_k;
-  if (tid == 0) total = 0;
-  for (int i = tid; i < ROWS * LPR * V; i += RT_NT) (&dg[0][0])[i] = 0.f;
-  __syncthreads();
   int part = 0;
   for (int e = tid; e < p.experts; e += RT_NT) part += p.counts_in[e];
-  if (part) atomicAdd(&total, part);
+  part = lane_reduce<64>(part, [](int a, int b) { return a + b; });
+  if ((tid & 63) == 0) totals[tid >> 6] = part;
+#pragma unroll
+  for (int i = 0; i < V; ++i) dg[g][e0 + i] = 0.f;
+  chosen[g][lane] = 0u;
   __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < RT_NT / 64; ++w) total += totals[w];
   const float scale = total > 0 ? (p.dloss ? p.dloss[0] : 1.f) * p.balance * (float)p.experts /
                                       ((float)total * (float)max(1, p.counts_in[p.experts]))
                                 : 0.f;
-  for (int e = tid; e < LPR * V; e += RT_NT)
-    share[e] = e < p.experts ? scale * (float)p.counts_in[e] : 0.f;
-  __syncthreads();
+  float share[V];                            // b_e
+#pragma unroll
+  for (int i = 0; i < V; ++i) share[i] = e0 + i < p.experts ? scale * (float)p.counts_in[e0 + i] : 0.f;
   for (int64_t s0 = (int64_t)blockIdx.x * ROWS; s0 < p.tokens; s0 += (int64_t)gridDim.x * ROWS) {
     const int64_t t = s0 + g;
     const bool in = t < p.tokens, on = in && (!p.mask || p.mask[t]);
-    float l[V], pr[V];
+    float l[V], pr[V], d[V], o[V];
     rt_load<T, V>(static_cast<const T *>(p.logits) + (in ? t : s0) * p.ld, e0, p.experts, p.vec, l);
-    const int n = (int)min((int64_t)ROWS, p.tokens - s0) * k;
-    if (p.dgate)
-      for (int i = tid; i < n; i += RT_NT) {
-        const int e = p.index_in[s0 * k + i];
-        if (e >= 0 && e < p.experts) atomicAdd(&dg[i / k][e], p.dgate[s0 * k + i]);
+    for (int j = lane; j < k; j += LPR) {
+      const int e = in ? p.index_in[t * k + j] : -1;
+      if (e >= 0 && e < p.experts) {
+        dg[g][e] = p.dgate ? p.dgate[t * k + j] : 0.f;
+        atomicOr(&chosen[g][e / V], 1u << (e % V));
       }
-    __syncthreads();
+    }
+    __builtin_amdgcn_wave_barrier();
+    const uint32_t sel = chosen[g][lane];
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = dg[g][e0 + i];
+    __builtin_amdgcn_wave_barrier();
+    chosen[g][lane] = 0u;
+#pragma unroll
+    for (int i = 0; i < V; ++i) dg[g][e0 + i] = 0.f;
+    __builtin_amdgcn_wave_barrier();
     uint32_t best = 0u;
 #pragma unroll
     for (int i = 0; i < V; ++i) best = max(best, on ? rt_key(l[i]) : 0u);
-    const uint32_t top = rt_max<LPR>(best);
+    const uint32_t top = lane_max<LPR>(best);
     const float inv = 1.f / rt_softmax<LPR, V>(l, e0, p.experts, top, pr);
-    float o[V], s1 = 0.f;
+    float s1 = 0.f;
     if (!p.renorm) {
-      float d[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         pr[i] *= inv;
-        d[i] = share[e0 + i] + dg[g][e0 + i];
+        d[i] += share[i];
         s1 = fmaf(pr[i], d[i], s1);
       }
-      s1 = rt_sum<LPR>(s1);
+      s1 = lane_sum<LPR>(s1);
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = pr[i] * (d[i] - s1);
     } else {
-      // which experts were chosen: those whose index is listed
-      float gs = 0.f, gd = 0.f;
-      uint32_t sel = 0u;
-      for (int j = 0; j < k; ++j) {
-        const int e = in ? p.index_in[t * k + j] - e0 : -1;
-        if (e >= 0 && e < V) sel |= 1u << e;
-      }
+      float gs = 0.f, gd = 0.f;              // sums over the chosen of p and p dgate
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float gi = (sel >> i) & 1u ? pr[i] : 0.f;
         gs += gi;
-        gd = fmaf(gi, dg[g][e0 + i], gd);
-        pr[i] *= inv;
-        s1 = fmaf(pr[i], share[e0 + i], s1);
+        gd = fmaf(gi, d[i], gd);
+        s1 = fmaf(pr[i], share[i], s1);
       }
-      gs = rt_sum<LPR>(gs);
-      gd = rt_sum<LPR>(gd);
-      s1 = rt_sum<LPR>(s1);
+      gs = lane_sum<LPR>(gs);
+      gd = lane_sum<LPR>(gd);
+      s1 = lane_sum<LPR>(s1) * inv;
       const float ginv = gs > 0.f ? 1.f / gs : 0.f, mean = gd * ginv;
-      // p of the chosen back from the normalised value: gate = p / (inv gs)
-      const float back = ginv / inv;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        o[i] = pr[i] * (share[e0 + i] - s1);
-        if ((sel >> i) & 1u) o[i] = fmaf(pr[i] * back, dg[g][e0 + i] - mean, o[i]);
+        o[i] = pr[i] * inv * (share[i] - s1);
+        if ((sel >> i) & 1u) o[i] = fmaf(pr[i] * ginv, d[i] - mean, o[i]);
       }
     }
-    if (in) {
-      const bool live = top != 0u;
-      T *out = static_cast<T *>(p.dlogits) + t * p.ldd;
+    if (!in) continue;
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (e0 + i < p.experts) {
-          const float v = live ? o[i] : 0.f;
-          if constexpr (sizeof(T) == 4) out[e0 + i] = v;
-          else out[e0 + i] = __builtin_bit_cast(uint16_t, (__bf16)v);
-        }
-    }
-    __syncthreads();
-    if (p.dgate)
-      for (int i = tid; i < n; i += RT_NT) {
-        const int e = p.index_in[s0 * k + i];
-        if (e >= 0 && e < p.experts) dg[i / k][e] = 0.f;
-      }
-    __syncthreads();
+    for (int i = 0; i < V; ++i) o[i] = top != 0u ? o[i] : 0.f;
+    rt_store<T, V>(static_cast<T *>(p.dlogits) + t * p.ldd, e0, p.experts, p.vec_out, o);
   }
 }
 
 void rt_chunks(int64_t tokens, int *chunk, int *chunks) {
-  int64_t c = std::max<int64_t>(RT_CHUNK, (tokens + RT_CHUNKS - 1) / RT_CHUNKS);
-  c = (c + 63) / 64 * 64;
+  int64_t c = RT_ONE;
+  if (tokens > RT_ONE) {
+    c = std::max<int64_t>(RT_CHUNK, (tokens + RT_CHUNKS - 1) / RT_CHUNKS);
+    if (c > RT_CHUNK) c = (c + 63) / 64 * 64;
+  }
   *chunk = (int)c;
   *chunks = (int)std::max<int64_t>(1, (tokens + c - 1) / c);
 }
@@ -518,9 +518,8 @@ RtParams rt_params(const RouterDesc &d) {
 }  // namespace
 
 size_t router_scratch_bytes(int64_t tokens, int64_t experts) {
-  int chunk, chunks;
-  rt_chunks(tokens, &chunk, &chunks);
-  return sizeof(int) * chunks * (experts + 1) + sizeof(float) * (chunks + 1) * experts;
+  if (tokens <= RT_ONE) return 256;          // not used
+  return sizeof(int) * RT_CHUNKS * (experts + 1) + sizeof(float) * (RT_CHUNKS + 1) * experts;
 }
 
 hipError_t launch_router_fwd(const RouterDesc &d, hipStream_t s) {
@@ -528,8 +527,10 @@ hipError_t launch_router_fwd(const RouterDesc &d, hipStream_t s) {
   p.index = d.index; p.gate = d.gate; p.counts = d.counts; p.loss = d.loss;
   p.offsets = d.offsets; p.position = d.position; p.row_token = d.row_token; p.rows = d.rows;
   p.hist = static_cast<int *>(d.scratch);
-  p.psum = reinterpret_cast<float *>(p.hist + (int64_t)p.chunks * (d.experts + 1));
-  p.ptot = p.psum + (int64_t)p.chunks * d.experts;
+  if (p.chunks > 1) {
+    p.psum = reinterpret_cast<float *>(p.hist + (int64_t)RT_CHUNKS * (d.experts + 1));
+    p.ptot = p.psum + (int64_t)RT_CHUNKS * d.experts;
+  }
   const bool one = p.chunks == 1;
   hipError_t e = rt_shape(d.experts, [&](auto lpr, auto v) {
     constexpr int L = decltype(lpr)::value, V = decltype(v)::value;
@@ -544,7 +545,7 @@ hipError_t launch_router_fwd(const RouterDesc &d, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || one) return e;
-  hipLaunchKernelGGL(router_scan, dim3((p.experts + RT_SCAN_E) / RT_SCAN_E), dim3(RT_NT), 0, s, p);
+  hipLaunchKernelGGL(router_scan, dim3(p.experts + 1), dim3(RT_NT), 0, s, p);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(router_plan, dim3(p.row_token ? p.chunks : 1), dim3(RT_NT), 0, s, p);
   return hipGetLastError();
@@ -555,6 +556,7 @@ hipError_t launch_router_bwd(const RouterDesc &d, hipStream_t s) {
   RtParams p = rt_params(d);
   p.index_in = d.index; p.counts_in = d.counts; p.dgate = d.dgate; p.dloss = d.dloss;
   p.dlogits = d.dlogits; p.ldd = d.ldd;
+  p.vec_out = (reinterpret_cast<uintptr_t>(d.dlogits) & 15u) == 0 && d.ldd * (d.bf16 ? 2 : 4) % 16 == 0;
   return rt_shape(d.experts, [&](auto lpr, auto v) {
     constexpr int L = decltype(lpr)::value, V = decltype(v)::value;
     const int64_t rows = RT_NT / L;
