@@ -551,42 +551,65 @@ def soap_mx4_gemm_k(groups, M, N, K, offsets, a_data, a_scale, b_data, b_scale, 
                                  _raw(b_data), _raw(b_scale), dtype, _raw(C), _stream(stream)))
 
 
-def _floats(t, name):
-    """SOAP_F32 or SOAP_BF16 of a GPU tensor of activations whose rows are contiguous."""
-    import torch
-    if not isinstance(t, torch.Tensor):
+_torch = None
+
+
+def _T():
+    """torch, imported when a tensor is first needed."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _current_stream(t, name):
+    """Raw current stream of the current device, where t must live."""
+    T = _T()
+    if not isinstance(t, T.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t)}")
-    _here(t, name)
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must live on the GPU")
+    if dev != T.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is "
+                         f"cuda:{T.cuda.current_device()}")
+    raw = getattr(T._C, "_cuda_getCurrentRawStream", None)
+    return raw(dev) if raw is not None else T.cuda.current_stream().cuda_stream
+
+
+def _floats(t, name, cols=None):
+    """SOAP_F32 or SOAP_BF16 of a tensor of activations ([rows, cols] if cols is given)
+    whose rows are contiguous."""
+    T = _T()
+    if cols is not None and (t.dim() != 2 or t.shape[1] != cols):
+        raise ValueError(f"{name} must be [rows, {cols}], got {tuple(t.shape)}")
     if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    if t.dtype == torch.bfloat16:
+    if t.dtype is T.bfloat16:
         return SOAP_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is T.float32:
         return SOAP_F32
     raise TypeError(f"{name} must be float32 or bfloat16, got {t.dtype}")
 
 
-def _here(t, name):
-    import torch
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
-
-
-def _exactly(t, name, dtype, shape):
-    """Checks a contiguous tensor of a given type and shape on the current device."""
-    import torch
-    if not isinstance(t, torch.Tensor):
+def _exactly(t, name, dtype, shape, like=None):
+    """Checks a contiguous tensor of a given type and shape, on like's device (or, without
+    one, on a GPU)."""
+    T = _T()
+    if not isinstance(t, T.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t)}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    _here(t, name)
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must live on the GPU")
+    if like is not None and dev != like.get_device():
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
     return t
 
 
@@ -595,20 +618,17 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _on_stream(stream, inputs):
-    """(context to allocate outputs in, raw stream).  With a stream of one's own the
-    outputs belong to it and the inputs are kept from reuse until it has read them."""
-    import contextlib
-
-    import torch
-    if stream is None:
-        return contextlib.nullcontext(), torch.cuda.current_stream().cuda_stream
+def _on(stream, inputs, call, *args, **kwargs):
+    """call(...) on a stream of one's own: its outputs belong to that stream, and its
+    inputs are kept from reuse until the stream has read them."""
+    T = _T()
     if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream)
+        stream = T.cuda.ExternalStream(stream)
     for t in inputs:
         if t is not None:
             t.record_stream(stream)
-    return torch.cuda.stream(stream), stream.cuda_stream
+    with T.cuda.stream(stream):
+        return call(*args, **kwargs)
 
 
 class LayerNorm:
@@ -617,7 +637,6 @@ class LayerNorm:
     by torch.  Inputs are float32 or bfloat16 [rows, cols] with contiguous rows."""
 
     def __init__(self, weight=None, bias=None, eps: float = 1e-5, cols: Optional[int] = None):
-        import torch
         given = [t for t in (weight, bias) if t is not None]
         if cols is None:
             if not given:
@@ -625,51 +644,53 @@ class LayerNorm:
             cols = given[0].numel()
         for t, name in ((weight, "weight"), (bias, "bias")):
             if t is not None:
-                _exactly(t, name, torch.float32, (cols,))
+                _exactly(t, name, _T().float32, (cols,))
         self.weight, self.bias, self.eps, self.cols = weight, bias, eps, cols
 
-    def _matrix(self, t, name):
-        kind = _floats(t, name)
-        if t.dim() != 2 or t.shape[1] != self.cols:
-            raise ValueError(f"{name} must be [rows, {self.cols}], got {tuple(t.shape)}")
-        return kind
+    def _params(self, x):
+        for t, name in ((self.weight, "weight"), (self.bias, "bias")):
+            if t is not None and t.get_device() != x.get_device():
+                raise ValueError(f"{name} is on {t.device}, not on {x.device}")
 
     def forward(self, x, stream=None):
         """(y, mean, rstd): y of x's type, the statistics float32 [rows]."""
-        import torch
-        kind = self._matrix(x, "x")
-        rows = x.shape[0]
-        ctx, raw = _on_stream(stream, (x, self.weight, self.bias))
-        with ctx:
-            y = torch.empty((rows, self.cols), dtype=x.dtype, device=x.device)
-            mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
-        _check(lib().soap_layer_norm_forward(rows, self.cols, kind, x.data_ptr(), _ld(x),
-                                             _raw(self.weight), _raw(self.bias), self.eps,
-                                             y.data_ptr(), self.cols, mean.data_ptr(),
-                                             rstd.data_ptr(), raw))
+        if stream is not None:
+            return _on(stream, (x, self.weight, self.bias), self.forward, x)
+        raw, kind, cols = _current_stream(x, "x"), _floats(x, "x", self.cols), self.cols
+        self._params(x)
+        rows, f32 = x.shape[0], _torch.float32
+        y = x.new_empty((rows, cols))
+        mean, rstd = x.new_empty(rows, dtype=f32), x.new_empty(rows, dtype=f32)
+        w, b = self.weight, self.bias
+        _check(lib().soap_layer_norm_forward(
+            rows, cols, kind, x.data_ptr(), _ld(x), None if w is None else w.data_ptr(),
+            None if b is None else b.data_ptr(), self.eps, y.data_ptr(), cols, mean.data_ptr(),
+            rstd.data_ptr(), raw))
         return y, mean, rstd
 
     def backward(self, dy, x, mean, rstd, stream=None):
         """(dx, dweight, dbias); dweight and dbias are None without a weight and a bias."""
-        import torch
-        kind = self._matrix(x, "x")
-        if self._matrix(dy, "dy") != kind or dy.shape != x.shape:
-            raise ValueError("dy must have x's type and shape")
-        rows = x.shape[0]
-        _exactly(mean, "mean", torch.float32, (rows,))
-        _exactly(rstd, "rstd", torch.float32, (rows,))
-        ctx, raw = _on_stream(stream, (dy, x, mean, rstd, self.weight))
-        L = lib()
-        with ctx:
-            dx = torch.empty((rows, self.cols), dtype=x.dtype, device=x.device)
-            dweight = torch.empty_like(self.weight) if self.weight is not None else None
-            dbias = torch.empty_like(self.bias) if self.bias is not None else None
-            need = L.soap_layer_norm_workspace_bytes(rows, self.cols)
-            work = torch.empty(max(need, 16), dtype=torch.uint8, device=x.device)
-        _check(L.soap_layer_norm_backward(rows, self.cols, kind, dy.data_ptr(), _ld(dy),
-                                          x.data_ptr(), _ld(x), _raw(self.weight), mean.data_ptr(),
-                                          rstd.data_ptr(), dx.data_ptr(), self.cols, _raw(dweight),
-                                          _raw(dbias), work.data_ptr(), need, raw))
+        if stream is not None:
+            return _on(stream, (dy, x, mean, rstd, self.weight, self.bias), self.backward, dy, x, mean, rstd)
+        raw, kind, cols = _current_stream(x, "x"), _floats(x, "x", self.cols), self.cols
+        self._params(x)
+        if dy.dtype is not x.dtype or dy.shape != x.shape or dy.get_device() != x.get_device():
+            raise ValueError("dy must have x's type, shape and device")
+        _floats(dy, "dy")
+        rows, f32 = x.shape[0], _torch.float32
+        _exactly(mean, "mean", f32, (rows,), x)
+        _exactly(rstd, "rstd", f32, (rows,), x)
+        L, w, b = lib(), self.weight, self.bias
+        dx = x.new_empty((rows, cols))
+        dweight = x.new_empty(cols, dtype=f32) if w is not None else None
+        dbias = x.new_empty(cols, dtype=f32) if b is not None else None
+        need = L.soap_layer_norm_workspace_bytes(rows, cols)
+        work = x.new_empty(max(need, 16), dtype=_torch.uint8)
+        _check(L.soap_layer_norm_backward(
+            rows, cols, kind, dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x),
+            None if w is None else w.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), cols,
+            None if w is None else dweight.data_ptr(), None if b is None else dbias.data_ptr(),
+            work.data_ptr(), need, raw))
         return dx, dweight, dbias
 
 
@@ -691,57 +712,58 @@ class Router:
         self.experts, self.top_k, self.balance = experts, top_k, balance
         self.flags = SOAP_ROUTER_RENORMALIZE if renormalize else 0
 
-    def _args(self, logits, mask):
-        import torch
-        kind = _floats(logits, "logits")
-        if logits.dim() != 2 or logits.shape[1] != self.experts:
-            raise ValueError(f"logits must be [tokens, {self.experts}], got {tuple(logits.shape)}")
-        if mask is not None:
-            _exactly(mask, "mask", torch.bool, (logits.shape[0],))
-        return kind
-
     def forward(self, logits, mask=None, stream=None) -> Routing:
-        import torch
-        kind = self._args(logits, mask)
+        if stream is not None:
+            return _on(stream, (logits, mask), self.forward, logits, mask)
+        raw, kind = _current_stream(logits, "logits"), _floats(logits, "logits", self.experts)
         tokens, k, E = logits.shape[0], self.top_k, self.experts
+        if mask is not None:
+            _exactly(mask, "mask", _torch.bool, (tokens,), logits)
         L = lib()
-        ctx, raw = _on_stream(stream, (logits, mask))
         n, rows = tokens * k, L.soap_router_rows(tokens, E, k)
         need = L.soap_router_workspace_bytes(tokens, E)
+        # one allocation of integers and one of floats, cut into the outputs
+        ints = logits.new_empty(2 * n + 2 * (E + 1) + rows, dtype=_torch.int32)
+        floats = logits.new_empty(n + 1, dtype=_torch.float32)
+        work = logits.new_empty(max(need, 16), dtype=_torch.uint8)
+        at, ft, c = ints.data_ptr(), floats.data_ptr(), 2 * n
+        _check(L.soap_router_forward(
+            tokens, E, k, kind, logits.data_ptr(), _ld(logits), None if mask is None else mask.data_ptr(),
+            self.flags, self.balance, at, ft, at + 4 * c, ft + 4 * n, at + 4 * (c + E + 1), at + 4 * n,
+            at + 4 * (c + 2 * (E + 1)), work.data_ptr(), need, raw))
         r = Routing()
-        with ctx:
-            ints = torch.empty(2 * n + 2 * (E + 1) + rows, dtype=torch.int32, device=logits.device)
-            floats = torch.empty(n + 1, dtype=torch.float32, device=logits.device)
-            work = torch.empty(max(need, 16), dtype=torch.uint8, device=logits.device)
-        index, position, r.counts, r.offsets, r.row_token = ints.split([n, n, E + 1, E + 1, rows])
-        gate, r.loss = floats.split([n, 1])
-        r.index, r.position, r.gate = index.view(tokens, k), position.view(tokens, k), gate.view(tokens, k)
-        at, ft = ints.data_ptr(), floats.data_ptr()
-        _check(L.soap_router_forward(tokens, E, k, kind, logits.data_ptr(), _ld(logits), _raw(mask),
-                                     self.flags, self.balance, at, ft, at + 8 * n, ft + 4 * n,
-                                     at + 8 * n + 4 * (E + 1), at + 4 * n, at + 8 * n + 8 * (E + 1),
-                                     work.data_ptr(), need, raw))
+        r.index = ints.as_strided((tokens, k), (k, 1), 0)
+        r.position = ints.as_strided((tokens, k), (k, 1), n)
+        r.counts = ints.as_strided((E + 1,), (1,), c)
+        r.offsets = ints.as_strided((E + 1,), (1,), c + E + 1)
+        r.row_token = ints.as_strided((rows,), (1,), c + 2 * (E + 1))
+        r.gate = floats.as_strided((tokens, k), (k, 1), 0)
+        r.loss = floats.as_strided((1,), (1,), n)
         return r
 
     def backward(self, logits, index, counts, dgate=None, dloss=None, mask=None, stream=None):
         """dlogits, of the logits' type, from the gradients of gate (float32
         [tokens, top_k]) and loss (float32 [1], None: 1)."""
-        import torch
-        kind = self._args(logits, mask)
+        if stream is not None:
+            return _on(stream, (logits, mask, index, counts, dgate, dloss), self.backward, logits, index,
+                       counts, dgate, dloss, mask)
+        raw, kind = _current_stream(logits, "logits"), _floats(logits, "logits", self.experts)
         tokens, k, E = logits.shape[0], self.top_k, self.experts
-        _exactly(index, "index", torch.int32, (tokens, k))
-        _exactly(counts, "counts", torch.int32, (E + 1,))
+        i32, f32 = _torch.int32, _torch.float32
+        if mask is not None:
+            _exactly(mask, "mask", _torch.bool, (tokens,), logits)
+        _exactly(index, "index", i32, (tokens, k), logits)
+        _exactly(counts, "counts", i32, (E + 1,), logits)
         if dgate is not None:
-            _exactly(dgate, "dgate", torch.float32, (tokens, k))
+            _exactly(dgate, "dgate", f32, (tokens, k), logits)
         if dloss is not None:
-            _exactly(dloss, "dloss", torch.float32, (1,))
-        ctx, raw = _on_stream(stream, (logits, mask, index, counts, dgate, dloss))
-        with ctx:
-            out = torch.empty((tokens, E), dtype=logits.dtype, device=logits.device)
-        _check(lib().soap_router_backward(tokens, E, k, kind, logits.data_ptr(), _ld(logits),
-                                          _raw(mask), self.flags, self.balance, index.data_ptr(),
-                                          counts.data_ptr(), _raw(dgate), _raw(dloss),
-                                          out.data_ptr(), E, raw))
+            _exactly(dloss, "dloss", f32, (1,), logits)
+        out = logits.new_empty((tokens, E))
+        _check(lib().soap_router_backward(
+            tokens, E, k, kind, logits.data_ptr(), _ld(logits), None if mask is None else mask.data_ptr(),
+            self.flags, self.balance, index.data_ptr(), counts.data_ptr(),
+            None if dgate is None else dgate.data_ptr(), None if dloss is None else dloss.data_ptr(),
+            out.data_ptr(), E, raw))
         return out
 
 
@@ -749,12 +771,14 @@ class Mx4:
     """A matrix, or a batch of them, in packed MXFP4 along its last axis of `k` values:
     ``data`` and ``scale`` uint8 [.., rows, bytes of a row]."""
 
+    __slots__ = ("data", "scale", "k")
+
     def __init__(self, data, scale, k: int):
-        import torch
+        u8, lead = _T().uint8, data.shape[:-1]
         padded = (k + 255) // 256 * 256
-        _exactly(data, "data", torch.uint8, (*data.shape[:-1], padded // 2))
-        _exactly(scale, "scale", torch.uint8, (*data.shape[:-1], padded // 32))
-        if data.dim() not in (2, 3):
+        _exactly(data, "data", u8, (*lead, padded // 2))
+        _exactly(scale, "scale", u8, (*lead, padded // 32), data)
+        if len(lead) not in (1, 2):
             raise ValueError("data must be [rows, bytes] or [batch, rows, bytes]")
         self.data, self.scale, self.k = data, scale, k
 
@@ -764,27 +788,29 @@ class Mx4:
 
     def values(self, dtype=None, stream=None):
         """What the packed values stand for, as float32 (default) or bfloat16 [.., rows, k]."""
-        import torch
-        dtype = dtype or torch.float32
-        if dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError(f"values are float32 or bfloat16, not {dtype}")
-        ctx, raw = _on_stream(stream, (self.data, self.scale))
-        with ctx:
-            out = torch.empty((*self.data.shape[:-1], self.k), dtype=dtype, device=self.data.device)
-        rows = out.numel() // self.k
-        _check(lib().soap_mx4_dequantize(rows, self.k, self.data.data_ptr(), self.scale.data_ptr(),
-                                         SOAP_BF16 if dtype == torch.bfloat16 else SOAP_F32,
-                                         out.data_ptr(), self.k, raw))
+        if stream is not None:
+            return _on(stream, (self.data, self.scale), self.values, dtype)
+        raw, kind, dtype = _current_stream(self.data, "data"), *_out_type(dtype)
+        out = self.data.new_empty((*self.data.shape[:-1], self.k), dtype=dtype)
+        _check(lib().soap_mx4_dequantize(out.numel() // self.k, self.k, self.data.data_ptr(),
+                                         self.scale.data_ptr(), kind, out.data_ptr(), self.k, raw))
         return out
 
 
-def _mx4_empty(batch, rows, k, device):
-    import torch
-    padded = (k + 255) // 256 * 256
-    lead = (rows,) if batch is None else (batch, rows)
+def _out_type(dtype):
+    T = _T()
+    if dtype is None or dtype is T.float32:
+        return SOAP_F32, T.float32
+    if dtype is T.bfloat16:
+        return SOAP_BF16, dtype
+    raise TypeError(f"results are float32 or bfloat16, not {dtype}")
+
+
+def _mx4_empty(x, lead, k):
+    """An Mx4 without contents, on x's device."""
+    padded, u8 = (k + 255) // 256 * 256, _torch.uint8
     m = Mx4.__new__(Mx4)
-    m.data = torch.empty((*lead, padded // 2), dtype=torch.uint8, device=device)
-    m.scale = torch.empty((*lead, padded // 32), dtype=torch.uint8, device=device)
+    m.data, m.scale = x.new_empty((*lead, padded // 2), dtype=u8), x.new_empty((*lead, padded // 32), dtype=u8)
     m.k = k
     return m
 
@@ -794,84 +820,77 @@ def mx4_quantize(x, along: str = "cols", row_index=None, stream=None):
     with blocks along its columns ("cols"), along its rows ("rows": the transposed
     matrix, [cols, rows]) or both (a pair, x read once).  row_index (int32 [n]) takes
     the rows row_index[i] of x, zeros where that is not a row of x."""
-    import torch
     if along not in ("cols", "rows", "both"):
         raise ValueError(f'along must be "cols", "rows" or "both", got {along!r}')
-    kind = _floats(x, "x")
-    if x.dim() not in (2, 3) or (x.dim() == 3 and not x.is_contiguous()):
+    if stream is not None:
+        return _on(stream, (x, row_index), mx4_quantize, x, along, row_index)
+    raw, kind, shape = _current_stream(x, "x"), _floats(x, "x"), x.shape
+    if len(shape) not in (2, 3) or (len(shape) == 3 and not x.is_contiguous()):
         raise ValueError("x must be [rows, cols] or contiguous [batch, rows, cols]")
-    batch = x.shape[0] if x.dim() == 3 else None
+    cols, x_rows, lead = shape[-1], shape[-2], shape[:-2]
+    rows = x_rows
     if row_index is not None:
-        if batch is not None:
+        if lead:
             raise ValueError("row_index takes a single matrix")
-        _exactly(row_index, "row_index", torch.int32, (row_index.numel(),))
-    cols, x_rows = x.shape[-1], x.shape[-2]
-    rows = x_rows if row_index is None else row_index.numel()
-    ctx, raw = _on_stream(stream, (x, row_index))
-    with ctx:
-        a = _mx4_empty(batch, rows, cols, x.device) if along != "rows" else None
-        b = _mx4_empty(batch, cols, rows, x.device) if along != "cols" else None
-    ld = _ld(x) if batch is None else cols
-    _check(lib().soap_mx4_quantize(batch or 1, rows, cols, kind, x.data_ptr(), ld, _raw(row_index),
-                                   x_rows, *((a.data.data_ptr(), a.scale.data_ptr()) if a else (None, None)),
-                                   *((b.data.data_ptr(), b.scale.data_ptr()) if b else (None, None)),
-                                   raw))
+        rows = row_index.numel()
+        _exactly(row_index, "row_index", _torch.int32, (rows,), x)
+    a = _mx4_empty(x, (*lead, rows), cols) if along != "rows" else None
+    b = _mx4_empty(x, (*lead, cols), rows) if along != "cols" else None
+    _check(lib().soap_mx4_quantize(
+        lead[0] if lead else 1, rows, cols, kind, x.data_ptr(), cols if lead else _ld(x),
+        None if row_index is None else row_index.data_ptr(), x_rows,
+        None if a is None else a.data.data_ptr(), None if a is None else a.scale.data_ptr(),
+        None if b is None else b.data.data_ptr(), None if b is None else b.scale.data_ptr(), raw))
     return (a, b) if along == "both" else a or b
 
 
-def _mx4_args(a, b, dtype, dims_b):
-    import torch
+def _mx4_check(a, b, dims_b):
     if a.data.dim() != 2 or b.data.dim() != dims_b:
         raise ValueError(f"a must be one matrix and b {'a batch' if dims_b == 3 else 'one matrix'}")
     if a.k != b.k:
         raise ValueError(f"a and b are summed over one axis: {a.k} and {b.k} values")
-    if dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError(f"products are float32 or bfloat16, not {dtype}")
-    return SOAP_BF16 if dtype == torch.bfloat16 else SOAP_F32
+    if a.data.get_device() != b.data.get_device():
+        raise ValueError(f"a is on {a.data.device}, b on {b.data.device}")
 
 
 def mx4_product(a: Mx4, b: Mx4, dtype=None, stream=None):
     """a b^T, float32 (default) or bfloat16 [a.rows, b.rows] (soap_mx4_gemm)."""
-    import torch
-    dtype = dtype or torch.float32
-    kind = _mx4_args(a, b, dtype, 2)
-    ctx, raw = _on_stream(stream, (a.data, a.scale, b.data, b.scale))
-    with ctx:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.data.device)
+    if stream is not None:
+        return _on(stream, (a.data, a.scale, b.data, b.scale), mx4_product, a, b, dtype)
+    _mx4_check(a, b, 2)
+    raw, kind, dtype = _current_stream(a.data, "a"), *_out_type(dtype)
+    out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
     _check(lib().soap_mx4_gemm(a.rows, b.rows, a.k, a.data.data_ptr(), a.scale.data_ptr(),
-                               b.data.data_ptr(), b.scale.data_ptr(), kind, out.data_ptr(), b.rows,
-                               raw))
+                               b.data.data_ptr(), b.scale.data_ptr(), kind, out.data_ptr(), b.rows, raw))
     return out
 
 
 def mx4_product_rows(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
     """Rows offsets[g] .. offsets[g + 1] of a times b[g]^T, [a.rows, b.rows]; zeros past the
     last group (soap_mx4_gemm_rows).  offsets: int32 [groups + 1] on the GPU."""
-    import torch
-    dtype = dtype or torch.float32
-    kind = _mx4_args(a, b, dtype, 3)
+    if stream is not None:
+        return _on(stream, (a.data, a.scale, b.data, b.scale, offsets), mx4_product_rows, a, b, offsets, dtype)
+    _mx4_check(a, b, 3)
+    raw, kind, dtype = _current_stream(a.data, "a"), *_out_type(dtype)
     groups = b.data.shape[0]
-    _exactly(offsets, "offsets", torch.int32, (groups + 1,))
-    ctx, raw = _on_stream(stream, (a.data, a.scale, b.data, b.scale, offsets))
-    with ctx:
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.data.device)
-    _check(lib().soap_mx4_gemm_rows(groups, a.rows, b.rows, a.k, offsets.data_ptr(),
-                                    a.data.data_ptr(), a.scale.data_ptr(), b.data.data_ptr(),
-                                    b.scale.data_ptr(), kind, out.data_ptr(), b.rows, raw))
+    _exactly(offsets, "offsets", _torch.int32, (groups + 1,), a.data)
+    out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
+    _check(lib().soap_mx4_gemm_rows(groups, a.rows, b.rows, a.k, offsets.data_ptr(), a.data.data_ptr(),
+                                    a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
+                                    out.data_ptr(), b.rows, raw))
     return out
 
 
 def mx4_product_k(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
     """a b^T summed over k = offsets[g] .. offsets[g + 1] for every g, [groups, a.rows, b.rows]:
     the layout of the batched steps' gradients (soap_mx4_gemm_k)."""
-    import torch
-    dtype = dtype or torch.float32
-    kind = _mx4_args(a, b, dtype, 2)
-    _exactly(offsets, "offsets", torch.int32, (offsets.numel(),))
+    if stream is not None:
+        return _on(stream, (a.data, a.scale, b.data, b.scale, offsets), mx4_product_k, a, b, offsets, dtype)
+    _mx4_check(a, b, 2)
+    raw, kind, dtype = _current_stream(a.data, "a"), *_out_type(dtype)
+    _exactly(offsets, "offsets", _torch.int32, (offsets.numel(),), a.data)
     groups = offsets.numel() - 1
-    ctx, raw = _on_stream(stream, (a.data, a.scale, b.data, b.scale, offsets))
-    with ctx:
-        out = torch.empty((groups, a.rows, b.rows), dtype=dtype, device=a.data.device)
+    out = a.data.new_empty((groups, a.rows, b.rows), dtype=dtype)
     _check(lib().soap_mx4_gemm_k(groups, a.rows, b.rows, a.k, offsets.data_ptr(), a.data.data_ptr(),
                                  a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
                                  out.data_ptr(), raw))
