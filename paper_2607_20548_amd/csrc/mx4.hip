@@ -123,8 +123,11 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
 // directions are formed in registers.  A block along the columns is eight lanes of
 // one row, a block along the rows one column of a lane; those go through LDS, so
 // that a column's 64 bytes (four blocks) are written together.  Workgroups of
-// consecutive rows run on one XCD, whose L2 joins what they write of a line.
-template <typename T, bool ROWS>
+// consecutive rows run on one XCD, whose L2 joins what they write of a line.  Without
+// an index no row is read twice: the loads leave the L2s to the stores (the 64 x 2048 x
+// 768 bank both ways 92 us against 103); with one, a token's row is read for each of
+// its experts and kept there (36 864 rows of 4096 tokens 28 us against 33).
+template <typename T, bool ROWS, bool GATHER>
 __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
   // column x's block of wave w: 16 bytes at x * 64 + 16 * (w ^ (x / 4 % 4))
   __shared__ __attribute__((aligned(16))) uint8_t lds[256 * 64 + 256 * 4];
@@ -146,13 +149,14 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
   for (int i = 0; i < 32; ++i) {
     const int64_t r = r0 + i;
     int64_t src = -1;
-    if (r < p.rows) src = p.row_index ? (int64_t)p.row_index[r] : r;
-    if (src >= p.x_rows) src = -1;
+    if (r < p.rows) src = GATHER ? (int64_t)p.row_index[r] : r;
+    if (GATHER && src >= p.x_rows) src = -1;
     raw[i] = Raw(0u);
     if (src < 0) continue;
     const T *xr = x + src * p.ldx + cw;
     if (all) {
-      raw[i] = __builtin_nontemporal_load(reinterpret_cast<const Raw *>(xr) + lane);
+      if constexpr (GATHER) raw[i] = *(reinterpret_cast<const Raw *>(xr) + lane);
+      else raw[i] = __builtin_nontemporal_load(reinterpret_cast<const Raw *>(xr) + lane);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -235,44 +239,62 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
         *reinterpret_cast<const uint32_t *>(lds + 256 * 64 + 4 * threadIdx.x);
 }
 
-// The values of a packed matrix: eight per thread.
-template <typename T>
+// The values of a packed matrix, along its rows as mx4_quantize_cols walks them: eight
+// values per lane, QC_UNITS independent loads at a time.  The values are written past
+// the L2s (a pass over memory follows or none does).
+template <typename T, int LPR>
 __global__ __launch_bounds__(256) void mx4_dequantize(Mx4Mat a, int64_t rows, int64_t cols, int64_t kp,
                                                       T *__restrict__ out, int64_t ldo, int vec) {
-  const int64_t per = (cols + 7) / 8, n = rows * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per, c = 8 * (i - r * per);
-    const uint32_t q = *reinterpret_cast<const uint32_t *>(a.data + r * (kp / 2) + c / 2);
-    const uint32_t byte = a.scale[r * (kp / 32) + c / 32];
-    const float s = byte == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte);
-    float v[8];
+  constexpr int ROWS = 256 / LPR;
+  const int lane = threadIdx.x % LPR;
+  for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; r < rows; r += (int64_t)gridDim.x * ROWS) {
+    const uint8_t *dr = a.data + r * (kp / 2), *sr = a.scale + r * (kp / 32);
+    T *o = out + r * ldo;
+    for (int64_t c0 = 8 * lane; c0 < cols; c0 += QC_UNITS * LPR * 8) {
+      uint32_t q[QC_UNITS], byte[QC_UNITS];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t m = (q >> (4 * j)) & 7u;
-      float f = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
-      v[j] = ((q >> (4 * j)) & 8u ? -f : f) * s;
-    }
-    T *o = out + r * ldo + c;
-    if (vec && c + 8 <= cols) {
-      if constexpr (sizeof(T) == 4) {
-        typedef float v4f __attribute__((ext_vector_type(4)));
-        __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f *>(o));
-        __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<v4f *>(o + 4));
-      } else {
-        v4u w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) |
-                 ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16);
-        __builtin_nontemporal_store(w, reinterpret_cast<v4u *>(o));
+      for (int u = 0; u < QC_UNITS; ++u) {
+        const int64_t c = c0 + u * LPR * 8;
+        q[u] = byte[u] = 0u;
+        if (c >= cols) continue;
+        q[u] = *reinterpret_cast<const uint32_t *>(dr + c / 2);
+        byte[u] = sr[c / 32];
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < cols) {
-          if constexpr (sizeof(T) == 4) o[j] = v[j];
-          else o[j] = __builtin_bit_cast(uint16_t, (__bf16)v[j]);
+      for (int u = 0; u < QC_UNITS; ++u) {
+        const int64_t c = c0 + u * LPR * 8;
+        if (c >= cols) continue;
+        const float s = byte[u] == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte[u]);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          // code m = 0, 1: 0.5 m; else (1 + 0.5 (m % 2)) 2^(m / 2 - 1)
+          const uint32_t m = (q[u] >> (4 * j)) & 7u;
+          const float f = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
+          v[j] = ((q[u] >> (4 * j)) & 8u ? -f : f) * s;
         }
+        if (vec && c + 8 <= cols) {
+          if constexpr (sizeof(T) == 4) {
+            typedef float v4f __attribute__((ext_vector_type(4)));
+            __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f *>(o + c));
+            __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<v4f *>(o + c + 4));
+          } else {
+            v4u w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) |
+                     ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16);
+            __builtin_nontemporal_store(w, reinterpret_cast<v4u *>(o + c));
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c + j < cols) {
+              if constexpr (sizeof(T) == 4) o[c + j] = v[j];
+              else o[c + j] = __builtin_bit_cast(uint16_t, (__bf16)v[j]);
+            }
+        }
+      }
     }
   }
 }
@@ -812,7 +834,11 @@ hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s) {
   if (tiles == 0) return hipSuccess;
   if (tiles > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)tiles, (unsigned)d.batch);
-#define SOAP_MXQ(T, R) hipLaunchKernelGGL((mx4_quantize_tile<T, R>), grid, dim3(256), 0, s, p)
+#define SOAP_MXQ(T, R)                                                                                    \
+  do {                                                                                                    \
+    if (d.row_index) hipLaunchKernelGGL((mx4_quantize_tile<T, R, true>), grid, dim3(256), 0, s, p);       \
+    else hipLaunchKernelGGL((mx4_quantize_tile<T, R, false>), grid, dim3(256), 0, s, p);                  \
+  } while (0)
   if (d.bf16) { if (d.data) SOAP_MXQ(uint16_t, true); else SOAP_MXQ(uint16_t, false); }
   else { if (d.data) SOAP_MXQ(float, true); else SOAP_MXQ(float, false); }
 #undef SOAP_MXQ
@@ -822,15 +848,15 @@ hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s) {
 hipError_t launch_mx4_dequantize(const Mx4Mat &a, int64_t rows, int64_t cols, bool bf16, void *out,
                                  int64_t ldo, hipStream_t s) {
   if (rows <= 0) return hipSuccess;
-  const int64_t n = rows * ((cols + 7) / 8);
-  const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 16384));
-  const bool vec = (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && ldo * (bf16 ? 2 : 4) % 16 == 0;
-  if (bf16)
-    hipLaunchKernelGGL((mx4_dequantize<uint16_t>), grid, dim3(256), 0, s, a, rows, cols, mx4_padded(cols),
-                       static_cast<uint16_t *>(out), ldo, (int)vec);
-  else
-    hipLaunchKernelGGL((mx4_dequantize<float>), grid, dim3(256), 0, s, a, rows, cols, mx4_padded(cols),
-                       static_cast<float *>(out), ldo, (int)vec);
+  const int64_t kp = mx4_padded(cols);
+  const bool half = kp == 256;                     // a row is half a wave's 512 values
+  const dim3 grid((unsigned)std::min<int64_t>((rows + (half ? 7 : 3)) / (half ? 8 : 4), 1 << 16));
+  const int vec = (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && ldo * (bf16 ? 2 : 4) % 16 == 0;
+#define SOAP_MXV(T, L) \
+  hipLaunchKernelGGL((mx4_dequantize<T, L>), grid, dim3(256), 0, s, a, rows, cols, kp, static_cast<T *>(out), ldo, vec)
+  if (bf16) { if (half) SOAP_MXV(uint16_t, 32); else SOAP_MXV(uint16_t, 64); }
+  else { if (half) SOAP_MXV(float, 32); else SOAP_MXV(float, 64); }
+#undef SOAP_MXV
   return hipGetLastError();
 }
 

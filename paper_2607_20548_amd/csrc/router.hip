@@ -73,6 +73,14 @@ __device__ __forceinline__ float rt_unkey(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
 
+// The key of the value alone, of a bfloat16's key with an expert in its lower half: the
+// lower bits are ones below zero, zeros above, as in the value's own key.
+template <bool UNIQUE>
+__device__ __forceinline__ uint32_t rt_value(uint32_t k) {
+  if (!UNIQUE || k == 0u) return k;
+  return (k & 0xffff0000u) | (k & 0x80000000u ? 0u : 0xffffu);
+}
+
 // The lane's logits e0 .. e0 + V - 1 of a row; -inf past the last expert.
 template <typename T, int V>
 __device__ __forceinline__ void rt_load(const T *row, int e0, int experts, int vec, float *v) {
@@ -232,6 +240,7 @@ __device__ void rt_loss(const RtParams &p, C counts, P psum) {
 // ONE: the whole batch is one chunk and everything is done here.
 template <typename T, int LPR, int V, bool ONE>
 __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
+  constexpr bool UNIQUE = sizeof(T) == 2;            // keys with the expert's number in them
   constexpr int ROWS = RT_NT / LPR;                  // tokens of a pass
   constexpr int SLOTS = (RT_MAX_K + LPR - 1) / LPR;  // choices of a lane
   __shared__ int hist[RT_MAX_E + 1];
@@ -256,9 +265,11 @@ __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       key[i] = on ? rt_key(l[i]) : 0u;
+      // a bfloat16's key leaves 16 bits free: the expert, the lowest the largest
+      if (UNIQUE && key[i]) key[i] = (key[i] & 0xffff0000u) | (uint32_t)(0xffff - (e0 + i));
       best = max(best, key[i]);
     }
-    const uint32_t top = lane_max<LPR>(best);
+    const uint32_t topu = lane_max<LPR>(best), top = rt_value<UNIQUE>(topu);
     const float mx = rt_unkey(top);
     const float s = rt_softmax<LPR, V>(l, e0, p.experts, top, pr);
     if (top != 0u) {
@@ -269,7 +280,7 @@ __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
     }
     int pick[SLOTS];
     float e[SLOTS], chosen = 0.f;
-    uint32_t now = top;
+    uint32_t now = topu;
 #pragma unroll
     for (int slot = 0; slot < SLOTS; ++slot) {
       pick[slot] = -1;
@@ -283,14 +294,20 @@ __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
           now = lane_max<LPR>(best);
         }
         uint32_t at = 0x7fffffffu;               // the lowest expert that has it
+        if constexpr (UNIQUE) {
+          at = 0xffffu - (now & 0xffffu);
 #pragma unroll
-        for (int i = V - 1; i >= 0; --i) at = key[i] == now ? (uint32_t)(e0 + i) : at;
-        at = lane_reduce<LPR>(at, [](uint32_t a, uint32_t b) { return min(a, b); });
+          for (int i = 0; i < V; ++i) key[i] = key[i] == now ? 0u : key[i];
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = (uint32_t)(e0 + i) == at ? 0u : key[i];
+          for (int i = V - 1; i >= 0; --i) at = key[i] == now ? (uint32_t)(e0 + i) : at;
+          at = lane_reduce<LPR>(at, [](uint32_t a, uint32_t b) { return min(a, b); });
+#pragma unroll
+          for (int i = 0; i < V; ++i) key[i] = (uint32_t)(e0 + i) == at ? 0u : key[i];
+        }
         if (lane == j && now != 0u) {
           pick[slot] = (int)at;
-          mine = now;
+          mine = rt_value<UNIQUE>(now);
         }
       }
       e[slot] = pick[slot] >= 0 ? expf(rt_unkey(mine) - mx) : 0.f;
