@@ -371,6 +371,14 @@ __device__ __forceinline__ bool mx_tile(const MxParams &p, int64_t t, int g, MxT
   return true;
 }
 
+// Rows [0, rows) of a packed matrix (or of its scales), `bytes` each, as a buffer:
+// loads past them give zeros.
+constexpr int MX_RSRC_WORD3 = 0x00020000;    // raw 32-bit data
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mx_buffer(const uint8_t *base, int rows, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), (short)0, (int)(uint32_t)(rows * bytes),
+                                           MX_RSRC_WORD3);
+}
+
 // This workgroup's tile of a product by TM x TN: column tn, row tile in o.  Tiles
 // that run together share operands in their XCD's L2: one product gives every XCD a
 // contiguous run of tiles, eight tiles of rows by all tiles of columns at a time;
@@ -515,30 +523,30 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  const int am = (int)min((int64_t)TM, o.m1 - m0) - 1, bm = (int)min((int64_t)TN, p.N - n0) - 1;
-  const uint8_t *abase = p.A + m0 * p.bytes, *bbase = p.B + (o.b0 + n0) * p.bytes;
+  const int am = (int)min((int64_t)TM, o.m1 - m0), bm = (int)min((int64_t)TN, p.N - n0);   // rows there are
   const int64_t srow = p.bytes / 16;
-  const uint8_t *asbase = p.As + m0 * srow, *bsbase = p.Bs + (o.b0 + n0) * srow;
+  const auto abuf = mx_buffer(p.A + m0 * p.bytes, am, p.bytes);
+  const auto bbuf = mx_buffer(p.B + (o.b0 + n0) * p.bytes, bm, p.bytes);
+  const auto asbuf = mx_buffer(p.As + m0 * srow, am, srow);
+  const auto bsbuf = mx_buffer(p.Bs + (o.b0 + n0) * srow, bm, srow);
   // thread -> rows lr + 32 i, unit lg of A's and B's rows
   const int lr = tid >> 3, lg = tid & 7;
-  uint32_t off[UNITS];
-#pragma unroll
-  for (int i = 0; i < UNITS; ++i)
-    off[i] = (uint32_t)((i < TM / 32 ? min(32 * i + lr, am) : min(32 * i - TM + lr, bm)) * p.bytes + 16 * lg);
-  // and rows of scales tid + 256 i
+  const uint32_t off = (uint32_t)(lr * p.bytes + 16 * lg), row32 = (uint32_t)(32 * p.bytes);
+  // and rows of scales tid + 256 i of A's and B's rows together
   uint32_t soff[SU];
 #pragma unroll
   for (int i = 0; i < SU; ++i) {
     const int r = 256 * i + tid;
-    soff[i] = (uint32_t)((r < TM ? min(r, am) : min(r - TM, bm)) * srow);
+    soff[i] = (uint32_t)((r < TM ? r : r - TM) * srow);
   }
   const int slabs = (int)(p.bytes >> 7);           // of a packed row; at least 2
   const int s0 = o.kb0 >> 3, s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : s0;
   const int dst = lr * 128 + 16 * (lg ^ ((lr >> 1) & 7));
   v4u r[UNITS], rs[SU];
   auto load = [&](int s, int i) {
-    const int64_t k = 128 * (int64_t)min(s, s1 - 1);
-    r[i] = *reinterpret_cast<const v4u *>((i < TM / 32 ? abase : bbase) + k + off[i]);
+    const int k = 128 * min(s, s1 - 1);
+    if (i < TM / 32) r[i] = __builtin_amdgcn_raw_buffer_load_b128(abuf, (int)(off + i * row32), k, 0);
+    else r[i] = __builtin_amdgcn_raw_buffer_load_b128(bbuf, (int)(off + (i - TM / 32) * row32), k, 0);
   };
   auto store = [&](int half, int i) {
     *reinterpret_cast<v4u *>(lds + half * L::DATA + i * 4096 + dst) = r[i];
@@ -548,9 +556,8 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
     const int at = 8 * min(s, slabs - 2);
 #pragma unroll
     for (int i = 0; i < SU; ++i) {
-      const uint2 *src = reinterpret_cast<const uint2 *>((256 * i + tid < TM ? asbase : bsbase) + at + soff[i]);
-      const uint2 lo = src[0], hi = src[1];
-      rs[i] = v4u{lo.x, lo.y, hi.x, hi.y};
+      if (256 * i + 64 * wave < TM) rs[i] = __builtin_amdgcn_raw_buffer_load_b128(asbuf, (int)soff[i], at, 0);
+      else rs[i] = __builtin_amdgcn_raw_buffer_load_b128(bsbuf, (int)soff[i], at, 0);
     }
   };
   auto store_scales = [&](int s) {
@@ -670,13 +677,14 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
 // next on its way through registers, and up to three workgroups per compute unit,
 // which cover each other's barriers, first loads and epilogues.
 template <int MODE, typename T, bool STREAM>
-__global__ __launch_bounds__(256, 3) void mx4_gemm_tile128(MxParams p) {
+__global__ __launch_bounds__(256, 4) void mx4_gemm_tile128(MxParams p) {
   constexpr int TM = 128, TN = 128, BI = 2, BJ = 2, UNITS = 8, DATA = 256 * 128;
   __shared__ __attribute__((aligned(16))) uint8_t lds[DATA + 256 * 8];
   int tn, g;
   MxTile o;
   if (!mx_my_tile<MODE, TM>(p, tn, g, o)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   const int xl = lane & 31, h = lane >> 5;
   const int64_t m0 = o.m0, n0 = (int64_t)tn * TN;
   if (m0 >= o.m1) return;
@@ -687,24 +695,27 @@ __global__ __launch_bounds__(256, 3) void mx4_gemm_tile128(MxParams p) {
     for (int j = 0; j < BJ; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  const int am = (int)min((int64_t)TM, o.m1 - m0) - 1, bm = (int)min((int64_t)TN, p.N - n0) - 1;
-  const uint8_t *abase = p.A + m0 * p.bytes, *bbase = p.B + (o.b0 + n0) * p.bytes;
+  const int am = (int)min((int64_t)TM, o.m1 - m0), bm = (int)min((int64_t)TN, p.N - n0);   // rows there are
   const int64_t srow = p.bytes / 16;
+  const auto abuf = mx_buffer(p.A + m0 * p.bytes, am, p.bytes);
+  const auto bbuf = mx_buffer(p.B + (o.b0 + n0) * p.bytes, bm, p.bytes);
+  // thread -> rows lr + 32 i, unit lg of A's and B's rows; its row of scales
   const int lr = tid >> 3, lg = tid & 7;
-  uint32_t off[UNITS];
-#pragma unroll
-  for (int i = 0; i < UNITS; ++i)
-    off[i] = (uint32_t)((i < 4 ? min(32 * i + lr, am) : min(32 * i - TM + lr, bm)) * p.bytes + 16 * lg);
-  const uint8_t *sbase = tid < TM ? p.As + (m0 + min(tid, am)) * srow : p.Bs + (o.b0 + n0 + min(tid - TM, bm)) * srow;
+  const uint32_t off = (uint32_t)(lr * p.bytes + 16 * lg), row32 = (uint32_t)(32 * p.bytes);
+  const bool of_a = wave < TM / 64;
+  const auto sbuf = of_a ? mx_buffer(p.As + m0 * srow, am, srow) : mx_buffer(p.Bs + (o.b0 + n0) * srow, bm, srow);
+  const uint32_t soff = (uint32_t)((of_a ? tid : tid - TM) * srow);
   const int s0 = o.kb0 >> 3, s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : s0;
   const int dst = lr * 128 + 16 * (lg ^ ((lr >> 1) & 7));
   v4u r[UNITS];
-  uint2 rs;
+  v2u rs;
   auto load = [&](int s) {
-    const int64_t k = 128 * (int64_t)s;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) r[i] = *reinterpret_cast<const v4u *>((i < 4 ? abase : bbase) + k + off[i]);
-    rs = *reinterpret_cast<const uint2 *>(sbase + 8 * (int64_t)s);
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(abuf, (int)(off + i * row32), 128 * s, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r[4 + i] = __builtin_amdgcn_raw_buffer_load_b128(bbuf, (int)(off + i * row32), 128 * s, 0);
+    rs = __builtin_amdgcn_raw_buffer_load_b64(sbuf, (int)soff, 8 * s, 0);
   };
   if (s1 > s0) load(s0);
   const int sw = (xl >> 1) & 7, arow = wm * 64 + xl, brow = TM + wn * 64 + xl;
@@ -713,7 +724,7 @@ __global__ __launch_bounds__(256, 3) void mx4_gemm_tile128(MxParams p) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) *reinterpret_cast<v4u *>(lds + i * 4096 + dst) = r[i];
-    *reinterpret_cast<uint2 *>(lds + DATA + 8 * tid) = rs;
+    *reinterpret_cast<v2u *>(lds + DATA + 8 * tid) = rs;
     __syncthreads();
     load(min(s + 1, s1 - 1));
     uint32_t mine = 0u;                            // bytes of the blocks that are this product's
