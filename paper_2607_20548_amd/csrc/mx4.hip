@@ -240,8 +240,9 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
 }
 
 // The values of a packed matrix, along its rows as mx4_quantize_cols walks them: eight
-// values per lane, QC_UNITS independent loads at a time.  The values are written past
-// the L2s (a pass over memory follows or none does).
+// values per lane, QC_UNITS independent loads at a time; the values, two to eight times
+// the bytes read, are written past the L2s (64 x 2048 x 768 both ways to bfloat16 115 us
+// against 128).
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void mx4_dequantize(Mx4Mat a, int64_t rows, int64_t cols, int64_t kp,
                                                       T *__restrict__ out, int64_t ldo, int vec) {
@@ -478,7 +479,7 @@ __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, 
 // wave per SIMD: nothing else fills a gap, and a burst of loads holds the wave up
 // until the L1 takes them, 27 cycles a kilobyte).  Loads into LDS without
 // registers, which have to wait for the slab they replace: 4096 x 4096 x 14336
-// @DMA@ us; slabs of 128 values, four of them in LDS: 134 us (64 bytes of a row
+// 133 us; slabs of 128 values, four of them in LDS: 134 us (64 bytes of a row
 // at a time take the L1 44 cycles a kilobyte).
 //
 // Slabs are whole in the packed rows; blocks outside [kb0, kb1), the neighbours'
@@ -674,8 +675,8 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
 }
 
 // Tiles of 128 x 128 for products of fewer or shorter tiles: one slab in LDS, the
-// next on its way through registers, and up to three workgroups per compute unit,
-// which cover each other's barriers, first loads and epilogues.
+// next on its way through registers, and four workgroups per compute unit, which cover
+// each other's barriers, first loads and epilogues.
 template <int MODE, typename T, bool STREAM>
 __global__ __launch_bounds__(256, 4) void mx4_gemm_tile128(MxParams p) {
   constexpr int TM = 128, TN = 128, BI = 2, BJ = 2, UNITS = 8, DATA = 256 * 128;
@@ -774,30 +775,130 @@ __global__ __launch_bounds__(256, 4) void mx4_gemm_tile128(MxParams p) {
                       lds + wave * 32 * STRIDE, acc);
 }
 
+// Few rows: 32 x 32 of C per workgroup, whose MXF_W waves take the slabs of K in turn
+// and add their sums in LDS in order.  Operands go from memory to registers, all of a
+// wave's loads of MXF_AHEAD slabs ahead of its matrix instructions; B is read once, at
+// the rate of HBM, by as many waves as there are.
+constexpr int MXF_W = 8, MXF_AHEAD = 2;
+template <int MODE, typename T>
+__global__ __launch_bounds__(64 * MXF_W) void mx4_gemm_few(MxParams p) {
+  __shared__ float part[MXF_W][16][64];
+  MxTile o;
+  const int64_t tm = blockIdx.x / p.tiles_n, tn = blockIdx.x - tm * p.tiles_n;
+  if (!mx_tile<MODE, 32>(p, tm, 0, o)) return;
+  const int64_t m0 = o.m0, n0 = tn * 32;
+  if (m0 >= o.m1) return;
+  const int tid = threadIdx.x, lane = tid & 63, xl = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int am = (int)min((int64_t)32, o.m1 - m0), bm = (int)min((int64_t)32, p.N - n0);   // rows there are
+  const int64_t srow = p.bytes / 16;
+  const auto abuf = mx_buffer(p.A + m0 * p.bytes, am, p.bytes);
+  const auto bbuf = mx_buffer(p.B + (o.b0 + n0) * p.bytes, bm, p.bytes);
+  const auto asbuf = mx_buffer(p.As + m0 * srow, am, srow);
+  const auto bsbuf = mx_buffer(p.Bs + (o.b0 + n0) * srow, bm, srow);
+  const int off = (int)(uint32_t)(xl * p.bytes + 16 * h), soff = (int)(uint32_t)(xl * srow);
+  const uint32_t pick = h ? 0x07050301u : 0x06040200u;
+  const int s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : 0;     // kb0 is 0 where K is not grouped
+  v16f acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  for (int s0 = wave; s0 < s1; s0 += MXF_W * MXF_AHEAD) {
+    v4u a[MXF_AHEAD][4], b[MXF_AHEAD][4];
+    v2u za[MXF_AHEAD], zb[MXF_AHEAD];
+#pragma unroll
+    for (int d = 0; d < MXF_AHEAD; ++d) {
+      const int s = min(s0 + d * MXF_W, s1 - 1);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) b[d][q] = __builtin_amdgcn_raw_buffer_load_b128(bbuf, off + 32 * q, 128 * s, 0);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) a[d][q] = __builtin_amdgcn_raw_buffer_load_b128(abuf, off + 32 * q, 128 * s, 0);
+      za[d] = __builtin_amdgcn_raw_buffer_load_b64(asbuf, soff, 8 * s, 0);
+      zb[d] = __builtin_amdgcn_raw_buffer_load_b64(bsbuf, soff, 8 * s, 0);
+    }
+#pragma unroll
+    for (int d = 0; d < MXF_AHEAD; ++d) {
+      const int s = s0 + d * MXF_W;
+      uint32_t mine = 0u;                          // bytes of the blocks that hold values
+#pragma unroll
+      for (int q = 0; q < 4; ++q) mine |= 8 * s + 2 * q + h < o.kb1 ? 0xffu << (8 * q) : 0u;
+      const uint32_t sa = __builtin_amdgcn_perm(za[d].y, za[d].x, pick) & mine;
+      const uint32_t sb = __builtin_amdgcn_perm(zb[d].y, zb[d].x, pick) & mine;
+      auto step = [&](auto qc) {
+        constexpr int q = decltype(qc)::value;
+        const v8i va = {(int)a[d][q].x, (int)a[d][q].y, (int)a[d][q].z, (int)a[d][q].w, 0, 0, 0, 0};
+        const v8i vb = {(int)b[d][q].x, (int)b[d][q].y, (int)b[d][q].z, (int)b[d][q].w, 0, 0, 0, 0};
+        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va, vb, acc, 4, 4, q, (int)sa, q, (int)sb);
+      };
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});
+      step(std::integral_constant<int, 2>{});
+      step(std::integral_constant<int, 3>{});
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[r];
+  __syncthreads();
+  // register r of lane (xl, h) is C[8 (r / 4) + 4 h + r % 4][xl]
+  T *C = static_cast<T *>(p.C);
+#pragma unroll
+  for (int e = tid; e < 1024; e += 64 * MXF_W) {
+    const int y = e >> 5, x = e & 31, r = 4 * (y >> 3) + (y & 3), l = x + 32 * ((y >> 2) & 1);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < MXF_W; ++w) v += part[w][r][l];
+    if (m0 + y >= o.m1 || n0 + x >= p.N) continue;
+    T *c = C + (m0 + y) * p.ldc + n0 + x;
+    if constexpr (sizeof(T) == 4) *c = v;
+    else *c = __builtin_bit_cast(uint16_t, (__bf16)v);
+  }
+}
+
 // Gradients larger than the L2s (32 MB) are written past them: through them, one of
 // 403 MB pushed its operands out, 180 us against 105; one that fits is found there by
-// its reader.  The outputs of 256-tiles are at least as large.
+// its reader.  The outputs of 256-tiles are about as large or larger.
 constexpr int64_t MX_L2 = 32 << 20;
 
-// 256 x 256 where they fill the compute units, one each (4096 x 4096 x 14336 120 us
-// against 155 in 128-tiles, 2048 x 2048 x 2048 22 against 12, 512 x 14336 x 4096 38
-// against 25).  Grouped products leave the last tile of a group part empty and have
-// few slabs: 128-tiles, three workgroups a compute unit (the weight gradients of 64
-// experts of 2048 x 768, 512 rows each, 108 us against 125 to 138 with two).
+// Few rows: where 32 x 32 tiles are no more than the compute units, or twice that for
+// at most 16 rows: 1 x 14336 x 4096 (448 tiles) 8.4 us against 11.5 in 128-tiles, 16
+// rows 10.2 against 11.6, 32 rows 12.6 against 11.9; 64 x 4096 x 14336 (256 tiles) 22
+// against 30, 96 rows 39 against 31; 1 x 50257 x 2048 (1571 tiles) 22 against 14.  Grouped rows: while the launch, with a tile
+// more for every group that may have none, stays below 1536 (8 tokens, 2 of 8
+// experts of 2048 x 2048, 1152 tiles: 11 against 14; 128 tokens, 1600: 15.5 against 15.1;
+// 8 tokens, 8 of 64 experts of 2048 x 768, 3096: 24 against 14).
+constexpr int64_t MX_FEW = 256, MX_FEW_GROUPED = 1536;
+// 256 x 256 where they fill 0.8 of the rounds of one a compute unit that they take:
+// 4096 x 4096 x 14336 (1.0) 117 us against 155 in 128-tiles, 6000 x 5000 x 4096 (0.9) 75
+// against 85, 32768 x 768 x 2048 (0.75) 40 against 37, 16384 x 1100 x 4096 (0.5) 86
+// against 77, 512 x 14336 x 4096 (0.4) 38 against 25.  Grouped products leave the last
+// tile of a group part empty and have few slabs: 128-tiles, four workgroups a compute
+// unit (the weight gradients of 64 experts of 2048 x 768, 512 rows each, 105 us; with
+// two and two slabs in LDS 125 to 138).
+constexpr int64_t MX_CUS = 256;
+
 template <int MODE, typename T>
 hipError_t mx_launch(MxParams p, hipStream_t s) {
-  auto tiles = [&](int bt) {
+  auto tiles = [&](int bt) -> int64_t {
     const int64_t tm = (p.M + bt - 1) / bt + (MODE == MX_ROWS ? p.groups + 1 : 0), tn = (p.N + bt - 1) / bt;
     p.tiles_m = (int)tm;
     p.tiles_n = (int)tn;
-    if constexpr (MODE == MX_ONE) return tm * tn;
+    if (MODE == MX_ONE || bt == 32) return tm * tn;
     const int64_t deals = (tm + MX_DEAL - 1) / MX_DEAL * (MODE == MX_K ? p.groups : 1);
     return (deals + 7) / 8 * 8 * MX_DEAL * tn;
   };
-  int64_t n = tiles(256);
+  int64_t n;
+  if constexpr (MODE != MX_K) {
+    n = tiles(32);
+    const bool few = n <= (MODE == MX_ROWS ? MX_FEW_GROUPED : p.M <= 16 ? 2 * MX_FEW : MX_FEW);
+    if (few) {
+      hipLaunchKernelGGL((mx4_gemm_few<MODE, T>), dim3((unsigned)n), dim3(64 * MXF_W), 0, s, p);
+      return hipGetLastError();
+    }
+  }
   if constexpr (MODE == MX_ONE) {
-    if (p.bytes >= 256) {
-      if (n >= 256) {
+    if (p.bytes >= 256) {                  // a load of scales brings two slabs'
+      n = tiles(256);
+      const double rounds = (double)((n + MX_CUS - 1) / MX_CUS * MX_CUS) * 65536.0;
+      if ((double)p.M * (double)p.N >= 0.8 * rounds) {
         hipLaunchKernelGGL((mx4_gemm_tile<T, 256, 256>), dim3((unsigned)n), dim3(256), 0, s, p);
       } else {
         n = tiles(128);
