@@ -247,3 +247,9 @@ def test_classes_refuse_on_the_gpu():
         soap.LayerNorm(cols=64, eps=0.0).forward(x)
     assert e.value.status == soap.SOAP_ERR_HPARAM
     assert np.isfinite(soap.LayerNorm(cols=64).forward(x)[0].cpu().numpy()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(2100, 9000), (1300, 8192), (9000, 700), (70000, 33), (40001, 250), (5000, 2048)])
+def test_workgroups_that_walk_over_rows(rows, cols, dtype):
+    check(make(rows, cols, dtype, seed=31), make(rows, cols, dtype, seed=32, shift=0.0), *params(cols), dtype)

@@ -367,3 +367,71 @@ def test_classes_refuse_on_the_gpu():
         a.values(torch.float16)
     with pytest.raises(ValueError):
         soap.Mx4(a.data, a.scale, 300)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 300), (3600, 4100, 513), (4096, 3841, 1280), (1000, 1100, 200),
+                                   (5000, 700, 256), (700, 5000, 257), (2000, 2100, 640), (16, 16000, 512),
+                                   (17, 16001, 300)])
+def test_larger_products(M, N, K, dtype):
+    """Every tile shape: few rows, 128-tiles with one and two slabs in LDS, 256-tiles."""
+    a, b = soap.mx4_quantize(randn(M, K, seed=21)), soap.mx4_quantize(randn(N, K, seed=22, scale=0.05))
+    close(soap.mx4_product(a, b, dtype), a.values().double(), b.values().double(), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("off", [0, 1])
+def test_larger_products_into_strided_rows(dtype, off):
+    for M, N, K in [(4096, 4093, 300), (2000, 1001, 640), (1500, 1203, 100)]:
+        a, b = soap.mx4_quantize(randn(M, K, seed=23)), soap.mx4_quantize(randn(N, K, seed=24))
+        want = soap.mx4_product(a, b, dtype)
+        ld = (N + 15) // 8 * 8 if off == 0 else N + 6
+        wide = torch.full((M, ld), 7.0, device="cuda", dtype=dtype)
+        kind = soap.SOAP_BF16 if dtype == torch.bfloat16 else soap.SOAP_F32
+        soap.soap_mx4_gemm(M, N, K, a.data, a.scale, b.data, b.scale, kind,
+                           wide.data_ptr() + off * wide.element_size(), ld)
+        assert torch.equal(wide[:, off:off + N], want)
+        assert (wide[:, :off] == 7).all() and (wide[:, off + N:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("sizes,N,K,tail", [([700, 0, 900, 33, 5, 2000], 777, 300, 100),
+                                            ([32 * (i % 5) for i in range(100)], 520, 256, 64),
+                                            ([0] * 70 + [1500, 1, 1, 1], 1000, 130, 0)])
+def test_larger_products_by_rows(sizes, N, K, tail, dtype):
+    M = sum(sizes) + tail
+    x, w = randn(M, K, seed=25), randn(len(sizes), N, K, seed=26, scale=0.1)
+    x[sum(sizes):] = float("nan")
+    a, b = soap.mx4_quantize(x), soap.mx4_quantize(w)
+    got = soap.mx4_product_rows(a, b, offsets_of(sizes), dtype)
+    av, bv, at = a.values().double(), b.values().double(), 0
+    for g, n in enumerate(sizes):
+        close(got[at:at + n], av[at:at + n], bv[g], dtype, g)
+        at += n
+    assert (got[at:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_larger_products_by_k(dtype):
+    """A gradient larger than the L2s, groups that start and end anywhere in a slab."""
+    sizes = [32 * ((7 * i) % 23) for i in range(40)]
+    K = sum(sizes) + 32
+    a, b = soap.mx4_quantize(randn(640, K, seed=27)), soap.mx4_quantize(randn(700, K, seed=28))
+    got = soap.mx4_product_k(a, b, offsets_of(sizes), dtype)
+    av, bv, at = a.values().double(), b.values().double(), 0
+    for g, n in enumerate(sizes):
+        if n:
+            close(got[g], av[:, at:at + n], bv[:, at:at + n], dtype, g)
+        else:
+            assert (got[g] == 0).all()
+        at += n
+
+
+def test_sums_of_a_long_axis():
+    """65 536 values of one sign: the running sum is exact to its own last bits."""
+    K = 65536
+    x = randn(40, K, seed=29).abs()
+    a = soap.mx4_quantize(x)
+    close(soap.mx4_product(a, a), a.values().double(), a.values().double(), torch.float32)
+    b = soap.mx4_quantize(randn(2000, 8192, seed=30).abs())
+    close(soap.mx4_product(b, b), b.values().double(), b.values().double(), torch.float32)
