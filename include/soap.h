@@ -407,6 +407,12 @@ size_t soap_mx4_scale_bytes(int64_t rows, int64_t k);
 int soap_mx4_quantize(int64_t batch, int64_t rows, int64_t cols, int dtype, const void *x, int64_t ldx,
                       const int32_t *row_index, int64_t x_rows, uint8_t *data, uint8_t *scale,
                       uint8_t *data_t, uint8_t *scale_t, hipStream_t stream);
+/* Rows of a packed matrix: row r of the output (rows x k) is row row_index[r] of the
+ * input (x_rows x k), or zeros where that is outside [0, x_rows).  A row that many
+ * rows take is quantised once and copied so. */
+int soap_mx4_gather(int64_t rows, int64_t k, const int32_t *row_index, int64_t x_rows,
+                    const uint8_t *x_data, const uint8_t *x_scale, uint8_t *data, uint8_t *scale,
+                    hipStream_t stream);
 /* The values of a packed matrix, rounded once to a bfloat16 output. */
 int soap_mx4_dequantize(int64_t rows, int64_t k, const uint8_t *data, const uint8_t *scale, int dtype,
                         void *out, int64_t ldo, hipStream_t stream);

@@ -53,7 +53,7 @@ EXPORTED = [
     "soap_layer_norm_forward", "soap_layer_norm_workspace_bytes", "soap_layer_norm_backward",
     "soap_router_rows", "soap_router_workspace_bytes", "soap_router_forward",
     "soap_router_backward", "soap_mx4_data_bytes", "soap_mx4_scale_bytes", "soap_mx4_quantize",
-    "soap_mx4_dequantize", "soap_mx4_gemm", "soap_mx4_gemm_rows", "soap_mx4_gemm_k",
+    "soap_mx4_gather", "soap_mx4_dequantize", "soap_mx4_gemm", "soap_mx4_gemm_rows", "soap_mx4_gemm_k",
 ]
 
 
@@ -136,6 +136,7 @@ def lib() -> ctypes.CDLL:
         "soap_mx4_scale_bytes": (_SZ, [_I64, _I64]),
         "soap_mx4_quantize": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _I64, _P, _P, _P, _P,
                                      _P]),
+        "soap_mx4_gather": (_INT, [_I64, _I64, _P, _I64, _P, _P, _P, _P, _P]),
         "soap_mx4_dequantize": (_INT, [_I64, _I64, _P, _P, _INT, _P, _I64, _P]),
         "soap_mx4_gemm": (_INT, [_I64, _I64, _I64, _P, _P, _P, _P, _INT, _P, _I64, _P]),
         "soap_mx4_gemm_rows": (_INT, [_I64, _I64, _I64, _I64, _P, _P, _P, _P, _P, _INT, _P, _I64,
@@ -528,6 +529,11 @@ def soap_mx4_quantize(batch, rows, cols, dtype, x, ldx, row_index, x_rows, data,
                                    _stream(stream)))
 
 
+def soap_mx4_gather(rows, k, row_index, x_rows, x_data, x_scale, data, scale, stream=None) -> None:
+    _check(lib().soap_mx4_gather(rows, k, _raw(row_index), x_rows, _raw(x_data), _raw(x_scale),
+                                 _raw(data), _raw(scale), _stream(stream)))
+
+
 def soap_mx4_dequantize(rows, k, data, scale, dtype, out, ldo, stream=None) -> None:
     _check(lib().soap_mx4_dequantize(rows, k, _raw(data), _raw(scale), dtype, _raw(out), ldo,
                                      _stream(stream)))
@@ -834,6 +840,16 @@ def mx4_quantize(x, along: str = "cols", row_index=None, stream=None):
             raise ValueError("row_index takes a single matrix")
         rows = row_index.numel()
         _exactly(row_index, "row_index", _torch.int32, (rows,), x)
+    if row_index is not None and along == "cols" and rows >= 8 * x_rows and rows * cols >= 1 << 25:
+        # Every row is taken often: quantised once and copied.  34 752 rows of 4096 tokens
+        # of 2048 values 20.6 us instead of 24, of 4096 values 29.6 instead of 47.  Below it
+        # loses: 10 176 rows of 1024 tokens 8.7 instead of 8.0, and rows taken four times
+        # (16 640 of 4096 tokens) 15.8 instead of 14.1.
+        once = mx4_quantize(x)
+        a = _mx4_empty(x, (rows,), cols)
+        _check(lib().soap_mx4_gather(rows, cols, row_index.data_ptr(), x_rows, once.data.data_ptr(),
+                                     once.scale.data_ptr(), a.data.data_ptr(), a.scale.data_ptr(), raw))
+        return a
     a = _mx4_empty(x, (*lead, rows), cols) if along != "rows" else None
     b = _mx4_empty(x, (*lead, cols), rows) if along != "cols" else None
     _check(lib().soap_mx4_quantize(

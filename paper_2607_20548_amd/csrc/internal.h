@@ -277,6 +277,8 @@ struct Mx4QuantDesc {
   uint8_t *data_t = nullptr, *scale_t = nullptr;   // along the rows, or null
 };
 hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s);
+hipError_t launch_mx4_gather(const Mx4Mat &x, int64_t x_rows, const int *row_index, int64_t rows,
+                             int64_t k, uint8_t *data, uint8_t *scale, hipStream_t s);
 hipError_t launch_mx4_dequantize(const Mx4Mat &a, int64_t rows, int64_t cols, bool bf16, void *out,
                                  int64_t ldo, hipStream_t s);
 // C = A B^T over k.  offsets (groups + 1 device ints, multiples of 32) null: one

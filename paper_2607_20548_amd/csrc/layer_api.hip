@@ -291,6 +291,21 @@ int soap_mx4_quantize(int64_t batch, int64_t rows, int64_t cols, int dtype, cons
   return done(soap::launch_mx4_quantize(d, stream), "MXFP4 quantisation");
 }
 
+int soap_mx4_gather(int64_t rows, int64_t k, const int32_t *row_index, int64_t x_rows,
+                    const uint8_t *x_data, const uint8_t *x_scale, uint8_t *data, uint8_t *scale,
+                    hipStream_t stream) {
+  SOAP_TRY(check_range("rows", rows, 0, INT32_MAX));
+  SOAP_TRY(check_range("k", k, 1, SOAP_MAX_ROWS));
+  SOAP_TRY(check_range("x_rows", x_rows, 0, INT32_MAX));
+  SOAP_TRY(check_bufs({{row_index, 4 * (size_t)rows, "row_index", false, true, 4},
+                       {x_data, soap_mx4_data_bytes(x_rows, k), "x_data", false, true, 16},
+                       {x_scale, soap_mx4_scale_bytes(x_rows, k), "x_scale", false, true, 16},
+                       {data, soap_mx4_data_bytes(rows, k), "data", true, true, 16},
+                       {scale, soap_mx4_scale_bytes(rows, k), "scale", true, true, 16}}));
+  return done(soap::launch_mx4_gather({x_data, x_scale}, x_rows, row_index, rows, k, data, scale, stream),
+              "MXFP4 rows");
+}
+
 int soap_mx4_dequantize(int64_t rows, int64_t k, const uint8_t *data, const uint8_t *scale, int dtype,
                         void *out, int64_t ldo, hipStream_t stream) {
   SOAP_TRY(check_range("rows", rows, 0, INT32_MAX));

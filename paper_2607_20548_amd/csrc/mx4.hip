@@ -239,6 +239,23 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
         *reinterpret_cast<const uint32_t *>(lds + 256 * 64 + 4 * threadIdx.x);
 }
 
+// Rows of a packed matrix, by an index: a wave per row, 16 bytes a lane (the scales 8).
+__global__ __launch_bounds__(256) void mx4_gather(Mx4Mat x, int64_t x_rows, const int *__restrict__ row_index,
+                                                  int64_t rows, int64_t kp, uint8_t *__restrict__ data,
+                                                  uint8_t *__restrict__ scale) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < rows; r += (int64_t)gridDim.x * 4) {
+    const int64_t src = row_index[r];
+    const bool in = src >= 0 && src < x_rows;
+    const v4u *from = reinterpret_cast<const v4u *>(x.data + (in ? src : 0) * (kp / 2));
+    v4u *to = reinterpret_cast<v4u *>(data + r * (kp / 2));
+    for (int64_t i = lane; i < kp / 32; i += 64) to[i] = in ? from[i] : v4u(0u);
+    const v2u *sfrom = reinterpret_cast<const v2u *>(x.scale + (in ? src : 0) * (kp / 32));
+    v2u *sto = reinterpret_cast<v2u *>(scale + r * (kp / 32));
+    for (int64_t i = lane; i < kp / 256; i += 64) sto[i] = in ? sfrom[i] : v2u(0u);
+  }
+}
+
 // The values of a packed matrix, along its rows as mx4_quantize_cols walks them: eight
 // values per lane, QC_UNITS independent loads at a time; the values, two to eight times
 // the bytes read, are written past the L2s (64 x 2048 x 768 both ways to bfloat16 115 us
@@ -954,6 +971,14 @@ hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s) {
   if (d.bf16) { if (d.data) SOAP_MXQ(uint16_t, true); else SOAP_MXQ(uint16_t, false); }
   else { if (d.data) SOAP_MXQ(float, true); else SOAP_MXQ(float, false); }
 #undef SOAP_MXQ
+  return hipGetLastError();
+}
+
+hipError_t launch_mx4_gather(const Mx4Mat &x, int64_t x_rows, const int *row_index, int64_t rows,
+                             int64_t k, uint8_t *data, uint8_t *scale, hipStream_t s) {
+  if (rows <= 0) return hipSuccess;
+  const dim3 grid((unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16));
+  hipLaunchKernelGGL(mx4_gather, grid, dim3(256), 0, s, x, x_rows, row_index, rows, mx4_padded(k), data, scale);
   return hipGetLastError();
 }
 

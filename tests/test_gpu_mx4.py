@@ -435,3 +435,28 @@ def test_sums_of_a_long_axis():
     close(soap.mx4_product(a, a), a.values().double(), a.values().double(), torch.float32)
     b = soap.mx4_quantize(randn(2000, 8192, seed=30).abs())
     close(soap.mx4_product(b, b), b.values().double(), b.values().double(), torch.float32)
+
+
+@pytest.mark.parametrize("rows,x_rows,k", [(5, 3, 1), (300, 40, 256), (1000, 77, 257), (4096, 512, 4100), (3, 0, 64)])
+def test_gathered_packed_rows(rows, x_rows, k):
+    x = soap.mx4_quantize(randn(x_rows, k, seed=33))
+    idx = torch.randint(-1, max(x_rows, 1), (rows,), device="cuda", dtype=torch.int32)
+    idx[0], idx[1] = x_rows, -(1 << 30)
+    data = torch.full((rows, x.data.shape[1]), 255, dtype=torch.uint8, device="cuda")
+    scale = torch.full((rows, x.scale.shape[1]), 255, dtype=torch.uint8, device="cuda")
+    soap.soap_mx4_gather(rows, k, idx, x_rows, x.data, x.scale, data, scale)
+    ok = ((idx >= 0) & (idx < x_rows))[:, None]
+    at = idx.long().clamp(0, max(x_rows - 1, 0))
+    pick = lambda t: torch.where(ok, t[at], torch.zeros_like(t[:1])) if x_rows else torch.zeros_like(data if t is x.data else scale)  # noqa: E731,E501
+    assert torch.equal(data, pick(x.data)) and torch.equal(scale, pick(x.scale))
+
+
+def test_rows_taken_often_are_the_same():
+    """Quantised once and copied, or row by row."""
+    x = randn(200, 2100, seed=34).bfloat16()
+    idx = torch.randint(-1, 200, (17000,), device="cuda", dtype=torch.int32)
+    idx[3] = 200
+    many = soap.mx4_quantize(x, row_index=idx)
+    few = [soap.mx4_quantize(x, row_index=idx[i:i + 1000].contiguous()) for i in range(0, 17000, 1000)]
+    assert torch.equal(many.data, torch.cat([f.data for f in few]))
+    assert torch.equal(many.scale, torch.cat([f.scale for f in few]))

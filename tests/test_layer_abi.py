@@ -241,3 +241,14 @@ def test_tensor_checks_of_the_classes():
         soap.mx4_quantize(torch.zeros(2, 8))
     with pytest.raises(ValueError):
         soap.Mx4(torch.zeros(2, 64, dtype=torch.uint8), torch.zeros(2, 8, dtype=torch.uint8), 64)
+
+
+def test_mx4_gather_refuses(L):
+    f = L.soap_mx4_gather
+    assert f(-1, 64, P(0), 4, P(1), P(2), P(3), P(4), None) == soap.SOAP_ERR_SHAPE
+    assert f(4, 0, P(0), 4, P(1), P(2), P(3), P(4), None) == soap.SOAP_ERR_SHAPE
+    assert f(4, 64, P(0), -4, P(1), P(2), P(3), P(4), None) == soap.SOAP_ERR_SHAPE
+    assert f(4, 64, None, 4, P(1), P(2), P(3), P(4), None) == soap.SOAP_ERR_NULL
+    assert f(4, 64, P(0), 4, P(1), P(2), P(3), None, None) == soap.SOAP_ERR_NULL
+    assert f(4, 64, P(0), 4, P(1), P(2), P(1, 16), P(4), None) == soap.SOAP_ERR_ALIAS
+    assert f(4, 64, P(0, 2), 4, P(1), P(2), P(3), P(4), None) == soap.SOAP_ERR_ALIGN
