@@ -20,6 +20,8 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // at any element
+typedef uint32_t v2u_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t v8u __attribute__((ext_vector_type(8)));
 
 // --------------------------------------------------------- quantisation
@@ -44,13 +46,15 @@ struct QuantParams {
   const int *row_index;
   uint8_t *data, *scale, *data_t, *scale_t;
   int64_t kp, rp;          // padded columns and rows
-  int vec;
 };
 
 // Along the columns only: eight values per lane, a block is four lanes of a row, so
 // that a wave's loads and stores are contiguous.  A row has LPR lanes, which walk
-// along it in QC_UNITS independent loads at a time.
+// along it in QC_UNITS independent loads at a time; short rows have fewer lanes, so
+// that all the loads are used (400 000 x 256 bfloat16 47 us with 16 lanes, 77 with 32;
+// 131 072 x 768 44 with 32, 60 with 64; 16384 x 4096 34 with 32, 30 with 64).
 constexpr int QC_UNITS = 4;
+int mx_lanes(int64_t kp, int64_t most16, int64_t most32) { return kp <= most16 ? 16 : kp <= most32 ? 32 : 64; }
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
   constexpr int ROWS = 256 / LPR;
@@ -74,12 +78,12 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
         const int64_t c = c0 + u * LPR * 8;
         raw[u] = Raw(0u);
         if (src < 0 || c >= p.cols) continue;
-        if (p.vec && c + 8 <= p.cols) {
+        if (c + 8 <= p.cols) {
           if constexpr (sizeof(T) == 4) {
-            const v4u lo = *reinterpret_cast<const v4u *>(xr + c), hi = *reinterpret_cast<const v4u *>(xr + c + 4);
+            const v4u lo = *reinterpret_cast<const v4u_any *>(xr + c), hi = *reinterpret_cast<const v4u_any *>(xr + c + 4);
             raw[u] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           } else {
-            raw[u] = *reinterpret_cast<const v4u *>(xr + c);
+            raw[u] = *reinterpret_cast<const v4u_any *>(xr + c);
           }
         } else {
 #pragma unroll
@@ -142,8 +146,9 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
   const int64_t ct = t / rt, r0 = ((t - ct * rt) * 4 + wave) * 32;
   const int64_t cw = ct * 256, c0 = cw + 4 * lane;
   const T *x = static_cast<const T *>(p.x) + b * p.sx;
-  const bool all = cw + 256 <= p.cols && p.vec;
+  const bool all = cw + 256 <= p.cols;
   typedef typename std::conditional<sizeof(T) == 4, v4u, v2u>::type Raw;
+  typedef typename std::conditional<sizeof(T) == 4, v4u_any, v2u_any>::type RawAny;
   Raw raw[32];
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
@@ -155,8 +160,8 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
     if (src < 0) continue;
     const T *xr = x + src * p.ldx + cw;
     if (all) {
-      if constexpr (GATHER) raw[i] = *(reinterpret_cast<const Raw *>(xr) + lane);
-      else raw[i] = __builtin_nontemporal_load(reinterpret_cast<const Raw *>(xr) + lane);
+      if constexpr (GATHER) raw[i] = *(reinterpret_cast<const RawAny *>(xr) + lane);
+      else raw[i] = __builtin_nontemporal_load(reinterpret_cast<const RawAny *>(xr) + lane);
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -256,59 +261,59 @@ __global__ __launch_bounds__(256) void mx4_gather(Mx4Mat x, int64_t x_rows, cons
   }
 }
 
-// The values of a packed matrix, along its rows as mx4_quantize_cols walks them: eight
-// values per lane, QC_UNITS independent loads at a time; the values, two to eight times
-// the bytes read, are written past the L2s (64 x 2048 x 768 both ways to bfloat16 115 us
-// against 128).
+// The values of a packed matrix, along its rows as mx4_quantize_cols walks them: 16 bytes
+// of values per lane, so that a wave's stores are contiguous (32 bytes of fp32 in two
+// stores, each with gaps: 49 152 x 2048 177 us instead of 73), QC_UNITS independent loads
+// at a time; the values, two to eight times the bytes read, are written past the L2s.
+// Lanes of a row: 200 000 x 512 bfloat16 48 us with 16, 57 with 32, 75 with 64; 131 072 x
+// 768 51 with 32, 73 with 64; 9000 x 11008 57 with 32, 47 with 64; fp32, half the values a
+// lane, 200 000 x 512 67 with 32, 70 with 64, 131 072 x 768 75 with 32, 63 with 64.
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void mx4_dequantize(Mx4Mat a, int64_t rows, int64_t cols, int64_t kp,
-                                                      T *__restrict__ out, int64_t ldo, int vec) {
-  constexpr int ROWS = 256 / LPR;
+                                                      T *__restrict__ out, int64_t ldo) {
+  constexpr int ROWS = 256 / LPR, N = 16 / (int)sizeof(T);
+  typedef typename std::conditional<N == 8, uint32_t, uint16_t>::type Codes;
   const int lane = threadIdx.x % LPR;
   for (int64_t r = (int64_t)blockIdx.x * ROWS + threadIdx.x / LPR; r < rows; r += (int64_t)gridDim.x * ROWS) {
     const uint8_t *dr = a.data + r * (kp / 2), *sr = a.scale + r * (kp / 32);
     T *o = out + r * ldo;
-    for (int64_t c0 = 8 * lane; c0 < cols; c0 += QC_UNITS * LPR * 8) {
+    for (int64_t c0 = N * lane; c0 < cols; c0 += QC_UNITS * LPR * N) {
       uint32_t q[QC_UNITS], byte[QC_UNITS];
 #pragma unroll
       for (int u = 0; u < QC_UNITS; ++u) {
-        const int64_t c = c0 + u * LPR * 8;
+        const int64_t c = c0 + u * LPR * N;
         q[u] = byte[u] = 0u;
         if (c >= cols) continue;
-        q[u] = *reinterpret_cast<const uint32_t *>(dr + c / 2);
+        q[u] = *reinterpret_cast<const Codes *>(dr + c / 2);
         byte[u] = sr[c / 32];
       }
 #pragma unroll
       for (int u = 0; u < QC_UNITS; ++u) {
-        const int64_t c = c0 + u * LPR * 8;
+        const int64_t c = c0 + u * LPR * N;
         if (c >= cols) continue;
         const float s = byte[u] == 255u ? __uint_as_float(0x7fc00000u) : mx_scale(byte[u]);
-        float v[8];
+        float v[N];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < N; ++j) {
           // code m = 0, 1: 0.5 m; else (1 + 0.5 (m % 2)) 2^(m / 2 - 1)
           const uint32_t m = (q[u] >> (4 * j)) & 7u;
           const float f = m < 2u ? 0.5f * (float)m : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
           v[j] = ((q[u] >> (4 * j)) & 8u ? -f : f) * s;
         }
-        if (vec && c + 8 <= cols) {
-          if constexpr (sizeof(T) == 4) {
-            typedef float v4f __attribute__((ext_vector_type(4)));
-            __builtin_nontemporal_store(v4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<v4f *>(o + c));
-            __builtin_nontemporal_store(v4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<v4f *>(o + c + 4));
-          } else {
-            v4u w;
+        if (c + N <= cols) {
+          v4u w;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) |
-                     ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16);
-            __builtin_nontemporal_store(w, reinterpret_cast<v4u *>(o + c));
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (N == 4) w[j] = __float_as_uint(v[j]);
+            else w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j]) |
+                        ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * j + 1]) << 16);
           }
+          __builtin_nontemporal_store(w, reinterpret_cast<v4u_any *>(o + c));
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
+          for (int j = 0; j < N; ++j)
             if (c + j < cols) {
-              if constexpr (sizeof(T) == 4) o[c + j] = v[j];
+              if constexpr (N == 4) o[c + j] = v[j];
               else o[c + j] = __builtin_bit_cast(uint16_t, (__bf16)v[j]);
             }
         }
@@ -945,20 +950,17 @@ hipError_t launch_mx4_quantize(const Mx4QuantDesc &d, hipStream_t s) {
   p.x = d.x; p.row_index = d.row_index;
   p.data = d.data; p.scale = d.scale; p.data_t = d.data_t; p.scale_t = d.scale_t;
   p.kp = mx4_padded(d.cols); p.rp = mx4_padded(d.rows);
-  const int elem = d.bf16 ? 2 : 4;
   if (!d.data_t) {
     if (d.rows == 0) return hipSuccess;
-    p.vec = reinterpret_cast<uintptr_t>(d.x) % 16 == 0 && d.ldx * elem % 16 == 0;
-    const bool half = p.kp == 256;               // a row is half a wave's 512 values
-    const int64_t rows = half ? 8 : 4;
+    const int lanes = mx_lanes(p.kp, 512, 1024), rows = 256 / lanes;
     const dim3 grid((unsigned)std::min<int64_t>((d.rows + rows - 1) / rows, 1 << 16), (unsigned)d.batch);
-#define SOAP_MXQ(T, L) hipLaunchKernelGGL((mx4_quantize_cols<T, L>), grid, dim3(256), 0, s, p)
-    if (d.bf16) { if (half) SOAP_MXQ(uint16_t, 32); else SOAP_MXQ(uint16_t, 64); }
-    else { if (half) SOAP_MXQ(float, 32); else SOAP_MXQ(float, 64); }
+#define SOAP_MXQ(T, L) \
+  if (lanes == L) hipLaunchKernelGGL((mx4_quantize_cols<T, L>), grid, dim3(256), 0, s, p)
+    if (d.bf16) { SOAP_MXQ(uint16_t, 16); SOAP_MXQ(uint16_t, 32); SOAP_MXQ(uint16_t, 64); }
+    else { SOAP_MXQ(float, 16); SOAP_MXQ(float, 32); SOAP_MXQ(float, 64); }
 #undef SOAP_MXQ
     return hipGetLastError();
   }
-  p.vec = reinterpret_cast<uintptr_t>(d.x) % (4 * elem) == 0 && d.ldx % 4 == 0;
   const int64_t tiles = (p.rp / 128) * (p.kp / 256);
   if (tiles == 0) return hipSuccess;
   if (tiles > INT32_MAX) return hipErrorInvalidValue;
@@ -986,13 +988,13 @@ hipError_t launch_mx4_dequantize(const Mx4Mat &a, int64_t rows, int64_t cols, bo
                                  int64_t ldo, hipStream_t s) {
   if (rows <= 0) return hipSuccess;
   const int64_t kp = mx4_padded(cols);
-  const bool half = kp == 256;                     // a row is half a wave's 512 values
-  const dim3 grid((unsigned)std::min<int64_t>((rows + (half ? 7 : 3)) / (half ? 8 : 4), 1 << 16));
-  const int vec = (reinterpret_cast<uintptr_t>(out) & 15u) == 0 && ldo * (bf16 ? 2 : 4) % 16 == 0;
-#define SOAP_MXV(T, L) \
-  hipLaunchKernelGGL((mx4_dequantize<T, L>), grid, dim3(256), 0, s, a, rows, cols, kp, static_cast<T *>(out), ldo, vec)
-  if (bf16) { if (half) SOAP_MXV(uint16_t, 32); else SOAP_MXV(uint16_t, 64); }
-  else { if (half) SOAP_MXV(float, 32); else SOAP_MXV(float, 64); }
+  const int lanes = bf16 ? mx_lanes(kp, 512, 2304) : mx_lanes(kp, 256, 512), per = 256 / lanes;
+  const dim3 grid((unsigned)std::min<int64_t>((rows + per - 1) / per, 1 << 16));
+#define SOAP_MXV(T, L)                                                                                  \
+  if (lanes == L)                                                                                       \
+  hipLaunchKernelGGL((mx4_dequantize<T, L>), grid, dim3(256), 0, s, a, rows, cols, kp, static_cast<T *>(out), ldo)
+  if (bf16) { SOAP_MXV(uint16_t, 16); SOAP_MXV(uint16_t, 32); SOAP_MXV(uint16_t, 64); }
+  else { SOAP_MXV(float, 16); SOAP_MXV(float, 32); SOAP_MXV(float, 64); }
 #undef SOAP_MXV
   return hipGetLastError();
 }
