@@ -20,24 +20,42 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint16_t v2h __attribute__((ext_vector_type(2)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // at any element
 typedef uint32_t v2u_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t v8u __attribute__((ext_vector_type(8)));
 
 // --------------------------------------------------------- quantisation
-__device__ __forceinline__ uint32_t mx_abs(float f) { return __float_as_uint(f) & 0x7fffffffu; }
-__device__ __forceinline__ uint32_t mx_byte(uint32_t amax) {
-  const uint32_t e = amax >> 23;
-  return e == 255u ? 255u : e > 2u ? e - 2u : 0u;
-}
+__device__ __forceinline__ uint32_t mx_byte(uint32_t e) { return e == 255u ? 255u : e > 2u ? e - 2u : 0u; }
 __device__ __forceinline__ float mx_scale(uint32_t byte) {
   return __uint_as_float(byte ? byte << 23 : 0x400000u);   // 2^-127 is subnormal
 }
-// Maximum over aligned groups of 8 lanes.
+// Two bfloat16 of a word: their maxima as integers, the low (high) halves of two words.
+__device__ __forceinline__ uint32_t mx_max(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2h, a), __builtin_bit_cast(v2h, b)));
+}
+__device__ __forceinline__ uint32_t mx_low(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t mx_high(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+// Two values into byte SEL of q.  Both forms round alike (all bfloat16 at all scales compared).
+template <int SEL>
+__device__ __forceinline__ uint32_t mx_cvt(uint32_t q, uint32_t a, uint32_t b, float s) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(a), __uint_as_float(b), s, SEL);
+}
+template <int SEL>
+__device__ __forceinline__ uint32_t mx_cvt(uint32_t q, uint32_t ab, float s) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(v2bf, ab), s, SEL);
+}
+// Maximum over aligned groups of 8 lanes, of a word or of its halves.
+template <typename V>
 __device__ __forceinline__ uint32_t mx_max8(uint32_t v) {
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));    // lane ^ 1
-  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));    // lane ^ 2
-  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));  // 7 - lane
+  auto most = [](uint32_t a, uint32_t b) {
+    if constexpr (std::is_same<V, v2h>::value) return mx_max(a, b);
+    else return max(a, b);
+  };
+  v = most(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));    // lane ^ 1
+  v = most(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));    // lane ^ 2
+  return most(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));  // 7 - lane
 }
 
 struct QuantParams {
@@ -107,7 +125,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
         for (int j = 0; j < 8; ++j) a = max(a, bits(j) & 0x7fffffffu);
         a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xB1, 0xF, 0xF, true));   // lane ^ 1
         a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xF, 0xF, true));   // lane ^ 2
-        const uint32_t byte = mx_byte(a);
+        const uint32_t byte = mx_byte(a >> 23);
         const float s = mx_scale(byte);
         uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, val(0), val(1), s, 0);
         q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(2), val(3), s, 1);
@@ -129,72 +147,119 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
 // that a column's 64 bytes (four blocks) are written together.  Workgroups of
 // consecutive rows run on one XCD, whose L2 joins what they write of a line.  Without
 // an index no row is read twice: the loads leave the L2s to the stores (the 64 x 2048 x
-// 768 bank both ways 92 us against 103); with one, a token's row is read for each of
-// its experts and kept there (36 864 rows of 4096 tokens 28 us against 33).
+// 768 bank both ways 91 us, 5.6 TB/s, against 103); with one, a token's row is read for
+// each of its experts and kept there (34 752 rows of 4096 tokens of 2048 18 us, against
+// 20 with branches around absent rows).  The rows' loads do not wait for each other: a
+// branch for every row or column that is not there took 65536 x 700 bfloat16 from 30 us
+// to 79.  Bfloat16 maxima and conversions work on pairs, both ways 49 152 x 2048 60 us
+// against 75 by single values (which held 256 registers).
 template <typename T, bool ROWS, bool GATHER>
 __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
   // column x's block of wave w: 16 bytes at x * 64 + 16 * (w ^ (x / 4 % 4))
   __shared__ __attribute__((aligned(16))) uint8_t lds[256 * 64 + 256 * 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t b = blockIdx.y;
-  const int64_t rt = (p.rp + 127) / 128;
-  int64_t t = blockIdx.x;
+  const int rt = (int)((p.rp + 127) / 128);
+  int t;
   {
     const int nt = gridDim.x, x = blockIdx.x & 7, per = nt >> 3, more = nt & 7;
-    t = x * per + min(x, more) + (blockIdx.x >> 3);
+    t = x * per + min(x, more) + (int)(blockIdx.x >> 3);
   }
-  const int64_t ct = t / rt, r0 = ((t - ct * rt) * 4 + wave) * 32;
+  const int64_t ct = __builtin_amdgcn_readfirstlane(t / rt), r0 = ((int64_t)(t - (int)ct * rt) * 4 + wave) * 32;
   const int64_t cw = ct * 256, c0 = cw + 4 * lane;
   const T *x = static_cast<const T *>(p.x) + b * p.sx;
-  const bool all = cw + 256 <= p.cols;
   typedef typename std::conditional<sizeof(T) == 4, v4u, v2u>::type Raw;
   typedef typename std::conditional<sizeof(T) == 4, v4u_any, v2u_any>::type RawAny;
+  // Lane i's row of x is row i's; bit i: there is one.
+  int mine = 0;
+  bool in = lane < 32 && r0 + lane < p.rows;
+  if constexpr (GATHER) {
+    if (in) mine = p.row_index[r0 + lane];
+    in = in && mine >= 0 && mine < p.x_rows;
+    if (!in) mine = 0;
+  }
+  const uint32_t ok = (uint32_t)__ballot(in);
+  const int last = __builtin_amdgcn_readfirstlane((int)min(p.rows - r0, (int64_t)32) - 1);
+  auto row = [&](int i) {
+    return x + (GATHER ? (int64_t)__builtin_amdgcn_readlane(mine, i) : r0 + min(i, last)) * p.ldx;
+  };
+  // Whole loads of every row, rows without values row 0's, those at the right edge the
+  // last four columns; what does not belong there goes out after all are on their way.
   Raw raw[32];
+  if (ok == 0u || p.cols < 4) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const int64_t r = r0 + i;
-    int64_t src = -1;
-    if (r < p.rows) src = GATHER ? (int64_t)p.row_index[r] : r;
-    if (GATHER && src >= p.x_rows) src = -1;
-    raw[i] = Raw(0u);
-    if (src < 0) continue;
-    const T *xr = x + src * p.ldx + cw;
-    if (all) {
-      if constexpr (GATHER) raw[i] = *(reinterpret_cast<const RawAny *>(xr) + lane);
-      else raw[i] = __builtin_nontemporal_load(reinterpret_cast<const RawAny *>(xr) + lane);
-    } else {
+    for (int i = 0; i < 32; ++i) {
+      raw[i] = Raw(0u);
+      if (!(ok >> i & 1u)) continue;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 3; ++j)
         if (c0 + j < p.cols) {
-          if constexpr (sizeof(T) == 4) raw[i][j] = __float_as_uint(xr[4 * lane + j]);
-          else raw[i][j / 2] |= (uint32_t)xr[4 * lane + j] << (16 * (j & 1));
+          if constexpr (sizeof(T) == 4) raw[i][j] = __float_as_uint(row(i)[c0 + j]);
+          else raw[i][j / 2] |= (uint32_t)row(i)[c0 + j] << (16 * (j & 1));
         }
     }
+  } else {
+    const int room = __builtin_amdgcn_readfirstlane((int)min(p.cols - cw, (int64_t)256));
+    const int left = min(room - 4, 0), c = min(4 * lane, room - 4);
+    const uint32_t at = (uint32_t)(c - left) * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      uint64_t base = reinterpret_cast<uint64_t>(row(i) + cw + left);
+      asm("" : "+s"(base));                    // the row's address stays a scalar, the lane's part an offset
+      typedef const char __attribute__((address_space(1))) *Global;
+      const auto from = reinterpret_cast<const RawAny __attribute__((address_space(1))) *>(reinterpret_cast<Global>(base) + at);
+      if constexpr (GATHER) raw[i] = *from;
+      else raw[i] = __builtin_nontemporal_load(from);
+    }
+    if (ok != ~0u || room < 256) {
+      const int d = 4 * lane - c;              // the lane's first column is at d; past 3 there is none
+      const bool one = d & 1, two = d & 2;
+      const uint32_t lane_ok = d > 3 ? 0u : ~0u;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const uint32_t keep = lane_ok & (ok >> i & 1u ? ~0u : 0u);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) raw[i][j] = one ? (j < 3 ? raw[i][j + 1] : 0u) : raw[i][j];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) raw[i][j] = two ? (j < 2 ? raw[i][j + 2] : 0u) : raw[i][j];
+        } else {
+          const uint64_t w = ((uint64_t)raw[i][1] << 32 | raw[i][0]) >> (16 * (d & 3));
+          raw[i] = Raw{(uint32_t)w, (uint32_t)(w >> 32)};
+        }
+        raw[i] &= keep;
+      }
+    }
   }
-  auto bits = [&](int i, int j) -> uint32_t {
-    if constexpr (sizeof(T) == 4) return raw[i][j];
-    else return (j & 1) ? raw[i][j / 2] & 0xffff0000u : raw[i][j / 2] << 16;
-  };
-  auto val = [&](int i, int j) { return __uint_as_float(bits(i, j)); };
+  // bfloat16 stays packed: two values a word, their maxima and conversions too
+  auto top = [&](int i, int w) { return raw[i][w] & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu); };
   if constexpr (ROWS) {
     uint8_t *data = p.data + b * p.rows * (p.kp / 2), *scale = p.scale + b * p.rows * (p.kp / 32);
     uint32_t keep[4];          // the byte of row 8 i + lane % 8 of the lane's block
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
+      uint32_t e[2];           // the largest exponents of the lane's blocks of rows i, i + 1
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          e[k] = mx_max8<uint32_t>(max(max(top(i + k, 0), top(i + k, 1)), max(top(i + k, 2), top(i + k, 3)))) >> 23;
+      } else {
+        const uint32_t m0 = mx_max(top(i, 0), top(i, 1)), m1 = mx_max(top(i + 1, 0), top(i + 1, 1));
+        const uint32_t m = mx_max8<v2h>(mx_max(mx_low(m0, m1), mx_high(m0, m1)));
+        e[0] = m >> 7 & 255u;
+        e[1] = m >> 23;
+      }
       uint32_t q = 0u;         // row i's four values, then row i + 1's
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        uint32_t a = 0u;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) a = max(a, bits(i + k, j) & 0x7fffffffu);
-        const uint32_t byte = mx_byte(mx_max8(a));
+        const uint32_t byte = mx_byte(e[k]);
         const float s = mx_scale(byte);
-        if (k == 0) {
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i, 0), val(i, 1), s, 0);
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i, 2), val(i, 3), s, 1);
+        if constexpr (sizeof(T) == 4) {
+          if (k == 0) { q = mx_cvt<0>(q, raw[i][0], raw[i][1], s); q = mx_cvt<1>(q, raw[i][2], raw[i][3], s); }
+          else { q = mx_cvt<2>(q, raw[i + 1][0], raw[i + 1][1], s); q = mx_cvt<3>(q, raw[i + 1][2], raw[i + 1][3], s); }
         } else {
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i + 1, 0), val(i + 1, 1), s, 2);
-          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(i + 1, 2), val(i + 1, 3), s, 3);
+          if (k == 0) { q = mx_cvt<0>(q, raw[i][0], s); q = mx_cvt<1>(q, raw[i][1], s); }
+          else { q = mx_cvt<2>(q, raw[i + 1][0], s); q = mx_cvt<3>(q, raw[i + 1][1], s); }
         }
         if (((i + k) & 7) == (lane & 7)) keep[i >> 3] = byte;
       }
@@ -210,20 +275,36 @@ __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
       if (r < p.rows) scale[r * (p.kp / 32) + c0 / 32] = (uint8_t)keep[i];
     }
   }
+  if constexpr (ROWS && sizeof(T) == 2) {      // nothing of the above is kept in registers for the below
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+v"(raw[i]));
+  }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    uint32_t a = 0u;
+    uint32_t a = 0u, e;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) a = max(a, bits(i, j) & 0x7fffffffu);
-    const uint32_t byte = mx_byte(a);
+      for (int i = 0; i < 32; ++i) a = max(a, top(i, j));
+      e = a >> 23;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) a = mx_max(a, top(i, j / 2));
+      e = j & 1 ? a >> 23 : a >> 7 & 255u;
+    }
+    const uint32_t byte = mx_byte(e);
     const float s = mx_scale(byte);
+    auto two = [&](auto sel, uint32_t q, int i) {        // rows i and i + 1 of the column
+      if constexpr (sizeof(T) == 4) return mx_cvt<decltype(sel)::value>(q, raw[i][j], raw[i + 1][j], s);
+      else return mx_cvt<decltype(sel)::value>(q, j & 1 ? mx_high(raw[i][j / 2], raw[i + 1][j / 2])
+                                                        : mx_low(raw[i][j / 2], raw[i + 1][j / 2]), s);
+    };
     v4u w;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, val(8 * k, j), val(8 * k + 1, j), s, 0);
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(8 * k + 2, j), val(8 * k + 3, j), s, 1);
-      q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(8 * k + 4, j), val(8 * k + 5, j), s, 2);
-      w[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, val(8 * k + 6, j), val(8 * k + 7, j), s, 3);
+      uint32_t q = two(std::integral_constant<int, 0>{}, 0u, 8 * k);
+      q = two(std::integral_constant<int, 1>{}, q, 8 * k + 2);
+      q = two(std::integral_constant<int, 2>{}, q, 8 * k + 4);
+      w[k] = two(std::integral_constant<int, 3>{}, q, 8 * k + 6);
     }
     const int c = 4 * lane + j;
     *reinterpret_cast<v4u *>(lds + c * 64 + 16 * (wave ^ (lane & 3))) = w;

@@ -460,3 +460,31 @@ def test_rows_taken_often_are_the_same():
     few = [soap.mx4_quantize(x, row_index=idx[i:i + 1000].contiguous()) for i in range(0, 17000, 1000)]
     assert torch.equal(many.data, torch.cat([f.data for f in few]))
     assert torch.equal(many.scale, torch.cat([f.scale for f in few]))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [1, 2, 3, 4, 5, 7, 255, 257, 258, 259, 260, 511, 770])
+def test_right_edges_among_nan(cols, dtype):
+    """What lies around the matrix, and rows that no index names, are not read into it."""
+    full = torch.full((70, cols + 9), torch.nan, device="cuda", dtype=dtype)
+    for off in (0, 1, 5):
+        x = full[1:67, off:off + cols]
+        x.copy_(randn(66, cols, seed=35 + off))
+        x[3] = torch.inf
+        check_quantise(x)
+        idx = torch.tensor([65, -1, 0, 66, 7, 7, -5, 1 << 30] * 9 + [64], device="cuda", dtype=torch.int32)
+        check_quantise(x, idx)
+        full.fill_(torch.nan)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [250, 300, 700, 1100, 2400, 4200])
+def test_values_into_strided_rows(cols, dtype):
+    """Every number of lanes a row, rows that start at any element."""
+    q = soap.mx4_quantize(randn(37, cols, seed=36))
+    want = q.values(torch.float32)
+    full = torch.full((37, cols + 5), 7.0, device="cuda", dtype=dtype)
+    kind = soap.SOAP_F32 if dtype == torch.float32 else soap.SOAP_BF16
+    soap.soap_mx4_dequantize(37, cols, q.data, q.scale, kind, full[:, 3:], full.stride(0))
+    assert torch.equal(full[:, 3:3 + cols], want.to(dtype))
+    assert (full[:, :3] == 7).all() and (full[:, 3 + cols:] == 7).all()
