@@ -589,8 +589,8 @@ __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, 
 // or padding, get scales of 2^-127 on both sides, whose products vanish (and no
 // NaN); loads past the last slab bring it again.
 // Measured: 8192 x 14336 x 4096 267 us (3600 TFLOP/s), 4096 x 4096 x 14336 114 (4200);
-// a loop of these instructions alone reaches 5600 on random data.  They are busy 0.53 of
-// the time, at 1.75 GHz: power, then waits for memory between slabs.
+// a loop of these instructions alone reaches 5600 on random data.  They are busy 0.51 of
+// the time and waves wait 0.22 of it, at 1.75 to 1.9 GHz.
 //
 // The B operand goes first, so that a lane holds four consecutive columns of one
 // row of C: results are rounded in registers, staged 32 rows at a time in the
@@ -784,8 +784,9 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
 // Tiles of 128 x 128 for products of fewer or shorter tiles: one slab in LDS, the
 // next on its way through registers, and four workgroups per compute unit, which cover
 // each other's barriers, first loads and epilogues.  Groups by rows (64 experts of 2048
-// x 768, 512 rows each) 46 to 57 us, of which the operands' way from the L2s is the
-// larger part; by k (their gradients) 94 to 110 us, bound by the 403 MB of them.
+// x 768, 512 rows each) 46 to 57 us, matrix instructions busy 0.34 of it and waves
+// waiting 0.36 of theirs; by k (their gradients) 94 to 110 us, busy 0.20: bound by the
+// 403 MB written.
 template <int MODE, typename T, bool STREAM>
 __global__ __launch_bounds__(256, 4) void mx4_gemm_tile128(MxParams p) {
   constexpr int TM = 128, TN = 128, BI = 2, BJ = 2, UNITS = 8, DATA = 256 * 128;
