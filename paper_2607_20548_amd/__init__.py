@@ -629,7 +629,9 @@ def _on(stream, inputs, call, *args, **kwargs):
     inputs are kept from reuse until the stream has read them."""
     T = _T()
     if isinstance(stream, int):
-        stream = T.cuda.ExternalStream(stream)
+        # the default stream's handle is 0, which ExternalStream takes for none given: it
+        # would hand out a stream of its pool, that waits for nothing
+        stream = T.cuda.ExternalStream(stream) if stream else T.cuda.default_stream()
     for t in inputs:
         if t is not None:
             t.record_stream(stream)
