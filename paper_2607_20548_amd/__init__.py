@@ -628,13 +628,18 @@ def _on(stream, inputs, call, *args, **kwargs):
     """call(...) on a stream of one's own: its outputs belong to that stream, and its
     inputs are kept from reuse until the stream has read them."""
     T = _T()
+    inputs = [t for t in inputs if t is not None]
+    for t in inputs:
+        if not isinstance(t, T.Tensor):
+            raise TypeError(f"expected a torch tensor, got {type(t)}")
+        if t.get_device() < 0:
+            raise ValueError("tensors must live on the GPU")
     if isinstance(stream, int):
         # the default stream's handle is 0, which ExternalStream takes for none given: it
         # would hand out a stream of its pool, that waits for nothing
         stream = T.cuda.ExternalStream(stream) if stream else T.cuda.default_stream()
     for t in inputs:
-        if t is not None:
-            t.record_stream(stream)
+        t.record_stream(stream)
     with T.cuda.stream(stream):
         return call(*args, **kwargs)
 
