@@ -335,7 +335,8 @@ typedef enum { SOAP_F32 = 0, SOAP_BF16 = 1 } soap_dtype;
  * The backward pass gives, with h = (x - mean) rstd and g = weight dy,
  *   dx = rstd (g - mean(g) - h mean(g h)),  dweight = sum_rows dy h,  dbias = sum_rows dy
  * (each NULL where it is not wanted, dx too); the workspace holds the partial
- * sums of dweight and dbias (it may be NULL if neither is wanted). */
+ * sums of dweight and dbias (it may be NULL if neither is wanted).  Its size never
+ * shrinks as rows or cols grow: one for the largest call serves the others. */
 int soap_layer_norm_forward(int64_t rows, int64_t cols, int dtype, const void *x, int64_t ldx,
                             const float *weight, const float *bias, float eps, void *y, int64_t ldy,
                             float *mean, float *rstd, hipStream_t stream);

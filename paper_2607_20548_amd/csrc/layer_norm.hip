@@ -446,8 +446,14 @@ hipError_t ln_launch(const LnParams &p, hipStream_t s) {
 
 }  // namespace
 
+// At least what ln_blocks_bwd workgroups write, and growing with both arguments, so that a
+// workspace of the largest call is enough for the others: even shares can take fewer
+// workgroups for more rows, and rows past 4096 columns take half as many.
 size_t layer_norm_part_bytes(int64_t rows, int64_t cols) {
-  return sizeof(float) * 2 * cols * ln_blocks_bwd(rows, cols);
+  const int64_t passes = ln_passes(rows, cols), narrow = std::min<int64_t>(cols, 4096);
+  const int64_t values = std::max(cols * std::min(passes, ln_most_bwd(cols)),
+                                  narrow * std::min(passes, ln_most_bwd(narrow)));
+  return sizeof(float) * 2 * values;
 }
 
 hipError_t launch_layer_norm_fwd(const LayerNormDesc &d, hipStream_t s) {

@@ -54,3 +54,34 @@ def test_other_objects_are_refused_alike_with_and_without_a_stream(stream):
         soap.LayerNorm(cols=4).forward([[1.0, 2.0, 3.0, 4.0]], stream=stream)
     with pytest.raises(TypeError, match="expected a torch tensor"):
         soap.mx4_quantize([[1.0]], stream=stream)
+
+
+ROWS = [0, 1, 3, 4, 5, 31, 32, 33, 127, 128, 129, 255, 256, 257, 511, 512, 513, 767, 768, 769, 1023, 1024, 1025,
+        1101, 2047, 2048, 2049, 2303, 4096, 4097, 8191, 8192, 8193, 16383, 16384, 16385, 32768, 65536, 65537,
+        1 << 20, 1 << 24]
+WIDTHS = [1, 64, 65, 256, 257, 1000, 2048, 2049, 2303, 4096, 4097, 8191, 8192, 8193, 14336, 16384]
+
+
+@pytest.fixture(scope="module")
+def built():
+    from paper_2607_20548_amd import build
+    build.build(force=False)
+    soap.lib()
+
+
+def test_a_workspace_of_the_largest_call_is_enough_for_the_others(built):
+    """The sizes never shrink as a call grows, in rows or in width."""
+    size = soap.soap_layer_norm_workspace_bytes
+    for cols in WIDTHS:
+        of = [size(rows, cols) for rows in [*range(2600), *(r for r in ROWS if r >= 2600)]]
+        assert of == sorted(of), cols
+    for rows in ROWS:
+        of = [size(rows, cols) for cols in WIDTHS]
+        assert of == sorted(of), rows
+    size = soap.soap_router_workspace_bytes
+    for experts in (1, 8, 64, 1000, 1024):
+        of = [size(tokens, experts) for tokens in ROWS]
+        assert of == sorted(of), experts
+    for tokens in ROWS:
+        of = [size(tokens, experts) for experts in range(1, 1025)]
+        assert of == sorted(of), tokens
