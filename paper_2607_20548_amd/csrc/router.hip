@@ -355,7 +355,7 @@ __global__ __launch_bounds__(RT_NT) void router_fwd(RtParams p) {
     for (int e = tid; e <= p.experts; e += RT_NT) p.counts[e] = hist[e];
     __syncthreads();
     if (p.loss && wave == 0) rt_loss(p, hist, psum[0]);
-    if (!p.row_token) return;
+    if (!p.offsets) return;                   // a plan without tokens has no other array
     rt_offsets(hist, p.experts, base, p.offsets);
     rt_assign(p, t0, t1, base, bits);
   }
@@ -411,7 +411,7 @@ __global__ __launch_bounds__(RT_NT) void router_plan(RtParams p) {
   __shared__ int base[RT_MAX_E];
   __shared__ unsigned long long bits[RT_MAX_E];
   if (blockIdx.x == 0 && p.loss && threadIdx.x < 64) rt_loss(p, p.counts, p.ptot);
-  if (!p.row_token) return;
+  if (!p.offsets) return;
   rt_offsets(p.counts, p.experts, base, blockIdx.x == 0 ? p.offsets : nullptr);
   for (int e = threadIdx.x; e < p.experts; e += RT_NT) base[e] += p.hist[(int64_t)e * RT_CHUNKS + blockIdx.x];
   __syncthreads();
@@ -570,7 +570,7 @@ hipError_t launch_router_fwd(const RouterDesc &d, hipStream_t s) {
   if (e != hipSuccess || one) return e;
   hipLaunchKernelGGL(router_scan, dim3(p.experts + 1), dim3(RT_NT), 0, s, p);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(router_plan, dim3(p.row_token ? p.chunks : 1), dim3(RT_NT), 0, s, p);
+  hipLaunchKernelGGL(router_plan, dim3(p.offsets ? p.chunks : 1), dim3(RT_NT), 0, s, p);
   return hipGetLastError();
 }
 

@@ -104,3 +104,16 @@ def test_inputs_dropped_after_a_call_are_not_reused_before_it(name):
     for a, b in zip(want, got):
         assert torch.equal(a, b), name
     assert taken
+
+
+# ------------------------------------------------------------ empty token axes
+def test_a_router_without_tokens_writes_its_offsets():
+    """index, gate, position and row_token are empty then and may be NULL."""
+    E = 9
+    counts, offsets = (torch.full((E + 1,), 7, dtype=torch.int32, device="cuda") for _ in range(2))
+    loss = torch.full((1,), 7.0, device="cuda")
+    need = soap.soap_router_workspace_bytes(0, E)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    soap.soap_router_forward(0, E, 2, soap.SOAP_F32, None, E, None, 0, 0.01, None, None, counts, loss, offsets, None,
+                             None, ws, need)
+    assert (counts == 0).all() and (offsets == 0).all() and loss.item() == 0
