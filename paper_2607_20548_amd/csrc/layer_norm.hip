@@ -470,11 +470,12 @@ hipError_t launch_layer_norm_bwd(const LayerNormDesc &d, hipStream_t s) {
   p.rows = d.rows; p.cols = (int)d.cols;
   p.x = d.x; p.ldx = d.ldx; p.dy = d.dy; p.lddy = d.lddy; p.w = d.weight;
   p.mean_in = d.mean; p.rstd_in = d.rstd; p.out = d.out; p.ldo = d.ldo;
-  p.part = d.dweight || d.dbias ? d.part : nullptr;
+  const bool sums = d.dweight || d.dbias;      // without rows they are zeros, from no partial sums
+  p.part = sums ? d.part : nullptr;
   hipError_t e = hipSuccess;
   if (d.rows > 0)
     e = d.bf16 ? ln_launch<true, uint16_t>(p, s) : ln_launch<true, float>(p, s);
-  if (e != hipSuccess || !p.part) return e;
+  if (e != hipSuccess || !sums) return e;
   hipLaunchKernelGGL(layer_norm_bwd_finish, dim3((unsigned)((d.cols + LN_FIN_COLS - 1) / LN_FIN_COLS), 2), dim3(LN_FIN),
                      0, s, p.part, (int)ln_blocks_bwd(d.rows, d.cols), p.cols, d.dweight,
                      d.dbias);

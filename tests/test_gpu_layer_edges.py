@@ -117,3 +117,15 @@ def test_a_router_without_tokens_writes_its_offsets():
     soap.soap_router_forward(0, E, 2, soap.SOAP_F32, None, E, None, 0, 0.01, None, None, counts, loss, offsets, None,
                              None, ws, need)
     assert (counts == 0).all() and (offsets == 0).all() and loss.item() == 0
+
+
+@pytest.mark.parametrize("which", ["dweight", "dbias", "both"])
+def test_a_layer_norm_without_rows_writes_its_sums(which):
+    """The workspace of no rows is empty and may be NULL."""
+    cols = 300
+    assert soap.soap_layer_norm_workspace_bytes(0, cols) == 0
+    dweight, dbias = (torch.full((cols,), 7.0, device="cuda") for _ in range(2))
+    soap.soap_layer_norm_backward(0, cols, soap.SOAP_BF16, None, cols, None, cols, None, None, None, None, cols,
+                                  None if which == "dbias" else dweight, None if which == "dweight" else dbias,
+                                  None, 0)
+    assert (dweight == (7 if which == "dbias" else 0)).all() and (dbias == (7 if which == "dweight" else 0)).all()
