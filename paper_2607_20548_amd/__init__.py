@@ -805,6 +805,8 @@ class Mx4:
             return _on(stream, (self.data, self.scale), self.values, dtype)
         raw, kind, dtype = _current_stream(self.data, "data"), *_out_type(dtype)
         out = self.data.new_empty((*self.data.shape[:-1], self.k), dtype=dtype)
+        if not self.k:
+            return out
         _check(lib().soap_mx4_dequantize(out.numel() // self.k, self.k, self.data.data_ptr(),
                                          self.scale.data_ptr(), kind, out.data_ptr(), self.k, raw))
         return out
@@ -883,6 +885,8 @@ def mx4_product(a: Mx4, b: Mx4, dtype=None, stream=None):
     _mx4_check(a, b, 2)
     raw, kind, dtype = _current_stream(a.data, "a"), *_out_type(dtype)
     out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
+    if not a.k:                                # sums of nothing
+        return out.zero_()
     _check(lib().soap_mx4_gemm(a.rows, b.rows, a.k, a.data.data_ptr(), a.scale.data_ptr(),
                                b.data.data_ptr(), b.scale.data_ptr(), kind, out.data_ptr(), b.rows, raw))
     return out
@@ -898,6 +902,8 @@ def mx4_product_rows(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
     groups = b.data.shape[0]
     _exactly(offsets, "offsets", _torch.int32, (groups + 1,), a.data)
     out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
+    if not a.k:
+        return out.zero_()
     _check(lib().soap_mx4_gemm_rows(groups, a.rows, b.rows, a.k, offsets.data_ptr(), a.data.data_ptr(),
                                     a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
                                     out.data_ptr(), b.rows, raw))

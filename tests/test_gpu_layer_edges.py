@@ -129,3 +129,21 @@ def test_a_layer_norm_without_rows_writes_its_sums(which):
                                   None if which == "dbias" else dweight, None if which == "dweight" else dbias,
                                   None, 0)
     assert (dweight == (7 if which == "dbias" else 0)).all() and (dbias == (7 if which == "dweight" else 0)).all()
+
+
+# ------------------------------------------------------- MXFP4 of empty matrices
+@pytest.mark.parametrize("dtype", [None, torch.bfloat16])
+def test_an_axis_of_no_values(dtype):
+    """What a layer without tokens has along its rows: no values, products that are zeros."""
+    a, b = (soap.mx4_quantize(torch.empty(0, n, device="cuda"), along="rows") for n in (40, 70))
+    kind = dtype or torch.float32
+    assert a.k == 0 and a.values(dtype).shape == (40, 0) and a.values(dtype).dtype == kind
+    out = soap.mx4_product(a, b, dtype)
+    assert out.shape == (40, 70) and out.dtype == kind and (out == 0).all()
+    bank = soap.Mx4(b.data.view(2, 35, 0), b.scale.view(2, 35, 0), 0)
+    assert bank.values(dtype).shape == (2, 35, 0)
+    o = torch.tensor([0, 32, 40], dtype=torch.int32, device="cuda")
+    out = soap.mx4_product_rows(a, bank, o, dtype)
+    assert out.shape == (40, 35) and out.dtype == kind and (out == 0).all()
+    out = soap.mx4_product_k(a, b, 0 * o, dtype)
+    assert out.shape == (2, 40, 70) and out.dtype == kind and (out == 0).all()
