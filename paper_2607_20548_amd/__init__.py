@@ -861,11 +861,12 @@ def mx4_quantize(x, along: str = "cols", row_index=None, stream=None):
         return a
     a = _mx4_empty(x, (*lead, rows), cols) if along != "rows" else None
     b = _mx4_empty(x, (*lead, cols), rows) if along != "cols" else None
-    _check(lib().soap_mx4_quantize(
-        lead[0] if lead else 1, rows, cols, kind, x.data_ptr(), cols if lead else _ld(x),
-        None if row_index is None else row_index.data_ptr(), x_rows,
-        None if a is None else a.data.data_ptr(), None if a is None else a.scale.data_ptr(),
-        None if b is None else b.data.data_ptr(), None if b is None else b.scale.data_ptr(), raw))
+    if rows and cols and 0 not in lead:        # there are values
+        _check(lib().soap_mx4_quantize(
+            lead[0] if lead else 1, rows, cols, kind, x.data_ptr(), cols if lead else _ld(x),
+            None if row_index is None else row_index.data_ptr(), x_rows,
+            None if a is None else a.data.data_ptr(), None if a is None else a.scale.data_ptr(),
+            None if b is None else b.data.data_ptr(), None if b is None else b.scale.data_ptr(), raw))
     return (a, b) if along == "both" else a or b
 
 
@@ -885,7 +886,7 @@ def mx4_product(a: Mx4, b: Mx4, dtype=None, stream=None):
     _mx4_check(a, b, 2)
     raw, kind, dtype = _current_stream(a.data, "a"), *_out_type(dtype)
     out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
-    if not a.k:                                # sums of nothing
+    if not a.k or not out.numel():             # sums of nothing, or no sums
         return out.zero_()
     _check(lib().soap_mx4_gemm(a.rows, b.rows, a.k, a.data.data_ptr(), a.scale.data_ptr(),
                                b.data.data_ptr(), b.scale.data_ptr(), kind, out.data_ptr(), b.rows, raw))
@@ -902,7 +903,7 @@ def mx4_product_rows(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
     groups = b.data.shape[0]
     _exactly(offsets, "offsets", _torch.int32, (groups + 1,), a.data)
     out = a.data.new_empty((a.rows, b.rows), dtype=dtype)
-    if not a.k:
+    if not a.k or not groups or not out.numel():
         return out.zero_()
     _check(lib().soap_mx4_gemm_rows(groups, a.rows, b.rows, a.k, offsets.data_ptr(), a.data.data_ptr(),
                                     a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
@@ -919,7 +920,11 @@ def mx4_product_k(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
     raw, kind, dtype = _current_stream(a.data, "a"), *_out_type(dtype)
     _exactly(offsets, "offsets", _torch.int32, (offsets.numel(),), a.data)
     groups = offsets.numel() - 1
+    if groups < 0:
+        raise ValueError("offsets must hold at least one value")
     out = a.data.new_empty((groups, a.rows, b.rows), dtype=dtype)
+    if not out.numel():
+        return out
     _check(lib().soap_mx4_gemm_k(groups, a.rows, b.rows, a.k, offsets.data_ptr(), a.data.data_ptr(),
                                  a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
                                  out.data_ptr(), raw))

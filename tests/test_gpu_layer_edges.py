@@ -147,3 +147,30 @@ def test_an_axis_of_no_values(dtype):
     assert out.shape == (40, 35) and out.dtype == kind and (out == 0).all()
     out = soap.mx4_product_k(a, b, 0 * o, dtype)
     assert out.shape == (2, 40, 70) and out.dtype == kind and (out == 0).all()
+
+
+def test_empty_batches_sides_and_groups():
+    """Matrices of no values in every direction are packed, and their products are empty or
+    zeros."""
+    for shape in [(0, 8, 64), (3, 0, 64), (3, 8, 0), (8, 0), (0, 0)]:
+        x = torch.empty(shape, device="cuda")
+        for along in ("cols", "rows"):
+            q = soap.mx4_quantize(x, along=along)
+            assert q.values().shape == (x if along == "cols" else x.mT).shape
+        a, b = soap.mx4_quantize(x, along="both")
+        assert a.values().shape == x.shape and b.values().shape == x.mT.shape
+    i32 = dict(dtype=torch.int32, device="cuda")
+    none = soap.mx4_quantize(torch.empty(5, 0, device="cuda"), row_index=torch.zeros(3, **i32))
+    assert none.values().shape == (3, 0)
+    a = soap.mx4_quantize(randn(40, 64))
+    no_bank = soap.mx4_quantize(torch.empty(0, 16, 64, device="cuda"))
+    out = soap.mx4_product_rows(a, no_bank, torch.zeros(1, **i32))      # every row is past the last group
+    assert out.shape == (40, 16) and (out == 0).all()
+    no_rows = soap.mx4_quantize(torch.empty(0, 64, device="cuda"))
+    assert soap.mx4_product(a, no_rows).shape == (40, 0) and soap.mx4_product(no_rows, a).shape == (0, 40)
+    assert soap.mx4_product_k(a, a, torch.zeros(1, **i32)).shape == (0, 40, 40)
+    assert soap.mx4_product_k(a, no_rows, torch.tensor([0, 32, 64], **i32)).shape == (2, 40, 0)
+    with pytest.raises(ValueError, match="offsets"):
+        soap.mx4_product_k(a, a, torch.empty(0, **i32))
+    with pytest.raises(ValueError, match="offsets"):
+        soap.mx4_product_rows(a, no_bank, torch.zeros(2, **i32))
