@@ -68,7 +68,7 @@ typedef enum {
   SOAP_ERR_HPARAM = -3,     /* beta outside [0,1), eps/lr/wd negative or not finite,
                                step < 1, unknown flag bits                       */
   SOAP_ERR_WORKSPACE = -4,  /* workspace smaller than the *_workspace_bytes value */
-  SOAP_ERR_ALIGN = -5,      /* a pointer is not 16-byte aligned                  */
+  SOAP_ERR_ALIGN = -5,      /* a pointer is not aligned as its entry point asks   */
   SOAP_ERR_ALIAS = -6,      /* grad overlaps a buffer the call writes, or two
                                written buffers overlap                           */
   SOAP_ERR_HIP = -7,        /* a HIP runtime call failed                         */
@@ -317,7 +317,8 @@ int soap_kl_factors_f32(int64_t m, int64_t n, const float *G, float *L, float *R
  *    bytes at a time, others an element at a time.  Parameters, their gradients,
  *    statistics, gates and losses are fp32, indices int32.  Other buffers are
  *    16-byte aligned where they are the library's own formats (packed matrices,
- *    workspaces) and element-aligned otherwise.
+ *    workspaces; the scales of packed matrices 8-byte aligned) and element-aligned
+ *    otherwise.
  *  - The token axis may be empty (rows = 0, tokens = 0: sums and counts are then
  *    zero) and goes up to SOAP_MAX_ROWS.
  *  - No output may overlap an input or another output; the range of a strided

@@ -22,6 +22,9 @@ struct Buf {
   size_t align;
 };
 
+// Scales of a matrix inside a packed bank start at any row's, of eight bytes at least.
+constexpr size_t MX4_SCALE_ALIGN = 8;
+
 size_t elem(int dtype) { return dtype == SOAP_BF16 ? 2 : 4; }
 
 // Bytes from the first to the last element of a strided matrix.
@@ -109,9 +112,9 @@ int check_product(int64_t groups, int64_t tile_groups, int64_t M, int64_t N, int
   SOAP_TRY(check_range("tiles of 128 x 128", (M / 128 * tile_groups + 4 * groups + 64) * ((N + 127) / 128), 0, INT32_MAX));
   return check_bufs({{offsets, grouped ? 4 * (size_t)(groups + 1) : 0, "offsets", false, true, 4},
                      {ad, soap_mx4_data_bytes(M, K), "a_data", false, true, 16},
-                     {as, soap_mx4_scale_bytes(M, K), "a_scale", false, true, 16},
+                     {as, soap_mx4_scale_bytes(M, K), "a_scale", false, true, MX4_SCALE_ALIGN},
                      {bd, soap_mx4_data_bytes(b_rows, K), "b_data", false, true, 16},
-                     {bs, soap_mx4_scale_bytes(b_rows, K), "b_scale", false, true, 16},
+                     {bs, soap_mx4_scale_bytes(b_rows, K), "b_scale", false, true, MX4_SCALE_ALIGN},
                      {C, c_bytes, "C", true, true, elem(dtype)}});
 }
 
@@ -281,9 +284,9 @@ int soap_mx4_quantize(int64_t batch, int64_t rows, int64_t cols, int dtype, cons
   SOAP_TRY(check_bufs({{x, span(row_index ? x_rows : batch * rows, cols, ldx, e), "x", false, true, e},
                        {row_index, 4 * (size_t)rows, "row_index", false, false, 4},
                        {data, b * soap_mx4_data_bytes(rows, cols), "data", true, false, 16},
-                       {scale, b * soap_mx4_scale_bytes(rows, cols), "scale", true, false, 16},
+                       {scale, b * soap_mx4_scale_bytes(rows, cols), "scale", true, false, MX4_SCALE_ALIGN},
                        {data_t, b * soap_mx4_data_bytes(cols, rows), "data_t", true, false, 16},
-                       {scale_t, b * soap_mx4_scale_bytes(cols, rows), "scale_t", true, false, 16}}));
+                       {scale_t, b * soap_mx4_scale_bytes(cols, rows), "scale_t", true, false, MX4_SCALE_ALIGN}}));
   soap::Mx4QuantDesc d;
   d.batch = batch; d.rows = rows; d.cols = cols; d.ldx = ldx; d.x_rows = x_rows;
   d.bf16 = dtype == SOAP_BF16; d.x = x; d.row_index = row_index;
@@ -299,9 +302,9 @@ int soap_mx4_gather(int64_t rows, int64_t k, const int32_t *row_index, int64_t x
   SOAP_TRY(check_range("x_rows", x_rows, 0, INT32_MAX));
   SOAP_TRY(check_bufs({{row_index, 4 * (size_t)rows, "row_index", false, true, 4},
                        {x_data, soap_mx4_data_bytes(x_rows, k), "x_data", false, true, 16},
-                       {x_scale, soap_mx4_scale_bytes(x_rows, k), "x_scale", false, true, 16},
+                       {x_scale, soap_mx4_scale_bytes(x_rows, k), "x_scale", false, true, MX4_SCALE_ALIGN},
                        {data, soap_mx4_data_bytes(rows, k), "data", true, true, 16},
-                       {scale, soap_mx4_scale_bytes(rows, k), "scale", true, true, 16}}));
+                       {scale, soap_mx4_scale_bytes(rows, k), "scale", true, true, MX4_SCALE_ALIGN}}));
   return done(soap::launch_mx4_gather({x_data, x_scale}, x_rows, row_index, rows, k, data, scale, stream),
               "MXFP4 rows");
 }
@@ -314,7 +317,7 @@ int soap_mx4_dequantize(int64_t rows, int64_t k, const uint8_t *data, const uint
   SOAP_TRY(check_ld("ldo", ldo, k));
   const size_t e = elem(dtype);
   SOAP_TRY(check_bufs({{data, soap_mx4_data_bytes(rows, k), "data", false, true, 16},
-                       {scale, soap_mx4_scale_bytes(rows, k), "scale", false, true, 16},
+                       {scale, soap_mx4_scale_bytes(rows, k), "scale", false, true, MX4_SCALE_ALIGN},
                        {out, span(rows, k, ldo, e), "out", true, true, e}}));
   return done(soap::launch_mx4_dequantize({data, scale}, rows, k, dtype == SOAP_BF16, out, ldo, stream),
               "MXFP4 values");

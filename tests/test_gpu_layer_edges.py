@@ -174,3 +174,50 @@ def test_empty_batches_sides_and_groups():
         soap.mx4_product_k(a, a, torch.empty(0, **i32))
     with pytest.raises(ValueError, match="offsets"):
         soap.mx4_product_rows(a, no_bank, torch.zeros(2, **i32))
+
+
+# ---------------------------------------------------- parts of a packed bank
+@pytest.mark.parametrize("k", [40, 256, 300, 700, 1200])
+def test_one_matrix_of_a_packed_bank(k):
+    """Its scales start at any multiple of eight bytes."""
+    rows = 37
+    bank = soap.mx4_quantize(randn(4, rows, k))
+    a = soap.mx4_quantize(randn(50, k, seed=1))
+    index = torch.arange(rows + 1, dtype=torch.int32, device="cuda").flip(0)      # one past the end
+    for e in range(4):
+        part = soap.Mx4(bank.data[e], bank.scale[e], k)
+        own = soap.Mx4(bank.data[e].clone(), bank.scale[e].clone(), k)
+        assert part.scale.data_ptr() % 8 == 0 and (k > 256 or part.scale.data_ptr() % 16 == 8 * (e % 2))
+        for dtype in (torch.float32, torch.bfloat16):
+            assert torch.equal(part.values(dtype), own.values(dtype))
+            assert torch.equal(soap.mx4_product(a, part, dtype), soap.mx4_product(a, own, dtype))
+            assert torch.equal(soap.mx4_product(part, a, dtype), soap.mx4_product(own, a, dtype))
+        o = torch.tensor([0, 32, 32, rows, rows], dtype=torch.int32, device="cuda")
+        assert torch.equal(soap.mx4_product_rows(part, bank, o), soap.mx4_product_rows(own, bank, o))
+        o = o // 32 * 32
+        assert torch.equal(soap.mx4_product_k(part, part, o), soap.mx4_product_k(own, own, o))
+        got = soap._mx4_empty(a.data, (rows + 1,), k)
+        soap.soap_mx4_gather(rows + 1, k, index, rows, part.data, part.scale, got.data, got.scale)
+        want = soap._mx4_empty(a.data, (rows + 1,), k)
+        soap.soap_mx4_gather(rows + 1, k, index, rows, own.data, own.scale, want.data, want.scale)
+        assert torch.equal(got.data, want.data) and torch.equal(got.scale, want.scale)
+
+
+@pytest.mark.parametrize("k", [40, 300])
+def test_quantising_into_one_matrix_of_a_packed_bank(k):
+    rows = 37
+    x = randn(rows, k, seed=2)
+    want = soap.mx4_quantize(x)
+    want_t = soap.mx4_quantize(x, along="rows")
+    bank, bank_t = soap._mx4_empty(x, (3, rows), k), soap._mx4_empty(x, (3, k), rows)
+    for m in (bank, bank_t):
+        m.data.fill_(7), m.scale.fill_(7)
+    # both in one pass, then each alone
+    for e, (d, dt) in enumerate([(True, True), (True, False), (False, True)]):
+        ptr = lambda m, on: (m.data[e], m.scale[e]) if on else (None, None)  # noqa: E731
+        soap.soap_mx4_quantize(1, rows, k, soap.SOAP_F32, x, k, None, 0, *ptr(bank, d), *ptr(bank_t, dt))
+        for m, on, w in ((bank, d, want), (bank_t, dt, want_t)):
+            if on:
+                assert torch.equal(m.data[e], w.data) and torch.equal(m.scale[e], w.scale)
+            else:
+                assert (m.data[e] == 7).all() and (m.scale[e] == 7).all()

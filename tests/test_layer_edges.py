@@ -85,3 +85,25 @@ def test_a_workspace_of_the_largest_call_is_enough_for_the_others(built):
     for tokens in ROWS:
         of = [size(tokens, experts) for experts in range(1, 1025)]
         assert of == sorted(of), tokens
+
+
+P8 = [0x7f0000000000 + (i << 24) for i in range(8)]
+
+
+def test_scales_need_eight_bytes_of_alignment(built):
+    """A packed row of up to 256 values has eight bytes of scales: matrices of a bank with an
+    odd number of rows start at any multiple of that.  (C overlaps an operand: no call is
+    made.)"""
+    L = soap.lib()
+    o = P8[5]
+    for off, code in ((0, soap.SOAP_ERR_ALIAS), (8, soap.SOAP_ERR_ALIAS), (4, soap.SOAP_ERR_ALIGN),
+                      (1, soap.SOAP_ERR_ALIGN)):
+        s0, s1 = P8[1] + off, P8[3] + off
+        for a, b in ((s0, P8[3]), (P8[1], s1)):
+            assert L.soap_mx4_gemm(4, 8, 64, P8[0], a, P8[2], b, 0, P8[0], 8, None) == code
+            assert L.soap_mx4_gemm_rows(2, 4, 8, 64, o, P8[0], a, P8[2], b, 0, P8[0], 8, None) == code
+            assert L.soap_mx4_gemm_k(2, 4, 8, 64, o, P8[0], a, P8[2], b, 0, P8[0], None) == code
+            assert L.soap_mx4_gather(4, 64, o, 4, P8[0], a, P8[0], b, None) == code
+        assert L.soap_mx4_dequantize(4, 64, P8[0], s0, 0, P8[0], 64, None) == code
+        assert L.soap_mx4_quantize(1, 8, 64, 0, P8[0], 64, None, 0, P8[0], s0, None, None, None) == code
+        assert L.soap_mx4_quantize(1, 8, 64, 0, P8[0], 64, None, 0, None, None, P8[0], s0, None) == code
