@@ -565,7 +565,7 @@ __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, 
   }
 }
 
-// The same product by tiles of TM x TN through LDS: four waves (2 x 2), each
+// One product by tiles of TM x TN through LDS: four waves (2 x 2), each
 // (TM / 2) x (TN / 2) in blocks of 32 x 32.  K advances in slabs of 256 values (128
 // bytes of a row, eight blocks, four matrix instructions of 64 values: lane (row,
 // h) takes block 2 q + h at step q), two in LDS and a third on its way through
@@ -585,9 +585,9 @@ __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, 
 // 133 us; slabs of 128 values, four of them in LDS: 134 us (64 bytes of a row
 // at a time take the L1 44 cycles a kilobyte).
 //
-// Slabs are whole in the packed rows; blocks outside [kb0, kb1), the neighbours'
-// or padding, get scales of 2^-127 on both sides, whose products vanish (and no
-// NaN); loads past the last slab bring it again.
+// Slabs are whole in the packed rows; their padding's blocks get scales of 2^-127 on
+// both sides, whose products vanish (and no NaN); loads past the last slab bring it
+// again.
 // Measured: 8192 x 14336 x 4096 267 us (3600 TFLOP/s), 4096 x 4096 x 14336 114 (4200);
 // a loop of these instructions alone reaches 5600 on random data.  They are busy 0.51 of
 // the time and waves wait 0.22 of it, at 1.75 to 1.9 GHz.
@@ -616,7 +616,7 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
   __shared__ __attribute__((aligned(1024))) uint8_t lds[L::BYTES];
   int tn, g;
   MxTile o;
-  if (!mx_my_tile<MX_ONE, TM>(p, tn, g, o)) return;
+  mx_my_tile<MX_ONE, TM>(p, tn, g, o);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   const int xl = lane & 31, h = lane >> 5;
@@ -634,9 +634,9 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
   const int am = (int)min((int64_t)TM, o.m1 - m0), bm = (int)min((int64_t)TN, p.N - n0);   // rows there are
   const int64_t srow = p.bytes / 16;
   const auto abuf = mx_buffer(p.A + m0 * p.bytes, am, p.bytes);
-  const auto bbuf = mx_buffer(p.B + (o.b0 + n0) * p.bytes, bm, p.bytes);
+  const auto bbuf = mx_buffer(p.B + n0 * p.bytes, bm, p.bytes);
   const auto asbuf = mx_buffer(p.As + m0 * srow, am, srow);
-  const auto bsbuf = mx_buffer(p.Bs + (o.b0 + n0) * srow, bm, srow);
+  const auto bsbuf = mx_buffer(p.Bs + n0 * srow, bm, srow);
   // thread -> rows lr + 32 i, unit lg of A's and B's rows
   const int lr = tid >> 3, lg = tid & 7;
   const uint32_t off = (uint32_t)(lr * p.bytes + 16 * lg), row32 = (uint32_t)(32 * p.bytes);
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
     soff[i] = (uint32_t)((r < TM ? r : r - TM) * srow);
   }
   const int slabs = (int)(p.bytes >> 7);           // of a packed row; at least 2
-  const int s0 = o.kb0 >> 3, s1 = o.kb1 > o.kb0 ? (o.kb1 + 7) >> 3 : s0;
+  const int s1 = (p.kb + 7) >> 3;                  // slabs that hold values
   const int dst = lr * 128 + 16 * (lg ^ ((lr >> 1) & 7));
   v4u r[UNITS], rs[SU];
   auto load = [&](int s, int i) {
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
   auto store_scales = [&](int s) {
 #pragma unroll
     for (int i = 0; i < SU; ++i)
-      *reinterpret_cast<v4u *>(lds + 2 * L::DATA + (((s - s0) >> 1) & 1) * L::SCALE + (256 * i + tid) * 16) = rs[i];
+      *reinterpret_cast<v4u *>(lds + 2 * L::DATA + ((s >> 1) & 1) * L::SCALE + (256 * i + tid) * 16) = rs[i];
   };
 
   v4u fa[2][BI], fb[2][BJ];
@@ -690,13 +690,13 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
     }
   };
   auto scales = [&](int f, int s) {
-    const int pair = s - ((s - s0) & 1);
-    const uint8_t *d = lds + 2 * L::DATA + (((s - s0) >> 1) & 1) * L::SCALE + 8 * min(s - min(pair, slabs - 2), 1);
-    uint32_t mine = 0u;                            // bytes of the blocks that are this product's
+    const int pair = s & ~1;
+    const uint8_t *d = lds + 2 * L::DATA + ((s >> 1) & 1) * L::SCALE + 8 * min(s - min(pair, slabs - 2), 1);
+    uint32_t mine = 0u;                            // bytes of the blocks that hold values
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int kb = 8 * s + 2 * q + h;
-      mine |= kb >= o.kb0 && kb < o.kb1 ? 0xffu << (8 * q) : 0u;
+      mine |= kb < p.kb ? 0xffu << (8 * q) : 0u;
     }
 #pragma unroll
     for (int i = 0; i < BI; ++i) {
@@ -748,27 +748,27 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
     }
     step(integral_constant<int, 3>{}, par, s + 2);
   };
-  if (s1 > s0) {
-    load_scales(s0);
+  if (s1 > 0) {
+    load_scales(0);
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load(s0, i);
-    store_scales(s0);
-    load_scales(s0 + 2);
+    for (int i = 0; i < UNITS; ++i) load(0, i);
+    store_scales(0);
+    load_scales(2);
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       store(0, i);
-      load(s0 + 1, i);
+      load(1, i);
     }
     mx_sync();
-    scales(0, s0);
+    scales(0, 0);
 #pragma unroll
     for (int u = 0; u < NU; ++u) frag(0, 0, 0, u);
 #pragma unroll
     for (int i = 0; i < NU / 2; ++i) {
       store(1, i);
-      load(s0 + 2, i);
+      load(2, i);
     }
-    for (int s = s0; s < s1; s += 2) {
+    for (int s = 0; s < s1; s += 2) {
       slab(integral_constant<int, 0>{}, s);
       slab(integral_constant<int, 1>{}, s + 1);
     }
@@ -777,7 +777,7 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
   constexpr int STRIDE = BJ * 32 * (int)sizeof(T) + 16;
   static_assert(4 * 32 * STRIDE <= L::BYTES, "the staged rows fit the LDS");
   mx_sync();
-  mx_store<TM == 256, T, BI, BJ>(p, static_cast<T *>(p.C) + o.c0, m0 + wm * (TM / 2), o.m1, n0 + wn * (TN / 2),
+  mx_store<TM == 256, T, BI, BJ>(p, static_cast<T *>(p.C), m0 + wm * (TM / 2), o.m1, n0 + wn * (TN / 2),
                       lds + wave * 32 * STRIDE, acc);
 }
 
