@@ -969,14 +969,38 @@ __global__ __launch_bounds__(64 * MXF_W) void mx4_gemm_few(MxParams p) {
 // its reader.  The outputs of 256-tiles are about as large or larger.
 constexpr int64_t MX_L2 = 32 << 20;
 
-// Few rows: where 32 x 32 tiles are no more than the compute units, or twice that for
-// at most 16 rows: 1 x 14336 x 4096 (448 tiles) 8.4 us against 11.5 in 128-tiles, 16
-// rows 10.2 against 11.6, 32 rows 12.6 against 11.9; 64 x 4096 x 14336 (256 tiles) 22
-// against 30, 96 rows 39 against 31; 1 x 50257 x 2048 (1571 tiles) 22 against 14.  Grouped rows: while the launch, with a tile
-// more for every group that may have none, stays below 1536 (8 tokens, 2 of 8
-// experts of 2048 x 2048, 1152 tiles: 11 against 14; 128 tokens, 1600: 15.5 against 15.1;
-// 8 tokens, 8 of 64 experts of 2048 x 768, 3096: 24 against 14).
-constexpr int64_t MX_FEW = 256, MX_FEW_GROUPED = 1536;
+// Few rows: 32 x 32 tiles, against 128-tiles, microseconds of the one / the other.
+//
+// While the tiles are no more than the compute units: 256 tiles of 16 rows, K = 512 3.2 /
+// 4.5, 2048 5.6 / 7.2, 4096 6.6 / 10.9, 14336 19 / 30; of 128 rows 3.6 / 4.9, 6.6 / 7.6,
+// 7.2 / 11, 20 / 30.  With 288 tiles of 32 rows and more it is over from K = 1024 on (6.3 /
+// 5.6, K = 4096 12.1 / 11.2).
+//
+// For at most mx_few_rows rows, up to twice as many: the eight waves load 16 slabs of 256
+// at a time, and where K fills those badly or has many of them only fewer rows pay.  400
+// tiles, every step of K below for 2, 4 .. 16 rows: K to 1280 3.8 / 4.5 (512, 8 rows) to 6.4 / 6.5
+// (1280, 16); 2048 7.5 / 7.2 at 2 rows, 8.9 / 7.4 at 16; 2560 7.8 / 8.2 at 8, 8.6 / 8.3 at 16; 2816
+// to 4864 9.4 / 11.3 at 8, 10.5 / 11.2 at 16 (4096); 5120 to 15360 12.8 / 13.3 (5120), 24.8 / 22.7
+// (10240) and 25.8 / 26.6 (12288) at 8, 14.5 / 13.6 to 36 / 30 at 16; 16384 35 / 34 at 2.
+constexpr int64_t MX_FEW = 256;
+int64_t mx_few_rows(int64_t slabs) {
+  if (slabs <= 5 || (slabs >= 11 && slabs <= 19)) return 16;
+  if (slabs == 8 || slabs > 60) return 0;
+  return slabs < 8 ? 4 : 8;
+}
+// Grouped rows: the launch has a row of tiles more for every group, which may have none, and
+// stays below MX_FEW_GROUPED tiles (64 experts of 2048 x 768, 8 of them a token: 4 tokens, 2328
+// tiles, 16 / 10).  The groups' rows fill at most M / 32 rows of tiles.  For K past 2560 the small
+// tiles win up to about 900 filled ones, whatever N (2 of 8 experts of 4096 x 1024: 768 18.5 / 23.1;
+// 2 of 4: 1152 27 / 24); for less K up to 500 where N is 256, 750 to 1000 where it is 2048 (2 of 4
+// to 16 experts of 2048 x 768: 384 11.1 / 10.7, 864 19.6 / 11.3; of 1024 x 512: 512 7.1 / 7.3, 768
+// 9.2 / 7.5).  Over 2002 shapes (4 to 64 experts, 1 to 512 tokens, K 256 to 7168, N 256 to 4096)
+// this takes 0.5 per cent longer than the better of the two, 31 at worst; by MX_FEW_GROUPED alone
+// 2.7 and 99.
+constexpr int64_t MX_FEW_GROUPED = 1536;
+bool mx_few_grouped(int64_t launched, int64_t filled, int64_t tiles_n, int64_t slabs) {
+  return launched <= MX_FEW_GROUPED && filled <= (slabs >= 11 ? 896 : std::min<int64_t>(768, 448 + 6 * tiles_n));
+}
 // 256 x 256 where they fill 0.8 of the rounds of one a compute unit that they take:
 // 4096 x 4096 x 14336 (1.0) 117 us against 155 in 128-tiles, 6000 x 5000 x 4096 (0.9) 75
 // against 85, 32768 x 768 x 2048 (0.75) 40 against 37, 16384 x 1100 x 4096 (0.5) 86
@@ -999,8 +1023,9 @@ hipError_t mx_launch(MxParams p, hipStream_t s) {
   int64_t n;
   if constexpr (MODE != MX_K) {
     n = tiles(32);
-    const bool few = n <= (MODE == MX_ROWS ? MX_FEW_GROUPED : p.M <= 16 ? 2 * MX_FEW : MX_FEW);
-    if (few) {
+    const int64_t slabs = p.bytes / 128;
+    if (MODE == MX_ROWS ? mx_few_grouped(n, (p.M + 31) / 32 * p.tiles_n, p.tiles_n, slabs)
+                        : n <= (p.M <= mx_few_rows(slabs) ? 2 * MX_FEW : MX_FEW)) {
       hipLaunchKernelGGL((mx4_gemm_few<MODE, T>), dim3((unsigned)n), dim3(64 * MXF_W), 0, s, p);
       return hipGetLastError();
     }

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2607_20548_amd as soap
+from tests.test_gpu_mx4 import close, offsets_of
 
 pytestmark = pytest.mark.gpu
 
@@ -221,3 +222,28 @@ def test_quantising_into_one_matrix_of_a_packed_bank(k):
                 assert torch.equal(m.data[e], w.data) and torch.equal(m.scale[e], w.scale)
             else:
                 assert (m.data[e] == 7).all() and (m.scale[e] == 7).all()
+
+
+# ------------------------------------------------- both sides of a choice of tiles
+@pytest.mark.parametrize("M,N,K", [(16, 16384, 1280), (16, 16384, 1300), (4, 9600, 1792), (5, 9600, 1792), (1, 9000, 2048),
+                                   (8, 16384, 2304), (9, 16384, 2304), (16, 9000, 2816), (16, 9000, 5000),
+                                   (3, 9000, 15400), (64, 4096, 600), (65, 4096, 600)])
+def test_dense_products_of_few_rows(M, N, K):
+    a, b = soap.mx4_quantize(randn(M, K)), soap.mx4_quantize(randn(N, K, seed=1))
+    for dtype in (torch.float32, torch.bfloat16):
+        close(soap.mx4_product(a, b, dtype), a.values().double(), b.values().double(), dtype)
+
+
+@pytest.mark.parametrize("tiles,N,K", [(34, 512, 600), (35, 512, 600), (28, 1024, 2900), (29, 1024, 2900),
+                                       (12, 2048, 300), (13, 2048, 300), (43, 1024, 2817)])
+def test_grouped_products_of_few_rows(tiles, N, K):
+    """`tiles` tiles of 32 rows in four groups, one of them without any, one with part of a tile."""
+    sizes = [32 * (tiles // 3), 0, 32 * (tiles - tiles // 3 - 2) + 11, 32]
+    a, b = soap.mx4_quantize(randn(32 * tiles, K)), soap.mx4_quantize(randn(4, N, K, seed=1))
+    av, bv = a.values().double(), b.values().double()
+    for dtype in (torch.float32, torch.bfloat16):
+        got, at = soap.mx4_product_rows(a, b, offsets_of(sizes), dtype), 0
+        for g, n in enumerate(sizes):
+            close(got[at:at + n], av[at:at + n], bv[g], dtype, g)
+            at += n
+        assert (got[at:] == 0).all()
