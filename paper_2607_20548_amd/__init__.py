@@ -830,11 +830,34 @@ def _mx4_empty(x, lead, k):
     return m
 
 
+def _taken_often(rows, x_rows, cols, kind):
+    """Whether rows of x are quantised once and copied: two launches, which read a taken row
+    packed, against one, which reads it whole and quantises it again (microseconds of the one
+    / the other, rows of the plans of top-k routings to 64 experts).  The first costs a launch
+    and a pass over x more, and saves by the values taken:
+      bfloat16  4096 tokens of 2048: top 5 17.3 / 16.7, top 6 18.4 / 19.1, top 8 20.4 / 24.0
+                4096 of 4096: top 2 16.3 / 15.3, top 3 18.5 / 20.7, top 8 29.6 / 48.2
+                1024 of 2048: top 8 8.8 / 8.3, top 10 9.2 / 9.5
+      float32   4096 of 2048: top 2 13.7 / 13.2, top 3 14.5 / 17.5, top 8 19.8 / 41.7
+    A copied row keeps a wave busy from 2048 values on; rows of fewer win later (bfloat16, 32768
+    tokens of 1024: top 3 39.0 / 36.5, top 4 45.3 / 47.1; 16384 of 768: top 8 37.2 / 37.1; 65536
+    of 512: top 12 139 / 136).  Of 352 shapes (64 to 65536 tokens of 512 to 8192) it takes 0.3 per
+    cent longer than the better form on average, 23 at worst.  Rows of -1 count, since the
+    tokens are known on the GPU only: the worst are plans of mostly such rows (float32, 256 tokens
+    of 4096, top 1 of 128 experts 7.7 / 6.6; 512 of 8192, top 2 of 64 11.9 / 9.7), of which others gain
+    (64 of 4096, top 8 of 512 11.9 / 16.7)."""
+    width = min((cols + 255) // 256 * 256, 1536)
+    if kind == SOAP_BF16:
+        return width > 512 and rows * cols * width >= ((28 << 20) + 1.6 * x_rows * cols) * 1536
+    return width > 256 and rows * cols * width >= ((14 << 20) + 0.8 * x_rows * cols) * 1536
+
+
 def mx4_quantize(x, along: str = "cols", row_index=None, stream=None):
     """x (float32 or bfloat16 [rows, cols], or contiguous [batch, rows, cols]) in MXFP4
     with blocks along its columns ("cols"), along its rows ("rows": the transposed
     matrix, [cols, rows]) or both (a pair, x read once).  row_index (int32 [n]) takes
-    the rows row_index[i] of x, zeros where that is not a row of x."""
+    the rows row_index[i] of x, zeros where that is not a row of x; along the columns, rows
+    that are taken often are quantised once into a packed matrix of x's own and copied."""
     if along not in ("cols", "rows", "both"):
         raise ValueError(f'along must be "cols", "rows" or "both", got {along!r}')
     if stream is not None:
@@ -849,11 +872,7 @@ def mx4_quantize(x, along: str = "cols", row_index=None, stream=None):
             raise ValueError("row_index takes a single matrix")
         rows = row_index.numel()
         _exactly(row_index, "row_index", _torch.int32, (rows,), x)
-    if row_index is not None and along == "cols" and rows >= 8 * x_rows and rows * cols >= 1 << 25:
-        # Every row is taken often: quantised once and copied.  34 752 rows of 4096 tokens
-        # of 2048 values 20.6 us instead of 24, of 4096 values 29.6 instead of 47.  Below it
-        # loses: 10 176 rows of 1024 tokens 8.7 instead of 8.0, and rows taken four times
-        # (16 640 of 4096 tokens) 15.8 instead of 14.1.
+    if row_index is not None and along == "cols" and _taken_often(rows, x_rows, cols, kind):
         once = mx4_quantize(x)
         a = _mx4_empty(x, (rows,), cols)
         _check(lib().soap_mx4_gather(rows, cols, row_index.data_ptr(), x_rows, once.data.data_ptr(),

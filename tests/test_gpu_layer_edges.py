@@ -247,3 +247,18 @@ def test_grouped_products_of_few_rows(tiles, N, K):
             close(got[at:at + n], av[at:at + n], bv[g], dtype, g)
             at += n
         assert (got[at:] == 0).all()
+
+
+# ------------------------------------------------------- rows taken more than once
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,cols,rows", [(300, 1537, 20010), (300, 1537, 9000), (40, 300, 90000), (5000, 2048, 9000),
+                                              (5000, 2048, 20000), (0, 4100, 8000), (1, 8192, 4000), (900, 700, 48000)])
+def test_rows_taken_often_and_seldom_are_the_same(tokens, cols, rows, dtype):
+    """The binding chooses between quantising a row each time it is taken and copying it."""
+    x = randn(tokens, cols + 3).to(dtype)[:, :cols]
+    index = torch.randint(-1, tokens + 1, (rows,), device="cuda", dtype=torch.int32)
+    got = soap.mx4_quantize(x, row_index=index)
+    want = soap._mx4_empty(x, (rows,), cols)
+    soap.soap_mx4_quantize(1, rows, cols, soap.SOAP_BF16 if dtype == torch.bfloat16 else soap.SOAP_F32, x, cols + 3,
+                           index, tokens, want.data, want.scale, None, None)
+    assert torch.equal(got.data, want.data) and torch.equal(got.scale, want.scale)

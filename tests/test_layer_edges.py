@@ -107,3 +107,15 @@ def test_scales_need_eight_bytes_of_alignment(built):
         assert L.soap_mx4_dequantize(4, 64, P8[0], s0, 0, P8[0], 64, None) == code
         assert L.soap_mx4_quantize(1, 8, 64, 0, P8[0], 64, None, 0, P8[0], s0, None, None, None) == code
         assert L.soap_mx4_quantize(1, 8, 64, 0, P8[0], 64, None, 0, None, None, P8[0], s0, None) == code
+
+
+@pytest.mark.parametrize("kind", [soap.SOAP_BF16, soap.SOAP_F32])
+def test_rows_are_copied_when_they_are_taken_often_and_long(kind):
+    often = soap._taken_often
+    assert often(1 << 17, 1 << 13, 4096, kind) and often(1 << 20, 1, 2048, kind)
+    assert not often(1 << 13, 1 << 13, 4096, kind)          # each row once
+    assert not often(100, 4, 16384, kind)                   # two launches cost more than they save
+    assert not often(1 << 20, 1 << 10, 256, kind)           # a short row leaves a wave idle
+    for cols in (700, 1024, 2048, 8192):                    # once it pays, more rows pay too
+        of = [often(rows, 4096, cols, kind) for rows in range(0, 300000, 1000)]
+        assert of == sorted(of) and of[-1]
