@@ -262,3 +262,105 @@ def test_rows_taken_often_and_seldom_are_the_same(tokens, cols, rows, dtype):
     soap.soap_mx4_quantize(1, rows, cols, soap.SOAP_BF16 if dtype == torch.bfloat16 else soap.SOAP_F32, x, cols + 3,
                            index, tokens, want.data, want.scale, None, None)
     assert torch.equal(got.data, want.data) and torch.equal(got.scale, want.scale)
+
+
+# ------------------------------------------- the functions of the C names, strided outputs
+KIND = {torch.float32: soap.SOAP_F32, torch.bfloat16: soap.SOAP_BF16}
+
+
+def framed(rows, cols, pad, off, dtype):
+    """[rows, cols] inside a wider matrix of sevens, and a check that those stay."""
+    wide = torch.full((rows, cols + pad + off), 7.0, device="cuda", dtype=dtype)
+
+    def kept():
+        return (wide[:, :off] == 7).all() and (wide[:, off + cols:] == 7).all()
+    return wide[:, off:off + cols], kept
+
+
+FRAMES = [(0, 0), (8, 8), (1, 0), (0, 1), (3, 2)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,off", FRAMES)
+@pytest.mark.parametrize("rows,cols", [(37, 100), (37, 1030), (70, 4096), (5, 9001)])
+def test_layer_norm_into_strided_rows(rows, cols, pad, off, dtype):
+    x, dy = randn(rows, cols).to(dtype), randn(rows, cols, seed=1).to(dtype)
+    norm = soap.LayerNorm(1 + 0.1 * randn(cols, seed=2), 0.1 * randn(cols, seed=3))
+    y, mean, rstd = norm.forward(x)
+    dx, dweight, dbias = norm.backward(dy, x, mean, rstd)
+    got, kept = framed(rows, cols, pad, off, dtype)
+    soap.soap_layer_norm_forward(rows, cols, KIND[dtype], x, cols, norm.weight, norm.bias, norm.eps, got,
+                                 got.stride(0), None, None)
+    assert torch.equal(got, y) and kept()
+    need = soap.soap_layer_norm_workspace_bytes(rows, cols)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    got, kept = framed(rows, cols, pad, off, dtype)
+    dw, db = torch.empty_like(dweight), torch.empty_like(dbias)
+    args = (rows, cols, KIND[dtype], dy, cols, x, cols, norm.weight, mean, rstd)
+    soap.soap_layer_norm_backward(*args, got, got.stride(0), dw, db, ws, need)
+    assert torch.equal(got, dx) and kept() and torch.equal(dw, dweight) and torch.equal(db, dbias)
+    got, kept = framed(rows, cols, pad, off, dtype)          # each output alone
+    soap.soap_layer_norm_backward(*args, got, got.stride(0), None, None, None, 0)
+    assert torch.equal(got, dx) and kept()
+    for a, b, want in ((dw, None, dweight), (None, db, dbias)):
+        (a if b is None else b).fill_(7)
+        soap.soap_layer_norm_backward(*args, None, 0, a, b, ws, need)
+        assert torch.equal(a if b is None else b, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,off", FRAMES)
+@pytest.mark.parametrize("tokens,experts,k", [(50, 64, 4), (300, 100, 8), (40, 600, 3)])
+def test_router_gradient_into_strided_rows(tokens, experts, k, pad, off, dtype):
+    l, dgate = randn(tokens, experts).to(dtype), randn(tokens, k, seed=1)
+    mask = randn(tokens, seed=2) > -1
+    dloss = torch.tensor([0.3], device="cuda")
+    for renorm in (True, False):
+        router = soap.Router(experts, k, renormalize=renorm, balance=0.1)
+        r = router.forward(l, mask)
+        want = router.backward(l, r.index, r.counts, dgate, dloss, mask)
+        got, kept = framed(tokens, experts, pad, off, dtype)
+        soap.soap_router_backward(tokens, experts, k, KIND[dtype], l, experts, mask, router.flags, 0.1, r.index,
+                                  r.counts, dgate, dloss, got, got.stride(0))
+        assert torch.equal(got, want) and kept()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad", [1, 8])
+def test_quantising_batches_of_strided_rows(pad, dtype):
+    batch, rows, cols = 3, 45, 300
+    wide = randn(batch, rows, cols + pad).to(dtype)
+    x = wide[:, :, :cols].contiguous()
+    want, want_t = soap.mx4_quantize(x, along="both")
+    got, got_t = soap._mx4_empty(x, (batch, rows), cols), soap._mx4_empty(x, (batch, cols), rows)
+    soap.soap_mx4_quantize(batch, rows, cols, KIND[dtype], wide, cols + pad, None, 0, got.data, got.scale, got_t.data,
+                           got_t.scale)
+    for a, b in ((got, want), (got_t, want_t)):
+        assert torch.equal(a.data, b.data) and torch.equal(a.scale, b.scale)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,off", FRAMES)
+@pytest.mark.parametrize("sizes,N,K", [([32, 0, 45], 70, 100), ([700, 0, 900, 33], 777, 300)])
+def test_grouped_products_into_strided_rows(sizes, N, K, pad, off, dtype):
+    M = sum(sizes) + 20
+    a, b = soap.mx4_quantize(randn(M, K)), soap.mx4_quantize(randn(len(sizes), N, K, seed=1))
+    o = offsets_of(sizes)
+    want = soap.mx4_product_rows(a, b, o, dtype)
+    got, kept = framed(M, N, pad, off, dtype)
+    soap.soap_mx4_gemm_rows(len(sizes), M, N, K, o, a.data, a.scale, b.data, b.scale, KIND[dtype], got, got.stride(0))
+    assert torch.equal(got, want) and kept()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N", [(40, 64), (33, 127)])
+def test_products_by_k_at_any_element(M, N, dtype):
+    sizes = [64, 0, 96, 32]
+    K = sum(sizes)
+    a, b, o = soap.mx4_quantize(randn(M, K)), soap.mx4_quantize(randn(N, K, seed=1)), offsets_of(sizes)
+    want = soap.mx4_product_k(a, b, o, dtype)
+    for off in (0, 1, 8):
+        flat = torch.full((4 * M * N + 16,), 7.0, device="cuda", dtype=dtype)
+        soap.soap_mx4_gemm_k(4, M, N, K, o, a.data, a.scale, b.data, b.scale, KIND[dtype], flat[off:])
+        assert torch.equal(flat[off:off + 4 * M * N].view(4, M, N), want)
+        assert (flat[:off] == 7).all() and (flat[off + 4 * M * N:] == 7).all()
