@@ -313,12 +313,13 @@ int soap_kl_factors_f32(int64_t m, int64_t n, const float *G, float *L, float *R
  * Streams, errors and ownership as above, with these differences:
  *  - Activations, logits and their gradients are fp32 or bfloat16 (soap_dtype),
  *    with a row stride ld* in elements (>= the number of columns), and need only
- *    the alignment of an element: 16-byte aligned rows are read and written 16
- *    bytes at a time, others an element at a time.  Parameters, their gradients,
- *    statistics, gates and losses are fp32, indices int32.  Other buffers are
- *    16-byte aligned where they are the library's own formats (packed matrices,
- *    workspaces; the scales of packed matrices 8-byte aligned) and element-aligned
- *    otherwise.
+ *    the alignment of an element.  Layer norm, quantisation and values move 16 bytes
+ *    at a time wherever a row starts; the router's rows and a product's C do where
+ *    they are 16-byte aligned, and go an element at a time elsewhere.  Parameters,
+ *    their gradients, statistics, gates and losses are fp32, indices int32.  Other
+ *    buffers are 16-byte aligned where they are the library's own formats (packed
+ *    matrices, workspaces; the scales of packed matrices 8-byte aligned) and
+ *    element-aligned otherwise.
  *  - The token axis may be empty (rows = 0, tokens = 0: sums and counts are then
  *    zero) and goes up to SOAP_MAX_ROWS.
  *  - No output may overlap an input or another output; the range of a strided
@@ -333,6 +334,7 @@ typedef enum { SOAP_F32 = 0, SOAP_BF16 = 1 } soap_dtype;
  *   y = weight (x - mean) rstd + bias
  * weight and bias hold cols floats (NULL: ones, zeros); mean and rstd receive
  * rows floats for the backward pass (NULL: not wanted); eps is finite and > 0.
+ * The sums are fp32: a row whose sum (x - mean)^2 passes their range has rstd 0.
  * The backward pass gives, with h = (x - mean) rstd and g = weight dy,
  *   dx = rstd (g - mean(g) - h mean(g h)),  dweight = sum_rows dy h,  dbias = sum_rows dy
  * (each NULL where it is not wanted, dx too); the workspace holds the partial

@@ -460,7 +460,8 @@ class MuonState:
 # ------------------------------------------------------------------------------
 # Operators of the layer around an expert bank.  The functions of the C names take
 # raw device pointers (ints) or tensors, whose element type and strides are the
-# caller's to get right; the classes below check them.
+# caller's to get right; the classes below check them.  None takes part in torch's
+# autograd: results have no graph, the gradients are calls of their own.
 def _raw(x) -> Optional[int]:
     if x is None or isinstance(x, int):
         return x
@@ -647,7 +648,8 @@ def _on(stream, inputs, call, *args, **kwargs):
 class LayerNorm:
     """Layer norm of rows of `cols` values with fp32 ``weight`` and ``bias`` (either may
     be None): soap_layer_norm_forward / _backward with outputs and workspace allocated
-    by torch.  Inputs are float32 or bfloat16 [rows, cols] with contiguous rows."""
+    by torch.  Inputs are float32 or bfloat16 [rows, cols] with contiguous rows (other
+    leading axes are the caller's to join); results have no autograd graph."""
 
     def __init__(self, weight=None, bias=None, eps: float = 1e-5, cols: Optional[int] = None):
         given = [t for t in (weight, bias) if t is not None]
@@ -719,7 +721,7 @@ class Router:
     """Top-k routing over `experts` with balance loss, counts and dispatch plan
     (soap_router_forward / _backward).  Logits are float32 or bfloat16
     [tokens, experts] with contiguous rows, mask a bool [tokens] (False: the token
-    does not route) or None."""
+    does not route) or None; results have no autograd graph."""
 
     def __init__(self, experts: int, top_k: int, renormalize: bool = True, balance: float = 0.01):
         self.experts, self.top_k, self.balance = experts, top_k, balance

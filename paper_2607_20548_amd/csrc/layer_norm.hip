@@ -17,9 +17,11 @@
 // registers and load their next row before they reduce the present one.
 //
 // Groups of a whole workgroup meet once per row: the variance is put together from
-// the waves' own means and squares about them.  Measured: 16384 x 4096 bfloat16 53 us
-// forward and 77 backward (5.1 and 5.2 TB/s; a copy of 1 GiB reaches 5.2), without the
-// row ahead and with two meetings 76 and 103.
+// the waves' own means and squares about them.  Measured: 16384 x 4096 bfloat16 53 us a
+// pass forward (5.1 TB/s; a copy of 1 GiB reaches 5.2) and 81 backward (in a kernel trace
+// 78, 5.2 TB/s, and 5 for the second kernel), without the row ahead and with two meetings
+// 76 and 103.  Rows that start between two 16 bytes are slower: 16384 x 2048 bfloat16 27 us
+// forward and 45 backward, x 2047 44 and 70.
 //
 // dw and db: every workgroup writes the sums over its rows, a second kernel
 // adds these partial sums in a fixed order, so results do not vary between
@@ -32,10 +34,14 @@
 namespace soap {
 namespace {
 
-// Workgroups of a launch at most.  Backward they are the rows of partial sums: two
-// for every compute unit where more than one fits it (16384 x 4096 bfloat16 77 us;
-// 256 workgroups 93, 768 79, 1024 90), one past 4096 columns (8192 x 8192 fp32 146 us
-// against 156 with 512, 4096 x 16384 bfloat16 92 against 102).
+// Workgroups of a launch at most.  Forward 1024 are four for every compute unit, more than
+// are resident at once where a thread holds 32 values (144 registers and more: 768), whose
+// last ones then start late: passes over changing inputs, 16384 x 4096 bfloat16 51.2 us (54
+// with 768), but 16384 x 2048 26.8 (24.9), x 2047 43.6 (36.1), 8192 x 8192 53.8 (47.5).
+// Backward they are the rows of partial sums: two for every compute unit where more than
+// one fits it (16384 x 4096 bfloat16 81.6 us; 256 workgroups 93, 768 86, 1024 95), one past
+// 4096 columns (8192 x 8192 fp32 153 us against 162 with 512, 4096 x 16384 bfloat16 96
+// against 110).
 constexpr int64_t LN_BLOCKS_FWD = 1024;
 int64_t ln_most_bwd(int64_t cols) { return cols <= 4096 ? 512 : 256; }
 constexpr int LN_FIN = 1024;             // threads of the second kernel,
@@ -260,7 +266,9 @@ __global__ __launch_bounds__(ln_threads<GROUP>()) void layer_norm_bwd(LnParams p
       nd[u] = ln_load<T>(dy, (u * GROUP + lane) * VEC, p.cols);
     }
   };
-  // past 8192 columns the next row does not fit the registers
+  // Past 8192 columns the next row does not fit the registers, and the present one does not
+  // quite: a thread keeps 20 (bfloat16) or 32 (fp32) of them in memory.  4096 x 16384
+  // bfloat16 98 us, 4.1 TB/s, fp32 175, 4.6.
   constexpr bool AHEAD = GROUP < 512;
   if (AHEAD) load(row);
   for (int k = 0; row - g < p.rows; row += step, k ^= 1) {

@@ -147,12 +147,13 @@ __global__ __launch_bounds__(256) void mx4_quantize_cols(QuantParams p) {
 // that a column's 64 bytes (four blocks) are written together.  Workgroups of
 // consecutive rows run on one XCD, whose L2 joins what they write of a line.  Without
 // an index no row is read twice: the loads leave the L2s to the stores (the 64 x 2048 x
-// 768 bank both ways 91 us, 5.6 TB/s, against 103); with one, a token's row is read for
-// each of its experts and kept there (34 752 rows of 4096 tokens of 2048 18 us, against
-// 20 with branches around absent rows).  The rows' loads do not wait for each other: a
+// 768 bank both ways 90 us, 5.6 TB/s, against 103); with one, a token's row is read for
+// each of its experts and kept there (34 752 rows of 4096 tokens of 2048 along the rows 18 us
+// on one input, 20.6 in a kernel trace over changing ones).  The rows' loads do not wait for each other: a
 // branch for every row or column that is not there took 65536 x 700 bfloat16 from 30 us
 // to 79.  Bfloat16 maxima and conversions work on pairs, both ways 49 152 x 2048 60 us
-// against 75 by single values (which held 256 registers).
+// against 75 by single values (which held 256 registers, as fp32 does; with an index and both
+// ways one fp32 value of a thread goes through memory).
 template <typename T, bool ROWS, bool GATHER>
 __global__ __launch_bounds__(256, 2) void mx4_quantize_tile(QuantParams p) {
   // column x's block of wave w: 16 bytes at x * 64 + 16 * (w ^ (x / 4 % 4))
@@ -588,9 +589,10 @@ __device__ __forceinline__ void mx_store(const MxParams &p, T *C, int64_t row0, 
 // Slabs are whole in the packed rows; their padding's blocks get scales of 2^-127 on
 // both sides, whose products vanish (and no NaN); loads past the last slab bring it
 // again.
-// Measured: 8192 x 14336 x 4096 267 us (3600 TFLOP/s), 4096 x 4096 x 14336 114 (4200);
-// a loop of these instructions alone reaches 5600 on random data.  They are busy 0.51 of
-// the time and waves wait 0.22 of it, at 1.75 to 1.9 GHz.
+// Measured: 8192 x 14336 x 4096 252 us (3800 TFLOP/s), 4096 x 4096 x 14336 110 (4400), of one
+// input again and again in a captured graph; over changing inputs in a kernel trace the first
+// takes 258 to 290.  A loop of these instructions alone reaches 5600 on random data.  They are
+// busy 0.50 of the time and waves wait 0.22 of it, at 1.75 to 1.9 GHz.
 //
 // The B operand goes first, so that a lane holds four consecutive columns of one
 // row of C: results are rounded in registers, staged 32 rows at a time in the
@@ -784,9 +786,10 @@ __global__ __launch_bounds__(256, TM == 256 ? 1 : 2) void mx4_gemm_tile(MxParams
 // Tiles of 128 x 128 for products of fewer or shorter tiles: one slab in LDS, the
 // next on its way through registers, and four workgroups per compute unit, which cover
 // each other's barriers, first loads and epilogues.  Groups by rows (64 experts of 2048
-// x 768, 512 rows each) 46 to 57 us, matrix instructions busy 0.34 of it and waves
-// waiting 0.36 of theirs; by k (their gradients) 94 to 110 us, busy 0.20: bound by the
-// 403 MB written.
+// x 768, 512 rows each) 45 to 58 us in a kernel trace, matrix instructions busy 0.35 of it and
+// waves waiting 0.36 of theirs; by k (their gradients) 94 to 105 us, busy 0.21: bound by the
+// 403 MB written.  Nothing splits a group's sum over workgroups: 2 groups of 64 x 64, 2048 k
+// each, take 10 us on two compute units, 512 x 512 x 65536 79 us on 16 (in the tiles above).
 template <int MODE, typename T, bool STREAM>
 __global__ __launch_bounds__(256, 4) void mx4_gemm_tile128(MxParams p) {
   constexpr int TM = 128, TN = 128, BI = 2, BJ = 2, UNITS = 8, DATA = 256 * 128;
@@ -888,8 +891,9 @@ __global__ __launch_bounds__(256, 4) void mx4_gemm_tile128(MxParams p) {
 // Few rows: 32 x 32 of C per workgroup, whose MXF_W waves take the slabs of K in turn
 // and add their sums in LDS in order.  Operands go from memory to registers, all of a
 // wave's loads of MXF_AHEAD slabs ahead of its matrix instructions; B is read once, by
-// as many waves as there are: 16 x 14336 x 4096 10.2 us, 3.1 TB/s of it, first loads and
-// the join of the waves' sums included (a launch alone takes 3).
+// as many waves as there are: 16 x 14336 x 4096 11.6 us in a kernel trace over changing
+// weights, 2.7 TB/s of them, 10.2 where the last-level cache has them, first loads and the
+// join of the waves' sums included (a launch alone takes 3).
 constexpr int MXF_W = 8, MXF_AHEAD = 2;
 template <int MODE, typename T>
 __global__ __launch_bounds__(64 * MXF_W) void mx4_gemm_few(MxParams p) {

@@ -29,9 +29,9 @@
 //
 // Bytes are few (32768 x 128 bfloat16, 8 of them: 12.6 MB, 2.4 us of HBM's time);
 // the rounds of the top-k, chains of a maximum and lane exchanges, and the launches
-// bound it.  Measured: 15 us for the choices, 4 for the scan, 6 for the plan (22 in
-// all); 8 x 64 fp32 6.4 us; the
-// gradient of 32768 x 128 15 us (2.3 TB/s).
+// bound it.  Measured: a pass 22 us, in a kernel trace, which lengthens short kernels, 15 for
+// the choices, 4 for the scan and 6 for the plan; 8 x 64 fp32 6.4 in the trace; the gradient of
+// 32768 x 128 fp32 a pass of 16.3 us (2.2 TB/s), 17.7 in the trace.
 #include "internal.h"
 #include "lanes.h"
 
