@@ -364,3 +364,32 @@ def test_products_by_k_at_any_element(M, N, dtype):
         soap.soap_mx4_gemm_k(4, M, N, K, o, a.data, a.scale, b.data, b.scale, KIND[dtype], flat[off:])
         assert torch.equal(flat[off:off + 4 * M * N].view(4, M, N), want)
         assert (flat[:off] == 7).all() and (flat[off + 4 * M * N:] == 7).all()
+
+
+def test_sums_over_the_longest_axis():
+    """2^25 values a row: a tile's packed rows reach 2^31 bytes.  The second group is the
+    last 4096 values but 64."""
+    K, M, N = 2 * soap.SOAP_MAX_ROWS, 131, 70
+    g = torch.Generator(device="cuda").manual_seed(7)
+
+    def packed(rows):
+        data = torch.randint(0, 256, (rows, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+        scale = torch.randint(120, 130, (rows, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+        return soap.Mx4(data, scale, K)
+    a, b = packed(M), packed(N)
+    ends = [0, K - 4096, K - 64]
+    got = soap.mx4_product_k(a, b, torch.tensor(ends, dtype=torch.int32, device="cuda"))
+    part = lambda m, lo, hi: soap.Mx4(m.data[:, lo // 2:hi // 2].contiguous(),  # noqa: E731
+                                      m.scale[:, lo // 32:hi // 32].contiguous(), hi - lo).values().double()
+    want, size = (torch.zeros(M, N, dtype=torch.float64, device="cuda") for _ in range(2))
+    step = 1 << 21
+    for lo in range(0, K, step):
+        av, bv = part(a, lo, lo + step), part(b, lo, lo + step)
+        if lo + step == K:
+            last = slice(step - 4096, step - 64)
+            close(got[1], av[:, last], bv[:, last], torch.float32)
+            av[:, step - 4096:] = 0
+        want += av @ bv.t().contiguous()
+        size += av.abs() @ bv.abs().t().contiguous()
+    assert ((got[0].double() - want).abs() <= (2 * (K // 64) + 2) * 2.0 ** -23 * size).all()
+    assert (got[0].double() - want).norm() <= 1e-3 * want.norm()       # random signs: far inside the bound
