@@ -449,6 +449,116 @@ int soap_mx4_gemm_k(int64_t groups, int64_t M, int64_t N, int64_t K, const int32
                     const uint8_t *a_data, const uint8_t *a_scale, const uint8_t *b_data,
                     const uint8_t *b_scale, int dtype, void *C, hipStream_t stream);
 
+/* ---- operators of a dense layer ----
+ * The entry of attention, the feed-forward block and a loss on the logits, with their
+ * gradients, under the rules of the operators around an expert bank above (types, empty
+ * token axes, no overlapping outputs, results that do not vary between runs). */
+
+/* RMS norm of every head of queries and keys and the rotation by its token's position, in
+ * one pass: of a head x of dim values (even, 2 .. SOAP_HEAD_MAX_DIM)
+ *   h = x / sqrt(sum x^2 / dim + eps),  y = w h
+ * and the pairs (a, b) of the first `rotary` values of y (even, 0 .. dim) are turned to
+ *   (a cos t - b sin t, b cos t + a sin t),  t = position frequencies[i] of pair i,
+ * pair i being the values i and i + rotary / 2, or 2 i and 2 i + 1 with
+ * SOAP_HEAD_INTERLEAVED.  q_heads queries and k_heads keys a token (0 .. SOAP_HEAD_MAX_HEADS;
+ * a side without heads is not touched); strides of tokens and heads are in elements, those of
+ * a head 1, so that q and k may lie in one fused row and heads in front of tokens.  Weights
+ * hold dim floats (NULL: ones), positions one int32 a token (NULL: 0, 1, ..), frequencies
+ * rotary / 2 doubles; the angle is formed in fp64.  Inputs may repeat (stride 0); an output's
+ * heads may not lie over each other, but between those of the other side.
+ * A head whose sum of squares passes fp32's range becomes zeros (NaN if it holds an infinity
+ * or a NaN).
+ * The backward pass takes the gradients of the outputs and the inputs again and gives, with
+ * g the gradient turned back,
+ *   dx = r (w g - h sum(w g h) / dim), r = h / x,  dw = sum over tokens and heads of g h
+ * (each NULL where it is not wanted); the workspace holds partial sums of the weights'
+ * gradients (it may be NULL if neither is wanted). */
+enum { SOAP_HEAD_INTERLEAVED = 1u << 0 };
+#define SOAP_HEAD_MAX_DIM 512
+#define SOAP_HEAD_MAX_HEADS 1024
+int soap_head_norm_forward(int64_t tokens, int64_t q_heads, int64_t k_heads, int64_t dim, int64_t rotary,
+                           int dtype, uint32_t flags, const void *q, int64_t q_token, int64_t q_head,
+                           const void *k, int64_t k_token, int64_t k_head, const float *q_weight,
+                           const float *k_weight, float eps, const int32_t *positions,
+                           const double *frequencies, void *q_out, int64_t q_out_token, int64_t q_out_head,
+                           void *k_out, int64_t k_out_token, int64_t k_out_head, hipStream_t stream);
+size_t soap_head_norm_workspace_bytes(int64_t tokens, int64_t dim);
+int soap_head_norm_backward(int64_t tokens, int64_t q_heads, int64_t k_heads, int64_t dim, int64_t rotary,
+                            int dtype, uint32_t flags, const void *dq_out, int64_t dq_out_token,
+                            int64_t dq_out_head, const void *dk_out, int64_t dk_out_token, int64_t dk_out_head,
+                            const void *q, int64_t q_token, int64_t q_head, const void *k, int64_t k_token,
+                            int64_t k_head, const float *q_weight, const float *k_weight, float eps,
+                            const int32_t *positions, const double *frequencies, void *dq, int64_t dq_token,
+                            int64_t dq_head, void *dk, int64_t dk_token, int64_t dk_head, float *dq_weight,
+                            float *dk_weight, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Gated feed-forward block in bfloat16 with fp32 sums:
+ *   G = X Wg,  U = X Wu,  H = act(G) U (values one by one),  Y = H Wd
+ * X tokens x m, Wg and Wu m x n, Wd n x p, Y tokens x p: the weights are stored "in" x "out"
+ * as the steps update them, each rounded to bfloat16.  m, n and p are multiples of 8; rows of
+ * X, Y and their gradients start at multiples of 16 bytes (ld a multiple of 8, up to
+ * SOAP_GATED_MAX_LD), the other matrices are dense.  act is x / (1 + exp(-x)) (SILU) or
+ * x (1 + erf(x / sqrt 2)) / 2 (GELU).  G, U (tokens x n, both or neither NULL) are kept for the
+ * backward pass.  Sums are fp32; G, U, H and Y are rounded to bfloat16 once, H from unrounded
+ * G and U.
+ * The backward pass gives, from dY, X and the kept G and U (H is computed again),
+ *   dH = dY Wd^T,  dG = dH U act'(G),  dU = dH act(G)
+ *   dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY
+ * (each NULL where it is not wanted): dG, dU and H are rounded to bfloat16 as operands, dX
+ * too, the weights' gradients are fp32 (what the steps read) or bfloat16 (grad_dtype).
+ * Without tokens they are zeros.  The workspace's size never shrinks as tokens, m, n or p grow. */
+typedef enum { SOAP_ACT_SILU = 0, SOAP_ACT_GELU = 1 } soap_activation;
+#define SOAP_GATED_MAX_HIDDEN 65536
+#define SOAP_GATED_MAX_LD (1 << 21)
+size_t soap_gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, int backward);
+int soap_gated_forward(int64_t tokens, int64_t m, int64_t n, int64_t p, int activation, const void *x,
+                       int64_t ldx, const void *w_gate, const void *w_up, const void *w_down, void *gate,
+                       void *up, void *y, int64_t ldy, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+int soap_gated_backward(int64_t tokens, int64_t m, int64_t n, int64_t p, int activation, const void *dy,
+                        int64_t lddy, const void *x, int64_t ldx, const void *w_gate, const void *w_up,
+                        const void *w_down, const void *gate, const void *up, void *dx, int64_t lddx,
+                        int grad_dtype, void *dw_gate, void *dw_up, void *dw_down, void *workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/* Distillation from a teacher's top logits: rows of logits z over `classes` (1 ..
+ * SOAP_DISTILL_MAX_CLASSES) against a list of `slots` (1 .. SOAP_DISTILL_MAX_SLOTS) classes
+ * index and values t of the teacher.  With tau the temperature, q = softmax(z / tau) and
+ *   p_j = softmax of t / tau over the list,  r = 0, or with SOAP_DISTILL_TAIL
+ *   p_j = exp(t_j) (t: the teacher's log probabilities),  r = max(0, 1 - sum p),
+ * r against q_rest, the sum of q over the classes not listed:
+ *   loss = tau^2 (sum_j p_j (log p_j - log q(index_j)) + r (log r - log q_rest))
+ * A slot whose index is outside [0, classes) is empty; its t is not read.  A list of empty
+ * slots has loss 0 and gradient 0; a term with p_j = 0 (or r = 0) is 0.  Where no class
+ * outside the list has a logit above -inf, r is taken as 0.  A class may be listed
+ * more than once: its p add up in the gradient.  Cross entropy to labels is slots = 1.
+ * stats (rows x 2 floats, may be NULL forward): log sum exp(z / tau), over all classes and
+ * (SOAP_DISTILL_TAIL, otherwise 0) over those not listed, for soap_distill_backward:
+ *   dlogits = dloss tau ((sum p + r) q - p)             at the listed classes, elsewhere
+ *   dlogits = dloss tau ((sum p + r) q - r q / q_rest)
+ * with dloss one float a row (NULL: ones); a row whose dloss is 0 gets zeros, whatever its
+ * logits.  soap_distill_forward_backward gives both in one pass over the logits.  Sums are
+ * fp32; a NaN or +inf among the logits makes its row NaN. */
+enum { SOAP_DISTILL_TAIL = 1u << 0 };
+#define SOAP_DISTILL_MAX_CLASSES (1 << 18)
+#define SOAP_DISTILL_MAX_SLOTS 512
+#define SOAP_DISTILL_MIN_TEMPERATURE 0.01
+#define SOAP_DISTILL_MAX_TEMPERATURE 100.0
+int soap_distill_forward(int64_t rows, int64_t classes, int64_t slots, int dtype, const void *logits,
+                         int64_t ld, const int32_t *index, int64_t ldi, int teacher_dtype,
+                         const void *teacher, int64_t ldt, uint32_t flags, float temperature, float *loss,
+                         float *stats, hipStream_t stream);
+int soap_distill_backward(int64_t rows, int64_t classes, int64_t slots, int dtype, const void *logits,
+                          int64_t ld, const int32_t *index, int64_t ldi, int teacher_dtype,
+                          const void *teacher, int64_t ldt, uint32_t flags, float temperature,
+                          const float *stats, const float *dloss, void *dlogits, int64_t ldd,
+                          hipStream_t stream);
+int soap_distill_forward_backward(int64_t rows, int64_t classes, int64_t slots, int dtype,
+                                  const void *logits, int64_t ld, const int32_t *index, int64_t ldi,
+                                  int teacher_dtype, const void *teacher, int64_t ldt, uint32_t flags,
+                                  float temperature, const float *dloss, float *loss, float *stats,
+                                  void *dlogits, int64_t ldd, hipStream_t stream);
+
 /* ---- measurement ---- */
 
 /* When enabled, every stage of soap_step / soap_step_batched records a pair

@@ -39,6 +39,18 @@ SOAP_MAX_ROWS = 1 << 24
 SOAP_ROUTER_RENORMALIZE = 1
 SOAP_ROUTER_MAX_EXPERTS = 1024
 SOAP_ROUTER_MAX_TOP_K = 32
+SOAP_HEAD_INTERLEAVED = 1
+SOAP_HEAD_MAX_DIM = 512
+SOAP_HEAD_MAX_HEADS = 1024
+SOAP_ACT_SILU = 0
+SOAP_ACT_GELU = 1
+SOAP_GATED_MAX_HIDDEN = 65536
+SOAP_GATED_MAX_LD = 1 << 21
+SOAP_DISTILL_TAIL = 1
+SOAP_DISTILL_MAX_CLASSES = 1 << 18
+SOAP_DISTILL_MAX_SLOTS = 512
+SOAP_DISTILL_MIN_TEMPERATURE = 0.01
+SOAP_DISTILL_MAX_TEMPERATURE = 100.0
 
 EXPORTED = [
     "soap_workspace_bytes", "soap_init_state", "soap_step", "soap_step_batched",
@@ -54,6 +66,9 @@ EXPORTED = [
     "soap_router_rows", "soap_router_workspace_bytes", "soap_router_forward",
     "soap_router_backward", "soap_mx4_data_bytes", "soap_mx4_scale_bytes", "soap_mx4_quantize",
     "soap_mx4_gather", "soap_mx4_dequantize", "soap_mx4_gemm", "soap_mx4_gemm_rows", "soap_mx4_gemm_k",
+    "soap_head_norm_forward", "soap_head_norm_workspace_bytes", "soap_head_norm_backward",
+    "soap_gated_workspace_bytes", "soap_gated_forward", "soap_gated_backward",
+    "soap_distill_forward", "soap_distill_backward", "soap_distill_forward_backward",
 ]
 
 
@@ -141,6 +156,24 @@ def lib() -> ctypes.CDLL:
         "soap_mx4_gemm": (_INT, [_I64, _I64, _I64, _P, _P, _P, _P, _INT, _P, _I64, _P]),
         "soap_mx4_gemm_rows": (_INT, [_I64, _I64, _I64, _I64, _P, _P, _P, _P, _P, _INT, _P, _I64,
                                       _P]),
+        "soap_head_norm_forward": (_INT, [_I64, _I64, _I64, _I64, _I64, _INT, _U32, _P, _I64, _I64, _P,
+                                          _I64, _I64, _P, _P, _F, _P, _P, _P, _I64, _I64, _P, _I64, _I64,
+                                          _P]),
+        "soap_head_norm_workspace_bytes": (_SZ, [_I64, _I64]),
+        "soap_head_norm_backward": (_INT, [_I64, _I64, _I64, _I64, _I64, _INT, _U32, _P, _I64, _I64, _P,
+                                           _I64, _I64, _P, _I64, _I64, _P, _I64, _I64, _P, _P, _F, _P, _P,
+                                           _P, _I64, _I64, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
+        "soap_gated_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64, _INT]),
+        "soap_gated_forward": (_INT, [_I64, _I64, _I64, _I64, _INT, _P, _I64, _P, _P, _P, _P, _P, _P,
+                                      _I64, _P, _SZ, _P]),
+        "soap_gated_backward": (_INT, [_I64, _I64, _I64, _I64, _INT, _P, _I64, _P, _I64, _P, _P, _P, _P,
+                                       _P, _P, _I64, _INT, _P, _P, _P, _P, _SZ, _P]),
+        "soap_distill_forward": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _I64, _INT, _P, _I64, _U32,
+                                        _F, _P, _P, _P]),
+        "soap_distill_backward": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _I64, _INT, _P, _I64,
+                                         _U32, _F, _P, _P, _P, _I64, _P]),
+        "soap_distill_forward_backward": (_INT, [_I64, _I64, _I64, _INT, _P, _I64, _P, _I64, _INT, _P,
+                                                 _I64, _U32, _F, _P, _P, _P, _P, _I64, _P]),
         "soap_mx4_gemm_k": (_INT, [_I64, _I64, _I64, _I64, _P, _P, _P, _P, _P, _INT, _P, _P]),
     }
     for name, (res, args) in sig.items():
@@ -558,6 +591,73 @@ def soap_mx4_gemm_k(groups, M, N, K, offsets, a_data, a_scale, b_data, b_scale, 
                                  _raw(b_data), _raw(b_scale), dtype, _raw(C), _stream(stream)))
 
 
+def soap_head_norm_forward(tokens, q_heads, k_heads, dim, rotary, dtype, flags, q, q_token, q_head, k,
+                           k_token, k_head, q_weight, k_weight, eps, positions, frequencies, q_out,
+                           q_out_token, q_out_head, k_out, k_out_token, k_out_head, stream=None) -> None:
+    _check(lib().soap_head_norm_forward(tokens, q_heads, k_heads, dim, rotary, dtype, flags, _raw(q), q_token,
+                                        q_head, _raw(k), k_token, k_head, _raw(q_weight), _raw(k_weight), eps,
+                                        _raw(positions), _raw(frequencies), _raw(q_out), q_out_token,
+                                        q_out_head, _raw(k_out), k_out_token, k_out_head, _stream(stream)))
+
+
+def soap_head_norm_workspace_bytes(tokens: int, dim: int) -> int:
+    return int(lib().soap_head_norm_workspace_bytes(tokens, dim))
+
+
+def soap_head_norm_backward(tokens, q_heads, k_heads, dim, rotary, dtype, flags, dq_out, dq_out_token,
+                            dq_out_head, dk_out, dk_out_token, dk_out_head, q, q_token, q_head, k, k_token,
+                            k_head, q_weight, k_weight, eps, positions, frequencies, dq, dq_token, dq_head, dk,
+                            dk_token, dk_head, dq_weight, dk_weight, workspace, workspace_bytes,
+                            stream=None) -> None:
+    _check(lib().soap_head_norm_backward(tokens, q_heads, k_heads, dim, rotary, dtype, flags, _raw(dq_out),
+                                         dq_out_token, dq_out_head, _raw(dk_out), dk_out_token, dk_out_head,
+                                         _raw(q), q_token, q_head, _raw(k), k_token, k_head, _raw(q_weight),
+                                         _raw(k_weight), eps, _raw(positions), _raw(frequencies), _raw(dq),
+                                         dq_token, dq_head, _raw(dk), dk_token, dk_head, _raw(dq_weight),
+                                         _raw(dk_weight), _raw(workspace), workspace_bytes, _stream(stream)))
+
+
+def soap_gated_workspace_bytes(tokens: int, m: int, n: int, p: int, backward: bool) -> int:
+    return int(lib().soap_gated_workspace_bytes(tokens, m, n, p, int(backward)))
+
+
+def soap_gated_forward(tokens, m, n, p, activation, x, ldx, w_gate, w_up, w_down, gate, up, y, ldy, workspace,
+                       workspace_bytes, stream=None) -> None:
+    _check(lib().soap_gated_forward(tokens, m, n, p, activation, _raw(x), ldx, _raw(w_gate), _raw(w_up),
+                                    _raw(w_down), _raw(gate), _raw(up), _raw(y), ldy, _raw(workspace),
+                                    workspace_bytes, _stream(stream)))
+
+
+def soap_gated_backward(tokens, m, n, p, activation, dy, lddy, x, ldx, w_gate, w_up, w_down, gate, up, dx, lddx,
+                        grad_dtype, dw_gate, dw_up, dw_down, workspace, workspace_bytes, stream=None) -> None:
+    _check(lib().soap_gated_backward(tokens, m, n, p, activation, _raw(dy), lddy, _raw(x), ldx, _raw(w_gate),
+                                     _raw(w_up), _raw(w_down), _raw(gate), _raw(up), _raw(dx), lddx, grad_dtype,
+                                     _raw(dw_gate), _raw(dw_up), _raw(dw_down), _raw(workspace),
+                                     workspace_bytes, _stream(stream)))
+
+
+def soap_distill_forward(rows, classes, slots, dtype, logits, ld, index, ldi, teacher_dtype, teacher, ldt, flags,
+                         temperature, loss, stats, stream=None) -> None:
+    _check(lib().soap_distill_forward(rows, classes, slots, dtype, _raw(logits), ld, _raw(index), ldi,
+                                      teacher_dtype, _raw(teacher), ldt, flags, temperature, _raw(loss),
+                                      _raw(stats), _stream(stream)))
+
+
+def soap_distill_backward(rows, classes, slots, dtype, logits, ld, index, ldi, teacher_dtype, teacher, ldt, flags,
+                          temperature, stats, dloss, dlogits, ldd, stream=None) -> None:
+    _check(lib().soap_distill_backward(rows, classes, slots, dtype, _raw(logits), ld, _raw(index), ldi,
+                                       teacher_dtype, _raw(teacher), ldt, flags, temperature, _raw(stats),
+                                       _raw(dloss), _raw(dlogits), ldd, _stream(stream)))
+
+
+def soap_distill_forward_backward(rows, classes, slots, dtype, logits, ld, index, ldi, teacher_dtype, teacher, ldt,
+                                  flags, temperature, dloss, loss, stats, dlogits, ldd, stream=None) -> None:
+    _check(lib().soap_distill_forward_backward(rows, classes, slots, dtype, _raw(logits), ld, _raw(index), ldi,
+                                               teacher_dtype, _raw(teacher), ldt, flags, temperature,
+                                               _raw(dloss), _raw(loss), _raw(stats), _raw(dlogits), ldd,
+                                               _stream(stream)))
+
+
 _torch = None
 
 
@@ -950,3 +1050,263 @@ def mx4_product_k(a: Mx4, b: Mx4, offsets, dtype=None, stream=None):
                                  a.scale.data_ptr(), b.data.data_ptr(), b.scale.data_ptr(), kind,
                                  out.data_ptr(), raw))
     return out
+
+
+# ------------------------------------------------------------------------------
+# Operators of a dense layer, under the same rules.
+class HeadNorm:
+    """RMS norm of every head of queries and keys and the rotation by its token's position, in one
+    pass (soap_head_norm_forward / _backward).  Heads are float32 or bfloat16 [tokens, heads, dim]
+    with contiguous values and any strides before them (views into a fused row of queries, keys and
+    values, or heads in front of tokens); weights float32 [dim] or None; positions int32 [tokens]
+    or None (0, 1, ..).  The first `rotary` values of a head (default: all) are turned, pairs being
+    its halves' values of one index or (interleaved) neighbours, by position * frequency:
+    frequencies float64 [rotary / 2], by default base ** (-2 i / rotary).  Results are contiguous
+    and have no autograd graph."""
+
+    def __init__(self, dim: int, q_weight=None, k_weight=None, eps: float = 1e-6, rotary: Optional[int] = None,
+                 base: float = 10000.0, frequencies=None, interleaved: bool = False):
+        T = _T()
+        if rotary is None:
+            rotary = dim if frequencies is None else 2 * frequencies.numel()
+        if dim < 2 or dim % 2 or rotary % 2 or not 0 <= rotary <= dim:
+            raise ValueError(f"dim and rotary must be even, rotary in [0, dim], got {dim} and {rotary}")
+        for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None:
+                _exactly(t, name, T.float32, (dim,))
+        if frequencies is not None:
+            _exactly(frequencies, "frequencies", T.float64, (rotary // 2,))
+        elif rotary:
+            given = [t for t in (q_weight, k_weight) if t is not None]
+            i = T.arange(0, rotary, 2, dtype=T.float64, device=given[0].device if given else "cuda")
+            frequencies = float(base) ** (-i / rotary)
+        self.dim, self.rotary, self.eps, self.frequencies = dim, rotary, eps, frequencies
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.flags = SOAP_HEAD_INTERLEAVED if interleaved else 0
+
+    def _side(self, t, name, like):
+        """A side's tensor checked: (heads, pointer, stride of tokens, stride of heads)."""
+        if t is None:
+            return 0, None, 0, 0
+        if t.dim() != 3 or t.shape[2] != self.dim or t.shape[0] != like.shape[0]:
+            raise ValueError(f"{name} must be [{like.shape[0]}, heads, {self.dim}], got {tuple(t.shape)}")
+        if t.stride(2) != 1:
+            raise ValueError(f"{name}: the values of a head must be contiguous")
+        if t.dtype is not like.dtype or t.get_device() != like.get_device():
+            raise ValueError(f"{name} is {t.dtype} on {t.device}, the other side {like.dtype} on {like.device}")
+        return t.shape[1], t.data_ptr(), t.stride(0), t.stride(1)
+
+    def _given(self, q, k, positions):
+        """The side that is there, its stream and type, the other tensors checked against it."""
+        one, name = (q, "q") if q is not None else (k, "k")
+        if one is None:
+            raise ValueError("neither queries nor keys are given")
+        raw = _current_stream(one, name)
+        if one.dim() != 3:
+            raise ValueError(f"{name} must be [tokens, heads, {self.dim}], got {tuple(one.shape)}")
+        kind = _floats(one, name)
+        if positions is not None:
+            _exactly(positions, "positions", _torch.int32, (one.shape[0],), one)
+        for t, n in ((self.q_weight, "q_weight"), (self.k_weight, "k_weight"), (self.frequencies, "frequencies")):
+            if t is not None and t.get_device() != one.get_device():
+                raise ValueError(f"{n} is on {t.device}, not on {one.device}")
+        return one, raw, kind
+
+    def _tensors(self, *more):
+        return (*more, self.q_weight, self.k_weight, self.frequencies)
+
+    def forward(self, q, k=None, positions=None, stream=None):
+        """(queries, keys), normed and turned; None for a side that is not given."""
+        if stream is not None:
+            return _on(stream, self._tensors(q, k, positions), self.forward, q, k, positions)
+        one, raw, kind = self._given(q, k, positions)
+        hq, qp, qt, qh = self._side(q, "q", one)
+        hk, kp, kt, kh = self._side(k, "k", one)
+        T, d, f = one.shape[0], self.dim, self.frequencies
+        yq = None if q is None else q.new_empty((T, hq, d))
+        yk = None if k is None else k.new_empty((T, hk, d))
+        wq, wk = self.q_weight, self.k_weight
+        _check(lib().soap_head_norm_forward(
+            T, hq, hk, d, self.rotary, kind, self.flags, qp, qt, qh, kp, kt, kh,
+            None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(), self.eps,
+            None if positions is None else positions.data_ptr(), None if f is None else f.data_ptr(),
+            None if q is None else yq.data_ptr(), hq * d, d, None if k is None else yk.data_ptr(), hk * d, d, raw))
+        return yq, yk
+
+    def backward(self, dq, dk, q, k=None, positions=None, stream=None):
+        """(dq, dk, dq_weight, dk_weight) from the gradients of forward's results and its
+        arguments; None for a side or a weight that is not there."""
+        if stream is not None:
+            return _on(stream, self._tensors(dq, dk, q, k, positions), self.backward, dq, dk, q, k, positions)
+        one, raw, kind = self._given(q, k, positions)
+        if (dq is None) != (q is None) or (dk is None) != (k is None):
+            raise ValueError("a side comes with its gradient")
+        hq, qp, qt, qh = self._side(q, "q", one)
+        hk, kp, kt, kh = self._side(k, "k", one)
+        gq, gqp, gqt, gqh = self._side(dq, "dq", one)
+        gk, gkp, gkt, gkh = self._side(dk, "dk", one)
+        if gq != hq or gk != hk:
+            raise ValueError(f"dq and dk have {gq} and {gk} heads, q and k {hq} and {hk}")
+        T, d, f, f32, L = one.shape[0], self.dim, self.frequencies, _torch.float32, lib()
+        oq = None if q is None else q.new_empty((T, hq, d))
+        ok = None if k is None else k.new_empty((T, hk, d))
+        wq, wk = self.q_weight, self.k_weight
+        dwq = one.new_empty(d, dtype=f32) if wq is not None and q is not None else None
+        dwk = one.new_empty(d, dtype=f32) if wk is not None and k is not None else None
+        need = L.soap_head_norm_workspace_bytes(T, d)
+        work = one.new_empty(max(need, 16), dtype=_torch.uint8)
+        _check(L.soap_head_norm_backward(
+            T, hq, hk, d, self.rotary, kind, self.flags, gqp, gqt, gqh, gkp, gkt, gkh, qp, qt, qh, kp, kt, kh,
+            None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(), self.eps,
+            None if positions is None else positions.data_ptr(), None if f is None else f.data_ptr(),
+            None if q is None else oq.data_ptr(), hq * d, d, None if k is None else ok.data_ptr(), hk * d, d,
+            None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(), work.data_ptr(), need,
+            raw))
+        return oq, ok, dwq, dwk
+
+
+_ACTIVATIONS = {"silu": SOAP_ACT_SILU, "gelu": SOAP_ACT_GELU}
+
+
+class GatedFeedForward:
+    """y = (act(x w_gate) * (x w_up)) w_down (soap_gated_forward / _backward): bfloat16 with fp32
+    sums.  Weights are contiguous bfloat16 [m, n], [m, n] and [n, p], "in" x "out" as the steps update
+    them, activation "silu" or "gelu"; inputs bfloat16 [tokens, m] with rows that start at multiples
+    of 16 bytes; m, n and p multiples of 8.  Results have no autograd graph."""
+
+    def __init__(self, w_gate, w_up, w_down, activation: str = "silu"):
+        if activation not in _ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}, got {activation!r}")
+        bf = _T().bfloat16
+        if w_gate.dim() != 2 or w_down.dim() != 2:
+            raise ValueError("weights must be [m, n], [m, n] and [n, p]")
+        self.m, self.n = w_gate.shape
+        self.p = w_down.shape[1]
+        _exactly(w_gate, "w_gate", bf, (self.m, self.n))
+        _exactly(w_up, "w_up", bf, (self.m, self.n), w_gate)
+        _exactly(w_down, "w_down", bf, (self.n, self.p), w_gate)
+        self.w_gate, self.w_up, self.w_down, self.act = w_gate, w_up, w_down, _ACTIVATIONS[activation]
+
+    def _rows(self, t, name, cols):
+        """Row stride of an input of `cols` bfloat16 values a row, on the weights' device."""
+        if t.dtype is not _torch.bfloat16:
+            raise TypeError(f"{name} must be bfloat16, got {t.dtype}")
+        _floats(t, name, cols)
+        if t.get_device() != self.w_gate.get_device():
+            raise ValueError(f"{name} is on {t.device}, not on {self.w_gate.device}")
+        return _ld(t)
+
+    def forward(self, x, keep: bool = True, stream=None):
+        """(y, gate, up): x w_gate and x w_up are kept for the backward pass, or None without `keep`."""
+        if stream is not None:
+            return _on(stream, (x, self.w_gate, self.w_up, self.w_down), self.forward, x, keep)
+        raw, ldx, L = _current_stream(x, "x"), self._rows(x, "x", self.m), lib()
+        T, m, n, p = x.shape[0], self.m, self.n, self.p
+        y = x.new_empty((T, p))
+        gate, up = (x.new_empty((T, n)), x.new_empty((T, n))) if keep else (None, None)
+        need = L.soap_gated_workspace_bytes(T, m, n, p, 0)
+        work = x.new_empty(max(need, 16), dtype=_torch.uint8)
+        _check(L.soap_gated_forward(
+            T, m, n, p, self.act, x.data_ptr(), ldx, self.w_gate.data_ptr(), self.w_up.data_ptr(),
+            self.w_down.data_ptr(), gate.data_ptr() if keep else None, up.data_ptr() if keep else None,
+            y.data_ptr(), p, work.data_ptr(), need, raw))
+        return y, gate, up
+
+    def backward(self, dy, x, gate, up, dtype=None, stream=None):
+        """(dx, dw_gate, dw_up, dw_down): the weights' gradients are float32 (default: what the steps
+        read) or bfloat16."""
+        if stream is not None:
+            return _on(stream, (dy, x, gate, up, self.w_gate, self.w_up, self.w_down), self.backward, dy, x, gate, up,
+                       dtype)
+        raw, L = _current_stream(x, "x"), lib()
+        kind, dtype = _out_type(dtype)
+        T, m, n, p, bf = x.shape[0], self.m, self.n, self.p, _torch.bfloat16
+        ldx, lddy = self._rows(x, "x", m), self._rows(dy, "dy", p)
+        if dy.shape[0] != T:
+            raise ValueError(f"dy has {dy.shape[0]} rows, x {T}")
+        _exactly(gate, "gate", bf, (T, n), x)
+        _exactly(up, "up", bf, (T, n), x)
+        dx = x.new_empty((T, m))
+        dw_gate, dw_up = x.new_empty((m, n), dtype=dtype), x.new_empty((m, n), dtype=dtype)
+        dw_down = x.new_empty((n, p), dtype=dtype)
+        need = L.soap_gated_workspace_bytes(T, m, n, p, 1)
+        work = x.new_empty(max(need, 16), dtype=_torch.uint8)
+        _check(L.soap_gated_backward(
+            T, m, n, p, self.act, dy.data_ptr(), lddy, x.data_ptr(), ldx, self.w_gate.data_ptr(),
+            self.w_up.data_ptr(), self.w_down.data_ptr(), gate.data_ptr(), up.data_ptr(), dx.data_ptr(), m, kind,
+            dw_gate.data_ptr(), dw_up.data_ptr(), dw_down.data_ptr(), work.data_ptr(), need, raw))
+        return dx, dw_gate, dw_up, dw_down
+
+
+class Distillation:
+    """Loss of rows of logits against a teacher's top classes, and its gradient
+    (soap_distill_forward / _backward / _forward_backward).  Logits are float32 or bfloat16
+    [rows, classes] with contiguous rows; index int32 [rows, slots] the listed classes (an index that is
+    no class: an empty slot) and teacher float32 or bfloat16 [rows, slots] its logits there or, with
+    `tail`, its log probabilities, what these leave being one more class.  Cross entropy to labels is a
+    list of one slot.  Results have no autograd graph."""
+
+    def __init__(self, temperature: float = 1.0, tail: bool = False):
+        if not SOAP_DISTILL_MIN_TEMPERATURE <= temperature <= SOAP_DISTILL_MAX_TEMPERATURE:
+            raise ValueError(f"temperature must lie in [{SOAP_DISTILL_MIN_TEMPERATURE}, "
+                             f"{SOAP_DISTILL_MAX_TEMPERATURE}], got {temperature}")
+        self.temperature, self.flags = float(temperature), SOAP_DISTILL_TAIL if tail else 0
+
+    def _list(self, logits, index, teacher):
+        """The leading arguments of the three entry points, and the stream."""
+        raw = _current_stream(logits, "logits")
+        if logits.dim() != 2:
+            raise ValueError(f"logits must be [rows, classes], got {tuple(logits.shape)}")
+        kind, (rows, classes) = _floats(logits, "logits"), logits.shape
+        slots = index.shape[-1] if index.dim() == 2 else -1
+        if slots < 0 or index.shape[0] != rows or teacher.shape != index.shape:
+            raise ValueError(f"index and teacher must be [{rows}, slots], got {tuple(index.shape)} and "
+                             f"{tuple(teacher.shape)}")
+        if index.dtype is not _torch.int32:
+            raise TypeError(f"index must be int32, got {index.dtype}")
+        t_kind = _floats(teacher, "teacher")
+        if index.stride(1) != 1 and slots > 1:
+            raise ValueError("index: the slots of a row must be contiguous")
+        for t, name in ((index, "index"), (teacher, "teacher")):
+            if t.get_device() != logits.get_device():
+                raise ValueError(f"{name} is on {t.device}, not on {logits.device}")
+        return (rows, classes, slots, kind, logits.data_ptr(), _ld(logits), index.data_ptr(), _ld(index), t_kind,
+                teacher.data_ptr(), _ld(teacher), self.flags, self.temperature), raw
+
+    def forward(self, logits, index, teacher, stream=None):
+        """(loss, stats): float32 [rows], and what backward takes, float32 [rows, 2] (log of the sums of
+        exponentials over all classes and, with `tail`, over those not listed)."""
+        if stream is not None:
+            return _on(stream, (logits, index, teacher), self.forward, logits, index, teacher)
+        args, raw = self._list(logits, index, teacher)
+        f32 = _torch.float32
+        loss, stats = logits.new_empty(args[0], dtype=f32), logits.new_empty((args[0], 2), dtype=f32)
+        _check(lib().soap_distill_forward(*args, loss.data_ptr(), stats.data_ptr(), raw))
+        return loss, stats
+
+    def backward(self, logits, index, teacher, stats, dloss=None, stream=None):
+        """dlogits, of the logits' type, from the gradient of the losses (float32 [rows], None: ones)."""
+        if stream is not None:
+            return _on(stream, (logits, index, teacher, stats, dloss), self.backward, logits, index, teacher, stats,
+                       dloss)
+        args, raw = self._list(logits, index, teacher)
+        _exactly(stats, "stats", _torch.float32, (args[0], 2), logits)
+        if dloss is not None:
+            _exactly(dloss, "dloss", _torch.float32, (args[0],), logits)
+        out = logits.new_empty(logits.shape)
+        _check(lib().soap_distill_backward(*args, stats.data_ptr(), None if dloss is None else dloss.data_ptr(),
+                                           out.data_ptr(), args[1], raw))
+        return out
+
+    def forward_backward(self, logits, index, teacher, dloss=None, stream=None):
+        """(loss, dlogits) in one pass over the logits, for a dloss that is known before the loss is
+        (the rows' weights in a mean)."""
+        if stream is not None:
+            return _on(stream, (logits, index, teacher, dloss), self.forward_backward, logits, index, teacher, dloss)
+        args, raw = self._list(logits, index, teacher)
+        if dloss is not None:
+            _exactly(dloss, "dloss", _torch.float32, (args[0],), logits)
+        loss, out = logits.new_empty(args[0], dtype=_torch.float32), logits.new_empty(logits.shape)
+        _check(lib().soap_distill_forward_backward(*args, None if dloss is None else dloss.data_ptr(), loss.data_ptr(),
+                                                   None, out.data_ptr(), args[1], raw))
+        return loss, out

@@ -1,0 +1,467 @@
+// RMS norm of every head of queries and keys and the rotation by its token's position,
+// forward and backward.
+//
+//   r = 1 / sqrt(sum x^2 / D + eps),  h = x r,  y = R (w h)
+//   g = R^T dy,  dx = r (w g - h sum(w g h) / D),  dw = sum over tokens and heads of g h
+//
+// R turns the pairs (a, b) of a head's first `rot` values by the token's angles
+// position * frequency: (a cos - b sin, b cos + a sin).  Pairs are values of the same index
+// in both halves of the turned part, or neighbours; the values past it are paired alike and
+// turned by 0.  Sums and statistics are fp32, outputs are rounded once.
+//
+// An angle reaches 2^31 radians and more, where fp32 (and fp64 of a product rounded to
+// radians) has no digits left of the turn: it is formed in fp64 in half turns, brought to
+// [-1, 1] there, and only then rounded for fp32 sine and cosine.
+//
+// Bound by HBM (2 and 3 values moved per element): LANES lanes of a wave hold a head, each
+// UNITS x VEC pairs (16 bytes of either half, or 32 bytes of neighbours), so that the
+// rotation stays within a lane, and the 64 / LANES groups of a wave take different heads of
+// one token, whose angles are formed once for all of them.
+//
+// dw: every workgroup walks over tokens and writes the sums over its own, a second kernel adds
+// these in a fixed order.
+#include "internal.h"
+#include "lanes.h"
+
+#include <algorithm>
+
+namespace soap {
+namespace {
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element
+
+constexpr int HN_THREADS = 256, HN_WAVES = HN_THREADS / 64;
+constexpr int64_t HN_BLOCKS_BWD = 512;   // two for every compute unit: rows of partial sums
+constexpr int64_t HN_FEW = 4096;         // waves that fill the chip: fewer tokens share heads out
+constexpr int HN_FIN = 1024, HN_FIN_COLS = 32;
+
+struct HnSide {                          // queries or keys
+  const void *x, *dy;
+  void *out;
+  const float *w;
+  int heads, chunks;                     // chunks of heads that a wave takes at once
+  int64_t xt, xh, dt, dh, ot, oh;        // strides of tokens and heads
+};
+struct HnParams {
+  int64_t tokens, tasks;
+  int dim, rot, split;
+  HnSide side[2];
+  float eps;
+  const int *pos;
+  const double *freq;
+  float *part;                           // [workgroup][2][dim]
+};
+
+template <typename T>
+constexpr int hn_vec() { return 16 / (int)sizeof(T); }
+
+// n of VEC values from p on, zeros after them.
+template <typename T>
+__device__ __forceinline__ v4u hn_load(const T *p, int n) {
+  if (n == hn_vec<T>()) return *reinterpret_cast<const v4u_any *>(p);
+  v4u q = v4u(0u);
+#pragma unroll
+  for (int i = 0; i < hn_vec<T>(); ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) q[i] = __float_as_uint(p[i]);
+      else q[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+    }
+  return q;
+}
+template <typename T>
+__device__ __forceinline__ float hn_value(const v4u &q, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(q[i]);
+  else return __uint_as_float((i & 1) ? q[i / 2] & 0xffff0000u : q[i / 2] << 16);
+}
+template <typename T>
+__device__ __forceinline__ void hn_store(T *p, int n, const float *v) {
+  v4u q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) q[i] = __float_as_uint(v[i]);
+    else
+      q[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i]) |
+             ((uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v[2 * i + 1]) << 16);
+  }
+  if (n == hn_vec<T>()) {
+    *reinterpret_cast<v4u_any *>(p) = q;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < hn_vec<T>(); ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 4) p[i] = v[i];
+      else p[i] = (uint16_t)(q[i / 2] >> (16 * (i & 1)));
+    }
+}
+
+// The VEC pairs of a lane's unit: columns of its two 16 bytes, how many values of each are
+// the head's, and where its frequencies are.
+struct HnUnit {
+  int c0, c1, n0, n1, turn, turned;      // turned: pairs with a frequency
+};
+template <int VEC, bool NEAR>
+__device__ __forceinline__ HnUnit hn_unit(const HnParams &p, int u) {
+  const int half = p.rot / 2, rest = (p.dim - p.rot) / 2, first = (half + VEC - 1) / VEC;
+  const bool in = u < first;             // the pairs that are turned, then the others
+  const int at = (in ? u : u - first) * VEC, n = min(max((in ? half : rest) - at, 0), VEC);
+  HnUnit r;
+  if (NEAR) {
+    r.c0 = (in ? 0 : p.rot) + 2 * at;
+    r.c1 = r.c0 + VEC;
+    r.n0 = min(2 * n, VEC);
+    r.n1 = 2 * n - r.n0;
+  } else {
+    r.c0 = (in ? 0 : p.rot) + at;
+    r.c1 = r.c0 + (in ? half : rest);
+    r.n0 = r.n1 = n;
+  }
+  r.turn = at;
+  r.turned = in ? n : 0;
+  return r;
+}
+
+// a[i], b[i]: the pairs in two loads.
+template <typename T, bool NEAR>
+__device__ __forceinline__ void hn_pairs(const v4u &q0, const v4u &q1, float *a, float *b) {
+  constexpr int VEC = hn_vec<T>();
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    if constexpr (NEAR) {
+      a[i] = 2 * i < VEC ? hn_value<T>(q0, (2 * i) % VEC) : hn_value<T>(q1, (2 * i) % VEC);
+      b[i] = 2 * i < VEC ? hn_value<T>(q0, (2 * i) % VEC + 1) : hn_value<T>(q1, (2 * i) % VEC + 1);
+    } else {
+      a[i] = hn_value<T>(q0, i);
+      b[i] = hn_value<T>(q1, i);
+    }
+  }
+}
+template <typename T, bool NEAR>
+__device__ __forceinline__ void hn_put(T *row, const HnUnit &u, const float *a, const float *b) {
+  constexpr int VEC = hn_vec<T>();
+  if constexpr (NEAR) {
+    float v[2 * VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      v[2 * i] = a[i];
+      v[2 * i + 1] = b[i];
+    }
+    hn_store<T>(row + u.c0, u.n0, v);
+    hn_store<T>(row + u.c1, u.n1, v + VEC);
+  } else {
+    hn_store<T>(row + u.c0, u.n0, a);
+    hn_store<T>(row + u.c1, u.n1, b);
+  }
+}
+template <int VEC, bool NEAR>
+__device__ __forceinline__ void hn_weights(const float *w, const HnUnit &u, float *a, float *b) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const int ia = NEAR ? 2 * i : i, ib = NEAR ? 2 * i + 1 : i;
+    const int nb = NEAR ? u.n0 + u.n1 : u.n1, cb = NEAR ? u.c0 : u.c1, na = NEAR ? nb : u.n0;
+    a[i] = w && ia < na ? w[u.c0 + ia] : 1.f;
+    b[i] = w && ib < nb ? w[cb + ib] : 1.f;
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void hn_angles(const HnParams &p, const HnUnit &u, int64_t token, float *c, float *s) {
+  const double pos = p.pos ? (double)p.pos[token] : (double)token;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    c[i] = 1.f;
+    s[i] = 0.f;
+    if (i < u.turned) {
+      double t = pos * p.freq[u.turn + i] * 0.31830988618379067154;   // 1 / pi: half turns
+      t -= 2.0 * rint(0.5 * t);
+      sincospif((float)t, &s[i], &c[i]);
+    }
+  }
+}
+
+template <typename T, int LANES, int UNITS, bool NEAR>
+__global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
+  constexpr int VEC = hn_vec<T>(), SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1;
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x % 64 / LANES;
+  const int64_t task = (int64_t)blockIdx.x * HN_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (task >= p.tasks) return;
+  const int64_t token = task / p.split;
+  HnUnit un[UNITS];
+  float co[UNITS][VEC], si[UNITS][VEC];
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    un[u] = hn_unit<VEC, NEAR>(p, u * LANES + lane);
+    hn_angles<VEC>(p, un[u], token, co[u], si[u]);
+  }
+  const float inv = 1.f / (float)p.dim;
+  int part = (int)(task - token * p.split);
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {
+    const HnSide &d = p.side[k];
+    if (part >= d.chunks) {
+      part -= d.chunks;
+      continue;
+    }
+    float wa[UNITS][VEC], wb[UNITS][VEC];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) hn_weights<VEC, NEAR>(d.w, un[u], wa[u], wb[u]);
+    const T *x = static_cast<const T *>(d.x) + token * d.xt;
+    T *y = static_cast<T *>(d.out) + token * d.ot;
+#pragma unroll 1
+    for (; part < d.chunks; part += p.split) {
+      v4u q[IT][UNITS][2];
+      const int h0 = part * IT * SLOTS + slot;
+#pragma unroll
+      for (int j = 0; j < IT; ++j) {
+        const T *row = x + (int64_t)min(h0 + j * SLOTS, d.heads - 1) * d.xh;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          q[j][u][0] = hn_load<T>(row + un[u].c0, un[u].n0);
+          q[j][u][1] = hn_load<T>(row + un[u].c1, un[u].n1);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < IT; ++j) {
+        float a[UNITS][VEC], b[UNITS][VEC], sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          hn_pairs<T, NEAR>(q[j][u][0], q[j][u][1], a[u], b[u]);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
+        }
+        const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
+        const int h = h0 + j * SLOTS;
+        if (h >= d.heads) continue;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          float ya[VEC], yb[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float ha = a[u][i] * r * wa[u][i], hb = b[u][i] * r * wb[u][i];
+            ya[i] = ha * co[u][i] - hb * si[u][i];
+            yb[i] = hb * co[u][i] + ha * si[u][i];
+          }
+          hn_put<T, NEAR>(y + (int64_t)h * d.oh, un[u], ya, yb);
+        }
+      }
+    }
+    part -= d.chunks;
+  }
+}
+
+// out: dx (none if null); part: the sums of g h over the workgroup's tokens (none if null).
+template <typename T, int LANES, int UNITS, bool NEAR>
+__global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
+  constexpr int VEC = hn_vec<T>(), SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1;
+  __shared__ float red[HN_WAVES][LANES * UNITS * VEC * 4];
+  const int lane = threadIdx.x % LANES, slot = threadIdx.x % 64 / LANES;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  HnUnit un[UNITS];
+  float dw[2][UNITS][2][VEC];
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    un[u] = hn_unit<VEC, NEAR>(p, u * LANES + lane);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) dw[0][u][0][i] = dw[0][u][1][i] = dw[1][u][0][i] = dw[1][u][1][i] = 0.f;
+  }
+  const float inv = 1.f / (float)p.dim;
+  for (int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave; task < p.tasks; task += (int64_t)gridDim.x * HN_WAVES) {
+    const int64_t token = task / p.split;
+    float co[UNITS][VEC], si[UNITS][VEC];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) hn_angles<VEC>(p, un[u], token, co[u], si[u]);
+    int part = (int)(task - token * p.split);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const HnSide &d = p.side[k];
+      const T *x = static_cast<const T *>(d.x) + token * d.xt, *dy = static_cast<const T *>(d.dy) + token * d.dt;
+      T *dx = static_cast<T *>(d.out) + token * d.ot;
+      float wa[UNITS][VEC], wb[UNITS][VEC];
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) hn_weights<VEC, NEAR>(d.w, un[u], wa[u], wb[u]);
+#pragma unroll 1
+      for (; part < d.chunks; part += p.split) {
+        v4u q[IT][UNITS][2], e[IT][UNITS][2];
+        const int h0 = part * IT * SLOTS + slot;
+#pragma unroll
+        for (int j = 0; j < IT; ++j) {
+          const int64_t h = min(h0 + j * SLOTS, d.heads - 1);
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            q[j][u][0] = hn_load<T>(x + h * d.xh + un[u].c0, un[u].n0);
+            q[j][u][1] = hn_load<T>(x + h * d.xh + un[u].c1, un[u].n1);
+            e[j][u][0] = hn_load<T>(dy + h * d.dh + un[u].c0, un[u].n0);
+            e[j][u][1] = hn_load<T>(dy + h * d.dh + un[u].c1, un[u].n1);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < IT; ++j) {
+          const int h = h0 + j * SLOTS;
+          float a[UNITS][VEC], b[UNITS][VEC], ga[UNITS][VEC], gb[UNITS][VEC], sum = 0.f, dot = 0.f;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            hn_pairs<T, NEAR>(q[j][u][0], q[j][u][1], a[u], b[u]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
+          }
+          const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
+          const bool live = h < d.heads;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+            float ea[VEC], eb[VEC];
+            hn_pairs<T, NEAR>(e[j][u][0], e[j][u][1], ea, eb);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+              a[u][i] *= r;
+              b[u][i] *= r;
+              const float ta = ea[i] * co[u][i] + eb[i] * si[u][i], tb = eb[i] * co[u][i] - ea[i] * si[u][i];
+              if (live) {
+                dw[k][u][0][i] = fmaf(ta, a[u][i], dw[k][u][0][i]);
+                dw[k][u][1][i] = fmaf(tb, b[u][i], dw[k][u][1][i]);
+              }
+              ga[u][i] = ta * wa[u][i];
+              gb[u][i] = tb * wb[u][i];
+              dot = fmaf(ga[u][i], a[u][i], fmaf(gb[u][i], b[u][i], dot));
+            }
+          }
+          dot = lane_sum<LANES>(dot) * inv;
+          if (!live || !d.out) continue;
+#pragma unroll
+          for (int u = 0; u < UNITS; ++u) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+              ga[u][i] = r * (ga[u][i] - a[u][i] * dot);
+              gb[u][i] = r * (gb[u][i] - b[u][i] * dot);
+            }
+            hn_put<T, NEAR>(dx + (int64_t)h * d.oh, un[u], ga[u], gb[u]);
+          }
+        }
+      }
+      part -= d.chunks;
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int ab = 0; ab < 2; ++ab)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          float v = dw[k][u][ab][i];
+#pragma unroll
+          for (int m = LANES; m < 64; m <<= 1) v += __shfl_xor(v, m);
+          if (slot == 0) red[wave][((k * UNITS + u) * 2 + ab) * VEC * LANES + i * LANES + lane] = v;
+        }
+  __syncthreads();
+  if (wave != 0 || slot != 0) return;
+  float *part = p.part + (int64_t)blockIdx.x * 2 * p.dim;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int ab = 0; ab < 2; ++ab)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const int at = NEAR ? 2 * i + ab : i, n = NEAR ? un[u].n0 + un[u].n1 : un[u].n0;
+          if (at >= n) continue;
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < HN_WAVES; ++w) v += red[w][((k * UNITS + u) * 2 + ab) * VEC * LANES + i * LANES + lane];
+          part[k * p.dim + (!NEAR && ab ? un[u].c1 : un[u].c0) + at] = v;
+        }
+}
+
+// The sums of the workgroups' rows, 32 columns of the queries' and keys' weights at a time.
+__global__ __launch_bounds__(HN_FIN) void head_norm_finish(const float *part, int blocks, int dim, float *dq, float *dk) {
+  constexpr int C = HN_FIN_COLS, S = HN_FIN / C;
+  __shared__ float red[HN_FIN];
+  const int at = blockIdx.x * C + threadIdx.x % C, s = threadIdx.x / C;
+  float v = 0.f;
+  if (at < 2 * dim)
+    for (int b = s; b < blocks; b += S) v += part[(int64_t)b * 2 * dim + at];
+  red[threadIdx.x] = v;
+  __syncthreads();
+  if (s != 0 || at >= 2 * dim) return;
+#pragma unroll
+  for (int k = 1; k < S; ++k) v += red[k * C + threadIdx.x];
+  if (at < dim && dq) dq[at] = v;
+  if (at >= dim && dk) dk[at - dim] = v;
+}
+
+struct HnShape {
+  int lanes, units;
+};
+HnShape hn_shape(int64_t dim, int64_t rot, int vec) {
+  const int64_t half = rot / 2, rest = (dim - rot) / 2, n = (half + vec - 1) / vec + (rest + vec - 1) / vec;
+  return {n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2};
+}
+int64_t hn_blocks_bwd(int64_t tasks) { return std::min((tasks + HN_WAVES - 1) / HN_WAVES, HN_BLOCKS_BWD); }
+
+HnParams hn_params(const HeadNormDesc &d, const HnShape &sh) {
+  HnParams p{};
+  p.tokens = d.tokens; p.dim = (int)d.dim; p.rot = (int)d.rotary; p.eps = d.eps;
+  p.pos = d.positions; p.freq = d.frequencies;
+  const int each = 64 / sh.lanes * (sh.units == 1 ? 2 : 1);
+  for (int k = 0; k < 2; ++k) {
+    const HeadNormSide &a = d.side[k];
+    HnSide &b = p.side[k];
+    b.x = a.x; b.dy = a.dy; b.out = a.out; b.w = a.weight;
+    b.heads = (int)a.heads; b.chunks = (int)((a.heads + each - 1) / each);
+    b.xt = a.x_token; b.xh = a.x_head; b.dt = a.dy_token; b.dh = a.dy_head; b.ot = a.out_token; b.oh = a.out_head;
+  }
+  const int64_t chunks = p.side[0].chunks + p.side[1].chunks;
+  p.split = (int)std::max<int64_t>(1, std::min(chunks, HN_FEW / std::max<int64_t>(d.tokens, 1)));
+  p.tasks = chunks ? d.tokens * p.split : 0;
+  return p;
+}
+
+template <bool BWD, typename T, bool NEAR>
+hipError_t hn_launch(const HnParams &p, const HnShape &sh, hipStream_t s) {
+  const int64_t blocks = BWD ? hn_blocks_bwd(p.tasks) : (p.tasks + HN_WAVES - 1) / HN_WAVES;
+#define SOAP_HN(L, U)                                                                                         \
+  if (sh.lanes == L && sh.units == U) {                                                                       \
+    if constexpr (BWD) hipLaunchKernelGGL((head_norm_bwd<T, L, U, NEAR>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
+    else hipLaunchKernelGGL((head_norm_fwd<T, L, U, NEAR>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
+    return hipGetLastError();                                                                                 \
+  }
+  SOAP_HN(8, 1) SOAP_HN(16, 1) SOAP_HN(32, 1) SOAP_HN(64, 1)
+  if constexpr (sizeof(T) == 4) { SOAP_HN(64, 2) }
+#undef SOAP_HN
+  return hipErrorInvalidValue;
+}
+
+template <bool BWD>
+hipError_t hn_start(const HeadNormDesc &d, const HnParams &p, const HnShape &sh, hipStream_t s) {
+  if (!p.tasks) return hipSuccess;
+  if (d.bf16) return d.near ? hn_launch<BWD, uint16_t, true>(p, sh, s) : hn_launch<BWD, uint16_t, false>(p, sh, s);
+  return d.near ? hn_launch<BWD, float, true>(p, sh, s) : hn_launch<BWD, float, false>(p, sh, s);
+}
+
+}  // namespace
+
+// Rows of partial sums as many as a backward pass has workgroups at most.
+size_t head_norm_part_bytes(int64_t tokens, int64_t dim) {
+  return tokens ? sizeof(float) * 2 * dim * HN_BLOCKS_BWD : 0;
+}
+
+hipError_t launch_head_norm_fwd(const HeadNormDesc &d, hipStream_t s) {
+  const HnShape sh = hn_shape(d.dim, d.rotary, d.bf16 ? 8 : 4);
+  return hn_start<false>(d, hn_params(d, sh), sh, s);
+}
+
+hipError_t launch_head_norm_bwd(const HeadNormDesc &d, hipStream_t s) {
+  const HnShape sh = hn_shape(d.dim, d.rotary, d.bf16 ? 8 : 4);
+  HnParams p = hn_params(d, sh);
+  const bool sums = d.side[0].dweight || d.side[1].dweight;
+  p.part = sums ? d.part : nullptr;
+  const hipError_t e = hn_start<true>(d, p, sh, s);
+  if (e != hipSuccess || !sums) return e;
+  hipLaunchKernelGGL(head_norm_finish, dim3((unsigned)((2 * d.dim + HN_FIN_COLS - 1) / HN_FIN_COLS)), dim3(HN_FIN), 0, s,
+                     p.part, p.tasks ? (int)hn_blocks_bwd(p.tasks) : 0, p.dim, d.side[0].dweight, d.side[1].dweight);
+  return hipGetLastError();
+}
+
+}  // namespace soap

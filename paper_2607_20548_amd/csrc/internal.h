@@ -293,6 +293,63 @@ struct Mx4GemmDesc {
 };
 hipError_t launch_mx4_gemm(const Mx4GemmDesc &d, hipStream_t s);
 
+// ------------------------------------------------- heads' norm and rotation
+// One of queries and keys: strides of tokens and heads in elements; weight, dweight and (backward)
+// out may be null, heads 0.
+struct HeadNormSide {
+  int64_t heads = 0;
+  const void *x = nullptr, *dy = nullptr;
+  void *out = nullptr;               // y or dx
+  const float *weight = nullptr;
+  float *dweight = nullptr;
+  int64_t x_token = 0, x_head = 0, dy_token = 0, dy_head = 0, out_token = 0, out_head = 0;
+};
+struct HeadNormDesc {
+  int64_t tokens = 0, dim = 0, rotary = 0;
+  bool bf16 = false, near = false;   // near: neighbours are pairs
+  HeadNormSide side[2];              // queries, keys
+  float eps = 0.f;
+  const int *positions = nullptr;    // null: the token's index
+  const double *frequencies = nullptr;
+  float *part = nullptr;
+};
+size_t head_norm_part_bytes(int64_t tokens, int64_t dim);
+hipError_t launch_head_norm_fwd(const HeadNormDesc &d, hipStream_t s);
+hipError_t launch_head_norm_bwd(const HeadNormDesc &d, hipStream_t s);
+
+// ----------------------------------------------------------- distillation
+constexpr int DISTILL_MAX_CLASSES = 1 << 18, DISTILL_MAX_SLOTS = 512;
+// With loss: loss and stats (may be null); with dlogits too: the gradient as well; with dlogits
+// alone: the gradient from stats.
+struct DistillDesc {
+  int64_t rows = 0, classes = 0, slots = 0, ld = 0, ldi = 0, ldt = 0, ldd = 0;
+  bool bf16 = false, teacher_bf16 = false, tail = false;
+  float tau = 1.f;
+  const void *logits = nullptr, *teacher = nullptr;
+  const int *index = nullptr;
+  const float *dloss = nullptr;
+  float *loss = nullptr, *stats = nullptr;
+  void *dlogits = nullptr;
+};
+hipError_t launch_distill(const DistillDesc &d, hipStream_t s);
+
+// ------------------------------------------------- gated feed-forward block
+// bfloat16 throughout but for the weights' gradients (grad_bf16: these too); gate and up are
+// both or none kept forward, and read backward; gradients that are not wanted are null.
+struct GatedDesc {
+  int64_t tokens = 0, m = 0, n = 0, p = 0, ldx = 0, ldy = 0, lddy = 0, lddx = 0;
+  int act = 0;
+  bool grad_bf16 = false;
+  const uint16_t *x = nullptr, *w_gate = nullptr, *w_up = nullptr, *w_down = nullptr, *dy = nullptr;
+  uint16_t *gate = nullptr, *up = nullptr;
+  uint16_t *y = nullptr, *dx = nullptr;
+  void *dw_gate = nullptr, *dw_up = nullptr, *dw_down = nullptr;
+  void *workspace = nullptr;
+};
+size_t gated_workspace_bytes(int64_t tokens, int64_t n, bool backward);
+hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s);
+hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s);
+
 // ------------------------------------------------- errors of the C ABI
 // The calling thread's error string (soap_last_error) and status.
 int api_fail(int code, const char *fmt, ...);

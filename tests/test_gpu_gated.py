@@ -1,0 +1,209 @@
+"""The gated feed-forward block on the GPU against the formulas in float64.
+
+Tolerances, from the arithmetic (u = 2^-24): a product's sum of k terms in fp32 is within (k + 8) u
+of the sum of their absolute values; bfloat16 results are within 2^-8 of themselves (half a
+step at a power of two) on top.  H = act(G) U carries its factors' errors (|act'| <= 1.13) and
+32 u (1 + |G|) for the activation, and is rounded, as dG and dU are, before the next product, which
+adds their errors times its other operand's absolute values."""
+import pytest
+import torch
+
+import paper_2607_20548_amd as soap
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+H = 2.0 ** -8
+BF = torch.bfloat16
+
+
+def randn(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+def act(x, name):
+    if name == "silu":
+        s = torch.sigmoid(x)
+        return x * s, s * (1 + x * (1 - s))
+    c = torch.special.ndtr(x)
+    return x * c, c + x * torch.exp(-0.5 * x * x) * 0.3989422804014327
+
+
+def product(a, b, ea=0.0, eb=0.0):
+    """a b and its bound, for operands with errors of ea and eb."""
+    size = a.abs() @ b.abs()
+    return a @ b, (a.shape[1] + 8) * U * size + (ea @ b.abs() if torch.is_tensor(ea) else 0) + (a.abs() @ eb if torch.is_tensor(eb) else 0)
+
+
+def within(got, want, bound, what):
+    if got.dtype == BF:
+        bound = bound + H * (want.abs() + bound)
+    else:
+        bound = bound + 2 * U * want.abs()
+    bad = ~((got.double() - want).abs() <= bound + 1e-37)
+    assert not bad.any(), (what, int(bad.sum()), bad.nonzero()[:3].tolist(), (got.double() - want).abs().max().item())
+
+
+def make(T, m, n, p, seed, scale=1.0):
+    x = (scale * randn(seed, T, m)).to(BF)
+    return (x, (m ** -0.5 * randn(seed + 1, m, n)).to(BF), (m ** -0.5 * randn(seed + 2, m, n)).to(BF),
+            (n ** -0.5 * randn(seed + 3, n, p)).to(BF), (0.01 * randn(seed + 4, T, p)).to(BF))
+
+
+def check(x, wg, wu, wd, dy, name="silu", dtype=torch.float32):
+    block = soap.GatedFeedForward(wg, wu, wd, activation=name)
+    y, gate, up = block.forward(x)
+    alone, none, _ = block.forward(x, keep=False)
+    assert none is None and torch.equal(alone, y)
+    X, G, V, D, Y = (t.double() for t in (x, wg, wu, wd, dy))
+    g, eg = product(X, G)
+    u, eu = product(X, V)
+    within(gate, g, eg, "gate")
+    within(up, u, eu, "up")
+    a, _ = act(g, name)
+    h = a * u
+    eh = 1.13 * eg * u.abs() + a.abs() * eu + 32 * U * (1 + g.abs()) * u.abs()
+    eh = eh + H * (h.abs() + eh)
+    want, bound = product(h, D, eh)
+    within(y, want, bound, "y")
+
+    dx, dwg, dwu, dwd = block.backward(dy, x, gate, up, dtype=dtype)
+    assert dwg.dtype is (dtype or torch.float32)
+    g, u = gate.double(), up.double()
+    a, da = act(g, name)
+    slope = 32 * U * (1 + g.abs())
+    dh, edh = product(Y, D.T)
+    h = a * u
+    eh = slope * u.abs()
+    eh = eh + H * (h.abs() + eh)
+    dg, edg = dh * u * da, u.abs() * (edh * 1.13 + dh.abs() * slope)
+    edg = edg + H * (dg.abs() + edg)
+    du, edu = dh * a, a.abs() * edh + dh.abs() * slope
+    edu = edu + H * (du.abs() + edu)
+    one, e1 = product(dg, G.T, edg)
+    two, e2 = product(du, V.T, edu)
+    within(dx, one + two, 2 * (e1 + e2), "dx")
+    within(dwg, *product(X.T, dg, 0.0, edg), "dw_gate")
+    within(dwu, *product(X.T, du, 0.0, edu), "dw_up")
+    within(dwd, *product(h.T, Y, eh.T.contiguous()), "dw_down")
+
+
+@pytest.mark.parametrize("T,m,n,p", [
+    (1, 8, 8, 8), (1, 64, 128, 64), (2, 2048, 512, 1024), (5, 136, 200, 72), (16, 512, 1024, 512), (17, 1000, 264, 328),
+    (33, 256, 136, 264), (64, 512, 640, 512), (65, 72, 1032, 520), (127, 256, 256, 128), (130, 128, 384, 136),
+    (300, 520, 776, 264), (777, 392, 520, 648), (1025, 256, 512, 256)])
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_sizes(T, m, n, p, name):
+    check(*make(T, m, n, p, T + m), name, torch.float32 if name == "silu" else BF)
+
+
+def test_large():
+    check(*make(2100, 1032, 2056, 1032, 3))
+
+
+def test_views():
+    """Rows of x and dy cut out of wider ones, whose other values are no numbers."""
+    x, wg, wu, wd, dy = make(70, 136, 264, 72, 5)
+    for cut in (8, 24):
+        wx, wy = (torch.full((70, t.shape[1] + 2 * cut), float("nan"), device="cuda", dtype=BF) for t in (x, dy))
+        wx[:, cut:-cut], wy[:, cut:-cut] = x, dy
+        check(wx[:, cut:-cut], wg, wu, wd, wy[:, cut:-cut])
+
+
+def test_activations_far_out():
+    """Gates of hundreds either way, where exp over- and underflows."""
+    check(*make(40, 64, 64, 64, 6, scale=200.0), "silu")
+    check(*make(40, 64, 64, 64, 6, scale=200.0), "gelu")
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
+def test_tokens_stay_apart(T):
+    """A token that is no number changes no other token's results."""
+    x, wg, wu, wd, dy = make(T, 200, 328, 264, 7)
+    block = soap.GatedFeedForward(wg, wu, wd)
+    y, gate, up = block.forward(x)
+    dx = block.backward(dy, x, gate, up)[0]
+    bad, dbad = x.clone(), dy.clone()
+    bad[1] = float("nan")
+    dbad[1] = float("inf")
+    y2, gate2, up2 = block.forward(bad)
+    dx2 = block.backward(dbad, bad, gate2, up2)[0]
+    keep = torch.arange(T, device="cuda") != 1
+    assert torch.equal(y2[keep], y[keep]) and torch.equal(dx2[keep], dx[keep])
+    assert y2[1].isnan().all()
+
+
+def test_gradient_against_differences():
+    """<gradient, v> of small weights against the difference quotient of the loss in float64: the
+    kernel's gradients are within their bfloat16 operands' 3 * 2^-8 of the terms' sizes, the quotient
+    within h^2 of the third derivative."""
+    x, wg, wu, wd, dy = make(6, 16, 24, 16, 8)
+    block = soap.GatedFeedForward(wg, wu, wd)
+    _, gate, up = block.forward(x)
+    grads = block.backward(dy, x, gate, up)
+    leaves = [t.double() for t in (x, wg, wu, wd)]
+
+    def loss(x, wg, wu, wd):
+        return ((act(x @ wg, "silu")[0] * (x @ wu)) @ wd * dy.double()).sum()
+
+    for i, got in enumerate(grads):
+        v, h = randn(20 + i, *leaves[i].shape).double(), 1e-4
+        hi, lo = list(leaves), list(leaves)
+        hi[i], lo[i] = leaves[i] + h * v, leaves[i] - h * v
+        want = (loss(*hi) - loss(*lo)) / (2 * h)
+        size = (got.double().abs() * v.abs()).sum() + 0.01 * dy.double().abs().sum()
+        assert abs((got.double() * v).sum() - want) <= 4 * H * size
+
+
+def test_no_tokens():
+    x, wg, wu, wd, dy = make(4, 64, 72, 80, 9)
+    block = soap.GatedFeedForward(wg, wu, wd)
+    y, gate, up = block.forward(x[:0])
+    assert y.shape == (0, 80) and gate.shape == (0, 72)
+    dx, *dw = block.backward(dy[:0], x[:0], gate, up)
+    assert dx.shape == (0, 64) and not any(w.any() for w in dw)
+
+
+def test_gradients_that_are_not_wanted():
+    """The C entry point with single gradients, into a wider dx."""
+    T, m, n, p = 50, 64, 136, 72
+    x, wg, wu, wd, dy = make(T, m, n, p, 10)
+    block = soap.GatedFeedForward(wg, wu, wd)
+    _, gate, up = block.forward(x)
+    want = block.backward(dy, x, gate, up)
+    need = soap.soap_gated_workspace_bytes(T, m, n, p, True)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for i in range(4):
+        out = torch.full((T, m + 16), 7.0, device="cuda", dtype=BF) if i == 0 else torch.full_like(want[i], 7.0)
+        dst = [None] * 4
+        dst[i] = out[:, 8:] if i == 0 else out
+        soap.soap_gated_backward(T, m, n, p, 0, dy, p, x, m, wg, wu, wd, gate, up, dst[0], m + 16, soap.SOAP_F32, *dst[1:],
+                                 work, need)
+        assert torch.equal(out[:, 8:-8] if i == 0 else out, want[i])
+        if i == 0:
+            assert (out[:, :8] == 7).all() and (out[:, -8:] == 7).all()
+
+
+@pytest.mark.parametrize("T", [1, 20, 200])
+def test_stream_graph_and_bits(T):
+    x, wg, wu, wd, dy = make(T, 256, 520, 264, 11)
+    block = soap.GatedFeedForward(wg, wu, wd)
+
+    def run(**kw):
+        y, gate, up = block.forward(x, **kw)
+        return (y, gate, up, *block.backward(dy, x, gate, up, **kw))
+
+    want = run()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = run(stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    for i in range(4):
+        x.copy_(randn(30 + i, T, 256))
+        graph.replay()
+        want = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out)), i
