@@ -25,6 +25,7 @@
 #include "internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace soap {
 namespace {
@@ -35,9 +36,10 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) v4s lds_v4s;
-typedef __attribute__((address_space(3))) void lds_void;
+typedef int v4i __attribute__((ext_vector_type(4)));
 
 constexpr int GP_THREADS = 256, GP_KB = 64;      // four waves; k of a slab
+constexpr int GP_RING = 5;                       // operands' slabs in LDS
 constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows in LDS
 constexpr int GP_RSRC = 0x00020000;              // raw 32-bit data
 
@@ -54,45 +56,77 @@ struct GpParams {
   // gated: C[0] the product, kept G and U (or null); dgated: C[0] = dG, C[1] = dU, H
   const uint16_t *gate, *up;
   uint16_t *keep_gate, *keep_up, *hidden;
-  int act;
 };
 
 __device__ __forceinline__ uint16_t gp_round(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 __device__ __forceinline__ float gp_float(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
 
-// The activation and, for the gradient, its derivative.
-__device__ __forceinline__ float gp_act(float x, int act) {
-  if (act == SOAP_ACT_SILU) return x / (1.f + expf(-x));
-  return 0.5f * x * (1.f + erff(x * 0.70710678118654752440f));
-}
-__device__ __forceinline__ float gp_dact(float x, int act) {
-  if (act == SOAP_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-x));
-    return s * (1.f + x * (1.f - s));
+// The activation, and its derivative.  The hardware's exponential and reciprocal are within an
+// fp32 step each, far inside the rounding to bfloat16 that follows.
+struct GpAct {
+  float a, d;
+};
+template <int ACT>
+__device__ __forceinline__ GpAct gp_act(float x) {
+  GpAct r;
+  if constexpr (ACT == SOAP_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896340736f));
+    r.a = x * s;
+    r.d = fmaf(r.a, 1.f - s, s);
+  } else {
+    const float c = 0.5f + 0.5f * erff(x * 0.70710678118654752440f);
+    r.a = x * c;
+    r.d = fmaf(x * 0.39894228040143267794f, __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f), c);
   }
-  return 0.5f * (1.f + erff(x * 0.70710678118654752440f)) + x * 0.39894228040143267794f * expf(-0.5f * x * x);
+  return r;
 }
+__device__ __forceinline__ uint32_t gp_pack(float a, float b) { return gp_round(a) | (uint32_t)gp_round(b) << 16; }
 
-// What one operand's blocks of a slab are loaded from: rows of its matrix from the tile's
-// first on, `left` bytes to the matrix' end.
+// What one operand's blocks of a slab are loaded from: the tile's first row of its matrix, or of
+// the slab's k, and the bytes from there to the matrix' end.
 struct GpSource {
   const char *base;
-  int64_t left;
+  int64_t left, step;          // step: to the next slab
+  __device__ __forceinline__ void start(const uint16_t *q, bool kc, int x0, int X, int K, int64_t ld2) {
+    base = (const char *)q + (kc ? x0 * ld2 : 2 * (int64_t)x0);
+    left = kc ? (X - x0 - 1) * ld2 + 2 * (int64_t)K : (K - 1) * ld2 + 2 * (int64_t)(X - x0);
+    step = kc ? 2 * GP_KB : GP_KB * ld2;
+  }
+  __device__ __forceinline__ void next() {
+    base += step;
+    left -= step;
+  }
+  // Offsets stay below 2^31 (rows of a tile are at most 256, of 2^22 bytes).
+  __device__ __forceinline__ v4i buffer() const {
+    const int hi = (int)(left >> 32);
+    const uint32_t lo = (uint32_t)left;
+    const uint32_t n = hi < 0 ? 0u : hi > 0 || lo > 0x7fffffffu ? 0x7fffffffu : lo;
+    const uint64_t a = reinterpret_cast<uint64_t>(base);
+    v4i r = {(int)(uint32_t)a, (int)(uint32_t)(a >> 32) & 0xffff, (int)n, GP_RSRC};
+    // five wait states between a vector instruction that may have written it and the loads
+    asm volatile("s_nop 4" : "+s"(r));
+    return r;
+  }
 };
-__device__ __forceinline__ void gp_load(const GpSource &s, uint8_t *lds, uint32_t offset) {
-  const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(s.base), (short)0,
-                                                   (int)(uint32_t)min(max(s.left, (int64_t)0), (int64_t)0xfffffff0), GP_RSRC);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)lds, 16, (int)offset, 0, 0, 0);
+constexpr uint32_t GP_OUT = 0x80000000u;         // in an offset: past every buffer's end
+
+// 16 bytes a lane from `offset` of a buffer to LDS at `lds` + 16 lane.  Written out because the
+// compiler holds every transposing read until all such loads have arrived; the kernel waits for
+// them itself, before the barrier in front of their slab's first read.  They write no register.
+__device__ __forceinline__ void gp_load(const v4i &buffer, uint32_t lds, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer)
+               : "m0");
 }
 
-// NB: blocks of 32 x 32 on a side of a wave's share; tiles of 64 NB.
-template <bool AK, bool BK, int EPI, int NB>
+// NB: blocks of 32 x 32 on a side of a wave's share; tiles of 64 NB.  ACT: of the epilogues
+// with an activation.
+template <bool AK, bool BK, int EPI, int NB, int ACT>
 __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpParams p) {
   constexpr int TB = 64 * NB, SUB = TB / 64, OP = SUB * GP_BLOCK, LOADS = 2 * SUB;
   constexpr int SLD = TB + 4;                    // staging row of the epilogue, floats
   constexpr int BAND = 64;
-  static_assert(BAND * SLD * 4 <= 4 * OP, "the epilogue's band fits the slabs");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * OP];
+  static_assert(BAND * SLD * 4 <= GP_RING * OP, "the epilogue's band fits the slabs");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[GP_RING * OP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, xl = lane & 31, h = lane >> 5;
 
@@ -103,8 +137,8 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     const int t = x * q + min(x, r) + (blockIdx.x >> 3);
     const int group = t / (8 * p.tiles_n), first = 8 * group, size = min(p.tiles_m - first, 8);
     const int in = t - group * 8 * p.tiles_n;
-    tm = first + in % size;
-    tn = in / size;
+    tm = __builtin_amdgcn_readfirstlane(first + in % size);
+    tn = __builtin_amdgcn_readfirstlane(in / size);
   }
   int which = 0;
   if (p.pairs) {
@@ -118,7 +152,6 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
 
   // a wave's loads: of block j >> 3 the rows 8 (j & 7) .., j = wave + 4 i
   uint32_t offa[LOADS], offb[LOADS];
-  int ua[2], ub[2];                              // the k unit that a lane's loads begin at
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
     const int j = wave + 4 * i, s = j >> 3, row = 8 * (j & 7) + (lane >> 3);
@@ -127,34 +160,43 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     const int sb = TWO ? s >> 1 : s;
     offb[i] = BK ? (uint32_t)((64 * sb + row) * ldb2) + 16 * uk : (uint32_t)(row * ldb2) + 128 * sb + 16 * ux;
   }
-  ua[0] = ub[0] = (lane & 7) ^ ((8 * (wave & 7) + (lane >> 3)) >> 1 & 7);
-  ua[1] = ub[1] = ua[0];                         // rows 32 apart permute alike
+  // the unit of eight k that a lane loads, the same in all its rows
+  const int unit = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);
+  const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
   const int nk1 = (p.K + GP_KB - 1) / GP_KB, nk = nk1 * p.segments;
 
-  auto load = [&](int kt) {
-    const int seg = kt >= nk1, k0 = (kt - seg * nk1) * GP_KB;
-    uint8_t *la = lds + (kt & 1) * 2 * OP, *lb = la + OP;
-    auto source = [&](const uint16_t *q, bool kc, int x0, int X, int64_t ld2) {
-      GpSource s;
-      if (kc) {
-        s.base = (const char *)q + x0 * ld2 + 2 * k0;
-        s.left = (X - x0 - 1) * ld2 + 2 * (p.K - k0);
-      } else {
-        s.base = (const char *)q + k0 * ld2 + 2 * x0;
-        s.left = (p.K - k0 - 1) * ld2 + 2 * (X - x0);
-      }
-      return s;
-    };
-    const GpSource a = source(p.A[seg], AK, m0, p.M, lda2);
-    const GpSource b0 = source(p.B[TWO ? 0 : p.segments > 1 ? seg : which], BK, n0, p.N, ldb2);
-    const GpSource b1 = TWO ? source(p.B[1], BK, n0, p.N, ldb2) : b0;
-    const bool dead = k0 + 8 * ua[0] >= p.K;     // a unit of k past the end
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int j = wave + 4 * i, s = j >> 3;
-      gp_load(a, la + j * 1024, AK && dead ? 0xfffffff0u : offa[i]);
-      gp_load(TWO && (s & 1) ? b1 : b0, lb + j * 1024, BK && dead ? 0xfffffff0u : offb[i]);
+  // A slab of A and one of B take a place each of a ring of five, in the order A0 B0 A1 B1 ..: what
+  // slab k frees takes B of slab k + 2, which then has a slab's time to arrive, and A of slab k + 3,
+  // which has two.
+  struct Stream {
+    GpSource s0, s1;
+    v4i r0, r1;
+    int left, slab, place;                       // of k in the segment; the next slab; its place
+    uint32_t dead, to;
+  } sa, sb;
+  sa.slab = sb.slab = sa.place = 0;
+  sb.place = 1;
+  auto begin = [&](Stream &s, bool is_a) {       // the next slab of an operand: its loads may follow
+    if (s.slab == 0 || (p.segments > 1 && s.slab == nk1)) {
+      const int seg = s.slab != 0;
+      if (is_a) s.s0.start(p.A[seg], AK, m0, p.M, p.K, lda2);
+      else s.s0.start(seg || which ? p.B[1] : p.B[0], BK, n0, p.N, p.K, ldb2);
+      if (TWO && !is_a) s.s1.start(p.B[1], BK, n0, p.N, p.K, ldb2);
+      s.left = p.K;
     }
+    s.r0 = s.s0.buffer();
+    if (TWO && !is_a) s.r1 = s.s1.buffer();
+    s.dead = 8 * unit >= s.left ? GP_OUT : 0u;   // a unit past the end of k
+    s.to = base + s.place * OP + wave * 1024;
+    s.s0.next();
+    if (TWO && !is_a) s.s1.next();
+    s.left -= GP_KB;
+    ++s.slab;
+    s.place = s.place >= 3 ? s.place - 3 : s.place + 2;
+  };
+  auto load = [&](bool is_a, int i) {
+    if (is_a) gp_load(sa.r0, sa.to + 4096 * i, AK ? offa[i] | sa.dead : offa[i]);
+    else gp_load(TWO && (i >> 1 & 1) ? sb.r1 : sb.r0, sb.to + 4096 * i, BK ? offb[i] | sb.dead : offb[i]);
   };
 
   // fragments: the 8 k from 16 q + 8 h on of row `x` (a multiple of 32, and the lane's)
@@ -171,6 +213,25 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
 
+  // The epilogue's bands of 64 rows: a thread's units of eight columns, GP_THREADS apart.
+  constexpr int UNITS = (TWO ? TB / 2 : TB) / 8, EACH = BAND * UNITS / GP_THREADS;
+  float *stage = reinterpret_cast<float *>(lds);
+  const int c = 8 * (tid % UNITS), col = n0 + c;  // GP_THREADS is a multiple of UNITS
+  auto row_of = [&](int ps, int v) {
+    const int r = (tid + GP_THREADS * v) / UNITS;
+    return m0 + (r >> 5) * 32 * NB + 32 * ps + (r & 31);
+  };
+  // G and U of two bands, loaded during the main loop, and two bands ahead from then on: before a
+  // band's stores, which they would otherwise wait for, one counter counting both
+  v4u kg[2][EPI == GP_DGATED ? EACH : 1], ku[2][EPI == GP_DGATED ? EACH : 1];
+  auto kept = [&](int set, int ps, int v) {
+    const int row = row_of(ps, v);
+    if (row >= p.M || col >= p.N) return;
+    const int64_t at = (int64_t)row * p.ldc + col;
+    kg[set][v] = *reinterpret_cast<const v4u *>(p.gate + at);
+    ku[set][v] = *reinterpret_cast<const v4u *>(p.up + at);
+  };
+
   v16f acc[NB][NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -179,115 +240,144 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  if (nk) load(0);
-  for (int kt = 0; kt < nk; ++kt) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
-    __syncthreads();
-    if (kt + 1 < nk) load(kt + 1);
-    const uint8_t *la = lds + (kt & 1) * 2 * OP, *lb = la + OP;
+  v8bf fa[2][NB], fb[2][NB];
+  const uint8_t *la = lds, *lb = lds + OP;       // the slab that is read
+  auto read = [&](int f, int q, int u) {         // the u-th of a step's 2 NB fragments
+    const int i = u >> 1;
+    if (!(u & 1)) fa[f][i] = frag(la, AK, wm * 32 * NB + 32 * i, q);
+    // gated: a wave's columns are half the gate's, in even blocks, and half up's
+    else fb[f][i] = TWO && NB == 2 ? frag(lb, BK, 64 * i + 32 * wn, q) : frag(lb, BK, wn * 32 * NB + 32 * i, q);
+  };
+  // One step's matrix instructions, on fragments f, with the reads of the next step's (of step q) and
+  // the loads l0 .. l1, of B then of A, spread among them.
+  auto step = [&](int f, int q, int l0, int l1) {
+    constexpr int MM = NB * NB, RD = 3 * MM / 4;
 #pragma unroll
-    for (int q = 0; q < GP_KB / 16; ++q) {
-      v8bf fa[NB], fb[NB];
+    for (int u = 0; u < MM; ++u) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        fa[i] = frag(la, AK, wm * 32 * NB + 32 * i, q);
-        // gated: the first half of a wave's columns are the gate's, in block 2 w, then up's in 2 w + 1
-        fb[i] = TWO && NB == 2 ? frag(lb, BK, 64 * i + 32 * wn, q) : frag(lb, BK, wn * 32 * NB + 32 * i, q);
-      }
+      for (int v = min(u, RD) * 2 * NB / RD; v < min(u + 1, RD) * 2 * NB / RD; ++v) read(f ^ 1, q, v);
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+      for (int v = l0 + u * (l1 - l0) / MM; v < l0 + (u + 1) * (l1 - l0) / MM; ++v) load(v >= LOADS, v % LOADS);
+      acc[u / NB][u % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[f][u % NB], fa[f][u / NB], acc[u / NB][u % NB], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  };
+  // All but a wave's last `flying` loads, and its reads, then all waves'.
+#define GP_ARRIVED(flying)                                                                                \
+  do {                                                                                                    \
+    __builtin_amdgcn_sched_barrier(0);                                                                    \
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(flying) : "memory"); /* LDS changed */ \
+    __builtin_amdgcn_sched_barrier(0);                                                                    \
+  } while (0)
+  // Loads are spread over the four steps from the barrier that frees their places on: the memory
+  // pipe takes 27 cycles for a wave's, all of a step's 512 for five from each of four waves, and
+  // one that it does not take yet holds its wave's matrix instructions up.
+  constexpr int L1 = 2 * LOADS * 5 / 16, L2 = 2 * LOADS * 10 / 16, L3 = 2 * LOADS * 13 / 16;
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {                  // A0, B0, A1
+    if (u & 1) begin(sb, false);
+    else begin(sa, true);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load(!(u & 1), i);
   }
-  __syncthreads();
+  begin(sb, false);
+  begin(sa, true);
+#pragma unroll
+  for (int v = 0; v < L1; ++v) load(v >= LOADS, v % LOADS);
+  if constexpr (EPI == GP_DGATED) {
+#pragma unroll
+    for (int v = 0; v < 2 * EACH; ++v) kept(v / EACH, v / EACH, v % EACH);
+  }
+  GP_ARRIVED(LOADS + L1);
+#pragma unroll
+  for (int u = 0; u < 2 * NB; ++u) read(0, 0, u);
+  int pa = 0;                                    // the place of A's slab
+  for (int kt = 0; kt < nk; ++kt) {
+    __builtin_amdgcn_sched_barrier(0);
+    step(0, 1, L1, L2);
+    step(1, 2, L2, L3);
+    step(0, 3, L3, 2 * LOADS);
+    GP_ARRIVED(LOADS);
+    begin(sb, false);
+    begin(sa, true);
+    pa = pa >= 3 ? pa - 3 : pa + 2;
+    la = lds + pa * OP;
+    lb = pa == 4 ? lds : la + OP;
+    step(1, 0, 0, L1);
+  }
+  GP_ARRIVED(0);
 
-  // Bands of 64 rows through LDS.  Accumulator register r of block (i, j) holds row
-  // 8 (r / 4) + 4 h + r % 4, column xl of it.
-  float *stage = reinterpret_cast<float *>(lds);
-  constexpr int BANDS = TB / BAND;
-#pragma unroll
-  for (int ps = 0; ps < BANDS; ++ps) {
+  // Bands of 64 rows, 32 of either half of the tile, through LDS.  B's values came first in the
+  // matrix instructions: register r of block (i, j) holds row xl of A's, column
+  // 8 (r / 4) + 4 h + r % 4 of B's, so that a lane writes four columns at once.
+#pragma unroll 1
+  for (int ps = 0; ps < NB; ++ps) {
     if (ps) __syncthreads();
-    if (wm == ps * BAND / (32 * NB)) {
+    auto put = [&](const v16f(&a)[NB]) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < NB; ++j) {
+        // columns of the gate come first, then up's: 32 NB of a wave are 16 NB of each
+        const int at = !TWO ? wn * 32 * NB + 32 * j : (j >= NB / 2 ? TB / 2 : 0) + wn * 16 * NB + 32 * (j % (NB / 2));
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            // columns of the gate come first, then up's: 32 NB of a wave are 16 NB of each
-            const int col = !TWO ? wn * 32 * NB + 32 * j
-                                 : (j >= NB / 2 ? TB / 2 : 0) + wn * 16 * NB + 32 * (j % (NB / 2 ? NB / 2 : 1));
-            stage[(32 * i + 8 * (r >> 2) + 4 * h + (r & 3)) * SLD + col + xl] = acc[(2 * ps) % NB + i][j][r];
-          }
-    }
-    __syncthreads();
-    const int row0 = m0 + BAND * ps;
-    if constexpr (EPI == GP_GATED) {
-      constexpr int UNITS = TB / 2 / 8;          // of eight columns
-#pragma unroll
-      for (int v = tid; v < BAND * UNITS; v += GP_THREADS) {
-        const int r = v / UNITS, c = 8 * (v % UNITS), row = row0 + r, col = n0 + c;
-        if (row >= p.M || col >= p.N) continue;
-        v4u og, ou, oh;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint16_t g[2], u[2], o[2];
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            const float x = stage[r * SLD + c + 2 * e + w], y = stage[r * SLD + TB / 2 + c + 2 * e + w];
-            g[w] = gp_round(x);
-            u[w] = gp_round(y);
-            o[w] = gp_round(gp_act(x, p.act) * y);
-          }
-          og[e] = g[0] | (uint32_t)g[1] << 16;
-          ou[e] = u[0] | (uint32_t)u[1] << 16;
-          oh[e] = o[0] | (uint32_t)o[1] << 16;
-        }
-        const int64_t at = (int64_t)row * p.ldc + col;
-        *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[0]) + at) = oh;
-        if (p.keep_gate) {
-          *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
-          *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
-        }
+        for (int r = 0; r < 16; r += 4)
+          *reinterpret_cast<float4 *>(stage + (32 * wm + xl) * SLD + at + 2 * r + 4 * h) =
+              make_float4(a[j][r], a[j][r + 1], a[j][r + 2], a[j][r + 3]);
       }
-    } else {
-      constexpr int UNITS = TB / 8;
+    };
+    if (ps == 0) put(acc[0]);
+    else if (ps == 1) put(acc[1]);
+    else if (ps == 2) put(acc[NB - 2]);
+    else put(acc[NB - 1]);
+    __syncthreads();
 #pragma unroll
-      for (int v = tid; v < BAND * UNITS; v += GP_THREADS) {
-        const int r = v / UNITS, c = 8 * (v % UNITS), row = row0 + r, col = n0 + c;
-        if (row >= p.M || col >= p.N) continue;
-        const float *x = stage + r * SLD + c;
+    for (int v = 0; v < EACH; ++v) {
+      const int row = row_of(ps, v);
+      if (row < p.M && col < p.N) {
+        const float *x = stage + (tid + GP_THREADS * v) / UNITS * SLD + c;
         const int64_t at = (int64_t)row * p.ldc + col;
-        if constexpr (EPI == GP_F32) {
+        if constexpr (EPI == GP_GATED) {
+          v4u og, ou, oh;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float g0 = x[2 * e], g1 = x[2 * e + 1], u0 = x[TB / 2 + 2 * e], u1 = x[TB / 2 + 2 * e + 1];
+            og[e] = gp_pack(g0, g1);
+            ou[e] = gp_pack(u0, u1);
+            oh[e] = gp_pack(gp_act<ACT>(g0).a * u0, gp_act<ACT>(g1).a * u1);
+          }
+          *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[0]) + at) = oh;
+          if (p.keep_gate) {
+            *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
+            *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
+          }
+        } else if constexpr (EPI == GP_F32) {
           float *o = static_cast<float *>(p.C[which]) + at;
           *reinterpret_cast<float4 *>(o) = make_float4(x[0], x[1], x[2], x[3]);
           *reinterpret_cast<float4 *>(o + 4) = make_float4(x[4], x[5], x[6], x[7]);
         } else if constexpr (EPI == GP_BF16) {
           v4u o;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = gp_round(x[2 * e]) | (uint32_t)gp_round(x[2 * e + 1]) << 16;
+          for (int e = 0; e < 4; ++e) o[e] = gp_pack(x[2 * e], x[2 * e + 1]);
           *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[which]) + at) = o;
         } else {
-          const v4u g = *reinterpret_cast<const v4u *>(p.gate + at), u = *reinterpret_cast<const v4u *>(p.up + at);
           v4u og, ou, oh;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            uint16_t a[2], b[2], o[2];
+            float a[2], b[2], o[2];
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              const float gv = gp_float((uint16_t)(g[e] >> 16 * w)), uv = gp_float((uint16_t)(u[e] >> 16 * w));
-              const float d = x[2 * e + w], f = gp_act(gv, p.act);
-              a[w] = gp_round(d * uv * gp_dact(gv, p.act));
-              b[w] = gp_round(d * f);
-              o[w] = gp_round(f * uv);
+              const float u = gp_float((uint16_t)(ku[0][v][e] >> 16 * w)), d = x[2 * e + w];
+              const GpAct f = gp_act<ACT>(gp_float((uint16_t)(kg[0][v][e] >> 16 * w)));
+              a[w] = d * u * f.d;
+              b[w] = d * f.a;
+              o[w] = f.a * u;
             }
-            og[e] = a[0] | (uint32_t)a[1] << 16;
-            ou[e] = b[0] | (uint32_t)b[1] << 16;
-            oh[e] = o[0] | (uint32_t)o[1] << 16;
+            og[e] = gp_pack(a[0], a[1]);
+            ou[e] = gp_pack(b[0], b[1]);
+            oh[e] = gp_pack(o[0], o[1]);
           }
+          kg[0][v] = kg[1][v];
+          ku[0][v] = ku[1][v];
+          if (ps + 2 < NB) kept(1, ps + 2, v);
           *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[0]) + at) = og;
           *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[1]) + at) = ou;
           *reinterpret_cast<v4u *>(p.hidden + at) = oh;
@@ -297,15 +387,25 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   }
 }
 
-template <bool AK, bool BK, int EPI>
-hipError_t gp_launch(GpParams p, hipStream_t s) {
-  constexpr int TB = 128;
-  if (p.M <= 0 || p.N <= 0) return hipSuccess;
+template <bool AK, bool BK, int EPI, int NB, int ACT>
+hipError_t gp_tiles(GpParams p, hipStream_t s) {
+  constexpr int TB = 64 * NB;
   p.tiles_m = (p.M + TB - 1) / TB;
   const int width = EPI == GP_GATED ? TB / 2 : TB;
   p.tiles_n = (p.N + width - 1) / width * (p.pairs ? 2 : 1);
-  hipLaunchKernelGGL((product_tiles<AK, BK, EPI, 2>), dim3((unsigned)p.tiles_m * p.tiles_n), dim3(GP_THREADS), 0, s, p);
+  hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT>), dim3((unsigned)p.tiles_m * p.tiles_n), dim3(GP_THREADS), 0, s, p);
   return hipGetLastError();
+}
+
+template <bool AK, bool BK, int EPI, int ACT = SOAP_ACT_SILU>
+hipError_t gp_launch(const GpParams &p, hipStream_t s) {
+  if (p.M <= 0 || p.N <= 0) return hipSuccess;
+  const int width = EPI == GP_GATED ? 128 : 256;
+  const int64_t large = (int64_t)((p.M + 255) / 256) * ((p.N + width - 1) / width) * (p.pairs ? 2 : 1);
+#ifdef GP_SMALL
+  if (EPI == GP_GATED || EPI == GP_DGATED) return gp_tiles<AK, BK, EPI, 2, ACT>(p, s);
+#endif
+  return large >= 224 ? gp_tiles<AK, BK, EPI, 4, ACT>(p, s) : gp_tiles<AK, BK, EPI, 2, ACT>(p, s);
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -322,8 +422,9 @@ hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s) {
   GpParams p{};
   p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.m; p.segments = 1;
   p.A[0] = d.x; p.lda = d.ldx; p.B[0] = d.w_gate; p.B[1] = d.w_up; p.ldb = d.n;
-  p.C[0] = hidden; p.ldc = d.n; p.keep_gate = d.gate; p.keep_up = d.up; p.act = d.act;
-  hipError_t e = gp_launch<true, false, GP_GATED>(p, s);
+  p.C[0] = hidden; p.ldc = d.n; p.keep_gate = d.gate; p.keep_up = d.up;
+  hipError_t e = d.act == SOAP_ACT_SILU ? gp_launch<true, false, GP_GATED, SOAP_ACT_SILU>(p, s)
+                                        : gp_launch<true, false, GP_GATED, SOAP_ACT_GELU>(p, s);
   if (e != hipSuccess) return e;
   p = GpParams{};
   p.M = (int)d.tokens; p.N = (int)d.p; p.K = (int)d.n; p.segments = 1;
@@ -341,8 +442,10 @@ hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
   if (d.tokens > 0) {
     p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.p; p.segments = 1;
     p.A[0] = d.dy; p.lda = d.lddy; p.B[0] = d.w_down; p.ldb = d.p;
-    p.C[0] = dg; p.C[1] = du; p.hidden = hidden; p.ldc = d.n; p.gate = d.gate; p.up = d.up; p.act = d.act;
-    if ((e = gp_launch<true, true, GP_DGATED>(p, s)) != hipSuccess) return e;
+    p.C[0] = dg; p.C[1] = du; p.hidden = hidden; p.ldc = d.n; p.gate = d.gate; p.up = d.up;
+    e = d.act == SOAP_ACT_SILU ? gp_launch<true, true, GP_DGATED, SOAP_ACT_SILU>(p, s)
+                               : gp_launch<true, true, GP_DGATED, SOAP_ACT_GELU>(p, s);
+    if (e != hipSuccess) return e;
     if (d.dx) {
       p = GpParams{};
       p.M = (int)d.tokens; p.N = (int)d.m; p.K = (int)d.n; p.segments = 2;

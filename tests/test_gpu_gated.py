@@ -96,8 +96,10 @@ def test_sizes(T, m, n, p, name):
     check(*make(T, m, n, p, T + m), name, torch.float32 if name == "silu" else BF)
 
 
-def test_large():
-    check(*make(2100, 1032, 2056, 1032, 3))
+@pytest.mark.parametrize("T,m,n,p", [(2100, 1032, 2056, 1032), (4104, 1032, 4168, 3592), (3900, 4040, 1032, 4104)])
+def test_large(T, m, n, p):
+    """Tiles of either size, some of them cut at their ends, in every product."""
+    check(*make(T, m, n, p, 3))
 
 
 def test_views():
