@@ -125,7 +125,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   constexpr int TB = 64 * NB, SUB = TB / 64, OP = SUB * GP_BLOCK, LOADS = 2 * SUB;
   constexpr int SLD = TB + 4;                    // staging row of the epilogue, floats
   constexpr int BAND = 64;
-  static_assert(BAND * SLD * 4 <= GP_RING * OP, "the epilogue's band fits the slabs");
+  static_assert(2 * BAND * SLD * 4 <= GP_RING * OP, "two of the epilogue's bands fit the ring");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[GP_RING * OP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, xl = lane & 31, h = lane >> 5;
@@ -221,8 +221,9 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     const int r = (tid + GP_THREADS * v) / UNITS;
     return m0 + (r >> 5) * 32 * NB + 32 * ps + (r & 31);
   };
-  // G and U of two bands, loaded during the main loop, and two bands ahead from then on: before a
-  // band's stores, which they would otherwise wait for, one counter counting both
+  // G and U of two bands, loaded during the first slab, and two bands ahead from then on: before
+  // a band's stores, which they would otherwise wait for, one counter counting both (8192 x 8192,
+  // K = 2048: one band ahead, behind the stores, 429 us)
   v4u kg[2][EPI == GP_DGATED ? EACH : 1], ku[2][EPI == GP_DGATED ? EACH : 1];
   auto kept = [&](int set, int ps, int v) {
     const int row = row_of(ps, v);
@@ -284,11 +285,11 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   begin(sa, true);
 #pragma unroll
   for (int v = 0; v < L1; ++v) load(v >= LOADS, v % LOADS);
+  GP_ARRIVED(LOADS + L1);
   if constexpr (EPI == GP_DGATED) {
 #pragma unroll
     for (int v = 0; v < 2 * EACH; ++v) kept(v / EACH, v / EACH, v % EACH);
   }
-  GP_ARRIVED(LOADS + L1);
 #pragma unroll
   for (int u = 0; u < 2 * NB; ++u) read(0, 0, u);
   int pa = 0;                                    // the place of A's slab
@@ -310,30 +311,30 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   // Bands of 64 rows, 32 of either half of the tile, through LDS.  B's values came first in the
   // matrix instructions: register r of block (i, j) holds row xl of A's, column
   // 8 (r / 4) + 4 h + r % 4 of B's, so that a lane writes four columns at once.
+  auto put = [&](const v16f(&a)[NB], float *to) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      // columns of the gate come first, then up's: 32 NB of a wave are 16 NB of each
+      const int at = !TWO ? wn * 32 * NB + 32 * j : (j >= NB / 2 ? TB / 2 : 0) + wn * 16 * NB + 32 * (j % (NB / 2));
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4 *>(to + (32 * wm + xl) * SLD + at + 2 * r + 4 * h) =
+            make_float4(a[j][r], a[j][r + 1], a[j][r + 2], a[j][r + 3]);
+    }
+  };
+  put(acc[0], stage);
 #pragma unroll 1
   for (int ps = 0; ps < NB; ++ps) {
-    if (ps) __syncthreads();
-    auto put = [&](const v16f(&a)[NB]) {
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        // columns of the gate come first, then up's: 32 NB of a wave are 16 NB of each
-        const int at = !TWO ? wn * 32 * NB + 32 * j : (j >= NB / 2 ? TB / 2 : 0) + wn * 16 * NB + 32 * (j % (NB / 2));
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<float4 *>(stage + (32 * wm + xl) * SLD + at + 2 * r + 4 * h) =
-              make_float4(a[j][r], a[j][r + 1], a[j][r + 2], a[j][r + 3]);
-      }
-    };
-    if (ps == 0) put(acc[0]);
-    else if (ps == 1) put(acc[1]);
-    else if (ps == 2) put(acc[NB - 2]);
-    else put(acc[NB - 1]);
-    __syncthreads();
+    __syncthreads();                             // the band is there, the one before it is read
+    float *now = stage + (ps & 1) * BAND * SLD, *next = stage + (~ps & 1) * BAND * SLD;
+    if (ps == 0) put(acc[1], next);
+    else if (ps == 1 && NB > 2) put(acc[NB - 2], next);
+    else if (ps == 2) put(acc[NB - 1], next);
 #pragma unroll
     for (int v = 0; v < EACH; ++v) {
       const int row = row_of(ps, v);
       if (row < p.M && col < p.N) {
-        const float *x = stage + (tid + GP_THREADS * v) / UNITS * SLD + c;
+        const float *x = now + (tid + GP_THREADS * v) / UNITS * SLD + c;
         const int64_t at = (int64_t)row * p.ldc + col;
         if constexpr (EPI == GP_GATED) {
           v4u og, ou, oh;
