@@ -20,9 +20,7 @@
 // Operands past their ends read as zeros (buffer bounds; units past the end of k are sent
 // out of bounds), so that sizes need no multiple of a tile; m, n and p are multiples of 8
 // and rows 16-byte aligned, so that no unit crosses an end.
-#include "soap.h"
-
-#include "internal.h"
+#include "products_bf16.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -30,18 +28,9 @@
 namespace soap {
 namespace {
 
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) v4s lds_v4s;
-typedef int v4i __attribute__((ext_vector_type(4)));
-
-constexpr int GP_THREADS = 256, GP_KB = 64;      // four waves; k of a slab
+constexpr int GP_KB = 64;                        // k of a slab
 constexpr int GP_RING = 5;                       // operands' slabs in LDS
 constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows in LDS
-constexpr int GP_RSRC = 0x00020000;              // raw 32-bit data
 
 enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART };
 
@@ -57,66 +46,6 @@ struct GpParams {
   const uint16_t *gate, *up;
   uint16_t *keep_gate, *keep_up, *hidden;
 };
-
-__device__ __forceinline__ uint16_t gp_round(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
-__device__ __forceinline__ float gp_float(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
-
-// The activation, and its derivative.  The hardware's exponential and reciprocal are within an
-// fp32 step each, far inside the rounding to bfloat16 that follows.
-struct GpAct {
-  float a, d;
-};
-template <int ACT>
-__device__ __forceinline__ GpAct gp_act(float x) {
-  GpAct r;
-  if constexpr (ACT == SOAP_ACT_SILU) {
-    const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504088896340736f));
-    r.a = x * s;
-    r.d = fmaf(r.a, 1.f - s, s);
-  } else {
-    const float c = 0.5f + 0.5f * erff(x * 0.70710678118654752440f);
-    r.a = x * c;
-    r.d = fmaf(x * 0.39894228040143267794f, __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f), c);
-  }
-  return r;
-}
-__device__ __forceinline__ uint32_t gp_pack(float a, float b) { return gp_round(a) | (uint32_t)gp_round(b) << 16; }
-
-// What one operand's blocks of a slab are loaded from: the tile's first row of its matrix, or of
-// the slab's k, and the bytes from there to the matrix' end.
-struct GpSource {
-  const char *base;
-  int64_t left, step;          // step: to the next slab
-  __device__ __forceinline__ void start(const uint16_t *q, bool kc, int x0, int X, int K, int64_t ld2) {
-    base = (const char *)q + (kc ? x0 * ld2 : 2 * (int64_t)x0);
-    left = kc ? (X - x0 - 1) * ld2 + 2 * (int64_t)K : (K - 1) * ld2 + 2 * (int64_t)(X - x0);
-    step = kc ? 2 * GP_KB : GP_KB * ld2;
-  }
-  __device__ __forceinline__ void next() {
-    base += step;
-    left -= step;
-  }
-  // Offsets stay below 2^31 (rows of a tile are at most 256, of 2^22 bytes).
-  __device__ __forceinline__ v4i buffer() const {
-    const int hi = (int)(left >> 32);
-    const uint32_t lo = (uint32_t)left;
-    const uint32_t n = hi < 0 ? 0u : hi > 0 || lo > 0x7fffffffu ? 0x7fffffffu : lo;
-    const uint64_t a = reinterpret_cast<uint64_t>(base);
-    v4i r = {(int)(uint32_t)a, (int)(uint32_t)(a >> 32) & 0xffff, (int)n, GP_RSRC};
-    // five wait states between a vector instruction that may have written it and the loads
-    asm volatile("s_nop 4" : "+s"(r));
-    return r;
-  }
-};
-constexpr uint32_t GP_OUT = 0x80000000u;         // in an offset: past every buffer's end
-
-// 16 bytes a lane from `offset` of a buffer to LDS at `lds` + 16 lane.  Written out because the
-// compiler holds every transposing read until all such loads have arrived; the kernel waits for
-// them itself, before the barrier in front of their slab's first read.  They write no register.
-__device__ __forceinline__ void gp_load(const v4i &buffer, uint32_t lds, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer)
-               : "m0");
-}
 
 // NB: blocks of 32 x 32 on a side of a wave's share; tiles of 64 NB.  ACT: of the epilogues
 // with an activation.
@@ -179,9 +108,9 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   auto begin = [&](Stream &s, bool is_a) {       // the next slab of an operand: its loads may follow
     if (s.slab == 0 || (p.segments > 1 && s.slab == nk1)) {
       const int seg = s.slab != 0;
-      if (is_a) s.s0.start(p.A[seg], AK, m0, p.M, p.K, lda2);
-      else s.s0.start(seg || which ? p.B[1] : p.B[0], BK, n0, p.N, p.K, ldb2);
-      if (TWO && !is_a) s.s1.start(p.B[1], BK, n0, p.N, p.K, ldb2);
+      if (is_a) s.s0.start(p.A[seg], AK, m0, p.M, p.K, lda2, GP_KB);
+      else s.s0.start(seg || which ? p.B[1] : p.B[0], BK, n0, p.N, p.K, ldb2, GP_KB);
+      if (TWO && !is_a) s.s1.start(p.B[1], BK, n0, p.N, p.K, ldb2, GP_KB);
       s.left = p.K;
     }
     s.r0 = s.s0.buffer();
@@ -208,9 +137,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     }
     const int i = lane & 15, r = i >> 2, u = (x & 32) / 8 + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
     const uint8_t *at = b + (16 * q + 8 * h + r) * 128 + 16 * (u ^ (4 * (r >> 1))) + 8 * (i & 1);
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)at);
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at + 4 * 128));
-    return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    return gp_read_transposed(at, 128);
   };
 
   // The epilogue's bands of 64 rows: a thread's units of eight columns, GP_THREADS apart.
@@ -410,15 +337,71 @@ hipError_t gp_launch(const GpParams &p, hipStream_t s) {
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+size_t wide(int64_t tokens, int64_t n) { return up256(2 * (size_t)tokens * (size_t)n); }
+// Parts of a product of few tokens: 64 columns a workgroup, fewer than 256 workgroups more than
+// the columns need.
+size_t few_bytes(int64_t tokens, int64_t n, int matrices) {
+  return up256(4 * (size_t)std::min(tokens, GATED_FEW) * matrices * 64 * (size_t)((n + 63) / 64 + 256));
+}
+
+hipError_t few_fwd(const GatedDesc &d, hipStream_t s) {
+  char *w = static_cast<char *>(d.workspace);
+  uint16_t *hidden = (uint16_t *)w, *low = (uint16_t *)(w + wide(d.tokens, d.n));
+  FewDesc f;
+  f.kind = FewDesc::GATE_UP; f.tokens = d.tokens; f.n = d.n; f.k = d.m; f.ldx = d.ldx; f.ldw = d.n;
+  f.x[0] = d.x; f.w[0] = d.w_gate; f.w[1] = d.w_up; f.part = (float *)(w + 2 * wide(d.tokens, d.n));
+  f.splits = few_splits_of(f);
+  hipError_t e = launch_product_few(f, s);
+  if (e != hipSuccess) return e;
+  GatedJoin j;
+  j.kind = GatedJoin::GATED; j.T = d.tokens; j.N = d.n; j.splits = f.splits; j.act = d.act; j.part = f.part;
+  j.out = hidden; j.low = low; j.keep_gate = d.gate; j.keep_up = d.up;
+  if ((e = launch_gated_join(j, s)) != hipSuccess) return e;
+  FewDesc g;
+  g.kind = FewDesc::HALVES; g.tokens = d.tokens; g.n = d.p; g.k = d.n; g.ldx = d.n; g.ldw = d.p;
+  g.x[0] = hidden; g.x[1] = low; g.w[0] = d.w_down; g.part = f.part;
+  g.splits = few_splits_of(g);
+  if ((e = launch_product_few(g, s)) != hipSuccess) return e;
+  j = GatedJoin();
+  j.T = d.tokens; j.N = d.p; j.splits = g.splits; j.part = g.part; j.out = d.y; j.ldo = d.ldy;
+  return launch_gated_join(j, s);
+}
+
+// dG, dU and H, and dX if it is wanted.
+hipError_t few_bwd(const GatedDesc &d, uint16_t *dg, uint16_t *du, uint16_t *hidden, float *part, hipStream_t s) {
+  FewDesc f;
+  f.kind = FewDesc::ROWS; f.tokens = d.tokens; f.n = d.n; f.k = d.p; f.ldx = d.lddy; f.ldw = d.p;
+  f.x[0] = d.dy; f.w[0] = d.w_down; f.part = part;
+  f.splits = few_splits_of(f);
+  hipError_t e = launch_product_few(f, s);
+  if (e != hipSuccess) return e;
+  GatedJoin j;
+  j.kind = GatedJoin::DGATED; j.T = d.tokens; j.N = d.n; j.splits = f.splits; j.act = d.act; j.part = part;
+  j.gate = d.gate; j.up = d.up; j.out = dg; j.out2 = du; j.hidden = hidden;
+  if ((e = launch_gated_join(j, s)) != hipSuccess || !d.dx) return e;
+  f = FewDesc();
+  f.kind = FewDesc::ROWS; f.tokens = d.tokens; f.n = d.m; f.k = d.n; f.ldx = d.n; f.ldw = d.n; f.segments = 2;
+  f.x[0] = dg; f.x[1] = du; f.w[0] = d.w_gate; f.w[1] = d.w_up; f.part = part;
+  f.splits = few_splits_of(f);
+  if ((e = launch_product_few(f, s)) != hipSuccess) return e;
+  j = GatedJoin();
+  j.T = d.tokens; j.N = d.m; j.splits = f.splits; j.part = part; j.out = d.dx; j.ldo = d.lddx;
+  return launch_gated_join(j, s);
+}
 
 }  // namespace
 
-size_t gated_workspace_bytes(int64_t tokens, int64_t n, bool backward) {
-  return (backward ? 3 : 1) * up256(2 * (size_t)tokens * (size_t)n);
+// H (and what its rounding leaves, of few tokens) or dG, dU and H, and the parts of few tokens.
+size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bool backward) {
+  if (!tokens) return 0;
+  const size_t parts = backward ? std::max(few_bytes(tokens, n, 1), few_bytes(tokens, m, 1))
+                                : std::max(few_bytes(tokens, n, 2), few_bytes(tokens, p, 1));
+  return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + parts;
 }
 
 hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s) {
   if (d.tokens <= 0) return hipSuccess;
+  if (d.tokens <= GATED_FEW) return few_fwd(d, s);
   uint16_t *hidden = static_cast<uint16_t *>(d.workspace);
   GpParams p{};
   p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.m; p.segments = 1;
@@ -440,7 +423,9 @@ hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
   uint16_t *dg = (uint16_t *)w, *du = (uint16_t *)(w + each), *hidden = (uint16_t *)(w + 2 * each);
   hipError_t e = hipSuccess;
   GpParams p{};
-  if (d.tokens > 0) {
+  if (d.tokens > 0 && d.tokens <= GATED_FEW) {
+    if ((e = few_bwd(d, dg, du, hidden, (float *)(w + 3 * each), s)) != hipSuccess) return e;
+  } else if (d.tokens > 0) {
     p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.p; p.segments = 1;
     p.A[0] = d.dy; p.lda = d.lddy; p.B[0] = d.w_down; p.ldb = d.p;
     p.C[0] = dg; p.C[1] = du; p.hidden = hidden; p.ldc = d.n; p.gate = d.gate; p.up = d.up;

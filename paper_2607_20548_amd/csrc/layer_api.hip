@@ -567,7 +567,7 @@ int soap_head_norm_backward(int64_t tokens, int64_t q_heads, int64_t k_heads, in
 // ------------------------------------------------- gated feed-forward block
 size_t soap_gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, int backward) {
   if (check_gated(tokens, m, n, p, SOAP_ACT_SILU) != SOAP_OK) return 0;
-  return soap::gated_workspace_bytes(tokens, n, backward != 0);
+  return soap::gated_workspace_bytes(tokens, m, n, p, backward != 0);
 }
 
 int soap_gated_forward(int64_t tokens, int64_t m, int64_t n, int64_t p, int activation, const void *x, int64_t ldx,
@@ -577,7 +577,7 @@ int soap_gated_forward(int64_t tokens, int64_t m, int64_t n, int64_t p, int acti
   SOAP_TRY(check_ld8("ldx", ldx, m));
   SOAP_TRY(check_ld8("ldy", ldy, p));
   if (!gate != !up) return api_fail(SOAP_ERR_NULL, "gate and up come together");
-  const size_t tn = 2 * (size_t)tokens * (size_t)n, need = soap::gated_workspace_bytes(tokens, n, false);
+  const size_t tn = 2 * (size_t)tokens * (size_t)n, need = soap::gated_workspace_bytes(tokens, m, n, p, false);
   SOAP_TRY(check_bufs({{x, span(tokens, m, ldx, 2), "x", false, true, 16},
                        {w_gate, 2 * (size_t)m * (size_t)n, "w_gate", false, true, 16},
                        {w_up, 2 * (size_t)m * (size_t)n, "w_up", false, true, 16},
@@ -605,7 +605,7 @@ int soap_gated_backward(int64_t tokens, int64_t m, int64_t n, int64_t p, int act
   SOAP_TRY(check_ld8("lddy", lddy, p));
   SOAP_TRY(check_ld8("ldx", ldx, m));
   if (dx) SOAP_TRY(check_ld8("lddx", lddx, m));
-  const size_t tn = 2 * (size_t)tokens * (size_t)n, need = soap::gated_workspace_bytes(tokens, n, true);
+  const size_t tn = 2 * (size_t)tokens * (size_t)n, need = soap::gated_workspace_bytes(tokens, m, n, p, true);
   const size_t mn = (size_t)m * (size_t)n, np = (size_t)n * (size_t)p, e = elem(grad_dtype);
   SOAP_TRY(check_bufs({{dy, span(tokens, p, lddy, 2), "dy", false, true, 16},
                        {x, span(tokens, m, ldx, 2), "x", false, true, 16},
