@@ -39,8 +39,9 @@ struct GpParams {
   const uint16_t *A[2], *B[2]; // B[1]: up's weights or gradients; A[1]: the second segment of k
   int64_t lda, ldb;
   int segments;                // of k, each with operands of its own
+  int splits;                  // parts of k, the grid's y; more than one write fp32 sums
   int tiles_m, tiles_n, pairs; // pairs: B and C by the tile's column (the second half: [1])
-  void *C[2];
+  void *C[2];                  // part: [part][matrix][M][N] floats
   int64_t ldc;
   // gated: C[0] the product, kept G and U (or null); dgated: C[0] = dG, C[1] = dU, H
   const uint16_t *gate, *up;
@@ -48,8 +49,8 @@ struct GpParams {
 };
 
 // NB: blocks of 32 x 32 on a side of a wave's share; tiles of 64 NB.  ACT: of the epilogues
-// with an activation.
-template <bool AK, bool BK, int EPI, int NB, int ACT>
+// with an activation.  TWO: columns of both gate and up.
+template <bool AK, bool BK, int EPI, int NB, int ACT, bool TWO>
 __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpParams p) {
   constexpr int TB = 64 * NB, SUB = TB / 64, OP = SUB * GP_BLOCK, LOADS = 2 * SUB;
   constexpr int SLD = TB + 4;                    // staging row of the epilogue, floats
@@ -75,7 +76,6 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     which = tn >= half;
     tn -= which ? half : 0;
   }
-  constexpr bool TWO = EPI == GP_GATED;          // columns of both matrices, 64 by 64
   const int m0 = tm * TB, n0 = tn * (TWO ? TB / 2 : TB);
   const int64_t lda2 = 2 * p.lda, ldb2 = 2 * p.ldb;
 
@@ -92,7 +92,8 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   // the unit of eight k that a lane loads, the same in all its rows
   const int unit = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);
   const uint32_t base = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds);
-  const int nk1 = (p.K + GP_KB - 1) / GP_KB, nk = nk1 * p.segments;
+  const int nk1 = (p.K + GP_KB - 1) / GP_KB, all = nk1 * p.segments;
+  const int s0 = (int)((int64_t)blockIdx.y * all / p.splits), nk = (int)((int64_t)(blockIdx.y + 1) * all / p.splits) - s0;
 
   // A slab of A and one of B take a place each of a ring of five, in the order A0 B0 A1 B1 ..: what
   // slab k frees takes B of slab k + 2, which then has a slab's time to arrive, and A of slab k + 3,
@@ -103,15 +104,18 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     int left, slab, place;                       // of k in the segment; the next slab; its place
     uint32_t dead, to;
   } sa, sb;
-  sa.slab = sb.slab = sa.place = 0;
+  sa.slab = sb.slab = s0;
+  sa.place = 0;
   sb.place = 1;
   auto begin = [&](Stream &s, bool is_a) {       // the next slab of an operand: its loads may follow
-    if (s.slab == 0 || (p.segments > 1 && s.slab == nk1)) {
-      const int seg = s.slab != 0;
+    if (s.slab == s0 || (p.segments > 1 && s.slab == nk1)) {
+      const int seg = p.segments > 1 && s.slab >= nk1, at = s.slab - (seg ? nk1 : 0);
       if (is_a) s.s0.start(p.A[seg], AK, m0, p.M, p.K, lda2, GP_KB);
       else s.s0.start(seg || which ? p.B[1] : p.B[0], BK, n0, p.N, p.K, ldb2, GP_KB);
       if (TWO && !is_a) s.s1.start(p.B[1], BK, n0, p.N, p.K, ldb2, GP_KB);
-      s.left = p.K;
+      s.s0.next(at);
+      if (TWO && !is_a) s.s1.next(at);
+      s.left = p.K - at * GP_KB;
     }
     s.r0 = s.s0.buffer();
     if (TWO && !is_a) s.r1 = s.s1.buffer();
@@ -141,9 +145,10 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   };
 
   // The epilogue's bands of 64 rows: a thread's units of eight columns, GP_THREADS apart.
-  constexpr int UNITS = (TWO ? TB / 2 : TB) / 8, EACH = BAND * UNITS / GP_THREADS;
+  constexpr int UNITS = (EPI == GP_GATED ? TB / 2 : TB) / 8, EACH = BAND * UNITS / GP_THREADS;
   float *stage = reinterpret_cast<float *>(lds);
-  const int c = 8 * (tid % UNITS), col = n0 + c;  // GP_THREADS is a multiple of UNITS
+  const int c = 8 * (tid % UNITS);               // GP_THREADS is a multiple of UNITS
+  const int second = EPI == GP_PART && TWO && c >= TB / 2, col = n0 + c - (second ? TB / 2 : 0);
   auto row_of = [&](int ps, int v) {
     const int r = (tid + GP_THREADS * v) / UNITS;
     return m0 + (r >> 5) * 32 * NB + 32 * ps + (r & 31);
@@ -277,8 +282,10 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
             *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
             *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
           }
-        } else if constexpr (EPI == GP_F32) {
-          float *o = static_cast<float *>(p.C[which]) + at;
+        } else if constexpr (EPI == GP_F32 || EPI == GP_PART) {
+          float *o = EPI == GP_F32 ? static_cast<float *>(p.C[which]) + at
+                                   : static_cast<float *>(p.C[0]) +
+                                         ((int64_t)blockIdx.y * (TWO ? 2 : 1) + second) * p.M * p.N + (int64_t)row * p.N + col;
           *reinterpret_cast<float4 *>(o) = make_float4(x[0], x[1], x[2], x[3]);
           *reinterpret_cast<float4 *>(o + 4) = make_float4(x[4], x[5], x[6], x[7]);
         } else if constexpr (EPI == GP_BF16) {
@@ -315,25 +322,72 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   }
 }
 
-template <bool AK, bool BK, int EPI, int NB, int ACT>
+template <bool AK, bool BK, int EPI, int NB, int ACT, bool TWO>
 hipError_t gp_tiles(GpParams p, hipStream_t s) {
   constexpr int TB = 64 * NB;
   p.tiles_m = (p.M + TB - 1) / TB;
-  const int width = EPI == GP_GATED ? TB / 2 : TB;
+  const int width = TWO ? TB / 2 : TB;
   p.tiles_n = (p.N + width - 1) / width * (p.pairs ? 2 : 1);
-  hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT>), dim3((unsigned)p.tiles_m * p.tiles_n), dim3(GP_THREADS), 0, s, p);
+  hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO>), dim3((unsigned)p.tiles_m * p.tiles_n, (unsigned)p.splits),
+                     dim3(GP_THREADS), 0, s, p);
   return hipGetLastError();
 }
 
+// Tiles of a product of M x N (of two matrices) and the parts of k that each is summed in.
+struct GpPlan {
+  int nb, splits;
+};
+constexpr int64_t GP_PARTS = (int64_t)256 * 256 * 256 * 4;   // bytes of all parts at most
+GpPlan gp_plan(int64_t M, int64_t N, int64_t slabs, bool two, bool pairs) {
+  const int64_t w = two ? 2 : 1;
+  auto tiles = [&](int64_t tb) { return (M + tb - 1) / tb * ((w * N + tb - 1) / tb) * (pairs ? 2 : 1); };
+  const int64_t large = tiles(256), small = tiles(128);
+  if (large >= 224) return {4, 1};
+  if (large >= 32 && slabs >= 16) {
+    const int64_t parts = std::min(256 / large, slabs / 8);
+    if (parts > 1) return {4, (int)parts};
+  }
+  return {2, (int)std::max<int64_t>(1, std::min(512 / small, slabs / 4))};
+}
+
+// The product, in parts of k and their sum where its tiles are few: into `part`.
 template <bool AK, bool BK, int EPI, int ACT = SOAP_ACT_SILU>
-hipError_t gp_launch(const GpParams &p, hipStream_t s) {
+hipError_t gp_launch(GpParams p, float *part, hipStream_t s) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
-  const int width = EPI == GP_GATED ? 128 : 256;
-  const int64_t large = (int64_t)((p.M + 255) / 256) * ((p.N + width - 1) / width) * (p.pairs ? 2 : 1);
-#ifdef GP_SMALL
-  if (EPI == GP_GATED || EPI == GP_DGATED) return gp_tiles<AK, BK, EPI, 2, ACT>(p, s);
-#endif
-  return large >= 224 ? gp_tiles<AK, BK, EPI, 4, ACT>(p, s) : gp_tiles<AK, BK, EPI, 2, ACT>(p, s);
+  constexpr bool TWO = EPI == GP_GATED;
+  const GpPlan plan = gp_plan(p.M, p.N, (int64_t)((p.K + GP_KB - 1) / GP_KB) * p.segments, TWO, p.pairs);
+  p.splits = plan.splits;
+  if (plan.splits == 1)
+    return plan.nb == 4 ? gp_tiles<AK, BK, EPI, 4, ACT, TWO>(p, s) : gp_tiles<AK, BK, EPI, 2, ACT, TWO>(p, s);
+  if (p.pairs) {                                 // one of the two after the other
+    p.pairs = 0;
+    for (int i = 0; i < 2; ++i) {
+      GpParams q = p;
+      q.B[0] = p.B[i];
+      q.C[0] = p.C[i];
+      const hipError_t e = gp_launch<AK, BK, EPI, ACT>(q, part, s);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
+  GatedJoin j;
+  j.T = p.M; j.N = p.N; j.splits = plan.splits; j.part = part; j.ldo = p.ldc; j.act = ACT;
+  if constexpr (EPI == GP_GATED) {
+    j.kind = GatedJoin::GATED;
+    j.out = static_cast<uint16_t *>(p.C[0]); j.keep_gate = p.keep_gate; j.keep_up = p.keep_up;
+  } else if constexpr (EPI == GP_DGATED) {
+    j.kind = GatedJoin::DGATED;
+    j.out = static_cast<uint16_t *>(p.C[0]); j.out2 = static_cast<uint16_t *>(p.C[1]);
+    j.hidden = p.hidden; j.gate = p.gate; j.up = p.up;
+  } else if constexpr (EPI == GP_F32) {
+    j.kind = GatedJoin::F32;
+    j.out_f32 = static_cast<float *>(p.C[0]);
+  } else {
+    j.out = static_cast<uint16_t *>(p.C[0]);
+  }
+  p.C[0] = part;
+  const hipError_t e = plan.nb == 4 ? gp_tiles<AK, BK, GP_PART, 4, 0, TWO>(p, s) : gp_tiles<AK, BK, GP_PART, 2, 0, TWO>(p, s);
+  return e != hipSuccess ? e : launch_gated_join(j, s);
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -391,57 +445,60 @@ hipError_t few_bwd(const GatedDesc &d, uint16_t *dg, uint16_t *du, uint16_t *hid
 
 }  // namespace
 
-// H (and what its rounding leaves, of few tokens) or dG, dU and H, and the parts of few tokens.
+// H (and what its rounding leaves, of few tokens) or dG, dU and H, and sums of parts of k.
 size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bool backward) {
   if (!tokens) return 0;
   const size_t parts = backward ? std::max(few_bytes(tokens, n, 1), few_bytes(tokens, m, 1))
                                 : std::max(few_bytes(tokens, n, 2), few_bytes(tokens, p, 1));
-  return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + parts;
+  const size_t tiled = tokens > GATED_FEW || backward ? (size_t)GP_PARTS : 0;   // its weights' gradients are always tiled
+  return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + std::max(parts, tiled);
 }
 
 hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s) {
   if (d.tokens <= 0) return hipSuccess;
   if (d.tokens <= GATED_FEW) return few_fwd(d, s);
   uint16_t *hidden = static_cast<uint16_t *>(d.workspace);
+  float *part = (float *)(static_cast<char *>(d.workspace) + wide(d.tokens, d.n) + wide(GATED_FEW, d.n));
   GpParams p{};
   p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.m; p.segments = 1;
   p.A[0] = d.x; p.lda = d.ldx; p.B[0] = d.w_gate; p.B[1] = d.w_up; p.ldb = d.n;
   p.C[0] = hidden; p.ldc = d.n; p.keep_gate = d.gate; p.keep_up = d.up;
-  hipError_t e = d.act == SOAP_ACT_SILU ? gp_launch<true, false, GP_GATED, SOAP_ACT_SILU>(p, s)
-                                        : gp_launch<true, false, GP_GATED, SOAP_ACT_GELU>(p, s);
+  hipError_t e = d.act == SOAP_ACT_SILU ? gp_launch<true, false, GP_GATED, SOAP_ACT_SILU>(p, part, s)
+                                        : gp_launch<true, false, GP_GATED, SOAP_ACT_GELU>(p, part, s);
   if (e != hipSuccess) return e;
   p = GpParams{};
   p.M = (int)d.tokens; p.N = (int)d.p; p.K = (int)d.n; p.segments = 1;
   p.A[0] = hidden; p.lda = d.n; p.B[0] = d.w_down; p.ldb = d.p;
   p.C[0] = d.y; p.ldc = d.ldy;
-  return gp_launch<true, false, GP_BF16>(p, s);
+  return gp_launch<true, false, GP_BF16>(p, part, s);
 }
 
 hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
   const size_t each = up256(2 * (size_t)d.tokens * (size_t)d.n);
   char *w = static_cast<char *>(d.workspace);
   uint16_t *dg = (uint16_t *)w, *du = (uint16_t *)(w + each), *hidden = (uint16_t *)(w + 2 * each);
+  float *part = (float *)(w + 3 * each);
   hipError_t e = hipSuccess;
   GpParams p{};
   if (d.tokens > 0 && d.tokens <= GATED_FEW) {
-    if ((e = few_bwd(d, dg, du, hidden, (float *)(w + 3 * each), s)) != hipSuccess) return e;
+    if ((e = few_bwd(d, dg, du, hidden, part, s)) != hipSuccess) return e;
   } else if (d.tokens > 0) {
     p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.p; p.segments = 1;
     p.A[0] = d.dy; p.lda = d.lddy; p.B[0] = d.w_down; p.ldb = d.p;
     p.C[0] = dg; p.C[1] = du; p.hidden = hidden; p.ldc = d.n; p.gate = d.gate; p.up = d.up;
-    e = d.act == SOAP_ACT_SILU ? gp_launch<true, true, GP_DGATED, SOAP_ACT_SILU>(p, s)
-                               : gp_launch<true, true, GP_DGATED, SOAP_ACT_GELU>(p, s);
+    e = d.act == SOAP_ACT_SILU ? gp_launch<true, true, GP_DGATED, SOAP_ACT_SILU>(p, part, s)
+                               : gp_launch<true, true, GP_DGATED, SOAP_ACT_GELU>(p, part, s);
     if (e != hipSuccess) return e;
     if (d.dx) {
       p = GpParams{};
       p.M = (int)d.tokens; p.N = (int)d.m; p.K = (int)d.n; p.segments = 2;
       p.A[0] = dg; p.A[1] = du; p.lda = d.n; p.B[0] = d.w_gate; p.B[1] = d.w_up; p.ldb = d.n;
       p.C[0] = d.dx; p.ldc = d.lddx;
-      if ((e = gp_launch<true, true, GP_BF16>(p, s)) != hipSuccess) return e;
+      if ((e = gp_launch<true, true, GP_BF16>(p, part, s)) != hipSuccess) return e;
     }
   }
   auto grad = [&](const GpParams &q) {
-    return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(q, s) : gp_launch<false, false, GP_F32>(q, s);
+    return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(q, part, s) : gp_launch<false, false, GP_F32>(q, part, s);
   };
   if (d.dw_gate || d.dw_up) {
     p = GpParams{};

@@ -173,7 +173,7 @@ __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
 }
 
 // ------------------------------------------------- the parts' sums
-enum { GJ_GATED, GJ_DGATED, GJ_BF16 };
+enum { GJ_GATED, GJ_DGATED, GJ_BF16, GJ_F32 };
 constexpr int GJ_THREADS = 256;
 
 // Eight columns of a row a thread.
@@ -200,6 +200,10 @@ __global__ __launch_bounds__(GJ_THREADS) void product_join(GatedJoin p) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
     *reinterpret_cast<v4u *>(p.out + row * p.ldo + col) = o;
+  } else if constexpr (MODE == GJ_F32) {
+    float *o = p.out_f32 + row * p.ldo + col;
+    *reinterpret_cast<float4 *>(o) = make_float4(x[0][0], x[0][1], x[0][2], x[0][3]);
+    *reinterpret_cast<float4 *>(o + 4) = make_float4(x[0][4], x[0][5], x[0][6], x[0][7]);
   } else if constexpr (MODE == GJ_GATED) {
     v4u og, ou, oh, ol;
 #pragma unroll
@@ -265,6 +269,7 @@ hipError_t gf_launch(const GfParams &p, hipStream_t s) {
 
 hipError_t launch_gated_join(const GatedJoin &p, hipStream_t s) {
   if (p.kind == GatedJoin::BF16) return gj_launch<GJ_BF16, 0>(p, s);
+  if (p.kind == GatedJoin::F32) return gj_launch<GJ_F32, 0>(p, s);
   if (p.kind == GatedJoin::GATED)
     return p.act == SOAP_ACT_SILU ? gj_launch<GJ_GATED, SOAP_ACT_SILU>(p, s) : gj_launch<GJ_GATED, SOAP_ACT_GELU>(p, s);
   return p.act == SOAP_ACT_SILU ? gj_launch<GJ_DGATED, SOAP_ACT_SILU>(p, s) : gj_launch<GJ_DGATED, SOAP_ACT_GELU>(p, s);

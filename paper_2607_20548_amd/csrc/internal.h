@@ -359,13 +359,14 @@ struct FewDesc {
 };
 int few_splits_of(const FewDesc &d);
 hipError_t launch_product_few(const FewDesc &d, hipStream_t s);
-// The sum of the parts, T x N (N a multiple of 8), and what is made of it.  BF16: out.  GATED: H into
+// The sum of the parts, T x N (N a multiple of 8), and what is made of it.  BF16: out, F32: out_f32.  GATED: H into
 // out (and what its rounding leaves into low), G and U kept or null.  DGATED: out = dG, out2 = dU, hidden.
 struct GatedJoin {
-  enum Kind { BF16, GATED, DGATED } kind = BF16;
+  enum Kind { BF16, F32, GATED, DGATED } kind = BF16;
   int64_t T = 0, N = 0, ldo = 0;
   int splits = 1, act = 0;
   const float *part = nullptr;
+  float *out_f32 = nullptr;
   const uint16_t *gate = nullptr, *up = nullptr;
   uint16_t *out = nullptr, *low = nullptr, *out2 = nullptr, *hidden = nullptr, *keep_gate = nullptr, *keep_up = nullptr;
 };
