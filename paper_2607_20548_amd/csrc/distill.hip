@@ -49,6 +49,9 @@ struct DsParams {
 
 enum { DS_LOSS = 1, DS_GRAD = 2 };
 
+// 2^x for x at or below about 0; results below 2^-126 are zeros.
+__device__ __forceinline__ float ds_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
 template <typename T>
 constexpr int ds_vec() { return 16 / (int)sizeof(T); }
 template <typename T>
@@ -67,25 +70,30 @@ __device__ __forceinline__ T ds_round(float v) {
   else return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// The unit whose first value is the row's `col` (which may lie before the row or, in part,
-// behind it): -inf outside.
+// A row's units of 16 bytes lie where those of memory do: whole ones first .. last - 1 (the shift
+// `mis` is in front of the row), and up to 2 (VEC - 1) single values in front of and behind them.
 template <typename T>
-__device__ __forceinline__ v4u ds_load(const T *row, int col, int classes) {
-  constexpr int VEC = ds_vec<T>();
-  if (col >= 0 && col + VEC <= classes) return *reinterpret_cast<const v4u_any *>(row + col);
-  v4u q;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (sizeof(T) == 4) {
-      q[i] = col + i >= 0 && col + i < classes ? __float_as_uint(row[col + i]) : 0xff800000u;
-    } else {
-      const int a = col + 2 * i, b = a + 1;
-      q[i] = (a >= 0 && a < classes ? (uint32_t)row[a] : 0xff80u) |
-             ((b >= 0 && b < classes ? (uint32_t)row[b] : 0xff80u) << 16);
-    }
+struct DsRow {
+  const T *z;
+  int mis, first, last, front, back, edges;   // back: the column behind the whole units
+  __device__ __forceinline__ DsRow(const T *row, int classes) {
+    constexpr int VEC = ds_vec<T>();
+    z = row;
+    mis = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    first = mis ? 1 : 0;
+    last = max((classes + mis) / VEC, first);
+    front = min(mis ? VEC - mis : 0, classes);
+    back = last * VEC - mis;
+    edges = front + max(classes - max(back, front), 0);
   }
-  return q;
-}
+  __device__ __forceinline__ bool whole(int unit) const { return unit >= first && unit < last; }
+  // Unit `at` + lane, `at` the same for all lanes: a base in scalar registers and a lane's offset.
+  __device__ __forceinline__ v4u load(int at, uint32_t lane) const {
+    const char *base = reinterpret_cast<const char *>(z) - mis * (int)sizeof(T) + (int64_t)at * 16;
+    return whole(at + (int)lane) ? *reinterpret_cast<const v4u_any *>(base + 16 * lane) : v4u(0u);
+  }
+  __device__ __forceinline__ int edge(int e) const { return e < front ? e : back + e - front; }   // its column
+};
 
 // A running maximum of z and the sum of exp2((z - maximum) scale) under it; without a value
 // above -inf the maximum is -inf and the sum 0 (or NaN, if there was one).
@@ -95,7 +103,7 @@ struct DsSum {
 __device__ __forceinline__ float ds_base(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ DsSum ds_join(DsSum a, DsSum b, float scale) {
   const float m = fmaxf(a.m, b.m);
-  return {m, a.s * (a.m == -INFINITY ? 1.f : exp2f((a.m - m) * scale)) + b.s * (b.m == -INFINITY ? 1.f : exp2f((b.m - m) * scale))};
+  return {m, a.s * (a.m == -INFINITY ? 1.f : ds_exp2((a.m - m) * scale)) + b.s * (b.m == -INFINITY ? 1.f : ds_exp2((b.m - m) * scale))};
 }
 template <int NT>
 __device__ __forceinline__ DsSum ds_join_all(DsSum v, float scale, DsSum *red) {
@@ -108,183 +116,215 @@ __device__ __forceinline__ DsSum ds_join_all(DsSum v, float scale, DsSum *red) {
   for (int w = 1; w < NT / 64; ++w) v = ds_join(v, red[w], scale);
   return v;
 }
-template <int NT, bool MAX>
-__device__ __forceinline__ float ds_reduce(float v, float *red) {
-  v = MAX ? lane_reduce<64>(v, [](float a, float b) { return fmaxf(a, b); }) : lane_sum<64>(v);
-  __syncthreads();                        // red may still be read
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int w = 1; w < NT / 64; ++w) v = MAX ? fmaxf(v, red[w]) : v + red[w];
-  return v;
-}
+// What the first wave finds in the teacher's list.
+struct DsList {
+  float most, logs, rest, weight;         // of log p: what is taken off t, and the divisor's log; weight: of q
+  int any, twice;                         // whether the list weighs anything; a class in two slots
+};
 
-// U: units of a thread that the registers hold (0: the row is read by and by, and again for
-// the gradient).
+// U: units of a thread that the registers hold, with workgroups that walk over rows and load the
+// next one's units as they write the present one's (0: one row, read by and by, and again for the
+// gradient).  The first wave sees to the list, beside the others' sums.
 template <typename T, int NT, int U, int WHAT>
 __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
-  constexpr int VEC = ds_vec<T>(), W = NT / 64, AHEAD = 4;
+  constexpr int VEC = ds_vec<T>(), AHEAD = 4;
   constexpr bool LOSS = WHAT & DS_LOSS, GRAD = WHAT & DS_GRAD;
   extern __shared__ uint32_t map[];       // of all classes and the shift, where `marked`
-  __shared__ float ps[DISTILL_MAX_SLOTS];
-  __shared__ int cls[DISTILL_MAX_SLOTS];
-  __shared__ float red[W];
-  __shared__ DsSum red2[2][W];
-  __shared__ int some, twice;
+  __shared__ float ps[DISTILL_MAX_SLOTS], zs[DISTILL_MAX_SLOTS];   // of the slots: log p, the student's logit,
+  __shared__ int cls[DISTILL_MAX_SLOTS];                           // the class, or -1
+  __shared__ DsSum red[2][NT / 64];
+  __shared__ DsList list;
   const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x / p.segments;
-  const int segment = blockIdx.x % p.segments;
-  const T *z = static_cast<const T *>(p.z) + row * p.ld;
-  const bool tail = p.tail;
+  const bool tail = p.tail, marked = GRAD || tail, leader = __builtin_amdgcn_readfirstlane(tid >> 6) == 0;
   const float inv = 1.f / p.tau;
-  // units lie where 16 bytes of the row do
-  const int mis = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-  const int units = (p.classes + mis + VEC - 1) / VEC;
-  const bool marked = GRAD || tail;
+  const int words = (p.classes + VEC + 31) / 32;
+  int64_t row = blockIdx.x / p.segments;
+  const int segment = blockIdx.x % p.segments;
+  const int64_t step = U ? gridDim.x : p.rows;
+  DsRow<T> z(static_cast<const T *>(p.z) + row * p.ld, p.classes);
+  // a slot of a row: class and teacher's value, and the student's logit (an empty slot: none)
+  auto slot = [&](int64_t r, int j, int &c, float &t) {
+    const bool in = j < p.slots;
+    c = in ? p.index[r * p.ldi + j] : -1;
+    t = 0.f;
+    if (in) {
+      if (p.t_bf16) t = ds_at(static_cast<const uint16_t *>(p.t) + r * p.ldt + j);
+      else t = static_cast<const float *>(p.t)[r * p.ldt + j];
+    }
+  };
+  auto look = [&](int &c, float &t) {
+    const bool in = c >= 0 && c < p.classes;
+    c = in ? c : -1;
+    t = in ? t : -INFINITY;
+    return in ? ds_at(z.z + c) : 0.f;
+  };
+  int early_c = -1;                       // the first 64, loaded ahead
+  float early_t = 0.f, early_z = 0.f;
+  if (leader) slot(row, tid, early_c, early_t);
   constexpr int HELD = U ? U : 1;
   v4u held[HELD];
   if constexpr (U > 0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) held[u] = ds_load<T>(z, (u * NT + tid) * VEC - mis, p.classes);
+    for (int u = 0; u < U; ++u) held[u] = z.load(u * NT, tid);
   }
-
-  // ---- the teacher's list
   if (marked)
-    for (int i = tid; i < (p.classes + mis + 31) / 32; i += NT) map[i] = 0u;
-  if (tid == 0) some = twice = 0;
-  float most = -INFINITY;
-  for (int j = tid; j < p.slots; j += NT) {
-    int c = p.index[row * p.ldi + j];
-    if (c < 0 || c >= p.classes) c = -1;
-    float t = -INFINITY;
-    if (c >= 0) {
-      t = p.t_bf16 ? ds_at(static_cast<const uint16_t *>(p.t) + row * p.ldt + j)
-                   : static_cast<const float *>(p.t)[row * p.ldt + j];
-    }
-    cls[j] = c;
-    ps[j] = t;
-    most = t > most || t != t ? t : most;
-  }
+    for (int i = tid; i < words; i += NT) map[i] = 0u;
   __syncthreads();
-  for (int j = tid; j < p.slots; j += NT) {
-    if (cls[j] < 0) continue;
-    some = 1;
-    if (marked) {
-        const int b = cls[j] + mis;
-        if (atomicOr(&map[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u) twice = 1;
-    }
-  }
-  float sum = 0.f, logs = 0.f;            // of p (before it is divided), and the log of the divisor
-  if (!tail) {
-    most = ds_base(ds_reduce<NT, true>(most, red));
-    for (int j = tid; j < p.slots; j += NT) {
-      ps[j] = (ps[j] - most) * inv;
-      sum += expf(ps[j]);
-    }
-    sum = ds_reduce<NT, false>(sum, red);
-    logs = logf(sum);
-  } else {
-    for (int j = tid; j < p.slots; j += NT) sum += expf(ps[j]);
-    sum = ds_reduce<NT, false>(sum, red);
-  }
-  const bool any = tail ? some : sum != 0.f;   // a list without a class weighs nothing
-  float rest = !tail || !any ? 0.f : sum == sum ? fmaxf(0.f, 1.f - sum) : sum;
 
-  auto bits = [&](int unit) -> uint32_t {
-    return VEC == 8 ? reinterpret_cast<const uint8_t *>(map)[unit]
-                    : (reinterpret_cast<const uint8_t *>(map)[unit >> 1] >> (4 * (unit & 1))) & 15u;
-  };
-
-  // ---- the student's sums: over all classes, or (tail) over those not listed and those listed
-  DsSum all = {-INFINITY, 0.f}, in = {-INFINITY, 0.f};
-  float lse = 0.f, lse_rest = 0.f;        // log sum exp(z / tau), in units of 1
-  if constexpr (LOSS) {
-    __syncthreads();                      // the bitmap is complete
-    auto add = [&](DsSum &a, const float *v) {
-      float m = v[0];
-#pragma unroll
-      for (int i = 1; i < VEC; ++i) m = fmaxf(m, v[i]);
-      m = fmaxf(m, a.m);
-      const float at = ds_base(m);
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) s += exp2f((v[i] - at) * p.scale);
-      a.s = m > a.m && a.m != -INFINITY ? fmaf(a.s, exp2f((a.m - m) * p.scale), s) : a.s + s;
-      a.m = m;
-    };
-    auto unit = [&](const v4u &q, int at) {
-      float v[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = ds_value<T>(q, i);
-      const uint32_t b = tail ? bits(at) : 0u;
-      if (b) {
-        float o[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          o[i] = b >> i & 1u ? v[i] : -INFINITY;
-          v[i] = b >> i & 1u ? -INFINITY : v[i];
+#pragma unroll 1
+  for (;;) {
+    const int mis = z.mis;
+    const int edge = z.edge(tid);         // the column of this thread's single value, where tid < z.edges
+    const float single = tid < z.edges ? ds_at(z.z + edge) : 0.f;
+    // ---- the teacher's list; where its classes are not needed for the sums it is looked at
+    // behind these, its first 64 slots' loads before them
+    if (leader) early_z = look(early_c, early_t);
+    auto find = [&]() {
+      DsList l = {0.f, 0.f, 0.f, 0.f, 0, 0};
+      float most = -INFINITY, sum = 0.f;
+      bool some = false, twice = false;
+#pragma unroll 1
+      for (int j = tid; j < p.slots; j += 64) {
+        int c = early_c;
+        float t = early_t, zv = early_z;
+        if (j >= 64) {
+          slot(row, j, c, t);
+          zv = look(c, t);
         }
-        add(in, o);
+        most = t > most || t != t ? t : most;
+        cls[j] = c;
+        ps[j] = t;
+        zs[j] = zv;
+        if (c < 0) continue;
+        some = true;
+        const int b = c + mis;
+        if (marked) twice |= atomicOr(&map[b >> 5], 1u << (b & 31)) >> (b & 31) & 1u;
       }
-      add(all, v);
+      if (!tail) l.most = ds_base(lane_reduce<64>(most, [](float a, float b) { return fmaxf(a, b); }));
+#pragma unroll 1
+      for (int j = tid; j < p.slots; j += 64) {
+        const float t = tail ? ps[j] : (ps[j] - l.most) * inv;
+        ps[j] = t;
+        sum += expf(t);
+      }
+      sum = lane_sum<64>(sum);
+      l.twice = __ballot(twice) != 0;
+      l.logs = tail ? 0.f : logf(sum);
+      l.any = tail ? __ballot(some) != 0 : sum != 0.f;       // a list without a class weighs nothing
+      l.rest = !tail || !l.any ? 0.f : sum == sum ? fmaxf(0.f, 1.f - sum) : sum;
+      l.weight = tail ? sum : 1.f;
+      if (tid == 0) list = l;
     };
-    if constexpr (U > 0) {
+    if (tail || !LOSS) {
+      if (leader) find();
+      __syncthreads();
+    }
+
+    auto bits = [&](int unit) -> uint32_t {
+      return VEC == 8 ? reinterpret_cast<const uint8_t *>(map)[unit]
+                      : (reinterpret_cast<const uint8_t *>(map)[unit >> 1] >> (4 * (unit & 1))) & 15u;
+    };
+
+    // ---- the student's sums: over all classes, or (tail) over those not listed and those listed
+    DsSum all = {-INFINITY, 0.f}, in = {-INFINITY, 0.f};
+    float lse = 0.f, lse_rest = 0.f;      // log sum exp(z / tau), in units of 1
+    if constexpr (LOSS) {
+      auto add = [&](DsSum &a, const float *v) {
+        float m = a.m;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (u * NT + tid < units) unit(held[u], u * NT + tid);
+        for (int i = 0; i < VEC; i += 2) m = fmaxf(fmaxf(v[i], v[i + 1]), m);
+        float s[2] = {0.f, 0.f};
+        const float at = ds_base(m);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[i & 1] += ds_exp2((v[i] - at) * p.scale);
+        if (m > a.m && a.m != -INFINITY) a.s *= ds_exp2((a.m - m) * p.scale);
+        a.s += s[0] + s[1];
+        a.m = m;
+      };
+      auto unit = [&](const v4u &q, int at) {
+        float v[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = ds_value<T>(q, i);
+        const uint32_t b = tail ? bits(at) : 0u;
+        if (b) {
+          float o[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            o[i] = b >> i & 1u ? v[i] : -INFINITY;
+            v[i] = b >> i & 1u ? -INFINITY : v[i];
+          }
+          add(in, o);
+        }
+        add(all, v);
+      };
+      if (tid < z.edges) {
+        const int b = edge + mis;
+        const DsSum one = {single, single == -INFINITY ? 0.f : single - single + 1.f};
+        if (tail && map[b >> 5] >> (b & 31) & 1u) in = one;
+        else all = one;
+      }
+      if constexpr (U > 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (z.whole(u * NT + tid)) unit(held[u], u * NT + tid);
+          __builtin_amdgcn_sched_barrier(0);   // units side by side would take the registers of others
+        }
+      } else {
+        for (int u0 = 0; u0 < z.last; u0 += AHEAD * NT) {
+          v4u q[AHEAD];
+#pragma unroll
+          for (int a = 0; a < AHEAD; ++a) q[a] = z.load(u0 + a * NT, tid);
+#pragma unroll
+          for (int a = 0; a < AHEAD; ++a)
+            if (z.whole(u0 + a * NT + tid)) unit(q[a], u0 + a * NT + tid);
+        }
+      }
+      if (leader && !tail) find();
+      all = ds_join_all<NT>(all, p.scale, red[0]);           // its barrier is the list's too
+      if (tail) {
+        in = ds_join_all<NT>(in, p.scale, red[1]);
+        lse_rest = fmaf(ds_base(all.m), inv, logf(all.s));   // -inf without a value
+      }
     } else {
-      for (int u0 = tid; u0 < units; u0 += AHEAD * NT) {
-        v4u q[AHEAD];
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) q[a] = ds_load<T>(z, (u0 + a * NT) * VEC - mis, p.classes);
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a)
-          if (u0 + a * NT < units) unit(q[a], u0 + a * NT);
-      }
+      lse = p.stats_in[2 * row];
+      lse_rest = p.stats_in[2 * row + 1];
     }
-    all = ds_join_all<NT>(all, p.scale, red2[0]);
-    if (tail) {
-      in = ds_join_all<NT>(in, p.scale, red2[1]);
-      lse_rest = fmaf(ds_base(all.m), inv, logf(all.s));      // -inf without a value
-    }
-  } else {
-    lse = p.stats_in[2 * row];
-    lse_rest = p.stats_in[2 * row + 1];
-  }
-  // the sums of all classes
-  const DsSum whole = LOSS && tail ? ds_join(all, in, p.scale) : all;
-  if constexpr (LOSS) lse = fmaf(ds_base(whole.m), inv, logf(whole.s));
-  if (tail && lse_rest == -INFINITY) rest = 0.f;
+    // the sums of all classes
+    const DsSum whole = LOSS && tail ? ds_join(all, in, p.scale) : all;
+    if constexpr (LOSS) lse = fmaf(ds_base(whole.m), inv, logf(whole.s));
+    const DsList l = list;
+    const float rest = tail && lse_rest == -INFINITY ? 0.f : l.rest;
 
-  if constexpr (LOSS) {
-    float part = 0.f;
-    const float base = ds_base(whole.m), logw = logf(whole.s);
-    for (int j = tid; j < p.slots; j += NT) {
-      if (cls[j] < 0) continue;
-      const float logp = tail ? ps[j] : ps[j] - logs, w = expf(logp);
-      if (w != 0.f) part += w * (logp - ((ds_at(z + cls[j]) - base) * inv - logw));
-    }
-    part = ds_reduce<NT, false>(part, red);
-    if (tid == 0) {
-      if (rest != 0.f) {
-        // log of the rest's share: both sums under their own maxima
-        const float share = (ds_base(all.m) - base) * inv + (logf(all.s) - logw);
-        part += rest * (logf(rest) - share);
+    if constexpr (LOSS) {
+      if (leader) {
+        float part = 0.f;
+        const float base = ds_base(whole.m), logw = logf(whole.s);
+#pragma unroll 1
+        for (int j = tid; j < p.slots; j += 64) {
+          if (cls[j] < 0) continue;
+          const float logp = ps[j] - l.logs, w = expf(logp);
+          if (w != 0.f) part += w * (logp - ((zs[j] - base) * inv - logw));
+        }
+        part = lane_sum<64>(part);
+        if (tid == 0) {
+          if (rest != 0.f) {
+            // log of the rest's share: both sums under their own maxima
+            const float share = (ds_base(all.m) - base) * inv + (logf(all.s) - logw);
+            part += rest * (logf(rest) - share);
+          }
+          p.loss[row] = p.tau * p.tau * part;
+          if (p.stats) {
+            p.stats[2 * row] = lse;
+            p.stats[2 * row + 1] = tail ? lse_rest : 0.f;
+          }
+        }
       }
-      p.loss[row] = p.tau * p.tau * part;
-      if (p.stats) {
-        p.stats[2 * row] = lse;
-        p.stats[2 * row + 1] = tail ? lse_rest : 0.f;
-      }
     }
-  }
+    if constexpr (!GRAD) return;
 
-  if constexpr (GRAD) {
-    if constexpr (!LOSS) __syncthreads(); // the bitmap is complete
     const float g = (p.dloss ? p.dloss[row] : 1.f) * p.tau;
-    const bool dead = !any || g == 0.f;   // zeros, also where logits are no numbers
-    const float weight = tail ? sum + rest : 1.f;
+    const bool dead = !l.any || g == 0.f; // zeros, also where logits are no numbers
+    const float weight = l.weight + rest;
     // weight q = mul_in exp2(..) with at_in; weight q - rest q / q_rest = mul exp2(..) with at, one
     // exponential under the rest's own sum
     float at, mul, at_in, mul_in;
@@ -292,86 +332,120 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
       at_in = ds_base(whole.m);
       mul_in = weight / whole.s;
       at = tail ? ds_base(all.m) : at_in;
-      mul = !tail ? mul_in : lse_rest == -INFINITY ? 0.f : (weight * exp2f((at - at_in) * p.scale) * (all.s / whole.s) - rest) / all.s;
+      mul = !tail ? mul_in : lse_rest == -INFINITY ? 0.f : (weight * ds_exp2((at - at_in) * p.scale) * (all.s / whole.s) - rest) / all.s;
     } else {
       at_in = lse == -INFINITY ? 0.f : lse;
       mul_in = lse == -INFINITY ? NAN : weight;
       at = tail ? (lse_rest == -INFINITY ? 0.f : lse_rest) : at_in;
-      mul = !tail ? mul_in : lse_rest == -INFINITY ? 0.f : weight * exp2f((lse_rest - lse) * DS_LOG2E) - rest;
+      mul = !tail ? mul_in : lse_rest == -INFINITY ? 0.f : weight * ds_exp2((lse_rest - lse) * DS_LOG2E) - rest;
     }
     mul *= g;
     // of a logit: under a maximum of logits, or under a log of sums
     auto power = [&](float v, float under) {
-      return exp2f(LOSS ? (v - under) * p.scale : fmaf(v, inv, -under) * DS_LOG2E);
+      return ds_exp2(LOSS ? (v - under) * p.scale : fmaf(v, inv, -under) * DS_LOG2E);
     };
     T *dz = static_cast<T *>(p.dz) + row * p.ldd;
-    auto put = [&](const v4u &q, int at_unit) {
-      const int col = at_unit * VEC - mis;
-      T v[VEC];
+    auto put = [&](const v4u &q, int first) {    // of unit first + lane
+      float v[VEC];
+      if (dead) {
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[i] = ds_round<T>(dead ? 0.f : mul * power(ds_value<T>(q, i), at));
-      const uint32_t b = bits(at_unit);
-      if (!b && col >= 0 && col + VEC <= p.classes) {
-        v4u w;
+        for (int i = 0; i < VEC; ++i) v[i] = 0.f;
+      } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
-          else w[i] = (uint32_t)v[2 * i] | (uint32_t)v[2 * i + 1] << 16;
-        }
-        *reinterpret_cast<v4u_any *>(dz + col) = w;
+        for (int i = 0; i < VEC; ++i) v[i] = mul * power(ds_value<T>(q, i), at);
+      }
+      const uint32_t b = bits(first + tid);
+      char *base = reinterpret_cast<char *>(dz) - mis * (int)sizeof(T) + (int64_t)first * 16;
+      T *to = reinterpret_cast<T *>(base + 16 * (uint32_t)tid);
+      v4u w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+        else w[i] = (uint32_t)ds_round<T>(v[2 * i]) | (uint32_t)ds_round<T>(v[2 * i + 1]) << 16;
+      }
+      if (!b) {
+        *reinterpret_cast<v4u_any *>(to) = w;
         return;
       }
 #pragma unroll
       for (int i = 0; i < VEC; ++i)
-        if (!(b >> i & 1u) && col + i >= 0 && col + i < p.classes) dz[col + i] = v[i];
+        if (!(b >> i & 1u)) {
+          if constexpr (sizeof(T) == 4) to[i] = v[i];
+          else to[i] = (T)(w[i / 2] >> (16 * (i & 1)));
+        }
     };
+    if (segment == 0 && tid < z.edges) {
+      const int b = edge + mis;
+      if (!(map[b >> 5] >> (b & 31) & 1u)) dz[edge] = ds_round<T>(dead ? 0.f : mul * power(single, at));
+    }
+    const bool more = row + step < p.rows;
+    // the listed classes; slots of one class write the same value
+    if (leader && segment == 0) {
+#pragma unroll 1
+      for (int j = tid; j < p.slots; j += 64) {
+        const int c = cls[j];
+        if (c < 0) continue;
+        float w = 0.f;
+        if (l.twice) {
+          for (int i = 0; i < p.slots; ++i)
+            if (cls[i] == c) w += expf(ps[i] - l.logs);
+        } else {
+          w = expf(ps[j] - l.logs);
+        }
+        dz[c] = ds_round<T>(dead ? 0.f : g * (mul_in * power(zs[j], at_in) - w));
+      }
+    }
+    const DsRow<T> zn(z.z + (more ? step * p.ld : 0), p.classes);
     if constexpr (U > 0) {
+      if (more && leader) slot(row + step, tid, early_c, early_t);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (u * NT + tid < units) put(held[u], u * NT + tid);
+      for (int u = 0; u < U; ++u) {
+        if (z.whole(u * NT + tid)) put(held[u], u * NT);
+        if (more) held[u] = zn.load(u * NT, tid);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
-      for (int u0 = segment * AHEAD * NT + tid; u0 < units; u0 += p.segments * AHEAD * NT) {
+      for (int u0 = segment * AHEAD * NT; u0 < z.last; u0 += p.segments * AHEAD * NT) {
         v4u q[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) q[a] = ds_load<T>(z, (u0 + a * NT) * VEC - mis, p.classes);
+        for (int a = 0; a < AHEAD; ++a) q[a] = z.load(u0 + a * NT, tid);
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a)
-          if (u0 + a * NT < units) put(q[a], u0 + a * NT);
+          if (z.whole(u0 + a * NT + tid)) put(q[a], u0 + a * NT);
       }
     }
-    // the listed classes; slots of one class write the same value
-    if (segment) return;
-    for (int j = tid; j < p.slots; j += NT) {
-      const int c = cls[j];
-      if (c < 0) continue;
-      float w = 0.f;
-      if (twice) {
-        for (int i = 0; i < p.slots; ++i)
-          if (cls[i] == c) w += expf(tail ? ps[i] : ps[i] - logs);
-      } else {
-        w = expf(tail ? ps[j] : ps[j] - logs);
-      }
-      dz[c] = ds_round<T>(dead ? 0.f : g * (mul_in * power(ds_at(z + c), at_in) - w));
-    }
+    if (!more) return;
+    z = zn;
+    row += step;
+    __syncthreads();                      // the bitmap and the list are read
+    for (int i = tid; i < words; i += NT) map[i] = 0u;
+    __syncthreads();
   }
 }
 
-// Threads and units for a row: held in registers up to 64 of them a thread.
+// Threads and units for a row: held in registers up to 128 of them a thread.
 template <typename T, int WHAT>
 hipError_t ds_launch(DsParams p, hipStream_t s) {
-  const int64_t n = (p.classes + 2 * ds_vec<T>() - 2) / ds_vec<T>();   // wherever rows start
-  const size_t lds = WHAT & DS_GRAD || p.tail ? 4 * ((p.classes + ds_vec<T>() + 31) / 32) : 0;
+  constexpr int VEC = ds_vec<T>();
+  // units wherever rows start: behind 16 bytes all at the same place, or anywhere
+  const bool even = p.ld * sizeof(T) % 16 == 0 || p.rows == 1;
+  const int64_t mis = even ? (int64_t)(reinterpret_cast<uintptr_t>(p.z) % 16 / sizeof(T)) : VEC - 1;
+  const int64_t n = (p.classes + mis + VEC - 1) / VEC;
+  const size_t lds = WHAT & DS_GRAD || p.tail ? 4 * ((p.classes + VEC + 31) / 32) : 0;
   // gradients alone need nothing of the rest of the row: few rows are cut
   p.segments = WHAT == DS_GRAD ? (int)std::max<int64_t>(1, std::min((n + 4095) / 4096, DS_FILL / p.rows)) : 1;
-  const dim3 grid((unsigned)(p.rows * p.segments));
-#define SOAP_DS(NT, U)                                                                     \
-  if (U == 0 || n <= (int64_t)NT * U) {                                                    \
-    hipLaunchKernelGGL((distill_kernel<T, NT, U, WHAT>), grid, dim3(NT), lds, s, p);         \
-    return hipGetLastError();                                                              \
+#define SOAP_DS(NT, U, BLOCKS)                                                                                \
+  if (U == 0 || n <= (int64_t)NT * U) {                                                                       \
+    const dim3 grid((unsigned)(U ? std::min<int64_t>(p.rows, BLOCKS) : p.rows * p.segments));                 \
+    hipLaunchKernelGGL((distill_kernel<T, NT, U, WHAT>), grid, dim3(NT), lds, s, p);                          \
+    return hipGetLastError();                                                                                 \
   }
-  if constexpr (WHAT == (DS_LOSS | DS_GRAD)) { SOAP_DS(256, 4) SOAP_DS(1024, 4) SOAP_DS(1024, 8) SOAP_DS(1024, 16) }
-  if (n <= 1024) { SOAP_DS(256, 0) }
-  SOAP_DS(1024, 0)
+  if constexpr (WHAT == (DS_LOSS | DS_GRAD)) {
+    SOAP_DS(128, 4, 2560) SOAP_DS(256, 4, 1280) SOAP_DS(256, 8, 1024) SOAP_DS(512, 8, 512) SOAP_DS(1024, 8, 256)
+    if constexpr (sizeof(T) == 4) { SOAP_DS(1024, 16, 256) } else { SOAP_DS(512, 32, 256) }
+  }
+  if (n <= 1024) { SOAP_DS(256, 0, 0) }
+  SOAP_DS(1024, 0, 0)
 #undef SOAP_DS
 }
 

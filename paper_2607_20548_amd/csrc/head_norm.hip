@@ -154,108 +154,157 @@ __device__ __forceinline__ void hn_put(T *row, const HnUnit &u, const float *a, 
     hn_store<T>(row + u.c1, u.n1, b);
   }
 }
-template <int VEC, bool NEAR>
-__device__ __forceinline__ void hn_weights(const float *w, const HnUnit &u, float *a, float *b) {
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+template <int VEC>
+__device__ __forceinline__ void hn_floats(const float *w, int n, float *v) {   // ones past n
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) {
-    const int ia = NEAR ? 2 * i : i, ib = NEAR ? 2 * i + 1 : i;
-    const int nb = NEAR ? u.n0 + u.n1 : u.n1, cb = NEAR ? u.c0 : u.c1, na = NEAR ? nb : u.n0;
-    a[i] = w && ia < na ? w[u.c0 + ia] : 1.f;
-    b[i] = w && ib < nb ? w[cb + ib] : 1.f;
+  for (int i = 0; i < VEC; ++i) v[i] = 1.f;
+  if (n == VEC) {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4) {
+      const v4f_any q = *reinterpret_cast<const v4f_any *>(w + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i + j] = q[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (i < n) v[i] = w[i];
   }
 }
-template <int VEC>
-__device__ __forceinline__ void hn_angles(const HnParams &p, const HnUnit &u, int64_t token, float *c, float *s) {
-  const double pos = p.pos ? (double)p.pos[token] : (double)token;
+template <int VEC, bool NEAR>
+__device__ __forceinline__ void hn_weights(const float *w, const HnUnit &u, float *a, float *b) {
+  float lo[VEC], hi[VEC];
+  hn_floats<VEC>(w + u.c0, w ? u.n0 : 0, lo);
+  hn_floats<VEC>(w + u.c1, w ? u.n1 : 0, hi);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
-    c[i] = 1.f;
-    s[i] = 0.f;
-    if (i < u.turned) {
-      double t = pos * p.freq[u.turn + i] * 0.31830988618379067154;   // 1 / pi: half turns
-      t -= 2.0 * rint(0.5 * t);
-      sincospif((float)t, &s[i], &c[i]);
-    }
+    a[i] = !NEAR ? lo[i] : 2 * i < VEC ? lo[(2 * i) % VEC] : hi[(2 * i) % VEC];
+    b[i] = !NEAR ? hi[i] : 2 * i < VEC ? lo[(2 * i) % VEC + 1] : hi[(2 * i) % VEC + 1];
   }
 }
 
+// Cosine and sine of a token's pairs: formed once by the wave, one a lane, and handed to the
+// lanes through LDS (`own`: the wave's).
+template <int VEC, int UNITS>
+__device__ __forceinline__ void hn_angles(const HnParams &p, const HnUnit *un, int64_t token, float2 *own,
+                                          float (*c)[VEC], float (*s)[VEC]) {
+  const double pos = p.pos ? (double)p.pos[token] : (double)token;
+  const int half = p.rot / 2;
+  __builtin_amdgcn_wave_barrier();               // what was there is read
+  for (int i = threadIdx.x & 63; i < half; i += 64) {
+    double t = pos * p.freq[i] * 0.31830988618379067154;   // 1 / pi: half turns
+    t -= 2.0 * rint(0.5 * t);
+    float x, y;
+    sincospif((float)t, &x, &y);
+    own[i] = make_float2(y, x);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const bool in = i < un[u].turned;
+      const float2 v = own[in ? un[u].turn + i : 0];
+      c[u][i] = in ? v.x : 1.f;
+      s[u][i] = in ? v.y : 0.f;
+    }
+}
+
+// Chunks of heads in turn: those of the queries, then those of the keys.
+template <typename T, int LANES, int UNITS, bool NEAR>
+struct HnHeads {
+  static constexpr int SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1;
+  v4u q[IT][UNITS][2];
+  __device__ __forceinline__ void load(const T *x, int64_t stride, int heads, int part, int slot, const HnUnit *un) {
+#pragma unroll
+    for (int j = 0; j < IT; ++j) {
+      const T *row = x + (int64_t)min(part * IT * SLOTS + slot + j * SLOTS, heads - 1) * stride;
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        q[j][u][0] = hn_load<T>(row + un[u].c0, un[u].n0);
+        q[j][u][1] = hn_load<T>(row + un[u].c1, un[u].n1);
+      }
+    }
+  }
+};
+
 template <typename T, int LANES, int UNITS, bool NEAR>
 __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
-  constexpr int VEC = hn_vec<T>(), SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1;
+  using Heads = HnHeads<T, LANES, UNITS, NEAR>;
+  constexpr int VEC = hn_vec<T>(), SLOTS = Heads::SLOTS, IT = Heads::IT;
+  __shared__ float2 angle[HN_WAVES][LANES * UNITS * VEC];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x % 64 / LANES;
-  const int64_t task = (int64_t)blockIdx.x * HN_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave;
   if (task >= p.tasks) return;
   const int64_t token = task / p.split;
+  const HnSide d0 = p.side[0], d1 = p.side[1];
+  const int all = d0.chunks + d1.chunks;
   HnUnit un[UNITS];
-  float co[UNITS][VEC], si[UNITS][VEC];
 #pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    un[u] = hn_unit<VEC, NEAR>(p, u * LANES + lane);
-    hn_angles<VEC>(p, un[u], token, co[u], si[u]);
-  }
+  for (int u = 0; u < UNITS; ++u) un[u] = hn_unit<VEC, NEAR>(p, u * LANES + lane);
+  auto fetch = [&](Heads &to, int at) {
+    const bool k = at >= d0.chunks;
+    to.load(static_cast<const T *>(k ? d1.x : d0.x) + token * (k ? d1.xt : d0.xt), k ? d1.xh : d0.xh,
+            k ? d1.heads : d0.heads, at - (k ? d0.chunks : 0), slot, un);
+  };
+  int at = (int)(task - token * p.split);
+  Heads now, next;
+  fetch(now, at);
+  float co[UNITS][VEC], si[UNITS][VEC];
+  hn_angles<VEC, UNITS>(p, un, token, angle[wave], co, si);
   const float inv = 1.f / (float)p.dim;
-  int part = (int)(task - token * p.split);
 #pragma unroll 1
-  for (int k = 0; k < 2; ++k) {
-    const HnSide &d = p.side[k];
-    if (part >= d.chunks) {
-      part -= d.chunks;
-      continue;
-    }
+  for (; at < all; at += p.split) {
+    if (at + p.split < all) fetch(next, at + p.split);
+    const bool k = at >= d0.chunks;
+    const int heads = k ? d1.heads : d0.heads, h0 = (at - (k ? d0.chunks : 0)) * IT * SLOTS + slot;
+    T *y = static_cast<T *>(k ? d1.out : d0.out) + token * (k ? d1.ot : d0.ot);
+    const int64_t oh = k ? d1.oh : d0.oh;
     float wa[UNITS][VEC], wb[UNITS][VEC];
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) hn_weights<VEC, NEAR>(d.w, un[u], wa[u], wb[u]);
-    const T *x = static_cast<const T *>(d.x) + token * d.xt;
-    T *y = static_cast<T *>(d.out) + token * d.ot;
-#pragma unroll 1
-    for (; part < d.chunks; part += p.split) {
-      v4u q[IT][UNITS][2];
-      const int h0 = part * IT * SLOTS + slot;
+    for (int u = 0; u < UNITS; ++u) hn_weights<VEC, NEAR>(k ? d1.w : d0.w, un[u], wa[u], wb[u]);
 #pragma unroll
-      for (int j = 0; j < IT; ++j) {
-        const T *row = x + (int64_t)min(h0 + j * SLOTS, d.heads - 1) * d.xh;
+    for (int j = 0; j < IT; ++j) {
+      float a[UNITS][VEC], b[UNITS][VEC], sum = 0.f;
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          q[j][u][0] = hn_load<T>(row + un[u].c0, un[u].n0);
-          q[j][u][1] = hn_load<T>(row + un[u].c1, un[u].n1);
-        }
+      for (int u = 0; u < UNITS; ++u) {
+        hn_pairs<T, NEAR>(now.q[j][u][0], now.q[j][u][1], a[u], b[u]);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
       }
+      const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
+      const int h = h0 + j * SLOTS;
+      if (h >= heads) continue;
 #pragma unroll
-      for (int j = 0; j < IT; ++j) {
-        float a[UNITS][VEC], b[UNITS][VEC], sum = 0.f;
+      for (int u = 0; u < UNITS; ++u) {
+        float ya[VEC], yb[VEC];
 #pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          hn_pairs<T, NEAR>(q[j][u][0], q[j][u][1], a[u], b[u]);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
+        for (int i = 0; i < VEC; ++i) {
+          const float ha = a[u][i] * r * wa[u][i], hb = b[u][i] * r * wb[u][i];
+          ya[i] = ha * co[u][i] - hb * si[u][i];
+          yb[i] = hb * co[u][i] + ha * si[u][i];
         }
-        const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
-        const int h = h0 + j * SLOTS;
-        if (h >= d.heads) continue;
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-          float ya[VEC], yb[VEC];
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            const float ha = a[u][i] * r * wa[u][i], hb = b[u][i] * r * wb[u][i];
-            ya[i] = ha * co[u][i] - hb * si[u][i];
-            yb[i] = hb * co[u][i] + ha * si[u][i];
-          }
-          hn_put<T, NEAR>(y + (int64_t)h * d.oh, un[u], ya, yb);
-        }
+        hn_put<T, NEAR>(y + (int64_t)h * oh, un[u], ya, yb);
       }
     }
-    part -= d.chunks;
+    now = next;
   }
 }
 
 // out: dx (none if null); part: the sums of g h over the workgroup's tokens (none if null).
 template <typename T, int LANES, int UNITS, bool NEAR>
 __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
-  constexpr int VEC = hn_vec<T>(), SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1;
+  using Heads = HnHeads<T, LANES, UNITS, NEAR>;
+  constexpr int VEC = hn_vec<T>(), SLOTS = Heads::SLOTS, IT = Heads::IT;
   __shared__ float red[HN_WAVES][LANES * UNITS * VEC * 4];
+  float2 *angle = reinterpret_cast<float2 *>(red[threadIdx.x >> 6]);   // twice as many places as pairs
   const int lane = threadIdx.x % LANES, slot = threadIdx.x % 64 / LANES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const HnSide d0 = p.side[0], d1 = p.side[1];
+  const int all = d0.chunks + d1.chunks;
   HnUnit un[UNITS];
   float dw[2][UNITS][2][VEC];
 #pragma unroll
@@ -265,82 +314,89 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
     for (int i = 0; i < VEC; ++i) dw[0][u][0][i] = dw[0][u][1][i] = dw[1][u][0][i] = dw[1][u][1][i] = 0.f;
   }
   const float inv = 1.f / (float)p.dim;
-  for (int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave; task < p.tasks; task += (int64_t)gridDim.x * HN_WAVES) {
-    const int64_t token = task / p.split;
-    float co[UNITS][VEC], si[UNITS][VEC];
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u) hn_angles<VEC>(p, un[u], token, co[u], si[u]);
-    int part = (int)(task - token * p.split);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const HnSide &d = p.side[k];
-      const T *x = static_cast<const T *>(d.x) + token * d.xt, *dy = static_cast<const T *>(d.dy) + token * d.dt;
-      T *dx = static_cast<T *>(d.out) + token * d.ot;
-      float wa[UNITS][VEC], wb[UNITS][VEC];
-#pragma unroll
-      for (int u = 0; u < UNITS; ++u) hn_weights<VEC, NEAR>(d.w, un[u], wa[u], wb[u]);
+  const int64_t stride = (int64_t)gridDim.x * HN_WAVES;
+  int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave, token = task / p.split;
+  int at = (int)(task - token * p.split);
+  Heads x, dy;
+  auto fetch = [&](Heads &tx, Heads &td, int64_t tok, int c) {
+    const bool k = c >= d0.chunks;
+    const int part = c - (k ? d0.chunks : 0), heads = k ? d1.heads : d0.heads;
+    tx.load(static_cast<const T *>(k ? d1.x : d0.x) + tok * (k ? d1.xt : d0.xt), k ? d1.xh : d0.xh, heads, part, slot, un);
+    td.load(static_cast<const T *>(k ? d1.dy : d0.dy) + tok * (k ? d1.dt : d0.dt), k ? d1.dh : d0.dh, heads, part, slot, un);
+  };
+  float co[UNITS][VEC], si[UNITS][VEC];
+  bool fresh = true;                             // the angles are another token's
 #pragma unroll 1
-      for (; part < d.chunks; part += p.split) {
-        v4u q[IT][UNITS][2], e[IT][UNITS][2];
-        const int h0 = part * IT * SLOTS + slot;
+  while (task < p.tasks) {
+    fetch(x, dy, token, at);
+    if (fresh) hn_angles<VEC, UNITS>(p, un, token, angle, co, si);
+    const int64_t now = token;
+    const int c = at;
+    at += p.split;
+    fresh = at >= all;
+    if (fresh) {
+      task += stride;
+      token = task / p.split;
+      at = (int)(task - token * p.split);
+    }
+    const bool k = c >= d0.chunks;
+    const int heads = k ? d1.heads : d0.heads, h0 = (c - (k ? d0.chunks : 0)) * IT * SLOTS + slot;
+    T *dx = static_cast<T *>(k ? d1.out : d0.out);
+    const bool wanted = dx != nullptr;
+    dx += now * (k ? d1.ot : d0.ot);
+    const int64_t oh = k ? d1.oh : d0.oh;
+    float wa[UNITS][VEC], wb[UNITS][VEC];
 #pragma unroll
-        for (int j = 0; j < IT; ++j) {
-          const int64_t h = min(h0 + j * SLOTS, d.heads - 1);
+    for (int u = 0; u < UNITS; ++u) hn_weights<VEC, NEAR>(k ? d1.w : d0.w, un[u], wa[u], wb[u]);
+    auto process = [&](float (&sums)[UNITS][2][VEC]) {
 #pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            q[j][u][0] = hn_load<T>(x + h * d.xh + un[u].c0, un[u].n0);
-            q[j][u][1] = hn_load<T>(x + h * d.xh + un[u].c1, un[u].n1);
-            e[j][u][0] = hn_load<T>(dy + h * d.dh + un[u].c0, un[u].n0);
-            e[j][u][1] = hn_load<T>(dy + h * d.dh + un[u].c1, un[u].n1);
+      for (int j = 0; j < IT; ++j) {
+        const int h = h0 + j * SLOTS;
+        float a[UNITS][VEC], b[UNITS][VEC], ga[UNITS][VEC], gb[UNITS][VEC], sum = 0.f, dot = 0.f;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          hn_pairs<T, NEAR>(x.q[j][u][0], x.q[j][u][1], a[u], b[u]);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
+        }
+        const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
+        const bool live = h < heads;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          float ea[VEC], eb[VEC];
+          hn_pairs<T, NEAR>(dy.q[j][u][0], dy.q[j][u][1], ea, eb);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            a[u][i] *= r;
+            b[u][i] *= r;
+            const float ta = ea[i] * co[u][i] + eb[i] * si[u][i], tb = eb[i] * co[u][i] - ea[i] * si[u][i];
+            if (live) {
+              sums[u][0][i] = fmaf(ta, a[u][i], sums[u][0][i]);
+              sums[u][1][i] = fmaf(tb, b[u][i], sums[u][1][i]);
+            }
+            ga[u][i] = ta * wa[u][i];
+            gb[u][i] = tb * wb[u][i];
+            dot = fmaf(ga[u][i], a[u][i], fmaf(gb[u][i], b[u][i], dot));
           }
         }
+        dot = lane_sum<LANES>(dot) * inv;
+        if (!live || !wanted) continue;
 #pragma unroll
-        for (int j = 0; j < IT; ++j) {
-          const int h = h0 + j * SLOTS;
-          float a[UNITS][VEC], b[UNITS][VEC], ga[UNITS][VEC], gb[UNITS][VEC], sum = 0.f, dot = 0.f;
+        for (int u = 0; u < UNITS; ++u) {
 #pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            hn_pairs<T, NEAR>(q[j][u][0], q[j][u][1], a[u], b[u]);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
+          for (int i = 0; i < VEC; ++i) {
+            ga[u][i] = r * (ga[u][i] - a[u][i] * dot);
+            gb[u][i] = r * (gb[u][i] - b[u][i] * dot);
           }
-          const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
-          const bool live = h < d.heads;
-#pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-            float ea[VEC], eb[VEC];
-            hn_pairs<T, NEAR>(e[j][u][0], e[j][u][1], ea, eb);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              a[u][i] *= r;
-              b[u][i] *= r;
-              const float ta = ea[i] * co[u][i] + eb[i] * si[u][i], tb = eb[i] * co[u][i] - ea[i] * si[u][i];
-              if (live) {
-                dw[k][u][0][i] = fmaf(ta, a[u][i], dw[k][u][0][i]);
-                dw[k][u][1][i] = fmaf(tb, b[u][i], dw[k][u][1][i]);
-              }
-              ga[u][i] = ta * wa[u][i];
-              gb[u][i] = tb * wb[u][i];
-              dot = fmaf(ga[u][i], a[u][i], fmaf(gb[u][i], b[u][i], dot));
-            }
-          }
-          dot = lane_sum<LANES>(dot) * inv;
-          if (!live || !d.out) continue;
-#pragma unroll
-          for (int u = 0; u < UNITS; ++u) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              ga[u][i] = r * (ga[u][i] - a[u][i] * dot);
-              gb[u][i] = r * (gb[u][i] - b[u][i] * dot);
-            }
-            hn_put<T, NEAR>(dx + (int64_t)h * d.oh, un[u], ga[u], gb[u]);
-          }
+          hn_put<T, NEAR>(dx + (int64_t)h * oh, un[u], ga[u], gb[u]);
         }
       }
-      part -= d.chunks;
-    }
+    };
+    if (k) process(dw[1]);
+    else process(dw[0]);
   }
   if (!p.part) return;
+  __syncthreads();                               // the angles' place is free
 #pragma unroll
   for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -381,6 +437,7 @@ __global__ __launch_bounds__(HN_FIN) void head_norm_finish(const float *part, in
   const int at = blockIdx.x * C + threadIdx.x % C, s = threadIdx.x / C;
   float v = 0.f;
   if (at < 2 * dim)
+#pragma unroll 16
     for (int b = s; b < blocks; b += S) v += part[(int64_t)b * 2 * dim + at];
   red[threadIdx.x] = v;
   __syncthreads();
@@ -396,7 +453,7 @@ struct HnShape {
 };
 HnShape hn_shape(int64_t dim, int64_t rot, int vec) {
   const int64_t half = rot / 2, rest = (dim - rot) / 2, n = (half + vec - 1) / vec + (rest + vec - 1) / vec;
-  return {n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2};
+  return {n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2};
 }
 int64_t hn_blocks_bwd(int64_t tasks) { return std::min((tasks + HN_WAVES - 1) / HN_WAVES, HN_BLOCKS_BWD); }
 
@@ -427,7 +484,7 @@ hipError_t hn_launch(const HnParams &p, const HnShape &sh, hipStream_t s) {
     else hipLaunchKernelGGL((head_norm_fwd<T, L, U, NEAR>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
     return hipGetLastError();                                                                                 \
   }
-  SOAP_HN(8, 1) SOAP_HN(16, 1) SOAP_HN(32, 1) SOAP_HN(64, 1)
+  SOAP_HN(4, 1) SOAP_HN(8, 1) SOAP_HN(16, 1) SOAP_HN(32, 1) SOAP_HN(64, 1)
   if constexpr (sizeof(T) == 4) { SOAP_HN(64, 2) }
 #undef SOAP_HN
   return hipErrorInvalidValue;

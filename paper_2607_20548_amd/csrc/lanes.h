@@ -1,4 +1,4 @@
-// Reductions over aligned groups of 8, 16, 32 or 64 lanes of a wave, in registers
+// Reductions over aligned groups of 4, 8, 16, 32 or 64 lanes of a wave, in registers
 // (DPP moves up to 16 lanes, row and half swaps past them): a fixed tree, every lane
 // gets the result, all of a group's lanes the same bits.
 #pragma once
@@ -18,13 +18,13 @@ __device__ __forceinline__ uint32_t lane_dpp(uint32_t v) {
 
 template <int LANES, typename T, typename F>
 __device__ __forceinline__ T lane_reduce(T v, F op) {
-  static_assert(LANES >= 8 && LANES <= 64 && (LANES & (LANES - 1)) == 0, "8 to 64 lanes");
+  static_assert(LANES >= 4 && LANES <= 64 && (LANES & (LANES - 1)) == 0, "4 to 64 lanes");
   static_assert(sizeof(T) == 4, "32-bit values");
   auto cast = [](uint32_t u) { return __builtin_bit_cast(T, u); };
   auto bits = [](T t) { return __builtin_bit_cast(uint32_t, t); };
   v = op(v, cast(lane_dpp<0xB1>(bits(v))));
   v = op(v, cast(lane_dpp<0x4E>(bits(v))));
-  v = op(v, cast(lane_dpp<0x141>(bits(v))));
+  if constexpr (LANES >= 8) v = op(v, cast(lane_dpp<0x141>(bits(v))));
   if constexpr (LANES >= 16) v = op(v, cast(lane_dpp<0x140>(bits(v))));
   if constexpr (LANES >= 32) {
     const auto r = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
