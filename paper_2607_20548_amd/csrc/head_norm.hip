@@ -16,7 +16,8 @@
 // Bound by HBM (2 and 3 values moved per element): LANES lanes of a wave hold a head, each
 // UNITS x VEC pairs (16 bytes of either half, or 32 bytes of neighbours), so that the
 // rotation stays within a lane, and the 64 / LANES groups of a wave take different heads of
-// one token, whose angles are formed once for all of them.
+// one token, whose angles are formed once for all of them, or where a token has few heads a
+// token each.
 //
 // dw: every workgroup walks over tokens and writes the sums over its own, a second kernel adds
 // these in a fixed order.
@@ -184,21 +185,33 @@ __device__ __forceinline__ void hn_weights(const float *w, const HnUnit &u, floa
   }
 }
 
-// Cosine and sine of a token's pairs: formed once by the wave, one a lane, and handed to the
-// lanes through LDS (`own`: the wave's).
-template <int VEC, int UNITS>
+__device__ __forceinline__ float2 hn_turn(double position, double frequency) {
+  double t = position * frequency * 0.31830988618379067154;      // 1 / pi: half turns
+  t -= 2.0 * rint(0.5 * t);
+  float2 r;
+  sincospif((float)t, &r.y, &r.x);
+  return r;
+}
+// Cosine and sine of the token's pairs.  Where the wave has one token they are formed once, one a
+// lane, and handed to the lanes through LDS (`own`: the wave's); a lane's own token's by itself.
+template <int VEC, int UNITS, bool EACH>
 __device__ __forceinline__ void hn_angles(const HnParams &p, const HnUnit *un, int64_t token, float2 *own,
                                           float (*c)[VEC], float (*s)[VEC]) {
   const double pos = p.pos ? (double)p.pos[token] : (double)token;
+  if constexpr (EACH) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float2 v = i < un[u].turned ? hn_turn(pos, p.freq[un[u].turn + i]) : make_float2(1.f, 0.f);
+        c[u][i] = v.x;
+        s[u][i] = v.y;
+      }
+    return;
+  }
   const int half = p.rot / 2;
   __builtin_amdgcn_wave_barrier();               // what was there is read
-  for (int i = threadIdx.x & 63; i < half; i += 64) {
-    double t = pos * p.freq[i] * 0.31830988618379067154;   // 1 / pi: half turns
-    t -= 2.0 * rint(0.5 * t);
-    float x, y;
-    sincospif((float)t, &x, &y);
-    own[i] = make_float2(y, x);
-  }
+  for (int i = threadIdx.x & 63; i < half; i += 64) own[i] = hn_turn(pos, p.freq[i]);
   __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -212,15 +225,16 @@ __device__ __forceinline__ void hn_angles(const HnParams &p, const HnUnit *un, i
     }
 }
 
-// Chunks of heads in turn: those of the queries, then those of the keys.
-template <typename T, int LANES, int UNITS, bool NEAR>
+// Chunks of heads in turn: those of the queries, then those of the keys.  A wave's slots take
+// heads of one token, or (EACH) the same heads of a token each.
+template <typename T, int LANES, int UNITS, bool NEAR, bool EACH>
 struct HnHeads {
-  static constexpr int SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1;
+  static constexpr int SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1, STEP = EACH ? 1 : SLOTS, MANY = IT * STEP;
   v4u q[IT][UNITS][2];
   __device__ __forceinline__ void load(const T *x, int64_t stride, int heads, int part, int slot, const HnUnit *un) {
 #pragma unroll
     for (int j = 0; j < IT; ++j) {
-      const T *row = x + (int64_t)min(part * IT * SLOTS + slot + j * SLOTS, heads - 1) * stride;
+      const T *row = x + (int64_t)min(part * MANY + (EACH ? 0 : slot) + j * STEP, heads - 1) * stride;
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
         q[j][u][0] = hn_load<T>(row + un[u].c0, un[u].n0);
@@ -230,16 +244,17 @@ struct HnHeads {
   }
 };
 
-template <typename T, int LANES, int UNITS, bool NEAR>
+template <typename T, int LANES, int UNITS, bool NEAR, bool EACH>
 __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
-  using Heads = HnHeads<T, LANES, UNITS, NEAR>;
-  constexpr int VEC = hn_vec<T>(), SLOTS = Heads::SLOTS, IT = Heads::IT;
+  using Heads = HnHeads<T, LANES, UNITS, NEAR, EACH>;
+  constexpr int VEC = hn_vec<T>(), IT = Heads::IT, STEP = Heads::STEP, MANY = Heads::MANY;
+  constexpr int TOKENS = EACH ? Heads::SLOTS : 1;            // of a wave
   __shared__ float2 angle[HN_WAVES][LANES * UNITS * VEC];
   const int lane = threadIdx.x % LANES, slot = threadIdx.x % 64 / LANES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave;
   if (task >= p.tasks) return;
-  const int64_t token = task / p.split;
+  const int64_t group = task / p.split, mine = group * TOKENS + (EACH ? slot : 0), token = min(mine, p.tokens - 1);
   const HnSide d0 = p.side[0], d1 = p.side[1];
   const int all = d0.chunks + d1.chunks;
   HnUnit un[UNITS];
@@ -250,17 +265,17 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
     to.load(static_cast<const T *>(k ? d1.x : d0.x) + token * (k ? d1.xt : d0.xt), k ? d1.xh : d0.xh,
             k ? d1.heads : d0.heads, at - (k ? d0.chunks : 0), slot, un);
   };
-  int at = (int)(task - token * p.split);
+  int at = (int)(task - group * p.split);
   Heads now, next;
   fetch(now, at);
   float co[UNITS][VEC], si[UNITS][VEC];
-  hn_angles<VEC, UNITS>(p, un, token, angle[wave], co, si);
+  hn_angles<VEC, UNITS, EACH>(p, un, token, angle[wave], co, si);
   const float inv = 1.f / (float)p.dim;
 #pragma unroll 1
   for (; at < all; at += p.split) {
     if (at + p.split < all) fetch(next, at + p.split);
     const bool k = at >= d0.chunks;
-    const int heads = k ? d1.heads : d0.heads, h0 = (at - (k ? d0.chunks : 0)) * IT * SLOTS + slot;
+    const int heads = k ? d1.heads : d0.heads, h0 = (at - (k ? d0.chunks : 0)) * MANY + (EACH ? 0 : slot);
     T *y = static_cast<T *>(k ? d1.out : d0.out) + token * (k ? d1.ot : d0.ot);
     const int64_t oh = k ? d1.oh : d0.oh;
     float wa[UNITS][VEC], wb[UNITS][VEC];
@@ -276,8 +291,8 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
         for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
       }
       const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
-      const int h = h0 + j * SLOTS;
-      if (h >= heads) continue;
+      const int h = h0 + j * STEP;
+      if (h >= heads || mine >= p.tokens) continue;
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
         float ya[VEC], yb[VEC];
@@ -295,10 +310,11 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
 }
 
 // out: dx (none if null); part: the sums of g h over the workgroup's tokens (none if null).
-template <typename T, int LANES, int UNITS, bool NEAR>
+template <typename T, int LANES, int UNITS, bool NEAR, bool EACH>
 __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
-  using Heads = HnHeads<T, LANES, UNITS, NEAR>;
-  constexpr int VEC = hn_vec<T>(), SLOTS = Heads::SLOTS, IT = Heads::IT;
+  using Heads = HnHeads<T, LANES, UNITS, NEAR, EACH>;
+  constexpr int VEC = hn_vec<T>(), IT = Heads::IT, STEP = Heads::STEP, MANY = Heads::MANY;
+  constexpr int TOKENS = EACH ? Heads::SLOTS : 1;            // of a wave
   __shared__ float red[HN_WAVES][LANES * UNITS * VEC * 4];
   float2 *angle = reinterpret_cast<float2 *>(red[threadIdx.x >> 6]);   // twice as many places as pairs
   const int lane = threadIdx.x % LANES, slot = threadIdx.x % 64 / LANES;
@@ -315,8 +331,8 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
   }
   const float inv = 1.f / (float)p.dim;
   const int64_t stride = (int64_t)gridDim.x * HN_WAVES;
-  int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave, token = task / p.split;
-  int at = (int)(task - token * p.split);
+  int64_t task = (int64_t)blockIdx.x * HN_WAVES + wave, group = task / p.split;
+  int at = (int)(task - group * p.split);
   Heads x, dy;
   auto fetch = [&](Heads &tx, Heads &td, int64_t tok, int c) {
     const bool k = c >= d0.chunks;
@@ -328,19 +344,19 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
   bool fresh = true;                             // the angles are another token's
 #pragma unroll 1
   while (task < p.tasks) {
-    fetch(x, dy, token, at);
-    if (fresh) hn_angles<VEC, UNITS>(p, un, token, angle, co, si);
-    const int64_t now = token;
+    const int64_t mine = group * TOKENS + (EACH ? slot : 0), now = min(mine, p.tokens - 1);
+    fetch(x, dy, now, at);
+    if (fresh) hn_angles<VEC, UNITS, EACH>(p, un, now, angle, co, si);
     const int c = at;
     at += p.split;
     fresh = at >= all;
     if (fresh) {
       task += stride;
-      token = task / p.split;
-      at = (int)(task - token * p.split);
+      group = task / p.split;
+      at = (int)(task - group * p.split);
     }
     const bool k = c >= d0.chunks;
-    const int heads = k ? d1.heads : d0.heads, h0 = (c - (k ? d0.chunks : 0)) * IT * SLOTS + slot;
+    const int heads = k ? d1.heads : d0.heads, h0 = (c - (k ? d0.chunks : 0)) * MANY + (EACH ? 0 : slot);
     T *dx = static_cast<T *>(k ? d1.out : d0.out);
     const bool wanted = dx != nullptr;
     dx += now * (k ? d1.ot : d0.ot);
@@ -351,7 +367,7 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
     auto process = [&](float (&sums)[UNITS][2][VEC]) {
 #pragma unroll
       for (int j = 0; j < IT; ++j) {
-        const int h = h0 + j * SLOTS;
+        const int h = h0 + j * STEP;
         float a[UNITS][VEC], b[UNITS][VEC], ga[UNITS][VEC], gb[UNITS][VEC], sum = 0.f, dot = 0.f;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
@@ -360,7 +376,7 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
           for (int i = 0; i < VEC; ++i) sum = fmaf(a[u][i], a[u][i], fmaf(b[u][i], b[u][i], sum));
         }
         const float r = 1.f / sqrtf(lane_sum<LANES>(sum) * inv + p.eps);
-        const bool live = h < heads;
+        const bool live = h < heads && mine < p.tokens;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
           float ea[VEC], eb[VEC];
@@ -450,10 +466,18 @@ __global__ __launch_bounds__(HN_FIN) void head_norm_finish(const float *part, in
 
 struct HnShape {
   int lanes, units;
+  bool each;
 };
-HnShape hn_shape(int64_t dim, int64_t rot, int vec) {
-  const int64_t half = rot / 2, rest = (dim - rot) / 2, n = (half + vec - 1) / vec + (rest + vec - 1) / vec;
-  return {n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2};
+// Lanes of a head, and whether a wave's slots take a token each: where its steps are fewer by
+// a quarter, the heads of one token leaving slots idle.
+HnShape hn_shape(const HeadNormDesc &d) {
+  const int64_t vec = d.bf16 ? 8 : 4, half = d.rotary / 2, rest = (d.dim - d.rotary) / 2;
+  const int64_t n = (half + vec - 1) / vec + (rest + vec - 1) / vec;
+  HnShape r{n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2, false};
+  const int64_t slots = 64 / r.lanes, it = r.units == 1 ? 2 : 1, q = d.side[0].heads, k = d.side[1].heads;
+  auto steps = [&](int64_t each) { return (q + each - 1) / each + (k + each - 1) / each; };
+  r.each = slots > 1 && 5 * steps(it) * ((d.tokens + slots - 1) / slots) < 4 * steps(it * slots) * d.tokens;
+  return r;
 }
 int64_t hn_blocks_bwd(int64_t tasks) { return std::min((tasks + HN_WAVES - 1) / HN_WAVES, HN_BLOCKS_BWD); }
 
@@ -461,7 +485,8 @@ HnParams hn_params(const HeadNormDesc &d, const HnShape &sh) {
   HnParams p{};
   p.tokens = d.tokens; p.dim = (int)d.dim; p.rot = (int)d.rotary; p.eps = d.eps;
   p.pos = d.positions; p.freq = d.frequencies;
-  const int each = 64 / sh.lanes * (sh.units == 1 ? 2 : 1);
+  const int slots = 64 / sh.lanes, each = (sh.each ? 1 : slots) * (sh.units == 1 ? 2 : 1);
+  const int64_t groups = sh.each ? (d.tokens + slots - 1) / slots : d.tokens;
   for (int k = 0; k < 2; ++k) {
     const HeadNormSide &a = d.side[k];
     HnSide &b = p.side[k];
@@ -470,22 +495,23 @@ HnParams hn_params(const HeadNormDesc &d, const HnShape &sh) {
     b.xt = a.x_token; b.xh = a.x_head; b.dt = a.dy_token; b.dh = a.dy_head; b.ot = a.out_token; b.oh = a.out_head;
   }
   const int64_t chunks = p.side[0].chunks + p.side[1].chunks;
-  p.split = (int)std::max<int64_t>(1, std::min(chunks, HN_FEW / std::max<int64_t>(d.tokens, 1)));
-  p.tasks = chunks ? d.tokens * p.split : 0;
+  p.split = (int)std::max<int64_t>(1, std::min(chunks, HN_FEW / std::max<int64_t>(groups, 1)));
+  p.tasks = chunks ? groups * p.split : 0;
   return p;
 }
 
 template <bool BWD, typename T, bool NEAR>
 hipError_t hn_launch(const HnParams &p, const HnShape &sh, hipStream_t s) {
   const int64_t blocks = BWD ? hn_blocks_bwd(p.tasks) : (p.tasks + HN_WAVES - 1) / HN_WAVES;
-#define SOAP_HN(L, U)                                                                                         \
-  if (sh.lanes == L && sh.units == U) {                                                                       \
-    if constexpr (BWD) hipLaunchKernelGGL((head_norm_bwd<T, L, U, NEAR>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
-    else hipLaunchKernelGGL((head_norm_fwd<T, L, U, NEAR>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
-    return hipGetLastError();                                                                                 \
+#define SOAP_HN(L, U, E)                                                                                         \
+  if (sh.lanes == L && sh.units == U && sh.each == E) {                                                          \
+    if constexpr (BWD) hipLaunchKernelGGL((head_norm_bwd<T, L, U, NEAR, E>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
+    else hipLaunchKernelGGL((head_norm_fwd<T, L, U, NEAR, E>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
+    return hipGetLastError();                                                                                    \
   }
-  SOAP_HN(4, 1) SOAP_HN(8, 1) SOAP_HN(16, 1) SOAP_HN(32, 1) SOAP_HN(64, 1)
-  if constexpr (sizeof(T) == 4) { SOAP_HN(64, 2) }
+  SOAP_HN(4, 1, false) SOAP_HN(8, 1, false) SOAP_HN(16, 1, false) SOAP_HN(32, 1, false) SOAP_HN(64, 1, false)
+  SOAP_HN(4, 1, true) SOAP_HN(8, 1, true) SOAP_HN(16, 1, true) SOAP_HN(32, 1, true)
+  if constexpr (sizeof(T) == 4) { SOAP_HN(64, 2, false) }
 #undef SOAP_HN
   return hipErrorInvalidValue;
 }
@@ -505,12 +531,12 @@ size_t head_norm_part_bytes(int64_t tokens, int64_t dim) {
 }
 
 hipError_t launch_head_norm_fwd(const HeadNormDesc &d, hipStream_t s) {
-  const HnShape sh = hn_shape(d.dim, d.rotary, d.bf16 ? 8 : 4);
+  const HnShape sh = hn_shape(d);
   return hn_start<false>(d, hn_params(d, sh), sh, s);
 }
 
 hipError_t launch_head_norm_bwd(const HeadNormDesc &d, hipStream_t s) {
-  const HnShape sh = hn_shape(d.dim, d.rotary, d.bf16 ? 8 : 4);
+  const HnShape sh = hn_shape(d);
   HnParams p = hn_params(d, sh);
   const bool sums = d.side[0].dweight || d.side[1].dweight;
   p.part = sums ? d.part : nullptr;

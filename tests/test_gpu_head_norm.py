@@ -94,7 +94,8 @@ def check(q, k, wq, wk, pos, freq, near, dq=None, dk=None, dim=None):
 SIZES = [  # tokens, query heads, key heads, dim, rotary
     (1, 16, 16, 128, 128), (3, 1, 1, 2, 2), (5, 7, 3, 80, 40), (257, 4, 1, 64, 64), (33, 9, 2, 96, 96),
     (64, 2, 2, 256, 256), (7, 3, 5, 18, 6), (2, 5, 4, 512, 512), (9, 2, 3, 510, 2), (4, 64, 8, 128, 64),
-    (11, 3, 2, 112, 0), (600, 12, 4, 128, 128), (5000, 3, 1, 32, 32), (13, 2, 1, 34, 34), (6, 17, 0, 128, 128)]
+    (11, 3, 2, 112, 0), (600, 12, 4, 128, 128), (5000, 3, 1, 32, 32), (13, 2, 1, 34, 34), (6, 17, 0, 128, 128),
+    (1001, 1, 1, 128, 64), (77, 3, 1, 256, 256), (130, 1, 0, 64, 64), (65, 5, 3, 24, 12)]
 
 
 @pytest.mark.parametrize("near", [False, True])
