@@ -8,14 +8,19 @@
 // the operands of the next product; act works on fp32 sums forward and on the kept (rounded)
 // G and U backward.
 //
-// Every product is one kernel, product_tiles: C = sum over k of A(x, k) B(y, k), its operands
-// in memory either k-contiguous ([x][k]: X, H, dY, dG, dU, and the weights seen from their
-// rows) or x-contiguous ([k][x]: the weights forward, and both operands of the weights'
-// gradients), so that nothing is transposed beforehand.  Both come to LDS as they are in
-// memory, by loads that write LDS themselves, in blocks of 64 rows of 128 bytes, 16-byte units
-// permuted within a row so that no two of a read's lanes meet in a bank: k-contiguous
-// blocks are read 16 bytes of a row at a time, x-contiguous ones by the transposing reads,
-// which give a lane four k of its own x.
+// Products of up to 64 tokens are product_few's; all others are one kernel's, product_tiles: C =
+// sum over k of A(x, k) B(y, k), its operands in memory either k-contiguous ([x][k]: X, H, dY,
+// dG, dU, and the weights seen from their rows) or x-contiguous ([k][x]: the weights forward, and
+// both operands of the weights' gradients), so that nothing is transposed beforehand.  Both come to
+// LDS as they are in memory, by loads that write LDS themselves, in blocks of 64 rows of 128
+// bytes, 16-byte units permuted within a row so that no two of a read's lanes meet in a bank:
+// k-contiguous blocks are read 16 bytes of a row at a time, x-contiguous ones by the transposing
+// reads, which give a lane four k of its own x.
+//
+// What bounds it: the matrix instructions (8192 x 2048 x 8192: 1354 TFLOP/s for dX, a ring of
+// five operand slabs ahead of them), and where one product has an activation behind it, the
+// outputs that all compute units write at the same time (dG, dU, H from G and U: 350 us, of which
+// 246 without their bytes).
 //
 // Operands past their ends read as zeros (buffer bounds; units past the end of k are sent
 // out of bounds), so that sizes need no multiple of a tile; m, n and p are multiples of 8
@@ -338,16 +343,32 @@ struct GpPlan {
   int nb, splits;
 };
 constexpr int64_t GP_PARTS = (int64_t)256 * 256 * 256 * 4;   // bytes of all parts at most
+// By the time of either, in microseconds, from measured kernels (200 to 1500 tokens, 600 to 8192
+// wide, both tiles in 1 to 16 parts; within about 15 per cent): a slab of 128-tiles takes 0.62
+// where each has a compute unit of its own, 1.05 for two of them on one; of 256-tiles 1.1, and 1.5
+// with all compute units busy; starting and writing a tile 4.5 and 9; parts cost a launch and
+// their bytes written and read.
 GpPlan gp_plan(int64_t M, int64_t N, int64_t slabs, bool two, bool pairs) {
   const int64_t w = two ? 2 : 1;
-  auto tiles = [&](int64_t tb) { return (M + tb - 1) / tb * ((w * N + tb - 1) / tb) * (pairs ? 2 : 1); };
-  const int64_t large = tiles(256), small = tiles(128);
-  if (large >= 224) return {4, 1};
-  if (large >= 32 && slabs >= 16) {
-    const int64_t parts = std::min(256 / large, slabs / 8);
-    if (parts > 1) return {4, (int)parts};
+  GpPlan best{2, 1};
+  double least = 1e300;
+  for (int nb = 2; nb <= 4; nb += 2) {
+    const int64_t tb = 64 * nb, tiles = (M + tb - 1) / tb * ((w * N + tb - 1) / tb) * (pairs ? 2 : 1);
+    for (int64_t s = 1; s <= 16 && (s == 1 || slabs / s >= 3); ++s) {
+      const double bytes = 4.0 * s * M * N * w * (pairs ? 2 : 1);
+      const int64_t blocks = tiles * s, each = (slabs + s - 1) / s;
+      if (s > 1 && (bytes > GP_PARTS || blocks > 1024)) break;
+      double t;
+      if (nb == 4) t = (double)((blocks + 255) / 256) * (9 + each * (1.1 + 0.4 * std::min(1.0, blocks / 256.0)));
+      else t = blocks <= 256 ? 4.5 + 0.62 * each : (double)((blocks + 511) / 512) * (4.5 + 1.05 * each);
+      if (s > 1) t += (pairs ? 8 : 4) + 0.36e-6 * bytes;
+      if (t < least) {
+        least = t;
+        best = {nb, (int)s};
+      }
+    }
   }
-  return {2, (int)std::max<int64_t>(1, std::min(512 / small, slabs / 4))};
+  return best;
 }
 
 // The product, in parts of k and their sum where its tiles are few: into `part`.
@@ -404,21 +425,16 @@ hipError_t few_fwd(const GatedDesc &d, hipStream_t s) {
   FewDesc f;
   f.kind = FewDesc::GATE_UP; f.tokens = d.tokens; f.n = d.n; f.k = d.m; f.ldx = d.ldx; f.ldw = d.n;
   f.x[0] = d.x; f.w[0] = d.w_gate; f.w[1] = d.w_up; f.part = (float *)(w + 2 * wide(d.tokens, d.n));
-  f.splits = few_splits_of(f);
-  hipError_t e = launch_product_few(f, s);
-  if (e != hipSuccess) return e;
   GatedJoin j;
-  j.kind = GatedJoin::GATED; j.T = d.tokens; j.N = d.n; j.splits = f.splits; j.act = d.act; j.part = f.part;
-  j.out = hidden; j.low = low; j.keep_gate = d.gate; j.keep_up = d.up;
-  if ((e = launch_gated_join(j, s)) != hipSuccess) return e;
+  j.kind = GatedJoin::GATED; j.act = d.act; j.out = hidden; j.low = low; j.keep_gate = d.gate; j.keep_up = d.up;
+  const hipError_t e = launch_product_few(f, j, s);
+  if (e != hipSuccess) return e;
   FewDesc g;
   g.kind = FewDesc::HALVES; g.tokens = d.tokens; g.n = d.p; g.k = d.n; g.ldx = d.n; g.ldw = d.p;
   g.x[0] = hidden; g.x[1] = low; g.w[0] = d.w_down; g.part = f.part;
-  g.splits = few_splits_of(g);
-  if ((e = launch_product_few(g, s)) != hipSuccess) return e;
   j = GatedJoin();
-  j.T = d.tokens; j.N = d.p; j.splits = g.splits; j.part = g.part; j.out = d.y; j.ldo = d.ldy;
-  return launch_gated_join(j, s);
+  j.out = d.y; j.ldo = d.ldy;
+  return launch_product_few(g, j, s);
 }
 
 // dG, dU and H, and dX if it is wanted.
@@ -426,21 +442,16 @@ hipError_t few_bwd(const GatedDesc &d, uint16_t *dg, uint16_t *du, uint16_t *hid
   FewDesc f;
   f.kind = FewDesc::ROWS; f.tokens = d.tokens; f.n = d.n; f.k = d.p; f.ldx = d.lddy; f.ldw = d.p;
   f.x[0] = d.dy; f.w[0] = d.w_down; f.part = part;
-  f.splits = few_splits_of(f);
-  hipError_t e = launch_product_few(f, s);
-  if (e != hipSuccess) return e;
   GatedJoin j;
-  j.kind = GatedJoin::DGATED; j.T = d.tokens; j.N = d.n; j.splits = f.splits; j.act = d.act; j.part = part;
-  j.gate = d.gate; j.up = d.up; j.out = dg; j.out2 = du; j.hidden = hidden;
-  if ((e = launch_gated_join(j, s)) != hipSuccess || !d.dx) return e;
+  j.kind = GatedJoin::DGATED; j.act = d.act; j.gate = d.gate; j.up = d.up; j.out = dg; j.out2 = du; j.hidden = hidden;
+  const hipError_t e = launch_product_few(f, j, s);
+  if (e != hipSuccess || !d.dx) return e;
   f = FewDesc();
   f.kind = FewDesc::ROWS; f.tokens = d.tokens; f.n = d.m; f.k = d.n; f.ldx = d.n; f.ldw = d.n; f.segments = 2;
   f.x[0] = dg; f.x[1] = du; f.w[0] = d.w_gate; f.w[1] = d.w_up; f.part = part;
-  f.splits = few_splits_of(f);
-  if ((e = launch_product_few(f, s)) != hipSuccess) return e;
   j = GatedJoin();
-  j.T = d.tokens; j.N = d.m; j.splits = f.splits; j.part = part; j.out = d.dx; j.ldo = d.lddx;
-  return launch_gated_join(j, s);
+  j.out = d.dx; j.ldo = d.lddx;
+  return launch_product_few(f, j, s);
 }
 
 }  // namespace
@@ -450,8 +461,11 @@ size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bo
   if (!tokens) return 0;
   const size_t parts = backward ? std::max(few_bytes(tokens, n, 1), few_bytes(tokens, m, 1))
                                 : std::max(few_bytes(tokens, n, 2), few_bytes(tokens, p, 1));
-  const size_t tiled = tokens > GATED_FEW || backward ? (size_t)GP_PARTS : 0;   // its weights' gradients are always tiled
-  return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + std::max(parts, tiled);
+  // parts of tiles' products: at most 16, of three slabs each; more tokens never need less
+  int64_t tiled = tokens > GATED_FEW ? tokens * (backward ? std::max(m, n) : std::max(2 * n, p)) : 0;
+  if (backward && tokens > 5 * GP_KB) tiled = std::max(tiled, n * std::max(m, p));
+  tiled = std::min(GP_PARTS, 64 * tiled);
+  return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + std::max(parts, up256((size_t)tiled));
 }
 
 hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s) {

@@ -1,4 +1,4 @@
-// Products of few rows for the gated feed-forward block: Y = X W over up to 128 tokens, bound by
+// Products of few rows for the gated feed-forward block: Y = X W over up to 64 tokens, bound by
 // reading the weights once.
 //
 // A workgroup takes 64 columns (of both the gate's and up's weights forward) and a part of k,
@@ -6,9 +6,9 @@
 // tokens, through a ring of its own in LDS and waits for nobody: 30 to 36 KB of each are in flight
 // while it multiplies the oldest, 120 to 144 KB for a compute unit.  Weights come as they lie
 // (x-contiguous rows of k, read transposed, or k-contiguous rows), the matrix instructions take
-// them as rows and 32 tokens as columns.  The waves' sums meet in LDS, in their order; each part of
-// k writes fp32 sums, and a second kernel adds the parts in their order and applies the
-// activation or its gradient, or rounds.
+// them as rows and 32 tokens as columns.  The waves' sums meet in LDS, in their order, and go
+// through the activation or its gradient, or are rounded, there, or where columns are few and k
+// has parts, are written as fp32 sums that a second kernel adds in their order.
 //
 // H is kept in two bfloat16 halves (its rounding and what that leaves), which costs matrix
 // instructions that the weights' loads cover, and no bytes to speak of.
@@ -28,7 +28,68 @@ struct GfParams {
   int64_t ldx, ldw;
   int segments, splits, chunks;
   float *part;                   // [split][matrix][T][N]
+  GatedJoin out;                 // of a product in one part
 };
+
+// ------------------------------------------------- what is made of the sums
+enum { GJ_PART, GJ_GATED, GJ_DGATED, GJ_BF16, GJ_F32 };
+
+// Of eight columns of a row: x[0], and x[1] of up's.
+template <int MODE, int ACT>
+__device__ __forceinline__ void gj_finish(const GatedJoin &p, const float (*x)[8], int64_t row, int64_t col) {
+  const int64_t at = row * p.N + col;
+  if constexpr (MODE == GJ_BF16) {
+    v4u o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
+    *reinterpret_cast<v4u *>(p.out + row * p.ldo + col) = o;
+  } else if constexpr (MODE == GJ_F32) {
+    float *o = p.out_f32 + row * p.ldo + col;
+    *reinterpret_cast<float4 *>(o) = make_float4(x[0][0], x[0][1], x[0][2], x[0][3]);
+    *reinterpret_cast<float4 *>(o + 4) = make_float4(x[0][4], x[0][5], x[0][6], x[0][7]);
+  } else if constexpr (MODE == GJ_GATED) {
+    v4u og, ou, oh, ol;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float hv[2], lo[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        hv[w] = gp_act<ACT>(x[0][2 * e + w]).a * x[1][2 * e + w];
+        lo[w] = hv[w] - gp_float(gp_round(hv[w]));
+      }
+      og[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
+      ou[e] = gp_pack(x[1][2 * e], x[1][2 * e + 1]);
+      oh[e] = gp_pack(hv[0], hv[1]);
+      ol[e] = gp_pack(lo[0], lo[1]);
+    }
+    *reinterpret_cast<v4u *>(p.out + at) = oh;
+    if (p.low) *reinterpret_cast<v4u *>(p.low + at) = ol;
+    if (p.keep_gate) {
+      *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
+      *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
+    }
+  } else {
+    const v4u g = *reinterpret_cast<const v4u *>(p.gate + at), u = *reinterpret_cast<const v4u *>(p.up + at);
+    v4u og, ou, oh;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float a[2], b[2], o[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const float uv = gp_float((uint16_t)(u[e] >> 16 * w)), d = x[0][2 * e + w];
+        const GpAct f = gp_act<ACT>(gp_float((uint16_t)(g[e] >> 16 * w)));
+        a[w] = d * uv * f.d;
+        b[w] = d * f.a;
+        o[w] = f.a * uv;
+      }
+      og[e] = gp_pack(a[0], a[1]);
+      ou[e] = gp_pack(b[0], b[1]);
+      oh[e] = gp_pack(o[0], o[1]);
+    }
+    *reinterpret_cast<v4u *>(p.out + at) = og;
+    *reinterpret_cast<v4u *>(p.out2 + at) = ou;
+    *reinterpret_cast<v4u *>(p.hidden + at) = oh;
+  }}
 
 // WK: weights k-contiguous.  TWO: gate's and up's.  NX: halves of X.  RB: 32s of tokens.
 template <bool WK, bool TWO, int NX, int RB>
@@ -38,7 +99,8 @@ struct GfShape {
   static constexpr int LOADS = SLAB / 1024;
 };
 
-template <bool WK, bool TWO, int NX, int RB>
+// FIN: what is made of the sums (GJ_PART: they are written as they are).
+template <bool WK, bool TWO, int NX, int RB, int FIN, int ACT>
 __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
   using S = GfShape<WK, TWO, NX, RB>;
   constexpr int M = S::M, RING = S::RING;
@@ -141,7 +203,7 @@ __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
 
   // register r of a block: column 8 (r / 4) + 4 h + r % 4 of the weights, token xl
   float *stage = reinterpret_cast<float *>(lds);
-  constexpr int UNITS = M * GF_COLS / 8;
+  constexpr int UNITS = GF_COLS / 8;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     __syncthreads();
@@ -154,26 +216,32 @@ __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
           *reinterpret_cast<float4 *>(stage + (wave * 32 + xl) * SLD + t * GF_COLS + 32 * j + 2 * r + 4 * h) =
               make_float4(acc[t][j][b][r], acc[t][j][b][r + 1], acc[t][j][b][r + 2], acc[t][j][b][r + 3]);
     __syncthreads();
+    const int c = 8 * (tid % UNITS), token = 32 * b + tid / UNITS, n = n0 + c;   // 32 rows of 8 units
+    if (token >= p.T || n >= p.N) continue;
+    float o[M][8];
 #pragma unroll
-    for (int v = tid; v < 32 * UNITS; v += GP_THREADS) {
-      const int c = 8 * (v % UNITS), t = c / GF_COLS, token = 32 * b + v / UNITS, n = n0 + c % GF_COLS;
-      if (token >= p.T || n >= p.N) continue;
-      float o[8];
+    for (int t = 0; t < M; ++t)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        o[e] = stage[(v / UNITS) * SLD + c + e];
+        const float *x = stage + tid / UNITS * SLD + t * GF_COLS + c + e;
+        o[t][e] = x[0];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) o[e] += stage[(w * 32 + v / UNITS) * SLD + c + e];
+        for (int w = 1; w < 4; ++w) o[t][e] += x[w * 32 * SLD];
       }
-      float *to = p.part + (((int64_t)z * M + t) * p.T + token) * p.N + n;
-      *reinterpret_cast<float4 *>(to) = make_float4(o[0], o[1], o[2], o[3]);
-      *reinterpret_cast<float4 *>(to + 4) = make_float4(o[4], o[5], o[6], o[7]);
+    if constexpr (FIN == GJ_PART) {
+#pragma unroll
+      for (int t = 0; t < M; ++t) {
+        float *to = p.part + (((int64_t)z * M + t) * p.T + token) * p.N + n;
+        *reinterpret_cast<float4 *>(to) = make_float4(o[t][0], o[t][1], o[t][2], o[t][3]);
+        *reinterpret_cast<float4 *>(to + 4) = make_float4(o[t][4], o[t][5], o[t][6], o[t][7]);
+      }
+    } else {
+      gj_finish<FIN, ACT>(p.out, o, token, n);
     }
   }
 }
 
 // ------------------------------------------------- the parts' sums
-enum { GJ_GATED, GJ_DGATED, GJ_BF16, GJ_F32 };
 constexpr int GJ_THREADS = 256;
 
 // Eight columns of a row a thread.
@@ -195,58 +263,7 @@ __global__ __launch_bounds__(GJ_THREADS) void product_join(GatedJoin p) {
       x[t][4] += b.x; x[t][5] += b.y; x[t][6] += b.z; x[t][7] += b.w;
     }
   }
-  if constexpr (MODE == GJ_BF16) {
-    v4u o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
-    *reinterpret_cast<v4u *>(p.out + row * p.ldo + col) = o;
-  } else if constexpr (MODE == GJ_F32) {
-    float *o = p.out_f32 + row * p.ldo + col;
-    *reinterpret_cast<float4 *>(o) = make_float4(x[0][0], x[0][1], x[0][2], x[0][3]);
-    *reinterpret_cast<float4 *>(o + 4) = make_float4(x[0][4], x[0][5], x[0][6], x[0][7]);
-  } else if constexpr (MODE == GJ_GATED) {
-    v4u og, ou, oh, ol;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float hv[2], lo[2];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        hv[w] = gp_act<ACT>(x[0][2 * e + w]).a * x[1][2 * e + w];
-        lo[w] = hv[w] - gp_float(gp_round(hv[w]));
-      }
-      og[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
-      ou[e] = gp_pack(x[1][2 * e], x[1][2 * e + 1]);
-      oh[e] = gp_pack(hv[0], hv[1]);
-      ol[e] = gp_pack(lo[0], lo[1]);
-    }
-    *reinterpret_cast<v4u *>(p.out + at) = oh;
-    if (p.low) *reinterpret_cast<v4u *>(p.low + at) = ol;
-    if (p.keep_gate) {
-      *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
-      *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
-    }
-  } else {
-    const v4u g = *reinterpret_cast<const v4u *>(p.gate + at), u = *reinterpret_cast<const v4u *>(p.up + at);
-    v4u og, ou, oh;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float a[2], b[2], o[2];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const float uv = gp_float((uint16_t)(u[e] >> 16 * w)), d = x[0][2 * e + w];
-        const GpAct f = gp_act<ACT>(gp_float((uint16_t)(g[e] >> 16 * w)));
-        a[w] = d * uv * f.d;
-        b[w] = d * f.a;
-        o[w] = f.a * uv;
-      }
-      og[e] = gp_pack(a[0], a[1]);
-      ou[e] = gp_pack(b[0], b[1]);
-      oh[e] = gp_pack(o[0], o[1]);
-    }
-    *reinterpret_cast<v4u *>(p.out + at) = og;
-    *reinterpret_cast<v4u *>(p.out2 + at) = ou;
-    *reinterpret_cast<v4u *>(p.hidden + at) = oh;
-  }
+  gj_finish<MODE, ACT>(p, x, row, col);
 }
 
 template <int MODE, int ACT>
@@ -256,12 +273,11 @@ hipError_t gj_launch(const GatedJoin &p, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <bool WK, bool TWO, int NX>
+template <bool WK, bool TWO, int NX, int FIN, int ACT = 0>
 hipError_t gf_launch(const GfParams &p, hipStream_t s) {
   const dim3 grid((unsigned)(p.chunks * p.splits)), block(GP_THREADS);
-  if (p.T <= 32) hipLaunchKernelGGL((product_few<WK, TWO, NX, 1>), grid, block, 0, s, p);
-  else if (p.T <= 64) hipLaunchKernelGGL((product_few<WK, TWO, NX, 2>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((product_few<WK, TWO, NX, 4>), grid, block, 0, s, p);
+  if (p.T <= 32) hipLaunchKernelGGL((product_few<WK, TWO, NX, 1, FIN, ACT>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((product_few<WK, TWO, NX, 2, FIN, ACT>), grid, block, 0, s, p);
   return hipGetLastError();
 }
 
@@ -275,21 +291,36 @@ hipError_t launch_gated_join(const GatedJoin &p, hipStream_t s) {
   return p.act == SOAP_ACT_SILU ? gj_launch<GJ_DGATED, SOAP_ACT_SILU>(p, s) : gj_launch<GJ_DGATED, SOAP_ACT_GELU>(p, s);
 }
 
-// Parts of k: as many as give every compute unit a workgroup, of two slabs a wave at least.
+// Parts of k: as many as give compute units a workgroup each and none a second, of two slabs a
+// wave at least (4096 x 14336, 16 tokens: 224 workgroups for the columns alone 85 us, 448 90; 2048
+// x 8192: 128 37, 256 33).
 int few_splits(int64_t N, int64_t slabs) {
   const int64_t chunks = (N + GF_COLS - 1) / GF_COLS;
-  return (int)std::max<int64_t>(1, std::min((256 + chunks - 1) / chunks, slabs / 8));
+  return (int)std::max<int64_t>(1, std::min(256 / chunks, slabs / 8));
 }
 
-hipError_t launch_product_few(const FewDesc &d, hipStream_t s) {
+// The product, and what is made of it.
+hipError_t launch_product_few(const FewDesc &d, const GatedJoin &out, hipStream_t s) {
   GfParams p{};
   p.T = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.k;
   p.X[0] = d.x[0]; p.X[1] = d.x[1]; p.W[0] = d.w[0]; p.W[1] = d.w[1]; p.ldx = d.ldx; p.ldw = d.ldw;
-  p.segments = d.segments; p.splits = d.splits; p.chunks = (p.N + GF_COLS - 1) / GF_COLS; p.part = d.part;
-  if (d.kind == FewDesc::GATE_UP) return gf_launch<false, true, 1>(p, s);
-  if (d.kind == FewDesc::HALVES) return gf_launch<false, false, 2>(p, s);
-  return gf_launch<true, false, 1>(p, s);
+  p.segments = d.segments; p.chunks = (p.N + GF_COLS - 1) / GF_COLS; p.part = d.part;
+  p.splits = few_splits(d.n, (d.k + GF_KB - 1) / GF_KB * d.segments);
+  p.out = out;
+  p.out.T = d.tokens; p.out.N = d.n; p.out.part = d.part; p.out.splits = p.splits;
+  const bool silu = out.act == SOAP_ACT_SILU;
+  hipError_t e;
+  if (p.splits == 1) {
+    if (d.kind == FewDesc::GATE_UP)
+      return silu ? gf_launch<false, true, 1, GJ_GATED, SOAP_ACT_SILU>(p, s) : gf_launch<false, true, 1, GJ_GATED, SOAP_ACT_GELU>(p, s);
+    if (d.kind == FewDesc::HALVES) return gf_launch<false, false, 2, GJ_BF16>(p, s);
+    if (out.kind == GatedJoin::BF16) return gf_launch<true, false, 1, GJ_BF16>(p, s);
+    return silu ? gf_launch<true, false, 1, GJ_DGATED, SOAP_ACT_SILU>(p, s) : gf_launch<true, false, 1, GJ_DGATED, SOAP_ACT_GELU>(p, s);
+  }
+  if (d.kind == FewDesc::GATE_UP) e = gf_launch<false, true, 1, GJ_PART>(p, s);
+  else if (d.kind == FewDesc::HALVES) e = gf_launch<false, false, 2, GJ_PART>(p, s);
+  else e = gf_launch<true, false, 1, GJ_PART>(p, s);
+  return e != hipSuccess ? e : launch_gated_join(p.out, s);
 }
-int few_splits_of(const FewDesc &d) { return few_splits(d.n, (d.k + GF_KB - 1) / GF_KB * d.segments); }
 
 }  // namespace soap

@@ -347,20 +347,9 @@ struct GatedDesc {
   void *workspace = nullptr;
 };
 size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bool backward);
-// Its products over up to GATED_FEW tokens, as fp32 sums of parts of k ([part][matrix][token][n]):
-// GATE_UP x w[0] and x w[1]; HALVES (x[0] + x[1]) w[0]; ROWS the sum over segments of x[i] w[i]^T.
-constexpr int64_t GATED_FEW = 128;
-struct FewDesc {
-  enum Kind { GATE_UP, HALVES, ROWS } kind = GATE_UP;
-  int64_t tokens = 0, n = 0, k = 0, ldx = 0, ldw = 0;
-  const uint16_t *x[2] = {nullptr, nullptr}, *w[2] = {nullptr, nullptr};
-  int segments = 1, splits = 1;
-  float *part = nullptr;
-};
-int few_splits_of(const FewDesc &d);
-hipError_t launch_product_few(const FewDesc &d, hipStream_t s);
-// The sum of the parts, T x N (N a multiple of 8), and what is made of it.  BF16: out, F32: out_f32.  GATED: H into
-// out (and what its rounding leaves into low), G and U kept or null.  DGATED: out = dG, out2 = dU, hidden.
+// The sum of parts of a product, T x N (N a multiple of 8), each [matrix][T][N] floats, and what
+// is made of it.  BF16: out, F32: out_f32.  GATED: H into out (and what its rounding leaves into
+// low), G and U kept or null.  DGATED: out = dG, out2 = dU, hidden.
 struct GatedJoin {
   enum Kind { BF16, F32, GATED, DGATED } kind = BF16;
   int64_t T = 0, N = 0, ldo = 0;
@@ -371,6 +360,18 @@ struct GatedJoin {
   uint16_t *out = nullptr, *low = nullptr, *out2 = nullptr, *hidden = nullptr, *keep_gate = nullptr, *keep_up = nullptr;
 };
 hipError_t launch_gated_join(const GatedJoin &p, hipStream_t s);
+// Products over up to GATED_FEW tokens, part: for sums of parts of k.  GATE_UP x w[0] and x w[1]
+// (out.kind GATED); HALVES (x[0] + x[1]) w[0] (BF16); ROWS the sum over segments of x[i] w[i]^T (BF16 or
+// DGATED).  out: without T, N, part and splits.
+constexpr int64_t GATED_FEW = 64;
+struct FewDesc {
+  enum Kind { GATE_UP, HALVES, ROWS } kind = GATE_UP;
+  int64_t tokens = 0, n = 0, k = 0, ldx = 0, ldw = 0;
+  const uint16_t *x[2] = {nullptr, nullptr}, *w[2] = {nullptr, nullptr};
+  int segments = 1;
+  float *part = nullptr;
+};
+hipError_t launch_product_few(const FewDesc &d, const GatedJoin &out, hipStream_t s);
 hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s);
 hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s);
 
