@@ -1,0 +1,181 @@
+"""The dense layer (examples/dense_layer.py): heads' norm, gated feed-forward and distillation
+together, with layer norm and the optimizer steps.
+
+Its outputs and gradients are compared with those of the same layer in float64.  A rounding to
+bfloat16 moves a tensor by at most 2^-8 of itself (its norm), and the longest way from the weights
+to a gradient (x, the first norm, q, its norm, attention, o, a, the second norm, G and U, H, f, y, the
+third norm, logits; their gradients back) has 26 of them; if all moved it the same way, by 26
+2^-8 = 0.10 in all, the angle to the exact tensor would have a cosine of 0.995.  The bound is 0.99,
+for the layer's own gains of more than 1."""
+import os
+import sys
+
+import pytest
+import torch
+
+import paper_2607_20548_amd as soap
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+sys.path.insert(0, os.path.join(ROOT, "examples"))
+import dense_layer  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+SIZES = [  # batch, length, m, n, heads, kv heads, dim, classes, slots
+    (2, 40, 64, 136, 4, 2, 16, 100, 8), (1, 1, 128, 96, 3, 3, 32, 56, 1), (3, 77, 200, 328, 6, 1, 40, 1000, 20)]
+
+
+def cosine(a, b):
+    a, b = a.double().reshape(-1), b.double().reshape(-1)
+    return (a @ b / (a.norm() * b.norm())).item()
+
+
+def layer_norm(x, w):
+    var, mean = torch.var_mean(x, dim=1, correction=0, keepdim=True)
+    return (x - mean) * torch.rsqrt(var + 1e-5) * w
+
+
+def turned(x, w, at):
+    y = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6) * w
+    half = x.shape[-1] // 2
+    angle = at.double()[:, None] * 10000.0 ** (-torch.arange(half, device="cuda").double() / half)
+    c, s = angle.cos()[:, None], angle.sin()[:, None]
+    a, b = y[..., :half], y[..., half:]
+    return torch.cat([a * c - b * s, b * c + a * s], -1)
+
+
+def reference(layer, p, x, batch):
+    """The layer in the arithmetic of p and x."""
+    T, d = x.shape[0], layer.dim
+    at = torch.arange(T // batch, device="cuda").repeat(batch)
+    q, k, v = (layer_norm(x, p["norm1"]) @ p["qkv"]).view(T, -1, d).split([layer.heads] + 2 * [layer.kv_heads], 1)
+    q, k = turned(q, p["q"], at), turned(k, p["k"], at)
+    o = dense_layer.attention(*(t.reshape(batch, T // batch, -1, d) for t in (q, k, v)))
+    a = x + o.reshape(T, -1) @ p["o"]
+    h = layer_norm(a, p["norm2"])
+    y = a + (torch.nn.functional.silu(h @ p["gate_up"][0]) * (h @ p["gate_up"][1])) @ p["down"]
+    return layer_norm(y, p["norm3"]) @ p["out"]
+
+
+def make(batch, length, m, n, heads, kv, dim, classes, slots, **kw):
+    layer = dense_layer.DenseLayer(m, n, heads, kv, dim, classes, seed=3, **kw)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for v in layer.vectors.values():
+        v += 0.2 * torch.randn(v.shape, generator=g, device="cuda")
+    layer.cast()
+    x = torch.randn(batch * length, m, generator=g, device="cuda").to(BF)
+    teacher, index = (2 * torch.randn(batch * length, classes, generator=g, device="cuda")).topk(slots, 1)
+    return layer, x, index.int(), teacher
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+def test_gradients(sizes):
+    batch, length = sizes[:2]
+    layer, x, index, teacher = make(*sizes)
+    rows = batch * length
+    if rows > 1:
+        index[-rows // 8:] = -1                                # padding: nothing to learn from
+    weight = torch.linspace(0.5, 1.5, rows, device="cuda") / rows
+    logits = layer.forward(x, batch)
+    loss, dlogits = soap.Distillation(2.0).forward_backward(logits, index, teacher, weight)
+    got = layer.backward(dlogits)
+    p = {**layer.w, **layer.vectors, "x": x}
+    p = {name: t.double().requires_grad_(True) for name, t in p.items()}
+    z = reference(layer, p, p["x"], batch)
+    live = (index >= 0).any(1)
+    share = torch.softmax(teacher.double() / 2, 1)
+    logq = torch.log_softmax(z / 2, 1).gather(1, index.long().clamp_min(0))
+    want = torch.where(live, 4 * (share * (share.log() - logq)).sum(1), 0.0)
+    (want * weight.double()).sum().backward()
+    assert cosine(logits, z) >= 0.99 and cosine(loss, want) >= 0.99
+    assert not loss[~live].any() and not dlogits[~live].any()
+    for name, t in p.items():
+        assert got[name].shape == t.shape
+        if t.grad.norm() > 1e-3 * weight.norm():               # one token attends to itself alone
+            assert cosine(got[name], t.grad) >= 0.99, name
+
+
+def test_gradients_against_differences():
+    """The layer's loss moves along a direction as its gradients say: the loss in float64, the
+    gradients the layer's, whose angle above is at most acos 0.99."""
+    layer, x, index, teacher = make(*SIZES[0])
+    rows = x.shape[0]
+    weight = torch.full((rows,), 1.0 / rows, device="cuda")
+    _, dlogits = soap.Distillation(tail=False).forward_backward(layer.forward(x, 2), index, teacher, weight)
+    got = layer.backward(dlogits)
+    p = {name: t.double() for name, t in {**layer.w, **layer.vectors}.items()}
+    share = torch.softmax(teacher.double(), 1)
+
+    def loss(p):
+        logq = torch.log_softmax(reference(layer, p, x.double(), 2), 1).gather(1, index.long())
+        return (share * (share.log() - logq)).sum(1).mean()
+
+    for name in p:
+        step = 1e-4 * got[name].double() / got[name].double().norm() * p[name].norm()
+        slope = (loss({**p, name: p[name] + step}) - loss({**p, name: p[name] - step})) / (2 * step.norm())
+        # of a unit vector along g: |exact gradient| cos(angle)
+        assert abs(slope / got[name].double().norm() - 1) <= 0.15, name
+
+
+@pytest.mark.parametrize("sizes", [SIZES[0], SIZES[2]])
+def test_token_by_token(sizes):
+    """Logits of tokens that come one after the other, with the keys and values of those before,
+    are the whole sequences'."""
+    batch, length = sizes[:2]
+    layer, x, *_ = make(*sizes)
+    length = min(length, 12)
+    x = x.view(batch, -1, x.shape[1])[:, :length].contiguous()
+    whole = layer.forward(x.view(batch * length, -1), batch).view(batch, length, -1)
+    past = []
+    first = layer.forward(x[:, :5].reshape(5 * batch, -1), batch, past).view(batch, 5, -1)
+    rest = [layer.forward(x[:, t].contiguous(), batch, past) for t in range(5, length)]
+    got = torch.cat([first, torch.stack(rest, 1)], 1)
+    assert past[0].shape[1] == length
+    # both are the same sums, rounded to bfloat16 in the same places: 13 roundings either way
+    for t in range(length):
+        assert cosine(got[:, t], whole[:, t]) >= 1 - (26 * 2.0 ** -8) ** 2 / 2
+
+
+@pytest.mark.parametrize("optimizer", ["muon", "soap"])
+def test_it_runs(optimizer):
+    losses = dense_layer.train(2, 24, 64, 128, 4, 2, 16, 200, 8, 4, optimizer=optimizer, lr=0.05)
+    assert len(losses) == 4 and all(v == v and 0 < v < 100 for v in losses)
+
+
+def test_a_step_in_a_graph():
+    """Forward and backward of the three operators captured once and replayed over other inputs,
+    with eager work between, give the eager bits."""
+    T, heads, dim, classes = 70, 4, 32, 136
+    randn = lambda seed, *s: torch.randn(s, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")  # noqa: E731
+    m = heads * dim
+    turn = soap.HeadNorm(dim, 1 + 0.1 * randn(1, dim), None)
+    block = soap.GatedFeedForward(*((0.1 * randn(i, *s)).to(BF) for i, s in ((2, (m, 200)), (3, (m, 200)), (4, (200, classes)))))
+    distill = soap.Distillation(1.5, tail=True)
+    x = randn(5, T, heads, dim).to(BF)
+    index = randn(6, T, classes).topk(5, 1)[1].int()
+    teacher = torch.log_softmax(randn(7, T, 9), 1)[:, :5].contiguous()
+    at = torch.arange(T, device="cuda", dtype=torch.int32)
+
+    def run():
+        y, _ = turn.forward(x, None, at)
+        z, gate, up = block.forward(y.view(T, m))
+        loss, dz = distill.forward_backward(z, index, teacher)
+        dy, *dw = block.backward(dz, y.view(T, m), gate, up)
+        dx, _, dweight, _ = turn.backward(dy.view(T, heads, dim), None, x, None, at)
+        return [loss, dx, dweight, *dw]
+
+    run()
+    torch.cuda.synchronize()
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(run())
+    for i in range(4):
+        x.copy_(randn(20 + i, T, heads, dim))
+        at.add_(1000)
+        for g in graphs:
+            g.replay()
+        want = run()
+        torch.cuda.synchronize()
+        for out in outs:
+            assert all(torch.equal(a, b) for a, b in zip(want, out)), i
