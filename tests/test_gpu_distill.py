@@ -119,6 +119,15 @@ def test_sizes(rows, classes, slots, dtype, tail):
     check(*make(rows, classes, slots, dtype, rows + classes, tail=tail), tail=tail)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("classes", [1023, 1024, 1025, 2048, 2056, 2560, 2561, 4095, 4096, 5120, 5121, 8192, 8200, 8201, 16384, 16392])
+def test_many_rows(classes, dtype):
+    """More rows than workgroups, which hold a row and fetch the next, on both sides of each of their
+    widths."""
+    check(*make(1500, classes, 12, dtype, classes), tail=False)
+    check(*make(530, classes, 12, dtype, classes, tail=True), tail=True)
+
+
 @pytest.mark.parametrize("tau", [0.05, 0.5, 2.0, 30.0])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_temperatures(dtype, tau):
