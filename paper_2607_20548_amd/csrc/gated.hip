@@ -34,7 +34,6 @@ namespace soap {
 namespace {
 
 constexpr int GP_KB = 64;                        // k of a slab
-constexpr int GP_RING = 5;                       // operands' slabs in LDS
 constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows in LDS
 
 enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART };
@@ -54,14 +53,14 @@ struct GpParams {
 };
 
 // NB: blocks of 32 x 32 on a side of a wave's share; tiles of 64 NB.  ACT: of the epilogues
-// with an activation.  TWO: columns of both gate and up.
-template <bool AK, bool BK, int EPI, int NB, int ACT, bool TWO>
-__global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpParams p) {
+// with an activation.  TWO: columns of both gate and up.  RING: operands' slabs in LDS (odd).
+template <bool AK, bool BK, int EPI, int NB, int ACT, bool TWO, int RING>
+__global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void product_tiles(GpParams p) {
   constexpr int TB = 64 * NB, SUB = TB / 64, OP = SUB * GP_BLOCK, LOADS = 2 * SUB;
   constexpr int SLD = TB + 4;                    // staging row of the epilogue, floats
   constexpr int BAND = 64;
-  static_assert(2 * BAND * SLD * 4 <= GP_RING * OP, "two of the epilogue's bands fit the ring");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[GP_RING * OP];
+  static_assert(2 * BAND * SLD * 4 <= RING * OP, "two of the epilogue's bands fit the ring");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[RING * OP];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1, xl = lane & 31, h = lane >> 5;
 
@@ -100,9 +99,9 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   const int nk1 = (p.K + GP_KB - 1) / GP_KB, all = nk1 * p.segments;
   const int s0 = (int)((int64_t)blockIdx.y * all / p.splits), nk = (int)((int64_t)(blockIdx.y + 1) * all / p.splits) - s0;
 
-  // A slab of A and one of B take a place each of a ring of five, in the order A0 B0 A1 B1 ..: what
+  // A slab of A and one of B take a place each of a ring, in the order A0 B0 A1 B1 ..: of five, what
   // slab k frees takes B of slab k + 2, which then has a slab's time to arrive, and A of slab k + 3,
-  // which has two.
+  // which has two; of nine, two slabs more.
   struct Stream {
     GpSource s0, s1;
     v4i r0, r1;
@@ -130,7 +129,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     if (TWO && !is_a) s.s1.next();
     s.left -= GP_KB;
     ++s.slab;
-    s.place = s.place >= 3 ? s.place - 3 : s.place + 2;
+    s.place = s.place >= RING - 2 ? s.place - (RING - 2) : s.place + 2;
   };
   auto load = [&](bool is_a, int i) {
     if (is_a) gp_load(sa.r0, sa.to + 4096 * i, AK ? offa[i] | sa.dead : offa[i]);
@@ -212,7 +211,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   // one that it does not take yet holds its wave's matrix instructions up.
   constexpr int L1 = 2 * LOADS * 5 / 16, L2 = 2 * LOADS * 10 / 16, L3 = 2 * LOADS * 13 / 16;
 #pragma unroll
-  for (int u = 0; u < 3; ++u) {                  // A0, B0, A1
+  for (int u = 0; u < RING - 2; ++u) {           // A0, B0, A1
     if (u & 1) begin(sb, false);
     else begin(sa, true);
 #pragma unroll
@@ -222,7 +221,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
   begin(sa, true);
 #pragma unroll
   for (int v = 0; v < L1; ++v) load(v >= LOADS, v % LOADS);
-  GP_ARRIVED(LOADS + L1);
+  GP_ARRIVED((RING - 4) * LOADS + L1);
   if constexpr (EPI == GP_DGATED) {
 #pragma unroll
     for (int v = 0; v < 2 * EACH; ++v) kept(v / EACH, v / EACH, v % EACH);
@@ -235,12 +234,12 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 ? 1 : 2) void product_tiles(GpP
     step(0, 1, L1, L2);
     step(1, 2, L2, L3);
     step(0, 3, L3, 2 * LOADS);
-    GP_ARRIVED(LOADS);
+    GP_ARRIVED((RING - 4) * LOADS);
     begin(sb, false);
     begin(sa, true);
-    pa = pa >= 3 ? pa - 3 : pa + 2;
+    pa = pa >= RING - 2 ? pa - (RING - 2) : pa + 2;
     la = lds + pa * OP;
-    lb = pa == 4 ? lds : la + OP;
+    lb = pa == RING - 1 ? lds : la + OP;
     step(1, 0, 0, L1);
   }
   GP_ARRIVED(0);
@@ -333,8 +332,10 @@ hipError_t gp_tiles(GpParams p, hipStream_t s) {
   p.tiles_m = (p.M + TB - 1) / TB;
   const int width = TWO ? TB / 2 : TB;
   p.tiles_n = (p.N + width - 1) / width * (p.pairs ? 2 : 1);
-  hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO>), dim3((unsigned)p.tiles_m * p.tiles_n, (unsigned)p.splits),
-                     dim3(GP_THREADS), 0, s, p);
+  const dim3 grid((unsigned)p.tiles_m * p.tiles_n, (unsigned)p.splits), block(GP_THREADS);
+  if (NB == 2 && (int64_t)grid.x * grid.y <= 256)
+    hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, NB == 2 ? 9 : 5>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 5>), grid, block, 0, s, p);
   return hipGetLastError();
 }
 
