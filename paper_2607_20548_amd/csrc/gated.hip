@@ -38,13 +38,22 @@ constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows 
 
 enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART };
 
+struct GpOther {               // product over the same k
+  int M, N, tiles_m, tiles_n;
+  const uint16_t *A, *B;
+  void *C;
+  int64_t lda, ldb, ldc;
+};
+
 struct GpParams {
   int M, N, K;                 // N: of one matrix; K: of one segment
-  const uint16_t *A[2], *B[2]; // B[1]: up's weights or gradients; A[1]: the second segment of k
+  const uint16_t *A[2], *B[2]; // [1]: up's weights, or the second segment of k
   int64_t lda, ldb;
   int segments;                // of k, each with operands of its own
   int splits;                  // parts of k, the grid's y; more than one write fp32 sums
-  int tiles_m, tiles_n, pairs; // pairs: B and C by the tile's column (the second half: [1])
+  int tiles_m, tiles_n;
+  int others;                  // of the weights' gradients: one launch takes all three
+  GpOther other[2];
   void *C[2];                  // part: [part][matrix][M][N] floats
   int64_t ldc;
   // gated: C[0] the product, kept G and U (or null); dgated: C[0] = dG, C[1] = dU, H
@@ -67,18 +76,24 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
   // the tile: a contiguous run for each XCD, eight tiles of rows by all columns at a time
   int tm, tn;
   {
-    const int nt = p.tiles_m * p.tiles_n, q = nt >> 3, r = nt & 7, x = blockIdx.x & 7;
-    const int t = x * q + min(x, r) + (blockIdx.x >> 3);
+    const int nt = gridDim.x, q = nt >> 3, r = nt & 7, x = blockIdx.x & 7;
+    int t = x * q + min(x, r) + (blockIdx.x >> 3);
+    if constexpr (!AK && !BK) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (i < p.others && t >= p.tiles_m * p.tiles_n) {
+          t -= p.tiles_m * p.tiles_n;
+          const GpOther o = p.other[i];
+          p.M = o.M; p.N = o.N; p.tiles_m = o.tiles_m; p.tiles_n = o.tiles_n;
+          p.A[0] = o.A; p.B[0] = o.B; p.C[0] = o.C; p.lda = o.lda; p.ldb = o.ldb; p.ldc = o.ldc;
+        } else {
+          break;
+        }
+    }
     const int group = t / (8 * p.tiles_n), first = 8 * group, size = min(p.tiles_m - first, 8);
     const int in = t - group * 8 * p.tiles_n;
     tm = __builtin_amdgcn_readfirstlane(first + in % size);
     tn = __builtin_amdgcn_readfirstlane(in / size);
-  }
-  int which = 0;
-  if (p.pairs) {
-    const int half = p.tiles_n >> 1;
-    which = tn >= half;
-    tn -= which ? half : 0;
   }
   const int m0 = tm * TB, n0 = tn * (TWO ? TB / 2 : TB);
   const int64_t lda2 = 2 * p.lda, ldb2 = 2 * p.ldb;
@@ -115,7 +130,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
     if (s.slab == s0 || (p.segments > 1 && s.slab == nk1)) {
       const int seg = p.segments > 1 && s.slab >= nk1, at = s.slab - (seg ? nk1 : 0);
       if (is_a) s.s0.start(p.A[seg], AK, m0, p.M, p.K, lda2, GP_KB);
-      else s.s0.start(seg || which ? p.B[1] : p.B[0], BK, n0, p.N, p.K, ldb2, GP_KB);
+      else s.s0.start(p.B[seg], BK, n0, p.N, p.K, ldb2, GP_KB);
       if (TWO && !is_a) s.s1.start(p.B[1], BK, n0, p.N, p.K, ldb2, GP_KB);
       s.s0.next(at);
       if (TWO && !is_a) s.s1.next(at);
@@ -287,7 +302,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
             *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
           }
         } else if constexpr (EPI == GP_F32 || EPI == GP_PART) {
-          float *o = EPI == GP_F32 ? static_cast<float *>(p.C[which]) + at
+          float *o = EPI == GP_F32 ? static_cast<float *>(p.C[0]) + at
                                    : static_cast<float *>(p.C[0]) +
                                          ((int64_t)blockIdx.y * (TWO ? 2 : 1) + second) * p.M * p.N + (int64_t)row * p.N + col;
           *reinterpret_cast<float4 *>(o) = make_float4(x[0], x[1], x[2], x[3]);
@@ -296,7 +311,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
           v4u o;
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = gp_pack(x[2 * e], x[2 * e + 1]);
-          *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[which]) + at) = o;
+          *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[0]) + at) = o;
         } else {
           v4u og, ou, oh;
 #pragma unroll
@@ -329,17 +344,24 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
 template <bool AK, bool BK, int EPI, int NB, int ACT, bool TWO>
 hipError_t gp_tiles(GpParams p, hipStream_t s) {
   constexpr int TB = 64 * NB;
-  p.tiles_m = (p.M + TB - 1) / TB;
   const int width = TWO ? TB / 2 : TB;
-  p.tiles_n = (p.N + width - 1) / width * (p.pairs ? 2 : 1);
-  const dim3 grid((unsigned)p.tiles_m * p.tiles_n, (unsigned)p.splits), block(GP_THREADS);
-  if (NB == 2 && (int64_t)grid.x * grid.y <= 256)
+  p.tiles_m = (p.M + TB - 1) / TB;
+  p.tiles_n = (p.N + width - 1) / width;
+  int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  for (int i = 0; i < p.others; ++i) {
+    GpOther &o = p.other[i];
+    o.tiles_m = (o.M + TB - 1) / TB;
+    o.tiles_n = (o.N + TB - 1) / TB;
+    tiles += (int64_t)o.tiles_m * o.tiles_n;
+  }
+  const dim3 grid((unsigned)tiles, (unsigned)p.splits), block(GP_THREADS);
+  if (NB == 2 && tiles * p.splits <= 256)
     hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, NB == 2 ? 9 : 5>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 5>), grid, block, 0, s, p);
   return hipGetLastError();
 }
 
-// Tiles of a product of M x N (of two matrices) and the parts of k that each is summed in.
+// Tiles of a product (64 nb on a side) and the parts of k that each is summed in.
 struct GpPlan {
   int nb, splits;
 };
@@ -347,22 +369,26 @@ constexpr int64_t GP_PARTS = (int64_t)256 * 256 * 256 * 4;   // bytes of all par
 // By the time of either, in microseconds, from measured kernels (200 to 1500 tokens, 600 to 8192
 // wide, both tiles in 1 to 16 parts; within about 15 per cent): a slab of 128-tiles takes 0.62
 // where each has a compute unit of its own, 1.05 for two of them on one; of 256-tiles 1.1, and 1.5
-// with all compute units busy; starting and writing a tile 4.5 and 9; parts cost a launch and
-// their bytes written and read.
-GpPlan gp_plan(int64_t M, int64_t N, int64_t slabs, bool two, bool pairs) {
-  const int64_t w = two ? 2 : 1;
+// with all compute units busy; starting and writing a tile 4.5 and 9; parts cost a launch for each
+// product and their bytes written and read.
+GpPlan gp_plan(const GpParams &p, bool two) {
+  const int64_t w = two ? 2 : 1, slabs = (int64_t)((p.K + GP_KB - 1) / GP_KB) * p.segments;
   GpPlan best{2, 1};
   double least = 1e300;
   for (int nb = 2; nb <= 4; nb += 2) {
-    const int64_t tb = 64 * nb, tiles = (M + tb - 1) / tb * ((w * N + tb - 1) / tb) * (pairs ? 2 : 1);
+    const int64_t tb = 64 * nb;
+    int64_t tiles = (p.M + tb - 1) / tb * ((w * p.N + tb - 1) / tb), values = (int64_t)p.M * p.N * w;
+    for (int i = 0; i < p.others; ++i) {
+      tiles += (p.other[i].M + tb - 1) / tb * ((p.other[i].N + tb - 1) / tb);
+      values += (int64_t)p.other[i].M * p.other[i].N;
+    }
     for (int64_t s = 1; s <= 16 && (s == 1 || slabs / s >= 3); ++s) {
-      const double bytes = 4.0 * s * M * N * w * (pairs ? 2 : 1);
-      const int64_t blocks = tiles * s, each = (slabs + s - 1) / s;
+      const int64_t blocks = tiles * s, each = (slabs + s - 1) / s, bytes = 4 * s * values;
       if (s > 1 && (bytes > GP_PARTS || blocks > 1024)) break;
       double t;
       if (nb == 4) t = (double)((blocks + 255) / 256) * (9 + each * (1.1 + 0.4 * std::min(1.0, blocks / 256.0)));
       else t = blocks <= 256 ? 4.5 + 0.62 * each : (double)((blocks + 511) / 512) * (4.5 + 1.05 * each);
-      if (s > 1) t += (pairs ? 8 : 4) + 0.36e-6 * bytes;
+      if (s > 1) t += 4 * (1 + p.others) + 0.36e-6 * bytes;
       if (t < least) {
         least = t;
         best = {nb, (int)s};
@@ -372,44 +398,42 @@ GpPlan gp_plan(int64_t M, int64_t N, int64_t slabs, bool two, bool pairs) {
   return best;
 }
 
-// The product, in parts of k and their sum where its tiles are few: into `part`.
+// The products, in parts of k and their sum where tiles are few: into `part`.
 template <bool AK, bool BK, int EPI, int ACT = SOAP_ACT_SILU>
 hipError_t gp_launch(GpParams p, float *part, hipStream_t s) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
   constexpr bool TWO = EPI == GP_GATED;
-  const GpPlan plan = gp_plan(p.M, p.N, (int64_t)((p.K + GP_KB - 1) / GP_KB) * p.segments, TWO, p.pairs);
+  const GpPlan plan = gp_plan(p, TWO);
   p.splits = plan.splits;
   if (plan.splits == 1)
     return plan.nb == 4 ? gp_tiles<AK, BK, EPI, 4, ACT, TWO>(p, s) : gp_tiles<AK, BK, EPI, 2, ACT, TWO>(p, s);
-  if (p.pairs) {                                 // one of the two after the other
-    p.pairs = 0;
-    for (int i = 0; i < 2; ++i) {
-      GpParams q = p;
-      q.B[0] = p.B[i];
-      q.C[0] = p.C[i];
-      const hipError_t e = gp_launch<AK, BK, EPI, ACT>(q, part, s);
-      if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
-  }
-  GatedJoin j;
-  j.T = p.M; j.N = p.N; j.splits = plan.splits; j.part = part; j.ldo = p.ldc; j.act = ACT;
+  GatedJoin j[3];
+  j[0].T = p.M; j[0].N = p.N; j[0].splits = plan.splits; j[0].ldo = p.ldc; j[0].act = ACT;
+  j[0].out = static_cast<uint16_t *>(p.C[0]);
   if constexpr (EPI == GP_GATED) {
-    j.kind = GatedJoin::GATED;
-    j.out = static_cast<uint16_t *>(p.C[0]); j.keep_gate = p.keep_gate; j.keep_up = p.keep_up;
+    j[0].kind = GatedJoin::GATED;
+    j[0].keep_gate = p.keep_gate; j[0].keep_up = p.keep_up;
   } else if constexpr (EPI == GP_DGATED) {
-    j.kind = GatedJoin::DGATED;
-    j.out = static_cast<uint16_t *>(p.C[0]); j.out2 = static_cast<uint16_t *>(p.C[1]);
-    j.hidden = p.hidden; j.gate = p.gate; j.up = p.up;
+    j[0].kind = GatedJoin::DGATED;
+    j[0].out2 = static_cast<uint16_t *>(p.C[1]); j[0].hidden = p.hidden; j[0].gate = p.gate; j[0].up = p.up;
   } else if constexpr (EPI == GP_F32) {
-    j.kind = GatedJoin::F32;
-    j.out_f32 = static_cast<float *>(p.C[0]);
-  } else {
-    j.out = static_cast<uint16_t *>(p.C[0]);
+    j[0].kind = GatedJoin::F32;
+    j[0].out_f32 = static_cast<float *>(p.C[0]);
   }
+  j[0].part = part;
   p.C[0] = part;
-  const hipError_t e = plan.nb == 4 ? gp_tiles<AK, BK, GP_PART, 4, 0, TWO>(p, s) : gp_tiles<AK, BK, GP_PART, 2, 0, TWO>(p, s);
-  return e != hipSuccess ? e : launch_gated_join(j, s);
+  for (int i = 0; i < p.others; ++i) {           // each product's parts behind the one before
+    GpOther &o = p.other[i];
+    j[i + 1] = j[0];
+    j[i + 1].T = o.M; j[i + 1].N = o.N; j[i + 1].ldo = o.ldc;
+    j[i + 1].out = static_cast<uint16_t *>(o.C); j[i + 1].out_f32 = static_cast<float *>(o.C);
+    float *mine = const_cast<float *>(j[i].part) + plan.splits * j[i].T * j[i].N;
+    j[i + 1].part = mine;
+    o.C = mine;
+  }
+  hipError_t e = plan.nb == 4 ? gp_tiles<AK, BK, GP_PART, 4, 0, TWO>(p, s) : gp_tiles<AK, BK, GP_PART, 2, 0, TWO>(p, s);
+  for (int i = 0; i <= p.others && e == hipSuccess; ++i) e = launch_gated_join(j[i], s);
+  return e;
 }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -464,7 +488,7 @@ size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bo
                                 : std::max(few_bytes(tokens, n, 2), few_bytes(tokens, p, 1));
   // parts of tiles' products: at most 16, of three slabs each; more tokens never need less
   int64_t tiled = tokens > GATED_FEW ? tokens * (backward ? std::max(m, n) : std::max(2 * n, p)) : 0;
-  if (backward && tokens > 5 * GP_KB) tiled = std::max(tiled, n * std::max(m, p));
+  if (backward && tokens > 5 * GP_KB) tiled = std::max(tiled, n * (2 * m + p));
   tiled = std::min(GP_PARTS, 64 * tiled);
   return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + std::max(parts, up256((size_t)tiled));
 }
@@ -512,24 +536,20 @@ hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
       if ((e = gp_launch<true, true, GP_BF16>(p, part, s)) != hipSuccess) return e;
     }
   }
-  auto grad = [&](const GpParams &q) {
-    return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(q, part, s) : gp_launch<false, false, GP_F32>(q, part, s);
+  p = GpParams{};
+  p.K = (int)d.tokens; p.segments = 1;
+  auto grad = [&](int64_t rows, int64_t cols, const uint16_t *a, int64_t lda, const uint16_t *b, int64_t ldb, void *c) {
+    if (!c) return;
+    if (!p.M) {
+      p.M = (int)rows; p.N = (int)cols; p.A[0] = a; p.B[0] = b; p.C[0] = c; p.lda = lda; p.ldb = ldb; p.ldc = cols;
+    } else {
+      p.other[p.others++] = GpOther{(int)rows, (int)cols, 0, 0, a, b, c, lda, ldb, cols};
+    }
   };
-  if (d.dw_gate || d.dw_up) {
-    p = GpParams{};
-    p.M = (int)d.m; p.N = (int)d.n; p.K = (int)d.tokens; p.segments = 1;
-    p.A[0] = d.x; p.lda = d.ldx; p.ldb = d.n; p.ldc = d.n;
-    p.pairs = d.dw_gate && d.dw_up;
-    p.B[0] = d.dw_gate ? dg : du; p.B[1] = du; p.C[0] = d.dw_gate ? d.dw_gate : d.dw_up; p.C[1] = d.dw_up;
-    if ((e = grad(p)) != hipSuccess) return e;
-  }
-  if (d.dw_down) {
-    p = GpParams{};
-    p.M = (int)d.n; p.N = (int)d.p; p.K = (int)d.tokens; p.segments = 1;
-    p.A[0] = hidden; p.lda = d.n; p.B[0] = d.dy; p.ldb = d.lddy; p.C[0] = d.dw_down; p.ldc = d.p;
-    if ((e = grad(p)) != hipSuccess) return e;
-  }
-  return e;
+  grad(d.m, d.n, d.x, d.ldx, dg, d.n, d.dw_gate);
+  grad(d.m, d.n, d.x, d.ldx, du, d.n, d.dw_up);
+  grad(d.n, d.p, hidden, d.n, d.dy, d.lddy, d.dw_down);
+  return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(p, part, s) : gp_launch<false, false, GP_F32>(p, part, s);
 }
 
 }  // namespace soap
