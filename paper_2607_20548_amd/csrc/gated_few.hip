@@ -291,12 +291,13 @@ hipError_t launch_gated_join(const GatedJoin &p, hipStream_t s) {
   return p.act == SOAP_ACT_SILU ? gj_launch<GJ_DGATED, SOAP_ACT_SILU>(p, s) : gj_launch<GJ_DGATED, SOAP_ACT_GELU>(p, s);
 }
 
-// Parts of k: as many as give compute units a workgroup each and none a second, of two slabs a
-// wave at least (4096 x 14336, 16 tokens: 224 workgroups for the columns alone 85 us, 448 90; 2048
-// x 8192: 128 37, 256 33).
+// Parts of k: as many as give compute units a workgroup each and none a second, of six slabs a
+// wave at least (4096 x 14336, 16 tokens: 224 workgroups for the columns alone 83 us, 448 93; one
+// token of 512 x 1024: parts of two slabs 20.0, of four 17.1, of six 14.4, of eight 14.5; 64 of
+// 1000 x 3000: 30.0, 27.9, 29.7 and 33.4).
 int few_splits(int64_t N, int64_t slabs) {
   const int64_t chunks = (N + GF_COLS - 1) / GF_COLS;
-  return (int)std::max<int64_t>(1, std::min(256 / chunks, slabs / 8));
+  return (int)std::max<int64_t>(1, std::min(256 / chunks, slabs / 24));
 }
 
 // The product, and what is made of it.
