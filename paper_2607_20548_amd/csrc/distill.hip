@@ -39,6 +39,7 @@ struct DsParams {
   int64_t rows, ld, ldt, ldi, ldd;
   int classes, slots, tail, t_bf16, segments;   // segments: workgroups of a row
   float tau, scale;                       // scale: log2(e) / tau
+  double inv;                             // 1 / tau
   const void *z, *t;
   const int *index;
   const float *dloss;
@@ -116,6 +117,27 @@ __device__ __forceinline__ DsSum ds_join_all(DsSum v, float scale, DsSum *red) {
   for (int w = 1; w < NT / 64; ++w) v = ds_join(v, red[w], scale);
   return v;
 }
+// log s within 2^-30: s = m 2^k, log m = 2 artanh f = 2 f (1 + f^2 / 3 + f^4 / 5 ..), f = (m - 1) /
+// (m + 1) of at most 0.172, of which only the first term needs more than fp32.
+__device__ __forceinline__ double ds_log(float s) {
+  if (!(s > 0.f && s < INFINITY)) return logf(s);
+  int k = __builtin_amdgcn_frexp_expf(s);
+  float m = __builtin_amdgcn_frexp_mantf(s);
+  if (m < 0.70710678f) {
+    m *= 2.f;
+    --k;
+  }
+  const float r = 1.f / (m + 1.f), f = (m - 1.f) * r, z = f * f;
+  const double left = ((double)m - 1.0 - f * ((double)m + 1.0)) * r;   // of f
+  const float more = 2.f * f * z * (1.f / 3 + z * (0.2f + z * (1.f / 7 + z * (1.f / 9 + z * (1.f / 11)))));
+  return k * 0.69314718055994530942 + 2.0 * (f + left) + more;
+}
+// Over a wave's lanes.
+__device__ __forceinline__ double ds_total(double v) {
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) v += __shfl_xor(v, k);
+  return v;
+}
 // What the first wave finds in the teacher's list.
 struct DsList {
   float most, logs, rest, weight;         // of log p: what is taken off t, and the divisor's log; weight: of q
@@ -136,7 +158,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
   __shared__ DsList list;
   const int tid = threadIdx.x;
   const bool tail = p.tail, marked = GRAD || tail, leader = __builtin_amdgcn_readfirstlane(tid >> 6) == 0;
-  const float inv = 1.f / p.tau;
+  const float inv = (float)p.inv;
   const int words = (p.classes + VEC + 31) / 32;
   int64_t row = blockIdx.x / p.segments;
   const int segment = blockIdx.x % p.segments;
@@ -181,7 +203,8 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
     if (leader) early_z = look(early_c, early_t);
     auto find = [&]() {
       DsList l = {0.f, 0.f, 0.f, 0.f, 0, 0};
-      float most = -INFINITY, sum = 0.f;
+      float most = -INFINITY;
+      double sum = 0.0;                   // fp64: what it leaves of 1 may be little
       bool some = false, twice = false;
 #pragma unroll 1
       for (int j = tid; j < p.slots; j += 64) {
@@ -205,14 +228,14 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
       for (int j = tid; j < p.slots; j += 64) {
         const float t = tail ? ps[j] : (ps[j] - l.most) * inv;
         ps[j] = t;
-        sum += expf(t);
+        sum += (double)expf(t);
       }
-      sum = lane_sum<64>(sum);
+      sum = ds_total(sum);
       l.twice = __ballot(twice) != 0;
-      l.logs = tail ? 0.f : logf(sum);
-      l.any = tail ? __ballot(some) != 0 : sum != 0.f;       // a list without a class weighs nothing
-      l.rest = !tail || !l.any ? 0.f : sum == sum ? fmaxf(0.f, 1.f - sum) : sum;
-      l.weight = tail ? sum : 1.f;
+      l.logs = tail ? 0.f : logf((float)sum);
+      l.any = tail ? __ballot(some) != 0 : sum != 0.0;       // a list without a class weighs nothing
+      l.rest = !tail || !l.any ? 0.f : (float)(sum == sum ? fmax(0.0, 1.0 - sum) : sum);
+      l.weight = tail ? (float)sum : 1.f;
       if (tid == 0) list = l;
     };
     if (tail || !LOSS) {
@@ -297,22 +320,23 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 
     if constexpr (LOSS) {
       if (leader) {
-        float part = 0.f;
-        const float base = ds_base(whole.m), logw = logf(whole.s);
+        double part = 0.0;                  // terms of both signs
+        const float base = ds_base(whole.m);
+        const double logw = ds_log(whole.s);
 #pragma unroll 1
         for (int j = tid; j < p.slots; j += 64) {
           if (cls[j] < 0) continue;
           const float logp = ps[j] - l.logs, w = expf(logp);
-          if (w != 0.f) part += w * (logp - ((zs[j] - base) * inv - logw));
+          if (w != 0.f) part += (double)w * ((double)logp - ((double)zs[j] - base) * p.inv + logw);
         }
-        part = lane_sum<64>(part);
+        part = ds_total(part);
         if (tid == 0) {
           if (rest != 0.f) {
             // log of the rest's share: both sums under their own maxima
-            const float share = (ds_base(all.m) - base) * inv + (logf(all.s) - logw);
-            part += rest * (logf(rest) - share);
+            const double share = ((double)ds_base(all.m) - base) * p.inv + ds_log(all.s) - logw;
+            part += (double)rest * (ds_log(rest) - share);
           }
-          p.loss[row] = p.tau * p.tau * part;
+          p.loss[row] = (float)(p.tau * p.tau * part);
           if (p.stats) {
             p.stats[2 * row] = lse;
             p.stats[2 * row + 1] = tail ? lse_rest : 0.f;
@@ -423,7 +447,11 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
   }
 }
 
-// Threads and units for a row: held in registers up to 128 of them a thread.
+// Threads and units for a row: held in up to 128 registers of a thread by as few threads as that
+// takes, with as many workgroups as the chip holds.  Loss and gradient, us: 4096 x 131072 bfloat16
+// 512 threads x 32 units 504 (4.25 TB/s), 1024 x 16 543, read twice 640; 4096 x 65536 fp32 465,
+// read twice 502; 8192 x 50257 bfloat16 1024 x 8 424, 512 x 16 449; 8192 x 16000 256 x 8 141, 512 x 4
+// 177; 8192 x 2000 128 x 4 25, 512 x 2 34.  Longer rows are read twice (4096 x 80000 fp32 607).
 template <typename T, int WHAT>
 hipError_t ds_launch(DsParams p, hipStream_t s) {
   constexpr int VEC = ds_vec<T>();
@@ -442,7 +470,7 @@ hipError_t ds_launch(DsParams p, hipStream_t s) {
   }
   if constexpr (WHAT == (DS_LOSS | DS_GRAD)) {
     SOAP_DS(128, 4, 2560) SOAP_DS(256, 4, 1280) SOAP_DS(256, 8, 1024) SOAP_DS(512, 8, 512) SOAP_DS(1024, 8, 256)
-    if constexpr (sizeof(T) == 4) { SOAP_DS(1024, 16, 256) } else { SOAP_DS(512, 32, 256) }
+    SOAP_DS(512, 32, 256)
   }
   if (n <= 1024) { SOAP_DS(256, 0, 0) }
   SOAP_DS(1024, 0, 0)
@@ -455,7 +483,7 @@ hipError_t ds_start(const DistillDesc &d, hipStream_t s) {
   DsParams p{};
   p.rows = d.rows; p.ld = d.ld; p.ldt = d.ldt; p.ldi = d.ldi; p.ldd = d.ldd;
   p.classes = (int)d.classes; p.slots = (int)d.slots; p.tail = d.tail; p.t_bf16 = d.teacher_bf16;
-  p.tau = d.tau; p.scale = DS_LOG2E / d.tau;
+  p.tau = d.tau; p.scale = DS_LOG2E / d.tau; p.inv = 1.0 / d.tau;
   p.z = d.logits; p.t = d.teacher; p.index = d.index; p.dloss = d.dloss;
   p.loss = d.loss; p.stats = d.stats; p.stats_in = d.stats; p.dz = d.dlogits;
   return d.bf16 ? ds_launch<uint16_t, WHAT>(p, s) : ds_launch<float, WHAT>(p, s);
