@@ -5,8 +5,8 @@
 //   dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY
 //
 // X is tokens x m, Wg and Wu m x n, Wd n x p.  H, dG and dU are rounded to bfloat16 once, as
-// the operands of the next product; act works on fp32 sums forward and on the kept (rounded)
-// G and U backward.
+// the operands of the next product (of up to 64 tokens to two bfloat16, whose products are added);
+// act works on fp32 sums forward and on the kept (rounded) G and U backward.
 //
 // Products of up to 64 tokens are product_few's; all others are one kernel's, product_tiles: C =
 // sum over k of A(x, k) B(y, k), its operands in memory either k-contiguous ([x][k]: X, H, dY,
@@ -40,7 +40,7 @@ enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART };
 
 struct GpOther {               // product over the same k
   int M, N, tiles_m, tiles_n;
-  const uint16_t *A, *B;
+  const uint16_t *A[2], *B[2];
   void *C;
   int64_t lda, ldb, ldc;
 };
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
           t -= p.tiles_m * p.tiles_n;
           const GpOther o = p.other[i];
           p.M = o.M; p.N = o.N; p.tiles_m = o.tiles_m; p.tiles_n = o.tiles_n;
-          p.A[0] = o.A; p.B[0] = o.B; p.C[0] = o.C; p.lda = o.lda; p.ldb = o.ldb; p.ldc = o.ldc;
+          p.A[0] = o.A[0]; p.A[1] = o.A[1]; p.B[0] = o.B[0]; p.B[1] = o.B[1]; p.C[0] = o.C; p.lda = o.lda; p.ldb = o.ldb; p.ldc = o.ldc;
         } else {
           break;
         }
@@ -462,18 +462,20 @@ hipError_t few_fwd(const GatedDesc &d, hipStream_t s) {
   return launch_product_few(g, j, s);
 }
 
-// dG, dU and H, and dX if it is wanted.
-hipError_t few_bwd(const GatedDesc &d, uint16_t *dg, uint16_t *du, uint16_t *hidden, float *part, hipStream_t s) {
+// dG, dU and H, each followed by its lower half, and dX if it is wanted.
+hipError_t few_bwd(const GatedDesc &d, uint16_t *const halves[6], float *part, hipStream_t s) {
   FewDesc f;
   f.kind = FewDesc::ROWS; f.tokens = d.tokens; f.n = d.n; f.k = d.p; f.ldx = d.lddy; f.ldw = d.p;
   f.x[0] = d.dy; f.w[0] = d.w_down; f.part = part;
   GatedJoin j;
-  j.kind = GatedJoin::DGATED; j.act = d.act; j.gate = d.gate; j.up = d.up; j.out = dg; j.out2 = du; j.hidden = hidden;
+  j.kind = GatedJoin::DGATED; j.act = d.act; j.gate = d.gate; j.up = d.up;
+  j.out = halves[0]; j.low = halves[1]; j.out2 = halves[2]; j.low2 = halves[3]; j.hidden = halves[4]; j.hidden_low = halves[5];
   const hipError_t e = launch_product_few(f, j, s);
   if (e != hipSuccess || !d.dx) return e;
   f = FewDesc();
-  f.kind = FewDesc::ROWS; f.tokens = d.tokens; f.n = d.m; f.k = d.n; f.ldx = d.n; f.ldw = d.n; f.segments = 2;
-  f.x[0] = dg; f.x[1] = du; f.w[0] = d.w_gate; f.w[1] = d.w_up; f.part = part;
+  f.kind = FewDesc::ROWS_HALVES; f.tokens = d.tokens; f.n = d.m; f.k = d.n; f.ldx = d.n; f.ldw = d.n; f.segments = 2;
+  for (int i = 0; i < 4; ++i) f.x[i] = halves[i];
+  f.w[0] = d.w_gate; f.w[1] = d.w_up; f.part = part;
   j = GatedJoin();
   j.out = d.dx; j.ldo = d.lddx;
   return launch_product_few(f, j, s);
@@ -481,7 +483,7 @@ hipError_t few_bwd(const GatedDesc &d, uint16_t *dg, uint16_t *du, uint16_t *hid
 
 }  // namespace
 
-// H (and what its rounding leaves, of few tokens) or dG, dU and H, and sums of parts of k.
+// H or dG, dU and H, of few tokens with their lower halves, and sums of parts of k.
 size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bool backward) {
   if (!tokens) return 0;
   const size_t parts = backward ? std::max(few_bytes(tokens, n, 1), few_bytes(tokens, m, 1))
@@ -490,7 +492,7 @@ size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bo
   int64_t tiled = tokens > GATED_FEW ? tokens * (backward ? std::max(m, n) : std::max(2 * n, p)) : 0;
   if (backward && tokens > 5 * GP_KB) tiled = std::max(tiled, n * (2 * m + p));
   tiled = std::min(GP_PARTS, 64 * tiled);
-  return (backward ? 3 * wide(tokens, n) : wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + std::max(parts, up256((size_t)tiled));
+  return (backward ? 3 : 1) * (wide(tokens, n) + wide(std::min(tokens, GATED_FEW), n)) + std::max(parts, up256((size_t)tiled));
 }
 
 hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s) {
@@ -513,14 +515,17 @@ hipError_t launch_gated_fwd(const GatedDesc &d, hipStream_t s) {
 }
 
 hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
-  const size_t each = up256(2 * (size_t)d.tokens * (size_t)d.n);
+  const bool few = d.tokens <= GATED_FEW;
+  const size_t each = wide(d.tokens, d.n), low = few ? each : 0;
   char *w = static_cast<char *>(d.workspace);
-  uint16_t *dg = (uint16_t *)w, *du = (uint16_t *)(w + each), *hidden = (uint16_t *)(w + 2 * each);
-  float *part = (float *)(w + 3 * each);
+  uint16_t *halves[6];
+  for (int i = 0; i < 6; ++i) halves[i] = (uint16_t *)(w + (i + 1) / 2 * each + i / 2 * low);
+  uint16_t *dg = halves[0], *du = halves[2], *hidden = halves[4];
+  float *part = (float *)(w + 3 * (each + low));
   hipError_t e = hipSuccess;
   GpParams p{};
-  if (d.tokens > 0 && d.tokens <= GATED_FEW) {
-    if ((e = few_bwd(d, dg, du, hidden, part, s)) != hipSuccess) return e;
+  if (d.tokens > 0 && few) {
+    if ((e = few_bwd(d, halves, part, s)) != hipSuccess) return e;
   } else if (d.tokens > 0) {
     p.M = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.p; p.segments = 1;
     p.A[0] = d.dy; p.lda = d.lddy; p.B[0] = d.w_down; p.ldb = d.p;
@@ -536,19 +541,22 @@ hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
       if ((e = gp_launch<true, true, GP_BF16>(p, part, s)) != hipSuccess) return e;
     }
   }
+  // the second segment: lower halves
   p = GpParams{};
-  p.K = (int)d.tokens; p.segments = 1;
-  auto grad = [&](int64_t rows, int64_t cols, const uint16_t *a, int64_t lda, const uint16_t *b, int64_t ldb, void *c) {
+  p.K = (int)d.tokens; p.segments = few ? 2 : 1;
+  auto grad = [&](int64_t rows, int64_t cols, const uint16_t *a, const uint16_t *a_low, int64_t lda, const uint16_t *b,
+                  const uint16_t *b_low, int64_t ldb, void *c) {
     if (!c) return;
     if (!p.M) {
-      p.M = (int)rows; p.N = (int)cols; p.A[0] = a; p.B[0] = b; p.C[0] = c; p.lda = lda; p.ldb = ldb; p.ldc = cols;
+      p.M = (int)rows; p.N = (int)cols; p.lda = lda; p.ldb = ldb; p.ldc = cols;
+      p.A[0] = a; p.A[1] = a_low; p.B[0] = b; p.B[1] = b_low; p.C[0] = c;
     } else {
-      p.other[p.others++] = GpOther{(int)rows, (int)cols, 0, 0, a, b, c, lda, ldb, cols};
+      p.other[p.others++] = GpOther{(int)rows, (int)cols, 0, 0, {a, a_low}, {b, b_low}, c, lda, ldb, cols};
     }
   };
-  grad(d.m, d.n, d.x, d.ldx, dg, d.n, d.dw_gate);
-  grad(d.m, d.n, d.x, d.ldx, du, d.n, d.dw_up);
-  grad(d.n, d.p, hidden, d.n, d.dy, d.lddy, d.dw_down);
+  grad(d.m, d.n, d.x, d.x, d.ldx, dg, halves[1], d.n, d.dw_gate);
+  grad(d.m, d.n, d.x, d.x, d.ldx, du, halves[3], d.n, d.dw_up);
+  grad(d.n, d.p, hidden, halves[5], d.n, d.dy, d.dy, d.lddy, d.dw_down);
   return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(p, part, s) : gp_launch<false, false, GP_F32>(p, part, s);
 }
 

@@ -10,8 +10,10 @@
 // through the activation or its gradient, or are rounded, there, or where columns are few and k
 // has parts, are written as fp32 sums that a second kernel adds in their order.
 //
-// H is kept in two bfloat16 halves (its rounding and what that leaves), which costs matrix
-// instructions that the weights' loads cover, and no bytes to speak of.
+// H forward and dG, dU and H backward are kept in two bfloat16 halves (their rounding and what that
+// leaves), which costs matrix instructions that the weights' loads cover, and no bytes to speak of:
+// of few roundings the largest would show in a result (six tokens' dX: 1.5 times the error of
+// its own rounding alone).
 #include "products_bf16.h"
 
 #include <algorithm>
@@ -24,7 +26,7 @@ constexpr int GF_W = GF_KB * GF_COLS * 2, GF_X = 32 * GF_KB * 2;   // bytes of a
 
 struct GfParams {
   int T, N, K;                   // K: of a segment
-  const uint16_t *X[2], *W[2];   // halves of X, or segments of both; gate's and up's weights
+  const uint16_t *X[4], *W[2];   // X by segment and half; W by segment, or gate's and up's
   int64_t ldx, ldw;
   int segments, splits, chunks;
   float *part;                   // [split][matrix][T][N]
@@ -33,6 +35,11 @@ struct GfParams {
 
 // ------------------------------------------------- what is made of the sums
 enum { GJ_PART, GJ_GATED, GJ_DGATED, GJ_BF16, GJ_F32 };
+
+// What the rounding of two values leaves, rounded: the lower halves.
+__device__ __forceinline__ uint32_t gj_low(const float (&v)[2]) {
+  return gp_pack(v[0] - gp_float(gp_round(v[0])), v[1] - gp_float(gp_round(v[1])));
+}
 
 // Of eight columns of a row: x[0], and x[1] of up's.
 template <int MODE, int ACT>
@@ -51,16 +58,13 @@ __device__ __forceinline__ void gj_finish(const GatedJoin &p, const float (*x)[8
     v4u og, ou, oh, ol;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float hv[2], lo[2];
+      float hv[2];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        hv[w] = gp_act<ACT>(x[0][2 * e + w]).a * x[1][2 * e + w];
-        lo[w] = hv[w] - gp_float(gp_round(hv[w]));
-      }
+      for (int w = 0; w < 2; ++w) hv[w] = gp_act<ACT>(x[0][2 * e + w]).a * x[1][2 * e + w];
       og[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
       ou[e] = gp_pack(x[1][2 * e], x[1][2 * e + 1]);
       oh[e] = gp_pack(hv[0], hv[1]);
-      ol[e] = gp_pack(lo[0], lo[1]);
+      ol[e] = gj_low(hv);
     }
     *reinterpret_cast<v4u *>(p.out + at) = oh;
     if (p.low) *reinterpret_cast<v4u *>(p.low + at) = ol;
@@ -70,7 +74,7 @@ __device__ __forceinline__ void gj_finish(const GatedJoin &p, const float (*x)[8
     }
   } else {
     const v4u g = *reinterpret_cast<const v4u *>(p.gate + at), u = *reinterpret_cast<const v4u *>(p.up + at);
-    v4u og, ou, oh;
+    v4u og, ou, oh, lg, lu, lh;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float a[2], b[2], o[2];
@@ -85,11 +89,20 @@ __device__ __forceinline__ void gj_finish(const GatedJoin &p, const float (*x)[8
       og[e] = gp_pack(a[0], a[1]);
       ou[e] = gp_pack(b[0], b[1]);
       oh[e] = gp_pack(o[0], o[1]);
+      lg[e] = gj_low(a);
+      lu[e] = gj_low(b);
+      lh[e] = gj_low(o);
     }
     *reinterpret_cast<v4u *>(p.out + at) = og;
     *reinterpret_cast<v4u *>(p.out2 + at) = ou;
     *reinterpret_cast<v4u *>(p.hidden + at) = oh;
-  }}
+    if (p.low) {
+      *reinterpret_cast<v4u *>(p.low + at) = lg;
+      *reinterpret_cast<v4u *>(p.low2 + at) = lu;
+      *reinterpret_cast<v4u *>(p.hidden_low + at) = lh;
+    }
+  }
+}
 
 // WK: weights k-contiguous.  TWO: gate's and up's.  NX: halves of X.  RB: 32s of tokens.
 template <bool WK, bool TWO, int NX, int RB>
@@ -143,7 +156,7 @@ __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
 #pragma unroll
     for (int t = 0; t < NX; ++t) {
       GpSource x;
-      x.start(NX > 1 ? p.X[t] : p.X[seg], true, 0, p.T, p.K, ldx2, GF_KB);
+      x.start(p.X[2 * seg + t], true, 0, p.T, p.K, ldx2, GF_KB);
       x.next(at);
       if (!live) x.left = 0;
       const v4i r = x.buffer();
@@ -304,7 +317,8 @@ int few_splits(int64_t N, int64_t slabs) {
 hipError_t launch_product_few(const FewDesc &d, const GatedJoin &out, hipStream_t s) {
   GfParams p{};
   p.T = (int)d.tokens; p.N = (int)d.n; p.K = (int)d.k;
-  p.X[0] = d.x[0]; p.X[1] = d.x[1]; p.W[0] = d.w[0]; p.W[1] = d.w[1]; p.ldx = d.ldx; p.ldw = d.ldw;
+  p.W[0] = d.w[0]; p.W[1] = d.w[1]; p.ldx = d.ldx; p.ldw = d.ldw;
+  for (int i = 0; i < 4; ++i) p.X[i] = d.x[i];
   p.segments = d.segments; p.chunks = (p.N + GF_COLS - 1) / GF_COLS; p.part = d.part;
   p.splits = few_splits(d.n, (d.k + GF_KB - 1) / GF_KB * d.segments);
   p.out = out;
@@ -315,11 +329,12 @@ hipError_t launch_product_few(const FewDesc &d, const GatedJoin &out, hipStream_
     if (d.kind == FewDesc::GATE_UP)
       return silu ? gf_launch<false, true, 1, GJ_GATED, SOAP_ACT_SILU>(p, s) : gf_launch<false, true, 1, GJ_GATED, SOAP_ACT_GELU>(p, s);
     if (d.kind == FewDesc::HALVES) return gf_launch<false, false, 2, GJ_BF16>(p, s);
-    if (out.kind == GatedJoin::BF16) return gf_launch<true, false, 1, GJ_BF16>(p, s);
+    if (d.kind == FewDesc::ROWS_HALVES) return gf_launch<true, false, 2, GJ_BF16>(p, s);
     return silu ? gf_launch<true, false, 1, GJ_DGATED, SOAP_ACT_SILU>(p, s) : gf_launch<true, false, 1, GJ_DGATED, SOAP_ACT_GELU>(p, s);
   }
   if (d.kind == FewDesc::GATE_UP) e = gf_launch<false, true, 1, GJ_PART>(p, s);
   else if (d.kind == FewDesc::HALVES) e = gf_launch<false, false, 2, GJ_PART>(p, s);
+  else if (d.kind == FewDesc::ROWS_HALVES) e = gf_launch<true, false, 2, GJ_PART>(p, s);
   else e = gf_launch<true, false, 1, GJ_PART>(p, s);
   return e != hipSuccess ? e : launch_gated_join(p.out, s);
 }

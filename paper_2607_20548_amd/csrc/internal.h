@@ -349,7 +349,7 @@ struct GatedDesc {
 size_t gated_workspace_bytes(int64_t tokens, int64_t m, int64_t n, int64_t p, bool backward);
 // The sum of parts of a product, T x N (N a multiple of 8), each [matrix][T][N] floats, and what
 // is made of it.  BF16: out, F32: out_f32.  GATED: H into out (and what its rounding leaves into
-// low), G and U kept or null.  DGATED: out = dG, out2 = dU, hidden.
+// low), G and U kept or null.  DGATED: out = dG, out2 = dU, hidden, and their lower halves or null.
 struct GatedJoin {
   enum Kind { BF16, F32, GATED, DGATED } kind = BF16;
   int64_t T = 0, N = 0, ldo = 0;
@@ -357,17 +357,19 @@ struct GatedJoin {
   const float *part = nullptr;
   float *out_f32 = nullptr;
   const uint16_t *gate = nullptr, *up = nullptr;
-  uint16_t *out = nullptr, *low = nullptr, *out2 = nullptr, *hidden = nullptr, *keep_gate = nullptr, *keep_up = nullptr;
+  uint16_t *out = nullptr, *out2 = nullptr, *hidden = nullptr, *keep_gate = nullptr, *keep_up = nullptr;
+  uint16_t *low = nullptr, *low2 = nullptr, *hidden_low = nullptr;
 };
 hipError_t launch_gated_join(const GatedJoin &p, hipStream_t s);
-// Products over up to GATED_FEW tokens, part: for sums of parts of k.  GATE_UP x w[0] and x w[1]
-// (out.kind GATED); HALVES (x[0] + x[1]) w[0] (BF16); ROWS the sum over segments of x[i] w[i]^T (BF16 or
-// DGATED).  out: without T, N, part and splits.
+// Products over up to GATED_FEW tokens, part: for sums of parts of k.  GATE_UP x[0] w[0] and x[0]
+// w[1] (out.kind GATED); HALVES (x[0] + x[1]) w[0] (BF16); ROWS x[0] w[0]^T (DGATED); ROWS_HALVES
+// the sum over two segments i of (x[2 i] + x[2 i + 1]) w[i]^T (BF16).  out: without T, N, part
+// and splits.
 constexpr int64_t GATED_FEW = 64;
 struct FewDesc {
-  enum Kind { GATE_UP, HALVES, ROWS } kind = GATE_UP;
+  enum Kind { GATE_UP, HALVES, ROWS, ROWS_HALVES } kind = GATE_UP;
   int64_t tokens = 0, n = 0, k = 0, ldx = 0, ldw = 0;
-  const uint16_t *x[2] = {nullptr, nullptr}, *w[2] = {nullptr, nullptr};
+  const uint16_t *x[4] = {}, *w[2] = {};
   int segments = 1;
   float *part = nullptr;
 };
