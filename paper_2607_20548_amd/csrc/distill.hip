@@ -11,7 +11,8 @@
 // logit above -inf, r counts as 0.
 //
 // Bound by HBM: a row is read once, and once more where a gradient is written from a row that the
-// registers did not hold.  One workgroup takes a row.  A thread keeps a running maximum and the
+// registers did not hold (both in one pass over 4096 x 131072 bfloat16 504 us, 4.25 TB/s; the
+// gradient alone of 999 x 50001 fp32, rows at every alignment, 93 us, 4.3 TB/s).  One workgroup takes a row.  A thread keeps a running maximum and the
 // sum of the exponentials under it, and the workgroup joins these once.  Logits are taken from
 // their maximum before anything else, so that neither a large one's digits nor a row of the
 // type's lowest values are lost.
@@ -451,7 +452,12 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 // takes, with as many workgroups as the chip holds.  Loss and gradient, us: 4096 x 131072 bfloat16
 // 512 threads x 32 units 504 (4.25 TB/s), 1024 x 16 543, read twice 640; 4096 x 65536 fp32 465,
 // read twice 502; 8192 x 50257 bfloat16 1024 x 8 424, 512 x 16 449; 8192 x 16000 256 x 8 141, 512 x 4
-// 177; 8192 x 2000 128 x 4 25, 512 x 2 34.  Longer rows are read twice (4096 x 80000 fp32 607).
+// 177; 8192 x 2000 128 x 4 25, 512 x 2 34.  Longer rows are read twice, by 1024 threads (4096 x 80000
+// fp32 608; 512 757, 256 826).  Loss alone, bfloat16: workgroups side by side hide each other's
+// joins, few rows need their threads (4096 x 2000: 128 threads 10.9, 256 13.0, 1024 47; 4096 x 32000:
+// 256 53, 1024 75; 600 x 131072: 38 and 41; 64 x 131072: 22 and 14).  The gradient alone: 4096 x
+// 8000: 256 37, 512 44, 1024 75; 600 x 32000: 20, 18.5 and 24; 2048 x 131072: 249, 228 and 220;
+// 999 x 50001 fp32: 512 101, 1024 93; 200 x 50000: 17 and 20.5.
 template <typename T, int WHAT>
 hipError_t ds_launch(DsParams p, hipStream_t s) {
   constexpr int VEC = ds_vec<T>();
@@ -460,7 +466,8 @@ hipError_t ds_launch(DsParams p, hipStream_t s) {
   const int64_t mis = even ? (int64_t)(reinterpret_cast<uintptr_t>(p.z) % 16 / sizeof(T)) : VEC - 1;
   const int64_t n = (p.classes + mis + VEC - 1) / VEC;
   const size_t lds = WHAT & DS_GRAD || p.tail ? 4 * ((p.classes + VEC + 31) / 32) : 0;
-  // gradients alone need nothing of the rest of the row: few rows are cut
+  // gradients alone need nothing of the rest of the row: few rows are cut into parts of 4096 units,
+  // up to DS_FILL workgroups in all (100 x 262144 bfloat16 27 us, whole 41)
   p.segments = WHAT == DS_GRAD ? (int)std::max<int64_t>(1, std::min((n + 4095) / 4096, DS_FILL / p.rows)) : 1;
 #define SOAP_DS(NT, U, BLOCKS)                                                                                \
   if (U == 0 || n <= (int64_t)NT * U) {                                                                       \
@@ -472,7 +479,14 @@ hipError_t ds_launch(DsParams p, hipStream_t s) {
     SOAP_DS(128, 4, 2560) SOAP_DS(256, 4, 1280) SOAP_DS(256, 8, 1024) SOAP_DS(512, 8, 512) SOAP_DS(1024, 8, 256)
     SOAP_DS(512, 32, 256)
   }
-  if (n <= 1024) { SOAP_DS(256, 0, 0) }
+  if constexpr (WHAT == DS_LOSS) {
+    if (n <= 1024) { SOAP_DS(128, 0, 0) }
+    if (n <= 4096 || p.rows >= 512) { SOAP_DS(256, 0, 0) }
+  }
+  if constexpr (WHAT == DS_GRAD) {
+    if (n <= 1024) { SOAP_DS(256, 0, 0) }
+    if (n <= 8192 || p.rows < 512) { SOAP_DS(512, 0, 0) }
+  }
   SOAP_DS(1024, 0, 0)
 #undef SOAP_DS
 }

@@ -17,10 +17,11 @@
 // k-contiguous blocks are read 16 bytes of a row at a time, x-contiguous ones by the transposing
 // reads, which give a lane four k of its own x.
 //
-// What bounds it: the matrix instructions (8192 x 2048 x 8192: 1354 TFLOP/s for dX, a ring of
-// five operand slabs ahead of them), and where one product has an activation behind it, the
-// outputs that all compute units write at the same time (dG, dU, H from G and U: 350 us, of which
-// 246 without their bytes).
+// What bounds it, 8192 x 2048 x 8192: matrix instructions where sums are long (dX 410 us, 1340 TFLOP/s,
+// busy 0.79 of the cycles; the weights' gradients 644, 1280), and where an activation is behind
+// them, the outputs that all compute units write at the same time (H, G and U 500 to 540; dG, dU and H from G
+// and U 350 to 370, of which 246 without their bytes).  The whole: 720 forward (1145 TFLOP/s), 1420
+// backward (1160).
 //
 // Operands past their ends read as zeros (buffer bounds; units past the end of k are sent
 // out of bounds), so that sizes need no multiple of a tile; m, n and p are multiples of 8
@@ -355,6 +356,8 @@ hipError_t gp_tiles(GpParams p, hipStream_t s) {
     tiles += (int64_t)o.tiles_m * o.tiles_n;
   }
   const dim3 grid((unsigned)tiles, (unsigned)p.splits), block(GP_THREADS);
+  // tiles that have a compute unit of their own may fill its LDS: more slabs on their way (128 x 4096
+  // x 14336 forward 126 -> 101 us, 300 x 4096 x 8192 gradients 260 -> 237; two on one take 80 KB each)
   if (NB == 2 && tiles * p.splits <= 256)
     hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, NB == 2 ? 9 : 5>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 5>), grid, block, 0, s, p);

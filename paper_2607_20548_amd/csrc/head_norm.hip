@@ -17,7 +17,8 @@
 // UNITS x VEC pairs (16 bytes of either half, or 32 bytes of neighbours), so that the
 // rotation stays within a lane, and the 64 / LANES groups of a wave take different heads of
 // one token, whose angles are formed once for all of them, or where a token has few heads a
-// token each.
+// token each.  16384 tokens of 16 + 16 heads of 128 bfloat16: 55 us forward (4.9 TB/s), 91 backward
+// (4.4 TB/s, with 5 for the second kernel).
 //
 // dw: every workgroup walks over tokens and writes the sums over its own, a second kernel adds
 // these in a fixed order.
@@ -33,8 +34,13 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element
 
 constexpr int HN_THREADS = 256, HN_WAVES = HN_THREADS / 64;
-constexpr int64_t HN_BLOCKS_BWD = 512;   // two for every compute unit: rows of partial sums
-constexpr int64_t HN_FEW = 4096;         // waves that fill the chip: fewer tokens share heads out
+// Workgroups backward, and rows of partial sums: two for every compute unit (the size above: 256
+// 119 us, 512 95, 1024 100, before the angles were shared).
+constexpr int64_t HN_BLOCKS_BWD = 512;
+// Waves that fill the chip: fewer tokens share their heads out over several (300 tokens of 64 + 64
+// heads of 256 fp32: 1 wave a token 45.6 us forward and 75 backward, up to 1024 waves 21 and 38, 4096
+// 15.3 and 31, 16384 16.9 and 34).
+constexpr int64_t HN_FEW = 4096;
 constexpr int HN_FIN = 1024, HN_FIN_COLS = 32;
 
 struct HnSide {                          // queries or keys
@@ -469,7 +475,8 @@ struct HnShape {
   bool each;
 };
 // Lanes of a head, and whether a wave's slots take a token each: where its steps are fewer by
-// a quarter, the heads of one token leaving slots idle.
+// a quarter, the heads of one token leaving slots idle (60000 tokens of 1 + 1 heads of 128 bfloat16:
+// 20 us, slots for heads 73).
 HnShape hn_shape(const HeadNormDesc &d) {
   const int64_t vec = d.bf16 ? 8 : 4, half = d.rotary / 2, rest = (d.dim - d.rotary) / 2;
   const int64_t n = (half + vec - 1) / vec + (rest + vec - 1) / vec;

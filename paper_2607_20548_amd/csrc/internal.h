@@ -365,6 +365,8 @@ hipError_t launch_gated_join(const GatedJoin &p, hipStream_t s);
 // w[1] (out.kind GATED); HALVES (x[0] + x[1]) w[0] (BF16); ROWS x[0] w[0]^T (DGATED); ROWS_HALVES
 // the sum over two segments i of (x[2 i] + x[2 i + 1]) w[i]^T (BF16).  out: without T, N, part
 // and splits.
+// (2048 x 8192 forward: 40 tokens 40 us, by tiles 47; 64 of 1000 x 3000 28, by tiles 29; 100 of 2048 x 8192
+// 54, by tiles 49.)
 constexpr int64_t GATED_FEW = 64;
 struct FewDesc {
   enum Kind { GATE_UP, HALVES, ROWS, ROWS_HALVES } kind = GATE_UP;
