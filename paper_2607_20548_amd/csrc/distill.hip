@@ -456,7 +456,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 // fp32 608; 512 757, 256 826).  Loss alone, bfloat16: workgroups side by side hide each other's
 // joins, few rows need their threads (4096 x 2000: 128 threads 10.9, 256 13.0, 1024 47; 4096 x 32000:
 // 256 53, 1024 75; 600 x 131072: 38 and 41; 64 x 131072: 22 and 14).  The gradient alone: 4096 x
-// 8000: 256 37, 512 44, 1024 75; 600 x 32000: 20, 18.5 and 24; 2048 x 131072: 249, 228 and 220;
+// 2000: 128 14.2, 256 16.2; 4096 x 8000: 128 41, 256 37, 512 44, 1024 75; 600 x 32000: 20, 18.5 and 24; 2048 x 131072: 249, 228 and 220;
 // 999 x 50001 fp32: 512 101, 1024 93; 200 x 50000: 17 and 20.5.
 template <typename T, int WHAT>
 hipError_t ds_launch(DsParams p, hipStream_t s) {
@@ -479,11 +479,13 @@ hipError_t ds_launch(DsParams p, hipStream_t s) {
     SOAP_DS(128, 4, 2560) SOAP_DS(256, 4, 1280) SOAP_DS(256, 8, 1024) SOAP_DS(512, 8, 512) SOAP_DS(1024, 8, 256)
     SOAP_DS(512, 32, 256)
   }
+  const bool most = p.rows * 256 > UINT32_MAX;   // a launch has fewer than 2^32 threads
   if constexpr (WHAT == DS_LOSS) {
-    if (n <= 1024) { SOAP_DS(128, 0, 0) }
+    if (n <= 1024 || most) { SOAP_DS(128, 0, 0) }
     if (n <= 4096 || p.rows >= 512) { SOAP_DS(256, 0, 0) }
   }
   if constexpr (WHAT == DS_GRAD) {
+    if (n <= 256 || most) { SOAP_DS(128, 0, 0) }
     if (n <= 1024) { SOAP_DS(256, 0, 0) }
     if (n <= 8192 || p.rows < 512) { SOAP_DS(512, 0, 0) }
   }

@@ -257,6 +257,23 @@ def test_rows_past_32_bits():
     assert (loss[:-1] == loss[0]).all() and torch.equal(dz[0], dz[-2]) and torch.equal(dz[12345], dz[0])
 
 
+def test_most_rows():
+    """As many rows as a call takes, in each of the three: the last ones as they are alone."""
+    rows, last = 1 << 24, 1000
+    z = (torch.arange(rows * 3, device="cuda") % 1009 / 200.0).view(rows, 3).bfloat16()
+    index = (torch.arange(rows, device="cuda", dtype=torch.int32) % 3)[:, None]
+    t = torch.zeros(rows, 1, device="cuda")
+    d = soap.Distillation()
+    loss, stats = d.forward(z, index, t)
+    dz = d.backward(z, index, t, stats)
+    both, dz_both = d.forward_backward(z, index, t)
+    want, want_stats = d.forward(z[-last:], index[-last:], t[-last:])
+    assert torch.equal(loss[-last:], want) and torch.equal(stats[-last:], want_stats)
+    assert torch.equal(dz[-last:], d.backward(z[-last:], index[-last:], t[-last:], want_stats))
+    want, want_dz = d.forward_backward(z[-last:], index[-last:], t[-last:])
+    assert torch.equal(both[-last:], want) and torch.equal(dz_both[-last:], want_dz)
+
+
 def test_no_rows():
     d = soap.Distillation()
     z, index, t = torch.empty(0, 10, device="cuda"), torch.empty(0, 2, device="cuda", dtype=torch.int32), torch.empty(0, 2, device="cuda")
