@@ -11,8 +11,9 @@
 // logit above -inf, r counts as 0.
 //
 // Bound by HBM: a row is read once, and once more where a gradient is written from a row that the
-// registers did not hold (both in one pass over 4096 x 131072 bfloat16 504 us, 4.25 TB/s; the
-// gradient alone of 999 x 50001 fp32, rows at every alignment, 93 us, 4.3 TB/s).  One workgroup takes a row.  A thread keeps a running maximum and the
+// registers did not hold (both in one pass over 4096 x 131072 bfloat16 487 us, 4.4 TB/s; the
+// loss alone 179 us, 6.0 TB/s; the gradient alone of 999 x 50001 fp32, rows at every alignment, 91 us,
+// 4.4 TB/s).  One workgroup takes a row.  A thread keeps a running maximum and the
 // sum of the exponentials under it, and the workgroup joins these once.  Logits are taken from
 // their maximum before anything else, so that neither a large one's digits nor a row of the
 // type's lowest values are lost.
@@ -34,6 +35,12 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element
 
 constexpr int64_t DS_FILL = 512;          // workgroups that fill the chip
+// Bytes of logits from which a call that reads them once loads past the caches (4096 x 131072 bfloat16
+// loss 202 us, past them 179; gradient of 4096 x 32000 120 and 112, of 1000 x 50257 54.0 and 54.7, of
+// 600 x 32000 18.7 and 22.1).  Gradients are always stored so (that of 4096 x 32000 before 131; loss
+// and gradient of 4096 x 131072 503 and 487, of 300 x 131072 73 and 61; of rows read twice, 4096 x 80000
+// fp32, 609 and 623: they are not).
+constexpr size_t DS_CACHED = 100 << 20;
 constexpr float DS_LOG2E = 1.44269504088896340736f;
 
 struct DsParams {
@@ -90,9 +97,13 @@ struct DsRow {
   }
   __device__ __forceinline__ bool whole(int unit) const { return unit >= first && unit < last; }
   // Unit `at` + lane, `at` the same for all lanes: a base in scalar registers and a lane's offset.
+  // FAR: past the caches.
+  template <bool FAR>
   __device__ __forceinline__ v4u load(int at, uint32_t lane) const {
     const char *base = reinterpret_cast<const char *>(z) - mis * (int)sizeof(T) + (int64_t)at * 16;
-    return whole(at + (int)lane) ? *reinterpret_cast<const v4u_any *>(base + 16 * lane) : v4u(0u);
+    if (!whole(at + (int)lane)) return v4u(0u);
+    if constexpr (FAR) return __builtin_nontemporal_load(reinterpret_cast<const v4u_any *>(base + 16 * lane));
+    else return *reinterpret_cast<const v4u_any *>(base + 16 * lane);
   }
   __device__ __forceinline__ int edge(int e) const { return e < front ? e : back + e - front; }   // its column
 };
@@ -148,7 +159,7 @@ struct DsList {
 // U: units of a thread that the registers hold, with workgroups that walk over rows and load the
 // next one's units as they write the present one's (0: one row, read by and by, and again for the
 // gradient).  The first wave sees to the list, beside the others' sums.
-template <typename T, int NT, int U, int WHAT>
+template <typename T, int NT, int U, int WHAT, bool FAR>
 __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
   constexpr int VEC = ds_vec<T>(), AHEAD = 4;
   constexpr bool LOSS = WHAT & DS_LOSS, GRAD = WHAT & DS_GRAD;
@@ -188,7 +199,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
   v4u held[HELD];
   if constexpr (U > 0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) held[u] = z.load(u * NT, tid);
+    for (int u = 0; u < U; ++u) held[u] = z.template load<FAR>(u * NT, tid);
   }
   if (marked)
     for (int i = tid; i < words; i += NT) map[i] = 0u;
@@ -297,7 +308,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
         for (int u0 = 0; u0 < z.last; u0 += AHEAD * NT) {
           v4u q[AHEAD];
 #pragma unroll
-          for (int a = 0; a < AHEAD; ++a) q[a] = z.load(u0 + a * NT, tid);
+          for (int a = 0; a < AHEAD; ++a) q[a] = z.template load<FAR>(u0 + a * NT, tid);
 #pragma unroll
           for (int a = 0; a < AHEAD; ++a)
             if (z.whole(u0 + a * NT + tid)) unit(q[a], u0 + a * NT + tid);
@@ -389,7 +400,9 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
         else w[i] = (uint32_t)ds_round<T>(v[2 * i]) | (uint32_t)ds_round<T>(v[2 * i + 1]) << 16;
       }
       if (!b) {
-        *reinterpret_cast<v4u_any *>(to) = w;
+        // past the caches, but where the row is to be read again from them
+        if constexpr (U > 0 || !LOSS) __builtin_nontemporal_store(w, reinterpret_cast<v4u_any *>(to));
+        else *reinterpret_cast<v4u_any *>(to) = w;
         return;
       }
 #pragma unroll
@@ -426,14 +439,14 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (z.whole(u * NT + tid)) put(held[u], u * NT);
-        if (more) held[u] = zn.load(u * NT, tid);
+        if (more) held[u] = zn.template load<FAR>(u * NT, tid);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
       for (int u0 = segment * AHEAD * NT; u0 < z.last; u0 += p.segments * AHEAD * NT) {
         v4u q[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) q[a] = z.load(u0 + a * NT, tid);
+        for (int a = 0; a < AHEAD; ++a) q[a] = z.template load<FAR>(u0 + a * NT, tid);
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a)
           if (z.whole(u0 + a * NT + tid)) put(q[a], u0 + a * NT);
@@ -449,8 +462,9 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 }
 
 // Threads and units for a row: held in up to 128 registers of a thread by as few threads as that
-// takes, with as many workgroups as the chip holds.  Loss and gradient, us: 4096 x 131072 bfloat16
-// 512 threads x 32 units 504 (4.25 TB/s), 1024 x 16 543, read twice 640; 4096 x 65536 fp32 465,
+// takes, with as many workgroups as the chip holds.  Loss and gradient, us (in part measured with
+// stores through the caches): 4096 x 131072 bfloat16 512 threads x 32 units 503, 1024 x 16 543, read
+// twice 640; 4096 x 65536 fp32 465,
 // read twice 502; 8192 x 50257 bfloat16 1024 x 8 424, 512 x 16 449; 8192 x 16000 256 x 8 141, 512 x 4
 // 177; 8192 x 2000 128 x 4 25, 512 x 2 34.  Longer rows are read twice, by 1024 threads (4096 x 80000
 // fp32 608; 512 757, 256 826).  Loss alone, bfloat16: workgroups side by side hide each other's
@@ -469,10 +483,14 @@ hipError_t ds_launch(DsParams p, hipStream_t s) {
   // gradients alone need nothing of the rest of the row: few rows are cut into parts of 4096 units,
   // up to DS_FILL workgroups in all (100 x 262144 bfloat16 27 us, whole 41)
   p.segments = WHAT == DS_GRAD ? (int)std::max<int64_t>(1, std::min((n + 4095) / 4096, DS_FILL / p.rows)) : 1;
+  // what no cache holds for the next pass is better kept out of them
+  const bool far = (size_t)p.rows * p.classes * sizeof(T) > DS_CACHED;
 #define SOAP_DS(NT, U, BLOCKS)                                                                                \
   if (U == 0 || n <= (int64_t)NT * U) {                                                                       \
     const dim3 grid((unsigned)(U ? std::min<int64_t>(p.rows, BLOCKS) : p.rows * p.segments));                 \
-    hipLaunchKernelGGL((distill_kernel<T, NT, U, WHAT>), grid, dim3(NT), lds, s, p);                          \
+    constexpr bool ONCE = U == 0 && WHAT != (DS_LOSS | DS_GRAD);                                              \
+    if (far && ONCE) hipLaunchKernelGGL((distill_kernel<T, NT, U, WHAT, ONCE>), grid, dim3(NT), lds, s, p);   \
+    else hipLaunchKernelGGL((distill_kernel<T, NT, U, WHAT, false>), grid, dim3(NT), lds, s, p);              \
     return hipGetLastError();                                                                                 \
   }
   if constexpr (WHAT == (DS_LOSS | DS_GRAD)) {
