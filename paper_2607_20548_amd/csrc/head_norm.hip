@@ -17,7 +17,7 @@
 // UNITS x VEC pairs (16 bytes of either half, or 32 bytes of neighbours), so that the
 // rotation stays within a lane, and the 64 / LANES groups of a wave take different heads of
 // one token, whose angles are formed once for all of them, or where a token has few heads a
-// token each.  16384 tokens of 16 + 16 heads of 128 bfloat16: 55 us forward (4.9 TB/s), 91 backward
+// token each.  16384 tokens of 16 + 16 heads of 128 bfloat16: 51 us forward (5.3 TB/s), 91 backward
 // (4.4 TB/s, with 5 for the second kernel).
 //
 // dw: every workgroup walks over tokens and writes the sums over its own, a second kernel adds
@@ -41,6 +41,10 @@ constexpr int64_t HN_BLOCKS_BWD = 512;
 // heads of 256 fp32: 1 wave a token 45.6 us forward and 75 backward, up to 1024 waves 21 and 38, 4096
 // 15.3 and 31, 16384 16.9 and 34).
 constexpr int64_t HN_FEW = 4096;
+// Bytes of heads from which their loads go past the caches, where a half is whole lines (16384 tokens of
+// 16 + 16 heads of 128 bfloat16: 56 and 51 us forward, 95 and 93 backward; 8192 of fp32 56 and 47, 83 and
+// 79; 3000 of bfloat16 13.5 and 14.5; halves of 64 bytes, 16384 of 64: 31.4 and 34.7).
+constexpr int64_t HN_CACHED = 60 << 20;
 constexpr int HN_FIN = 1024, HN_FIN_COLS = 32;
 
 struct HnSide {                          // queries or keys
@@ -63,10 +67,13 @@ struct HnParams {
 template <typename T>
 constexpr int hn_vec() { return 16 / (int)sizeof(T); }
 
-// n of VEC values from p on, zeros after them.
-template <typename T>
+// n of VEC values from p on, zeros after them.  FAR: past the caches.
+template <typename T, bool FAR>
 __device__ __forceinline__ v4u hn_load(const T *p, int n) {
-  if (n == hn_vec<T>()) return *reinterpret_cast<const v4u_any *>(p);
+  if (n == hn_vec<T>()) {
+    if constexpr (FAR) return __builtin_nontemporal_load(reinterpret_cast<const v4u_any *>(p));
+    else return *reinterpret_cast<const v4u_any *>(p);
+  }
   v4u q = v4u(0u);
 #pragma unroll
   for (int i = 0; i < hn_vec<T>(); ++i)
@@ -233,7 +240,7 @@ __device__ __forceinline__ void hn_angles(const HnParams &p, const HnUnit *un, i
 
 // Chunks of heads in turn: those of the queries, then those of the keys.  A wave's slots take
 // heads of one token, or (EACH) the same heads of a token each.
-template <typename T, int LANES, int UNITS, bool NEAR, bool EACH>
+template <typename T, int LANES, int UNITS, bool NEAR, bool EACH, bool FAR>
 struct HnHeads {
   static constexpr int SLOTS = 64 / LANES, IT = UNITS == 1 ? 2 : 1, STEP = EACH ? 1 : SLOTS, MANY = IT * STEP;
   v4u q[IT][UNITS][2];
@@ -243,16 +250,16 @@ struct HnHeads {
       const T *row = x + (int64_t)min(part * MANY + (EACH ? 0 : slot) + j * STEP, heads - 1) * stride;
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
-        q[j][u][0] = hn_load<T>(row + un[u].c0, un[u].n0);
-        q[j][u][1] = hn_load<T>(row + un[u].c1, un[u].n1);
+        q[j][u][0] = hn_load<T, FAR>(row + un[u].c0, un[u].n0);
+        q[j][u][1] = hn_load<T, FAR>(row + un[u].c1, un[u].n1);
       }
     }
   }
 };
 
-template <typename T, int LANES, int UNITS, bool NEAR, bool EACH>
+template <typename T, int LANES, int UNITS, bool NEAR, bool EACH, bool FAR>
 __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
-  using Heads = HnHeads<T, LANES, UNITS, NEAR, EACH>;
+  using Heads = HnHeads<T, LANES, UNITS, NEAR, EACH, FAR>;
   constexpr int VEC = hn_vec<T>(), IT = Heads::IT, STEP = Heads::STEP, MANY = Heads::MANY;
   constexpr int TOKENS = EACH ? Heads::SLOTS : 1;            // of a wave
   __shared__ float2 angle[HN_WAVES][LANES * UNITS * VEC];
@@ -316,9 +323,9 @@ __global__ __launch_bounds__(HN_THREADS) void head_norm_fwd(HnParams p) {
 }
 
 // out: dx (none if null); part: the sums of g h over the workgroup's tokens (none if null).
-template <typename T, int LANES, int UNITS, bool NEAR, bool EACH>
+template <typename T, int LANES, int UNITS, bool NEAR, bool EACH, bool FAR>
 __global__ __launch_bounds__(HN_THREADS) void head_norm_bwd(HnParams p) {
-  using Heads = HnHeads<T, LANES, UNITS, NEAR, EACH>;
+  using Heads = HnHeads<T, LANES, UNITS, NEAR, EACH, FAR>;
   constexpr int VEC = hn_vec<T>(), IT = Heads::IT, STEP = Heads::STEP, MANY = Heads::MANY;
   constexpr int TOKENS = EACH ? Heads::SLOTS : 1;            // of a wave
   __shared__ float red[HN_WAVES][LANES * UNITS * VEC * 4];
@@ -472,7 +479,7 @@ __global__ __launch_bounds__(HN_FIN) void head_norm_finish(const float *part, in
 
 struct HnShape {
   int lanes, units;
-  bool each;
+  bool each, far;
 };
 // Lanes of a head, and whether a wave's slots take a token each: where its steps are fewer by
 // a quarter, the heads of one token leaving slots idle (60000 tokens of 1 + 1 heads of 128 bfloat16:
@@ -480,9 +487,11 @@ struct HnShape {
 HnShape hn_shape(const HeadNormDesc &d) {
   const int64_t vec = d.bf16 ? 8 : 4, half = d.rotary / 2, rest = (d.dim - d.rotary) / 2;
   const int64_t n = (half + vec - 1) / vec + (rest + vec - 1) / vec;
-  HnShape r{n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2, false};
+  HnShape r{n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64, n <= 64 ? 1 : 2, false, false};
   const int64_t slots = 64 / r.lanes, it = r.units == 1 ? 2 : 1, q = d.side[0].heads, k = d.side[1].heads;
   auto steps = [&](int64_t each) { return (q + each - 1) / each + (k + each - 1) / each; };
+  const int64_t e = d.bf16 ? 2 : 4;
+  r.far = d.rotary == d.dim && d.dim / 2 * e % 128 == 0 && d.tokens * (q + k) * d.dim * e > HN_CACHED;
   r.each = slots > 1 && 5 * steps(it) * ((d.tokens + slots - 1) / slots) < 4 * steps(it * slots) * d.tokens;
   return r;
 }
@@ -510,16 +519,24 @@ HnParams hn_params(const HeadNormDesc &d, const HnShape &sh) {
 template <bool BWD, typename T, bool NEAR>
 hipError_t hn_launch(const HnParams &p, const HnShape &sh, hipStream_t s) {
   const int64_t blocks = BWD ? hn_blocks_bwd(p.tasks) : (p.tasks + HN_WAVES - 1) / HN_WAVES;
-#define SOAP_HN(L, U, E)                                                                                         \
+#define SOAP_HN_FAR(L, U, E, F)                                                                                  \
   if (sh.lanes == L && sh.units == U && sh.each == E) {                                                          \
-    if constexpr (BWD) hipLaunchKernelGGL((head_norm_bwd<T, L, U, NEAR, E>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
-    else hipLaunchKernelGGL((head_norm_fwd<T, L, U, NEAR, E>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
+    if constexpr (BWD) hipLaunchKernelGGL((head_norm_bwd<T, L, U, NEAR, E, F>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
+    else hipLaunchKernelGGL((head_norm_fwd<T, L, U, NEAR, E, F>), dim3((unsigned)blocks), dim3(HN_THREADS), 0, s, p); \
     return hipGetLastError();                                                                                    \
+  }
+#define SOAP_HN(L, U, E) SOAP_HN_FAR(L, U, E, false)
+  if constexpr (!NEAR) {
+    if (sh.far) {
+      SOAP_HN_FAR(8, 1, false, true) SOAP_HN_FAR(16, 1, false, true) SOAP_HN_FAR(32, 1, false, true)
+      if constexpr (sizeof(T) == 4) { SOAP_HN_FAR(64, 1, false, true) }
+    }
   }
   SOAP_HN(4, 1, false) SOAP_HN(8, 1, false) SOAP_HN(16, 1, false) SOAP_HN(32, 1, false) SOAP_HN(64, 1, false)
   SOAP_HN(4, 1, true) SOAP_HN(8, 1, true) SOAP_HN(16, 1, true) SOAP_HN(32, 1, true)
   if constexpr (sizeof(T) == 4) { SOAP_HN(64, 2, false) }
 #undef SOAP_HN
+#undef SOAP_HN_FAR
   return hipErrorInvalidValue;
 }
 

@@ -111,6 +111,17 @@ def test_sizes(tokens, hq, hk, dim, rot, dtype, near):
           (1e-2 * randn(seed + 5, tokens, hk, dim)).to(dtype) if hk else None)
 
 
+@pytest.mark.parametrize("tokens,hq,hk,dim,dtype", [
+    (4001, 22, 14, 128, torch.float32), (8001, 20, 13, 128, torch.bfloat16), (2001, 20, 13, 256, torch.float32),
+    (4001, 20, 13, 256, torch.bfloat16), (601, 40, 26, 512, torch.float32), (2001, 20, 13, 512, torch.bfloat16),
+    (8001, 20, 13, 64, torch.float32)])
+def test_more_than_caches_hold(tokens, hq, hk, dim, dtype):
+    """Sizes that are loaded past the caches."""
+    q, k, dq, dk = (0.1 + randn(i, tokens, h, dim).to(dtype) for i, h in ((1, hq), (2, hk), (3, hq), (4, hk)))
+    wq, wk = 1 + 0.2 * randn(5, dim), 1 + 0.2 * randn(6, dim)
+    check(q, k, wq, wk, None, frequencies(dim), False, dq, dk)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_views(dtype):
     """A fused row, rows at odd elements, heads in front of tokens, gradients that repeat."""
