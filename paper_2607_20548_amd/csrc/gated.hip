@@ -35,9 +35,12 @@ namespace soap {
 namespace {
 
 constexpr int GP_KB = 64;                        // k of a slab
+// Bytes of weights' gradients from which they are stored past the caches (bfloat16, 100 x 2048 x 8192:
+// 96.8 and 87.2 us, 777 x 1160 x 2744: 78.8 and 77.4, 1 x 512 x 1024: 24.0 and 27.7).
+constexpr int64_t GP_CACHED = 16 << 20;
 constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows in LDS
 
-enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART };
+enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART, GP_BF16_FAR, GP_F32_FAR };
 
 struct GpOther {               // product over the same k
   int M, N, tiles_m, tiles_n;
@@ -302,17 +305,26 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
             *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
             *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
           }
-        } else if constexpr (EPI == GP_F32 || EPI == GP_PART) {
-          float *o = EPI == GP_F32 ? static_cast<float *>(p.C[0]) + at
+        } else if constexpr (EPI == GP_F32 || EPI == GP_F32_FAR || EPI == GP_PART) {
+          float *o = EPI != GP_PART ? static_cast<float *>(p.C[0]) + at
                                    : static_cast<float *>(p.C[0]) +
                                          ((int64_t)blockIdx.y * (TWO ? 2 : 1) + second) * p.M * p.N + (int64_t)row * p.N + col;
-          *reinterpret_cast<float4 *>(o) = make_float4(x[0], x[1], x[2], x[3]);
-          *reinterpret_cast<float4 *>(o + 4) = make_float4(x[4], x[5], x[6], x[7]);
-        } else if constexpr (EPI == GP_BF16) {
+          v4f *to = reinterpret_cast<v4f *>(o);
+          const v4f lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
+          if constexpr (EPI == GP_F32_FAR) {
+            __builtin_nontemporal_store(lo, to);
+            __builtin_nontemporal_store(hi, to + 1);
+          } else {
+            to[0] = lo;
+            to[1] = hi;
+          }
+        } else if constexpr (EPI == GP_BF16 || EPI == GP_BF16_FAR) {
           v4u o;
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = gp_pack(x[2 * e], x[2 * e + 1]);
-          *reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[0]) + at) = o;
+          v4u *to = reinterpret_cast<v4u *>(static_cast<uint16_t *>(p.C[0]) + at);
+          if constexpr (EPI == GP_BF16_FAR) __builtin_nontemporal_store(o, to);
+          else *to = o;
         } else {
           v4u og, ou, oh;
 #pragma unroll
@@ -419,7 +431,7 @@ hipError_t gp_launch(GpParams p, float *part, hipStream_t s) {
   } else if constexpr (EPI == GP_DGATED) {
     j[0].kind = GatedJoin::DGATED;
     j[0].out2 = static_cast<uint16_t *>(p.C[1]); j[0].hidden = p.hidden; j[0].gate = p.gate; j[0].up = p.up;
-  } else if constexpr (EPI == GP_F32) {
+  } else if constexpr (EPI == GP_F32 || EPI == GP_F32_FAR) {
     j[0].kind = GatedJoin::F32;
     j[0].out_f32 = static_cast<float *>(p.C[0]);
   }
@@ -560,6 +572,8 @@ hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
   grad(d.m, d.n, d.x, d.x, d.ldx, dg, halves[1], d.n, d.dw_gate);
   grad(d.m, d.n, d.x, d.x, d.ldx, du, halves[3], d.n, d.dw_up);
   grad(d.n, d.p, hidden, halves[5], d.n, d.dy, d.dy, d.lddy, d.dw_down);
+  if ((d.grad_bf16 ? 2 : 4) * d.n * (2 * d.m + d.p) > GP_CACHED)
+    return d.grad_bf16 ? gp_launch<false, false, GP_BF16_FAR>(p, part, s) : gp_launch<false, false, GP_F32_FAR>(p, part, s);
   return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(p, part, s) : gp_launch<false, false, GP_F32>(p, part, s);
 }
 

@@ -21,6 +21,9 @@
 namespace soap {
 namespace {
 
+// Bytes of a product's weights from which they are loaded past the caches (16 x 4096 x 14336 forward 82.8 and
+// 79.1 us, 12 x 2048 x 8192 backward 89.2 and 82.1; 24 x 1000 x 3000 forward 23.4 and 31.3).
+constexpr int64_t GF_CACHED = 60 << 20;
 constexpr int GF_KB = 32, GF_COLS = 64;
 constexpr int GF_W = GF_KB * GF_COLS * 2, GF_X = 32 * GF_KB * 2;   // bytes of a slab's weights, of 32 tokens
 
@@ -28,7 +31,7 @@ struct GfParams {
   int T, N, K;                   // K: of a segment
   const uint16_t *X[4], *W[2];   // X by segment and half; W by segment, or gate's and up's
   int64_t ldx, ldw;
-  int segments, splits, chunks;
+  int segments, splits, chunks, far;
   float *part;                   // [split][matrix][T][N]
   GatedJoin out;                 // of a product in one part
 };
@@ -112,8 +115,9 @@ struct GfShape {
   static constexpr int LOADS = SLAB / 1024;
 };
 
-// FIN: what is made of the sums (GJ_PART: they are written as they are).
-template <bool WK, bool TWO, int NX, int RB, int FIN, int ACT>
+// FIN: what is made of the sums (GJ_PART: they are written as they are).  FAR: weights loaded past the
+// caches.
+template <bool WK, bool TWO, int NX, int RB, int FIN, int ACT, bool FAR>
 __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
   using S = GfShape<WK, TWO, NX, RB>;
   constexpr int M = S::M, RING = S::RING;
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(GP_THREADS, 1) void product_few(GfParams p) {
       const v4i r = w.buffer();
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        gp_load(r, to + t * GF_W + 1024 * i, (offw + (uint32_t)((WK ? 16 : 8) * i * ldw2)) | (WK ? dead : 0u));
+        gp_load<FAR>(r, to + t * GF_W + 1024 * i, (offw + (uint32_t)((WK ? 16 : 8) * i * ldw2)) | (WK ? dead : 0u));
     }
 #pragma unroll
     for (int t = 0; t < NX; ++t) {
@@ -289,8 +293,10 @@ hipError_t gj_launch(const GatedJoin &p, hipStream_t s) {
 template <bool WK, bool TWO, int NX, int FIN, int ACT = 0>
 hipError_t gf_launch(const GfParams &p, hipStream_t s) {
   const dim3 grid((unsigned)(p.chunks * p.splits)), block(GP_THREADS);
-  if (p.T <= 32) hipLaunchKernelGGL((product_few<WK, TWO, NX, 1, FIN, ACT>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((product_few<WK, TWO, NX, 2, FIN, ACT>), grid, block, 0, s, p);
+#define SOAP_FEW(RB, FAR) hipLaunchKernelGGL((product_few<WK, TWO, NX, RB, FIN, ACT, FAR>), grid, block, 0, s, p)
+  if (p.T <= 32) { if (p.far) SOAP_FEW(1, true); else SOAP_FEW(1, false); }
+  else { if (p.far) SOAP_FEW(2, true); else SOAP_FEW(2, false); }
+#undef SOAP_FEW
   return hipGetLastError();
 }
 
@@ -321,6 +327,7 @@ hipError_t launch_product_few(const FewDesc &d, const GatedJoin &out, hipStream_
   for (int i = 0; i < 4; ++i) p.X[i] = d.x[i];
   p.segments = d.segments; p.chunks = (p.N + GF_COLS - 1) / GF_COLS; p.part = d.part;
   p.splits = few_splits(d.n, (d.k + GF_KB - 1) / GF_KB * d.segments);
+  p.far = 2 * d.k * d.segments * d.n * (d.kind == FewDesc::GATE_UP ? 2 : 1) > GF_CACHED;
   p.out = out;
   p.out.T = d.tokens; p.out.N = d.n; p.out.part = d.part; p.out.splits = p.splits;
   const bool silu = out.act == SOAP_ACT_SILU;

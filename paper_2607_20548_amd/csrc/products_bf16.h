@@ -9,6 +9,7 @@
 namespace soap {
 namespace {
 
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -76,9 +77,15 @@ constexpr uint32_t GP_OUT = 0x80000000u;         // in an offset: past every buf
 // 16 bytes a lane from `offset` of a buffer to LDS at `lds` + 16 lane.  Written out because the
 // compiler holds every transposing read until all such loads have arrived; the kernel waits for
 // them itself, before the barrier in front of their slab's first read.  They write no register.
+// FAR: past the caches.
+template <bool FAR = false>
 __device__ __forceinline__ void gp_load(const v4i &buffer, uint32_t lds, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer)
-               : "m0");
+  if constexpr (FAR)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(offset), "s"(buffer)
+                 : "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer)
+                 : "m0");
 }
 
 // The eight k from 8 h on, h = lane / 32, of row lane % 32 of two half blocks: the transposing

@@ -104,7 +104,8 @@ def test_large(T, m, n, p):
 
 @pytest.mark.parametrize("T,m,n,p", [
     (7, 2048, 264, 136), (48, 4096, 136, 72), (64, 72, 8264, 40), (64, 2056, 136, 2600), (66, 136, 4104, 72), (130, 4096, 72, 264),
-    (321, 264, 264, 264), (1500, 72, 72, 80), (20000, 64, 40, 72), (200, 2056, 648, 1288), (3, 16, 65536, 24), (70, 24, 65536, 16)])
+    (321, 264, 264, 264), (1500, 72, 72, 80), (20000, 64, 40, 72), (200, 2056, 648, 1288), (3, 16, 65536, 24), (70, 24, 65536, 16),
+    (5, 2048, 8192, 1024), (40, 4096, 8192, 1032)])
 def test_parts_of_k(T, m, n, p):
     """Long sums of few tiles, cut into parts that are added afterwards, and short ones."""
     check(*make(T, m, n, p, T + n), dtype=BF if T % 2 else torch.float32)
