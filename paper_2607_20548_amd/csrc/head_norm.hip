@@ -17,8 +17,8 @@
 // UNITS x VEC pairs (16 bytes of either half, or 32 bytes of neighbours), so that the
 // rotation stays within a lane, and the 64 / LANES groups of a wave take different heads of
 // one token, whose angles are formed once for all of them, or where a token has few heads a
-// token each.  16384 tokens of 16 + 16 heads of 128 bfloat16: 51 us forward (5.3 TB/s), 91 backward
-// (4.4 TB/s, with 5 for the second kernel).
+// token each.  16384 tokens of 16 + 16 heads of 128 bfloat16: 50 us forward (5.4 TB/s), 89 backward
+// (4.5 TB/s, with 5 for the second kernel).
 //
 // dw: every workgroup walks over tokens and writes the sums over its own, a second kernel adds
 // these in a fixed order.
