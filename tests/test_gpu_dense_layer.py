@@ -179,3 +179,34 @@ def test_a_step_in_a_graph():
         torch.cuda.synchronize()
         for out in outs:
             assert all(torch.equal(a, b) for a, b in zip(want, out)), i
+
+
+def test_calls_at_once():
+    """The same objects used by two streams at the same time."""
+    randn = lambda seed, *s: torch.randn(s, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")  # noqa: E731
+    turn = soap.HeadNorm(64, 1 + 0.1 * randn(1, 64), 1 + 0.1 * randn(2, 64))
+    block = soap.GatedFeedForward(*((0.05 * randn(i, *s)).to(BF) for i, s in ((3, (512, 1000)), (4, (512, 1000)), (5, (1000, 2000)))))
+    distill = soap.Distillation(2.0, tail=True)
+
+    def run(seed, T):
+        q = randn(seed, T, 12, 64).to(BF)
+        tq, tk = turn.forward(q[:, :8], q[:, 8:])
+        dq = turn.backward(tq, tk, q[:, :8], q[:, 8:])
+        x = tq.reshape(T, 512)
+        z, gate, up = block.forward(x)
+        index = torch.arange(T * 7, device="cuda", dtype=torch.int32).view(T, 7) % 2000
+        loss, dz = distill.forward_backward(z, index, torch.full((T, 7), -3.0, device="cuda"))
+        return [tq, tk, *dq, z, loss, dz, *block.backward(dz, x, gate, up)]
+
+    sizes = (700, 60)
+    want = [run(10 + i, T) for i, T in enumerate(sizes)]
+    streams = [torch.cuda.Stream() for _ in sizes]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, T in enumerate(sizes):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(run(10 + i, T))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for out in got[i] for a, b in zip(out, want[i]))

@@ -165,6 +165,25 @@ def test_gradient_against_differences():
         assert abs((got.double() * v).sum() - want) <= 4 * H * size
 
 
+def test_offsets_past_32_bits():
+    """Rows of G, U, H and their gradients past 2^31 elements: the last ones, which alone have gradients,
+    as they are by themselves."""
+    T, m, n, p, last = 270000, 64, 8192, 72, 100
+    x, wg, wu, wd, dy = make(last, m, n, p, 12)
+    X, Y = torch.zeros(T, m, device="cuda", dtype=BF), torch.zeros(T, p, device="cuda", dtype=BF)
+    X[-last:], Y[-last:] = x, dy
+    block = soap.GatedFeedForward(wg, wu, wd)
+    y, gate, up = block.forward(X)
+    got = block.backward(Y, X, gate, up)
+    few, g, u = block.forward(x)
+    want = block.backward(dy, x, g, u)
+    assert not y[:-last].any() and not got[0][:-last].any()
+    # both within their bounds of the same sums: half steps of bfloat16 on either side of both
+    for a, b in zip((y[-last:], gate[-last:], up[-last:], got[0][-last:], *got[1:]), (few, g, u, *want)):
+        a, b = a.double(), b.double()
+        assert (a - b).norm() <= 4 * H * b.norm()
+
+
 def test_no_tokens():
     x, wg, wu, wd, dy = make(4, 64, 72, 80, 9)
     block = soap.GatedFeedForward(wg, wu, wd)

@@ -181,6 +181,34 @@ def test_gradient_against_differences(near):
         assert abs(got - want).item() <= (4 * h * h + 64 * U / h) * size
 
 
+def test_offsets_past_32_bits():
+    """Heads past 2^31 elements: the last tokens' as they are by themselves."""
+    T, heads, dim, last = 135000, 128, 128, 10
+    q = torch.ones(T, heads, dim, device="cuda", dtype=torch.bfloat16)
+    dq = torch.zeros_like(q)
+    q[-last:], dq[-last:] = randn(1, last, heads, dim), randn(2, last, heads, dim)
+    at = torch.arange(T, device="cuda", dtype=torch.int32)
+    norm = soap.HeadNorm(dim, 1 + 0.1 * randn(3, dim))
+    y, _ = norm.forward(q, None, at)
+    dx, _, dw, _ = norm.backward(dq, None, q, None, at)
+    args = q[-last:].contiguous(), None, at[-last:].contiguous()
+    want = norm.backward(dq[-last:].contiguous(), None, *args)
+    assert torch.equal(y[-last:], norm.forward(*args)[0]) and torch.equal(dx[-last:], want[0])
+    assert not dx[:-last].any() and (dw - want[2]).norm() <= 2.0 ** -18 * want[2].norm()
+
+
+def test_no_heads():
+    """A side of no heads beside one that has some, and two of none: weights' gradients of zeros."""
+    norm = soap.HeadNorm(32, torch.ones(32, device="cuda"), torch.ones(32, device="cuda"))
+    none, k = torch.empty(9, 0, 32, device="cuda"), randn(1, 9, 3, 32)
+    y, yk = norm.forward(none, k)
+    assert y.shape == none.shape and torch.equal(yk, norm.forward(None, k)[1])
+    dq, dk, dwq, dwk = norm.backward(none, k, none, k)
+    assert dq.shape == none.shape and not dwq.any() and torch.equal(dwk, norm.backward(None, k, None, k)[3])
+    _, _, dwq, dwk = norm.backward(none, none, none, none)
+    assert not dwq.any() and not dwk.any()
+
+
 def test_no_tokens():
     norm = soap.HeadNorm(32, torch.ones(32, device="cuda"), torch.ones(32, device="cuda"))
     q, k = torch.empty(0, 4, 32, device="cuda"), torch.empty(0, 2, 32, device="cuda")
