@@ -25,7 +25,10 @@ __device__ __forceinline__ uint16_t gp_round(float f) { return __builtin_bit_cas
 __device__ __forceinline__ float gp_float(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
 
 // The activation, and its derivative.  The hardware's exponential and reciprocal are within an
-// fp32 step each, far inside the rounding to bfloat16 that follows.
+// fp32 step each, far inside the rounding to bfloat16 that follows.  The normal distribution's
+// function is Hastings' rational approximation (Abramowitz and Stegun 7.1.26: erf within 1.5e-7),
+// whose exponential is the derivative's too (8192 x 2048 x 8192 forward 746 us, by erff 818; dG, dU and
+// H of 777 x 1160 x 2744 22.5 and 25.7).
 struct GpAct {
   float a, d;
 };
@@ -37,9 +40,12 @@ __device__ __forceinline__ GpAct gp_act(float x) {
     r.a = x * s;
     r.d = fmaf(r.a, 1.f - s, s);
   } else {
-    const float c = 0.5f + 0.5f * erff(x * 0.70710678118654752440f);
+    const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752440f, 1.f));
+    const float p = fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float q = 0.5f * t * p * e, c = x < 0.f ? q : 1.f - q;
     r.a = x * c;
-    r.d = fmaf(x * 0.39894228040143267794f, __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f), c);
+    r.d = fmaf(x * 0.39894228040143267794f, e, c);
   }
   return r;
 }
