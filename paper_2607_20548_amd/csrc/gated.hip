@@ -385,14 +385,15 @@ constexpr int64_t GP_PARTS = (int64_t)256 * 256 * 256 * 4;   // bytes of all par
 // wide, both tiles in 1 to 16 parts; within about 15 per cent): a slab of 128-tiles takes 0.62
 // where each has a compute unit of its own, 1.05 for two of them on one; of 256-tiles 1.1, and 1.5
 // with all compute units busy; starting and writing a tile 4.5 and 9; parts cost a launch for each
-// product and their bytes written and read.  Of up to four slabs the outputs are most of a tile's time,
-// which two 128-tiles on a compute unit cover for each other (gradients of 6 x 4096 x 14336 194 us, by
-// 256-tiles 223; of 200 x 4096 x 8192 172 and 179).
-GpPlan gp_plan(const GpParams &p, bool two) {
+// product and their bytes written and read.  Of up to `brief` slabs the outputs are most of a tile's
+// time, which two 128-tiles on a compute unit cover for each other (weights' gradients, four: 6 x 4096 x
+// 14336 194 us, by 256-tiles 223; 200 x 4096 x 8192 172 and 179; others, two: forward 2000 x 64 x 4096 33.5
+// and 35.8, but 4000 x 256 x 8192 132 and 119).
+GpPlan gp_plan(const GpParams &p, bool two, int brief) {
   const int64_t w = two ? 2 : 1, slabs = (int64_t)((p.K + GP_KB - 1) / GP_KB) * p.segments;
   GpPlan best{2, 1};
   double least = 1e300;
-  for (int nb = 2; nb <= (slabs <= 4 ? 2 : 4); nb += 2) {
+  for (int nb = 2; nb <= (slabs <= brief ? 2 : 4); nb += 2) {
     const int64_t tb = 64 * nb;
     int64_t tiles = (p.M + tb - 1) / tb * ((w * p.N + tb - 1) / tb), values = (int64_t)p.M * p.N * w;
     for (int i = 0; i < p.others; ++i) {
@@ -420,7 +421,7 @@ template <bool AK, bool BK, int EPI, int ACT = SOAP_ACT_SILU>
 hipError_t gp_launch(GpParams p, float *part, hipStream_t s) {
   if (p.M <= 0 || p.N <= 0) return hipSuccess;
   constexpr bool TWO = EPI == GP_GATED;
-  const GpPlan plan = gp_plan(p, TWO);
+  const GpPlan plan = gp_plan(p, TWO, !AK && !BK ? 4 : 2);
   p.splits = plan.splits;
   if (plan.splits == 1)
     return plan.nb == 4 ? gp_tiles<AK, BK, EPI, 4, ACT, TWO>(p, s) : gp_tiles<AK, BK, EPI, 2, ACT, TWO>(p, s);
