@@ -20,8 +20,8 @@
 // What bounds it, 8192 x 2048 x 8192: matrix instructions where sums are long (dX 410 us, 1340 TFLOP/s,
 // busy 0.79 of the cycles; the weights' gradients 625, 1320), and where an activation is behind
 // them, the outputs that all compute units write at the same time (H, G and U 490 to 540; dG, dU and
-// H from G and U 360, of which 246 without their bytes).  The whole: 703 forward (1170 TFLOP/s),
-// 1380 backward (1195).
+// H from G and U 360, of which 246 without their bytes).  The whole: 703 to 711 forward (1165
+// TFLOP/s), 1380 to 1405 backward (1185).
 //
 // Operands past their ends read as zeros (buffer bounds; units past the end of k are sent
 // out of bounds), so that sizes need no multiple of a tile; m, n and p are multiples of 8
