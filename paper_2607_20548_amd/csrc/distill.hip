@@ -328,7 +328,9 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
     const DsSum whole = LOSS && tail ? ds_join(all, in, p.scale) : all;
     if constexpr (LOSS) lse = fmaf(ds_base(whole.m), inv, logf(whole.s));
     const DsList l = list;
-    const float rest = tail && lse_rest == -INFINITY ? 0.f : l.rest;
+    // no class above -inf outside the list; a sum, as logs pass fp32's range under small temperatures
+    const bool alone = tail && (LOSS ? all.s == 0.f : lse_rest == -INFINITY);
+    const float rest = alone ? 0.f : l.rest;
 
     if constexpr (LOSS) {
       if (leader) {
@@ -368,12 +370,12 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
       at_in = ds_base(whole.m);
       mul_in = weight / whole.s;
       at = tail ? ds_base(all.m) : at_in;
-      mul = !tail ? mul_in : lse_rest == -INFINITY ? 0.f : (weight * ds_exp2((at - at_in) * p.scale) * (all.s / whole.s) - rest) / all.s;
+      mul = !tail ? mul_in : alone ? 0.f : (weight * ds_exp2((at - at_in) * p.scale) * (all.s / whole.s) - rest) / all.s;
     } else {
       at_in = lse == -INFINITY ? 0.f : lse;
       mul_in = lse == -INFINITY ? NAN : weight;
       at = tail ? (lse_rest == -INFINITY ? 0.f : lse_rest) : at_in;
-      mul = !tail ? mul_in : lse_rest == -INFINITY ? 0.f : weight * ds_exp2((lse_rest - lse) * DS_LOG2E) - rest;
+      mul = !tail ? mul_in : alone ? 0.f : weight * ds_exp2((lse_rest - lse) * DS_LOG2E) - rest;
     }
     mul *= g;
     // of a logit: under a maximum of logits, or under a log of sums

@@ -194,6 +194,21 @@ def test_masked_logits(dtype, tail):
     assert d.forward(z, index, t)[0][3] == math.inf
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rest_of_lowest_logits(dtype):
+    """With a tail, logits at the type's lowest value and a temperature under which their log of sums
+    passes fp32's range: the classes outside the list still take the rest."""
+    z, index, t = make(3, 300, 6, dtype, 4, tail=True)
+    z[:] = torch.finfo(dtype).min
+    d = soap.Distillation(temperature=0.25, tail=True)
+    want, loss_bound, dz, bound, _ = reference(torch.zeros_like(z), index, t, 0.25, True)
+    loss, both = d.forward_backward(z, index, t)
+    within(loss, want, loss_bound, "loss of both")
+    within(d.forward(z, index, t)[0], want, loss_bound, "loss")
+    step = 2.0 ** -8 if dtype == torch.bfloat16 else 4 * U
+    within(both, dz, bound * (1 + step) + step * dz.abs(), "dlogits")
+
+
 def test_not_numbers():
     """NaN and +inf stay in their row; rows without a list, and of dloss 0, are zeros all the same."""
     z, index, t = make(6, 3000, 5, torch.float32, 6)
