@@ -534,13 +534,16 @@ int soap_gated_backward(int64_t tokens, int64_t m, int64_t n, int64_t p, int act
  * outside the list has a logit above -inf, r is taken as 0.  A class may be listed
  * more than once: its p add up in the gradient.  Cross entropy to labels is slots = 1.
  * stats (rows x 2 floats, may be NULL forward): log sum exp(z / tau), over all classes and
- * (SOAP_DISTILL_TAIL, otherwise 0) over those not listed, for soap_distill_backward:
+ * (SOAP_DISTILL_TAIL, otherwise 0) over those not listed, for soap_distill_backward; with
+ * SOAP_DISTILL_SUMS rows x 6: these two, then the largest logit m and sum exp((z - m) / tau) of
+ * either (0, 0 without a tail).  From the logs alone q has an error of up to 2^-24 of their size,
+ * and none is left of logs past fp32's range; from the sums it is the single pass':
  *   dlogits = dloss tau ((sum p + r) q - p)             at the listed classes, elsewhere
  *   dlogits = dloss tau ((sum p + r) q - r q / q_rest)
  * with dloss one float a row (NULL: ones); a row whose dloss is 0 gets zeros, whatever its
  * logits.  soap_distill_forward_backward gives both in one pass over the logits.  Sums are
  * fp32; a NaN or +inf among the logits makes its row NaN. */
-enum { SOAP_DISTILL_TAIL = 1u << 0 };
+enum { SOAP_DISTILL_TAIL = 1u << 0, SOAP_DISTILL_SUMS = 1u << 2 };
 #define SOAP_DISTILL_MAX_CLASSES (1 << 18)
 #define SOAP_DISTILL_MAX_SLOTS 512
 #define SOAP_DISTILL_MIN_TEMPERATURE 0.01

@@ -47,6 +47,7 @@ SOAP_ACT_GELU = 1
 SOAP_GATED_MAX_HIDDEN = 65536
 SOAP_GATED_MAX_LD = 1 << 21
 SOAP_DISTILL_TAIL = 1
+SOAP_DISTILL_SUMS = 4
 SOAP_DISTILL_MAX_CLASSES = 1 << 18
 SOAP_DISTILL_MAX_SLOTS = 512
 SOAP_DISTILL_MIN_TEMPERATURE = 0.01
@@ -1252,7 +1253,7 @@ class Distillation:
                              f"{SOAP_DISTILL_MAX_TEMPERATURE}], got {temperature}")
         self.temperature, self.flags = float(temperature), SOAP_DISTILL_TAIL if tail else 0
 
-    def _list(self, logits, index, teacher):
+    def _list(self, logits, index, teacher, flags=0):
         """The leading arguments of the three entry points, and the stream."""
         raw = _current_stream(logits, "logits")
         if logits.dim() != 2:
@@ -1271,26 +1272,29 @@ class Distillation:
             if t.get_device() != logits.get_device():
                 raise ValueError(f"{name} is on {t.device}, not on {logits.device}")
         return (rows, classes, slots, kind, logits.data_ptr(), _ld(logits), index.data_ptr(), _ld(index), t_kind,
-                teacher.data_ptr(), _ld(teacher), self.flags, self.temperature), raw
+                teacher.data_ptr(), _ld(teacher), self.flags | flags, self.temperature), raw
 
     def forward(self, logits, index, teacher, stream=None):
-        """(loss, stats): float32 [rows], and what backward takes, float32 [rows, 2] (log of the sums of
-        exponentials over all classes and, with `tail`, over those not listed)."""
+        """(loss, stats): float32 [rows], and what backward takes, float32 [rows, 6] (log of the sums of
+        exponentials over all classes and, with `tail`, over those not listed; then the largest logit
+        and the sum under it of either)."""
         if stream is not None:
             return _on(stream, (logits, index, teacher), self.forward, logits, index, teacher)
-        args, raw = self._list(logits, index, teacher)
+        args, raw = self._list(logits, index, teacher, SOAP_DISTILL_SUMS)
         f32 = _torch.float32
-        loss, stats = logits.new_empty(args[0], dtype=f32), logits.new_empty((args[0], 2), dtype=f32)
+        loss, stats = logits.new_empty(args[0], dtype=f32), logits.new_empty((args[0], 6), dtype=f32)
         _check(lib().soap_distill_forward(*args, loss.data_ptr(), stats.data_ptr(), raw))
         return loss, stats
 
     def backward(self, logits, index, teacher, stats, dloss=None, stream=None):
-        """dlogits, of the logits' type, from the gradient of the losses (float32 [rows], None: ones)."""
+        """dlogits, of the logits' type, from the gradient of the losses (float32 [rows], None: ones).
+        Of `stats` the two logs will do (float32 [rows, 2]), within 2^-24 of whose size q is then."""
         if stream is not None:
             return _on(stream, (logits, index, teacher, stats, dloss), self.backward, logits, index, teacher, stats,
                        dloss)
-        args, raw = self._list(logits, index, teacher)
-        _exactly(stats, "stats", _torch.float32, (args[0], 2), logits)
+        sums = isinstance(stats, _T().Tensor) and stats.shape[1:] != (2,)
+        args, raw = self._list(logits, index, teacher, SOAP_DISTILL_SUMS if sums else 0)
+        _exactly(stats, "stats", _torch.float32, (args[0], 6 if sums else 2), logits)
         if dloss is not None:
             _exactly(dloss, "dloss", _torch.float32, (args[0],), logits)
         out = logits.new_empty(logits.shape)

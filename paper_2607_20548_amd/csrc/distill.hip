@@ -16,7 +16,8 @@
 // 4.4 TB/s).  One workgroup takes a row.  A thread keeps a running maximum and the
 // sum of the exponentials under it, and the workgroup joins these once.  Logits are taken from
 // their maximum before anything else, so that neither a large one's digits nor a row of the
-// type's lowest values are lost.
+// type's lowest values are lost; a gradient by itself takes maxima and sums from the loss' pass
+// (from a caller's logs of the sums alone it has what fp32 leaves of them).
 //
 // The listed classes are marked in a bitmap in LDS (a bit for a class, shifted like the row, so
 // that a unit of 16 bytes has its own byte or half of one): a unit without one, nearly every
@@ -27,6 +28,7 @@
 #include "lanes.h"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace soap {
 namespace {
@@ -46,6 +48,7 @@ constexpr float DS_LOG2E = 1.44269504088896340736f;
 struct DsParams {
   int64_t rows, ld, ldt, ldi, ldd;
   int classes, slots, tail, t_bf16, segments;   // segments: workgroups of a row
+  int wide;                               // floats of stats a row: 6, with the sums, or 2
   float tau, scale;                       // scale: log2(e) / tau
   double inv;                             // 1 / tau
   const void *z, *t;
@@ -57,6 +60,7 @@ struct DsParams {
 };
 
 enum { DS_LOSS = 1, DS_GRAD = 2 };
+constexpr int DS_WIDE = 6;
 
 // 2^x for x at or below about 0; results below 2^-126 are zeros.
 __device__ __forceinline__ float ds_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -128,6 +132,12 @@ __device__ __forceinline__ DsSum ds_join_all(DsSum v, float scale, DsSum *red) {
 #pragma unroll
   for (int w = 1; w < NT / 64; ++w) v = ds_join(v, red[w], scale);
   return v;
+}
+// A sum from its log alone, under a logit near that log: what fp32 leaves of it.
+__device__ __forceinline__ DsSum ds_from_log(float lse, float tau, double inv) {
+  if (lse == -INFINITY) return {lse, 0.f};
+  const float m = fminf(fmaxf((float)((double)lse * tau), -FLT_MAX), FLT_MAX);
+  return {m, lse < INFINITY ? expf((float)fmin(fmax((double)lse - (double)m * inv, -60.0), 60.0)) : NAN};
 }
 // log s within 2^-30: s = m 2^k, log m = 2 artanh f = 2 f (1 + f^2 / 3 + f^4 / 5 ..), f = (m - 1) /
 // (m + 1) of at most 0.172, of which only the first term needs more than fp32.
@@ -262,7 +272,6 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 
     // ---- the student's sums: over all classes, or (tail) over those not listed and those listed
     DsSum all = {-INFINITY, 0.f}, in = {-INFINITY, 0.f};
-    float lse = 0.f, lse_rest = 0.f;      // log sum exp(z / tau), in units of 1
     if constexpr (LOSS) {
       auto add = [&](DsSum &a, const float *v) {
         float m = a.m;
@@ -316,20 +325,20 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
       }
       if (leader && !tail) find();
       all = ds_join_all<NT>(all, p.scale, red[0]);           // its barrier is the list's too
-      if (tail) {
-        in = ds_join_all<NT>(in, p.scale, red[1]);
-        lse_rest = fmaf(ds_base(all.m), inv, logf(all.s));   // -inf without a value
-      }
-    } else {
-      lse = p.stats_in[2 * row];
-      lse_rest = p.stats_in[2 * row + 1];
+      if (tail) in = ds_join_all<NT>(in, p.scale, red[1]);
     }
-    // the sums of all classes
-    const DsSum whole = LOSS && tail ? ds_join(all, in, p.scale) : all;
-    if constexpr (LOSS) lse = fmaf(ds_base(whole.m), inv, logf(whole.s));
+    // the sums of all classes, and with a tail those of the classes not listed
+    DsSum whole = all;
+    if constexpr (LOSS) {
+      if (tail) whole = ds_join(all, in, p.scale);
+    } else {
+      const float *st = p.stats_in + p.wide * row;
+      whole = p.wide == DS_WIDE ? DsSum{st[2], st[3]} : ds_from_log(st[0], p.tau, p.inv);
+      all = !tail ? whole : p.wide == DS_WIDE ? DsSum{st[4], st[5]} : ds_from_log(st[1], p.tau, p.inv);
+    }
     const DsList l = list;
     // no class above -inf outside the list; a sum, as logs pass fp32's range under small temperatures
-    const bool alone = tail && (LOSS ? all.s == 0.f : lse_rest == -INFINITY);
+    const bool alone = tail && all.s == 0.f;
     const float rest = alone ? 0.f : l.rest;
 
     if constexpr (LOSS) {
@@ -352,8 +361,15 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
           }
           p.loss[row] = (float)(p.tau * p.tau * part);
           if (p.stats) {
-            p.stats[2 * row] = lse;
-            p.stats[2 * row + 1] = tail ? lse_rest : 0.f;
+            float *st = p.stats + p.wide * row;
+            st[0] = fmaf(base, inv, logf(whole.s));          // log sum exp(z / tau), -inf without a value
+            st[1] = tail ? fmaf(ds_base(all.m), inv, logf(all.s)) : 0.f;
+            if (p.wide == DS_WIDE) {
+              st[2] = whole.m;
+              st[3] = whole.s;
+              st[4] = tail ? all.m : 0.f;
+              st[5] = tail ? all.s : 0.f;
+            }
           }
         }
       }
@@ -365,23 +381,10 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
     const float weight = l.weight + rest;
     // weight q = mul_in exp2(..) with at_in; weight q - rest q / q_rest = mul exp2(..) with at, one
     // exponential under the rest's own sum
-    float at, mul, at_in, mul_in;
-    if (LOSS) {
-      at_in = ds_base(whole.m);
-      mul_in = weight / whole.s;
-      at = tail ? ds_base(all.m) : at_in;
-      mul = !tail ? mul_in : alone ? 0.f : (weight * ds_exp2((at - at_in) * p.scale) * (all.s / whole.s) - rest) / all.s;
-    } else {
-      at_in = lse == -INFINITY ? 0.f : lse;
-      mul_in = lse == -INFINITY ? NAN : weight;
-      at = tail ? (lse_rest == -INFINITY ? 0.f : lse_rest) : at_in;
-      mul = !tail ? mul_in : alone ? 0.f : weight * ds_exp2((lse_rest - lse) * DS_LOG2E) - rest;
-    }
+    const float at_in = ds_base(whole.m), mul_in = weight / whole.s, at = tail ? ds_base(all.m) : at_in;
+    float mul = !tail ? mul_in : alone ? 0.f : (weight * ds_exp2((at - at_in) * p.scale) * (all.s / whole.s) - rest) / all.s;
     mul *= g;
-    // of a logit: under a maximum of logits, or under a log of sums
-    auto power = [&](float v, float under) {
-      return ds_exp2(LOSS ? (v - under) * p.scale : fmaf(v, inv, -under) * DS_LOG2E);
-    };
+    auto power = [&](float v, float under) { return ds_exp2((v - under) * p.scale); };
     T *dz = static_cast<T *>(p.dz) + row * p.ldd;
     auto put = [&](const v4u &q, int first) {    // of unit first + lane
       float v[VEC];
@@ -519,6 +522,7 @@ hipError_t ds_start(const DistillDesc &d, hipStream_t s) {
   DsParams p{};
   p.rows = d.rows; p.ld = d.ld; p.ldt = d.ldt; p.ldi = d.ldi; p.ldd = d.ldd;
   p.classes = (int)d.classes; p.slots = (int)d.slots; p.tail = d.tail; p.t_bf16 = d.teacher_bf16;
+  p.wide = d.sums ? DS_WIDE : 2;
   p.tau = d.tau; p.scale = DS_LOG2E / d.tau; p.inv = 1.0 / d.tau;
   p.z = d.logits; p.t = d.teacher; p.index = d.index; p.dloss = d.dloss;
   p.loss = d.loss; p.stats = d.stats; p.stats_in = d.stats; p.dz = d.dlogits;

@@ -323,7 +323,7 @@ constexpr int DISTILL_MAX_CLASSES = 1 << 18, DISTILL_MAX_SLOTS = 512;
 // alone: the gradient from stats.
 struct DistillDesc {
   int64_t rows = 0, classes = 0, slots = 0, ld = 0, ldi = 0, ldt = 0, ldd = 0;
-  bool bf16 = false, teacher_bf16 = false, tail = false;
+  bool bf16 = false, teacher_bf16 = false, tail = false, sums = false;   // sums: stats hold them
   float tau = 1.f;
   const void *logits = nullptr, *teacher = nullptr;
   const int *index = nullptr;

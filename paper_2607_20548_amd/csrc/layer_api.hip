@@ -197,12 +197,14 @@ int check_distill(int64_t rows, int64_t classes, int64_t slots, int dtype, int64
   SOAP_TRY(check_ld("ld", ld, classes));
   SOAP_TRY(check_ld("ldi", ldi, slots));
   SOAP_TRY(check_ld("ldt", ldt, slots));
-  if (flags & ~(uint32_t)SOAP_DISTILL_TAIL) return api_fail(SOAP_ERR_HPARAM, "unknown flag bits 0x%x", flags);
+  if (flags & ~(uint32_t)(SOAP_DISTILL_TAIL | SOAP_DISTILL_SUMS)) return api_fail(SOAP_ERR_HPARAM, "unknown flag bits 0x%x", flags);
   if (!(temperature >= SOAP_DISTILL_MIN_TEMPERATURE && temperature <= SOAP_DISTILL_MAX_TEMPERATURE))
     return api_fail(SOAP_ERR_HPARAM, "temperature = %g is outside [%g, %g]", (double)temperature,
                     SOAP_DISTILL_MIN_TEMPERATURE, SOAP_DISTILL_MAX_TEMPERATURE);
   return SOAP_OK;
 }
+
+size_t stats_bytes(int64_t rows, uint32_t flags) { return (flags & SOAP_DISTILL_SUMS ? 24 : 8) * (size_t)rows; }
 
 soap::DistillDesc distill_desc(int64_t rows, int64_t classes, int64_t slots, int dtype, const void *logits, int64_t ld,
                                const int32_t *index, int64_t ldi, int teacher_dtype, const void *teacher, int64_t ldt,
@@ -210,6 +212,7 @@ soap::DistillDesc distill_desc(int64_t rows, int64_t classes, int64_t slots, int
   soap::DistillDesc d;
   d.rows = rows; d.classes = classes; d.slots = slots; d.ld = ld; d.ldi = ldi; d.ldt = ldt;
   d.bf16 = dtype == SOAP_BF16; d.teacher_bf16 = teacher_dtype == SOAP_BF16; d.tail = flags & SOAP_DISTILL_TAIL;
+  d.sums = flags & SOAP_DISTILL_SUMS;
   d.tau = temperature; d.logits = logits; d.index = index; d.teacher = teacher;
   return d;
 }
@@ -642,7 +645,7 @@ int soap_distill_forward(int64_t rows, int64_t classes, int64_t slots, int dtype
                        {index, span(rows, slots, ldi, 4), "index", false, true, 4},
                        {teacher, span(rows, slots, ldt, t), "teacher", false, true, t},
                        {loss, 4 * (size_t)rows, "loss", true, true, 4},
-                       {stats, 8 * (size_t)rows, "stats", true, false, 4}}));
+                       {stats, stats_bytes(rows, flags), "stats", true, false, 4}}));
   soap::DistillDesc d = distill_desc(rows, classes, slots, dtype, logits, ld, index, ldi, teacher_dtype, teacher, ldt, flags, temperature);
   d.loss = loss; d.stats = stats;
   return done(soap::launch_distill(d, stream), "distillation");
@@ -658,7 +661,7 @@ int soap_distill_backward(int64_t rows, int64_t classes, int64_t slots, int dtyp
   SOAP_TRY(check_bufs({{logits, span(rows, classes, ld, e), "logits", false, true, e},
                        {index, span(rows, slots, ldi, 4), "index", false, true, 4},
                        {teacher, span(rows, slots, ldt, t), "teacher", false, true, t},
-                       {stats, 8 * (size_t)rows, "stats", false, true, 4},
+                       {stats, stats_bytes(rows, flags), "stats", false, true, 4},
                        {dloss, 4 * (size_t)rows, "dloss", false, false, 4},
                        {dlogits, span(rows, classes, ldd, e), "dlogits", true, true, e}}));
   soap::DistillDesc d = distill_desc(rows, classes, slots, dtype, logits, ld, index, ldi, teacher_dtype, teacher, ldt, flags, temperature);
@@ -679,7 +682,7 @@ int soap_distill_forward_backward(int64_t rows, int64_t classes, int64_t slots, 
                        {teacher, span(rows, slots, ldt, t), "teacher", false, true, t},
                        {dloss, 4 * (size_t)rows, "dloss", false, false, 4},
                        {loss, 4 * (size_t)rows, "loss", true, true, 4},
-                       {stats, 8 * (size_t)rows, "stats", true, false, 4},
+                       {stats, stats_bytes(rows, flags), "stats", true, false, 4},
                        {dlogits, span(rows, classes, ldd, e), "dlogits", true, true, e}}));
   soap::DistillDesc d = distill_desc(rows, classes, slots, dtype, logits, ld, index, ldi, teacher_dtype, teacher, ldt, flags, temperature);
   d.dloss = dloss; d.loss = loss; d.stats = stats; d.dlogits = dlogits; d.ldd = ldd;

@@ -210,6 +210,13 @@ def test_distill_outputs_refused(L, which, over, code):
     assert distill(L, which, **over) == code
 
 
+@pytest.mark.parametrize("which", ["forward", "forward_backward"])
+def test_distill_sums_take_six_floats(L, which):
+    """A row of stats: two floats, or six with the sums; the loss lies behind four rows of two."""
+    assert distill(L, which, stats=P(3), loss=P(3, 32), flags=soap.SOAP_DISTILL_SUMS) == soap.SOAP_ERR_ALIAS
+    assert distill(L, which, flags=8) == soap.SOAP_ERR_HPARAM
+
+
 def test_workspace_sizes(L):
     """Zero for sizes that are refused, and never less for a larger call."""
     assert soap.soap_head_norm_workspace_bytes(4, 1) == 0 and soap.soap_head_norm_workspace_bytes(-1, 64) == 0

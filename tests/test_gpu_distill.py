@@ -194,6 +194,53 @@ def test_masked_logits(dtype, tail):
     assert d.forward(z, index, t)[0][3] == math.inf
 
 
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype,tau", [(torch.float32, 1.0), (torch.float32, 0.05), (torch.bfloat16, 1.0), (torch.bfloat16, 3.0)])
+@pytest.mark.parametrize("rows,classes", [(6, 300), (520, 2500), (7, 70000)])
+def test_gradient_from_stats_of_large_logits(rows, classes, dtype, tau, tail):
+    """Rows whose log of the sums has no digits left of the sum: their gradient from forward's stats is as
+    near to the formula as the single pass', which sees the logits (equal ones at the type's lowest value and
+    elsewhere, and others at some distance from zero)."""
+    z, index, t = make(rows, classes, 6, dtype, 4, tail=tail)
+    z[0] = torch.finfo(dtype).min
+    z[1] = 40000.0
+    z[2] = (z[2].float() + 40000.0).to(dtype)
+    z[3] = (4096.0 * z[3].float() - 1e6).to(dtype)
+    z[4] = -1e30
+    d = soap.Distillation(temperature=tau, tail=tail)
+    dloss = 0.5 + torch.rand(rows, device="cuda")
+    loss, stats = d.forward(z, index, t)
+    moved = z.double() - z.double().amax(1, keepdim=True)
+    want, loss_bound, dz, bound, _ = reference(moved, index, t, tau, tail)
+    within(loss, want, loss_bound + 1e-30, "loss")
+    both = d.forward_backward(z, index, t, dloss)[1]
+    apart = d.backward(z, index, t, stats, dloss)
+    g = dloss.double()[:, None]
+    step = 2.0 ** -8 if dtype == torch.bfloat16 else 4 * U
+    for got, what in ((both, "dlogits of both"), (apart, "dlogits")):
+        within(got, g * dz, g.abs() * (bound * (1 + step) + step * dz.abs()) + 1e-36, what)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+def test_gradient_from_logs(tail):
+    """Stats of the two logs alone, as a caller's own forward pass has them."""
+    z, index, t = make(40, 1001, 9, torch.float32, 17, tail=tail)
+    d = soap.Distillation(temperature=0.7, tail=tail)
+    _, stats = d.forward(z, index, t)
+    *_, dz, _, far = reference(z, index, t, 0.7, tail)
+    listed = torch.zeros(z.shape, device="cuda", dtype=torch.int32).scatter_add_(1, index.long(), torch.ones_like(index)) > 0
+    logs = torch.logsumexp(z.double() / 0.7, 1), torch.logsumexp(z.double().masked_fill(listed, -math.inf) / 0.7, 1)
+    logs = torch.stack([logs[0], logs[1] if tail else torch.zeros_like(logs[1])], 1)
+    # a sum of C terms (as above), a log, and the logit added to it
+    assert ((stats[:, :2] - logs).abs() <= (1001 / 512 + 72 + 4 * logs.abs()) * U).all()
+    for given in (stats[:, :2].contiguous(), logs.float()):
+        within(d.backward(z, index, t, given), dz, far * (1 + 4 * U) + 4 * U * dz.abs(), "dlogits")
+    with pytest.raises(ValueError):
+        d.backward(z, index, t, stats[:, :3].contiguous())
+    with pytest.raises(ValueError):
+        d.backward(z, index, t, stats[:, :2])
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rest_of_lowest_logits(dtype):
     """With a tail, logits at the type's lowest value and a temperature under which their log of sums
