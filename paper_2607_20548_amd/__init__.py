@@ -1062,8 +1062,8 @@ class HeadNorm:
     values, or heads in front of tokens); weights float32 [dim] or None; positions int32 [tokens]
     or None (0, 1, ..).  The first `rotary` values of a head (default: all) are turned, pairs being
     its halves' values of one index or (interleaved) neighbours, by position * frequency:
-    frequencies float64 [rotary / 2], by default base ** (-2 i / rotary).  Results are contiguous
-    and have no autograd graph."""
+    frequencies float64 [rotary / 2], by default base ** (-2 i / rotary), for which the constructor
+    waits for the current stream.  Results are contiguous and have no autograd graph."""
 
     def __init__(self, dim: int, q_weight=None, k_weight=None, eps: float = 1e-6, rotary: Optional[int] = None,
                  base: float = 10000.0, frequencies=None, interleaved: bool = False):
@@ -1081,6 +1081,10 @@ class HeadNorm:
             given = [t for t in (q_weight, k_weight) if t is not None]
             i = T.arange(0, rotary, 2, dtype=T.float64, device=given[0].device if given else "cuda")
             frequencies = float(base) ** (-i / rotary)
+            # calls on other streams, which wait for nothing, find them complete; in a capture they
+            # are part of the graph
+            if not T.cuda.is_current_stream_capturing():
+                T.cuda.current_stream(i.device).synchronize()
         self.dim, self.rotary, self.eps, self.frequencies = dim, rotary, eps, frequencies
         self.q_weight, self.k_weight = q_weight, k_weight
         self.flags = SOAP_HEAD_INTERLEAVED if interleaved else 0

@@ -263,3 +263,40 @@ def test_stream_graph_and_bits():
         want = (*norm.forward(q, k, pos), *norm.backward(dq, dk, q, k, pos))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out)), i
+
+
+def test_built_on_another_stream():
+    """Default frequencies are there once the object is: built on a busy stream and used at once on another
+    that has waited for nothing, with inputs that were ready before."""
+    q, w = randn(1, 300, 4, 64), 1 + 0.1 * randn(2, 64)
+    want = soap.HeadNorm(64, w).forward(q)[0]
+    x = randn(3, 4096, 4096)
+    busy, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(3):
+        with torch.cuda.stream(busy):
+            for _ in range(20):
+                x = (x @ x) * 1e-3
+            # what the allocator may hand the frequencies holds other values
+            stale = torch.full((32,), 7.0 + i, dtype=torch.float64, device="cuda")
+            del stale
+            norm = soap.HeadNorm(64, w)
+        got = norm.forward(q, stream=other)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), i
+
+
+def test_built_in_a_graph():
+    """An object built while a graph is captured, its frequencies part of the graph."""
+    q, w = randn(1, 30, 4, 64), 1 + 0.1 * randn(2, 64)
+    soap.HeadNorm(64, w).forward(q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = soap.HeadNorm(64, w).forward(q)[0]
+    for i in range(3):
+        q.copy_(randn(5 + i, 30, 4, 64))
+        graph.replay()
+        want = soap.HeadNorm(64, w).forward(q)[0]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
