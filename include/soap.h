@@ -530,7 +530,7 @@ int soap_gated_backward(int64_t tokens, int64_t m, int64_t n, int64_t p, int act
  * r against q_rest, the sum of q over the classes not listed:
  *   loss = tau^2 (sum_j p_j (log p_j - log q(index_j)) + r (log r - log q_rest))
  * A slot whose index is outside [0, classes) is empty, whatever its t.  A list of empty
- * slots has loss 0 and gradient 0; a term with p_j = 0 (or r = 0) is 0.  Where no class
+ * slots, or (without a tail) whose t are all -inf, has loss 0 and gradient 0; a term with p_j = 0 (or r = 0) is 0.  Where no class
  * outside the list has a logit above -inf, r is taken as 0.  A class may be listed
  * more than once: its p add up in the gradient.  Cross entropy to labels is slots = 1.
  * stats (rows x 2 floats, may be NULL forward): log sum exp(z / tau), over all classes and

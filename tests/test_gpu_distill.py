@@ -166,6 +166,27 @@ def test_lists(tail):
     assert loss[0] == 0 and not dz[0].any()
 
 
+@pytest.mark.parametrize("t_dtype", [torch.float32, torch.bfloat16])
+def test_teacher_of_no_weight(t_dtype):
+    """A list whose teacher has no logit above -inf weighs nothing, as an empty one: loss and gradient are
+    zeros, in every call, and the other rows' as they are without it."""
+    z, index, t = make(6, 700, 70, torch.float32, 13, t_dtype=t_dtype)
+    clean = t.clone()
+    t[1] = -math.inf
+    t[3, :2], index[3, 2:] = -math.inf, -1
+    t[4, 5] = -math.inf
+    clean[4, 5] = -math.inf
+    d = soap.Distillation(2.0)
+    loss, stats = d.forward(z, index, t)
+    both, dz = d.forward_backward(z, index, t)
+    apart = d.backward(z, index, t, stats)
+    want, dwant = d.forward_backward(z, index, clean)
+    for r in (1, 3):
+        assert loss[r] == 0 and both[r] == 0 and not dz[r].any() and not apart[r].any()
+    for r in (0, 2, 4, 5):
+        assert torch.equal(loss[r], want[r]) and torch.equal(both[r], want[r]) and torch.equal(dz[r], dwant[r])
+
+
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_masked_logits(dtype, tail):
