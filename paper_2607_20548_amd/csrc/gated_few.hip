@@ -39,9 +39,22 @@ struct GfParams {
 // ------------------------------------------------- what is made of the sums
 enum { GJ_PART, GJ_GATED, GJ_DGATED, GJ_BF16, GJ_F32 };
 
-// What the rounding of two values leaves, rounded: the lower halves.
-__device__ __forceinline__ uint32_t gj_low(const float (&v)[2]) {
-  return gp_pack(v[0] - gp_float(gp_round(v[0])), v[1] - gp_float(gp_round(v[1])));
+// Two values' rounding, and what it leaves, rounded: the lower halves.  An infinity leaves nothing; a
+// finite value past bfloat16's largest is that and a remainder.
+struct GjHalves {
+  uint32_t high, low;
+};
+__device__ __forceinline__ GjHalves gj_halves(const float (&v)[2]) {
+  uint32_t h[2];
+  float l[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    h[w] = gp_round(v[w]);
+    const bool past = (h[w] & 0x7fffu) == 0x7f80u, inf = fabsf(v[w]) == INFINITY;
+    h[w] -= past && !inf;
+    l[w] = inf ? 0.f : v[w] - gp_float((uint16_t)h[w]);
+  }
+  return {h[0] | h[1] << 16, gp_pack(l[0], l[1])};
 }
 
 // Of eight columns of a row: x[0], and x[1] of up's.
@@ -67,7 +80,11 @@ __device__ __forceinline__ void gj_finish(const GatedJoin &p, const float (*x)[8
       og[e] = gp_pack(x[0][2 * e], x[0][2 * e + 1]);
       ou[e] = gp_pack(x[1][2 * e], x[1][2 * e + 1]);
       oh[e] = gp_pack(hv[0], hv[1]);
-      ol[e] = gj_low(hv);
+      if (p.low) {
+        const GjHalves r = gj_halves(hv);
+        oh[e] = r.high;
+        ol[e] = r.low;
+      }
     }
     *reinterpret_cast<v4u *>(p.out + at) = oh;
     if (p.low) *reinterpret_cast<v4u *>(p.low + at) = ol;
@@ -92,9 +109,15 @@ __device__ __forceinline__ void gj_finish(const GatedJoin &p, const float (*x)[8
       og[e] = gp_pack(a[0], a[1]);
       ou[e] = gp_pack(b[0], b[1]);
       oh[e] = gp_pack(o[0], o[1]);
-      lg[e] = gj_low(a);
-      lu[e] = gj_low(b);
-      lh[e] = gj_low(o);
+      if (p.low) {
+        const GjHalves ra = gj_halves(a), rb = gj_halves(b), ro = gj_halves(o);
+        og[e] = ra.high;
+        lg[e] = ra.low;
+        ou[e] = rb.high;
+        lu[e] = rb.low;
+        oh[e] = ro.high;
+        lh[e] = ro.low;
+      }
     }
     *reinterpret_cast<v4u *>(p.out + at) = og;
     *reinterpret_cast<v4u *>(p.out2 + at) = ou;

@@ -237,3 +237,44 @@ def test_stream_graph_and_bits(T):
         want = run()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out)), i
+
+
+@pytest.mark.parametrize("T", [1, 32, 64, 65, 200])
+def test_infinite_hidden_values(T):
+    """H, dG and dU past fp32's range are infinite, and so are the sums over them, whatever the number of
+    tokens; the other tokens' Y and dX stay as they are."""
+    m, n, p = 72, 136, 80
+    x, wg, wu, wd, dy = (t.abs() + 0.01 for t in make(T, m, n, p, 14))
+    block = soap.GatedFeedForward(wg, wu, wd)
+    y, gate, up = block.forward(x)
+    dx = block.backward(dy, x, gate, up)[0]
+    big, dbig = x.clone(), dy.clone()
+    big[0] *= 1e20
+    dbig[0] *= 1e22
+    y2, gate2, up2 = block.forward(big)
+    dx2, *dw = block.backward(dbig, big, gate2, up2)
+    inf = float("inf")
+    assert (y2[0] == inf).all() and (dx2[0] == inf).all() and all((w == inf).all() for w in dw)
+    assert torch.equal(y2[1:], y[1:]) and torch.equal(dx2[1:], dx[1:])
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_hidden_values_past_bfloat16(T):
+    """A finite H that would round to infinity in bfloat16 stays finite where two are kept."""
+    x, wg, wu = (torch.zeros(s, device="cuda", dtype=BF) for s in ((T, 8), (8, 8), (8, 8)))
+    x[0, 0], x[0, 1] = 2.0 ** 64, 2.0 ** 55
+    wg[0], wu[0], wu[1] = 0.5, 2, -1
+    block = soap.GatedFeedForward(wg, wu, 0.25 * torch.eye(8, device="cuda", dtype=BF))
+    y, gate, up = block.forward(x)
+    h = (2 - 2.0 ** -9) * 2.0 ** 127
+    within(y[0], torch.full((8,), 0.25 * h, device="cuda", dtype=torch.float64), 2.0 ** -16 * h, "y")
+    dy = torch.zeros(T, 8, device="cuda", dtype=BF)
+    dy[0] = 2.0 ** -10
+    gate[0], up[0] = 127 / 64 * 2.0 ** 63, 129 / 128 * 2.0 ** 64
+    # dU = dH act(G) and H = act(G) U, of the kept G and U
+    _, _, dwu, dwd = block.backward(dy, x, gate, up)
+    du, h = 2.0 ** -12 * 127 / 64 * 2.0 ** 63, 127 / 64 * 129 / 128 * 2.0 ** 127
+    want = torch.zeros(8, 8, device="cuda", dtype=torch.float64)
+    want[0], want[1] = 2.0 ** 64 * du, 2.0 ** 55 * du
+    within(dwu, want, 2.0 ** -16 * want, "dw_up")
+    within(dwd, torch.full((8, 8), h * 2.0 ** -10, device="cuda", dtype=torch.float64), 2.0 ** -16 * h * 2.0 ** -10, "dw_down")
