@@ -24,11 +24,13 @@ constexpr int GP_RSRC = 0x00020000;              // raw 32-bit data
 __device__ __forceinline__ uint16_t gp_round(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 __device__ __forceinline__ float gp_float(uint16_t h) { return __uint_as_float((uint32_t)h << 16); }
 
-// The activation, and its derivative.  The hardware's exponential and reciprocal are within an
-// fp32 step each, far inside the rounding to bfloat16 that follows.  The normal distribution's
-// function is Hastings' rational approximation (Abramowitz and Stegun 7.1.26: erf within 1.5e-7),
-// whose exponential is the derivative's too (8192 x 2048 x 8192 forward 746 us, by erff 818; dG, dU and
-// H of 777 x 1160 x 2744 22.5 and 25.7).
+// The activation, and its derivative, to their own size: within x^2 2^-24 (the exponential's argument,
+// rounded twice) and 1e-6 of it, less than the 2^-16 of the two bfloat16 that few tokens keep as far
+// as the results are normal numbers.  The hardware's exponential and reciprocal are within an fp32
+// step each.  The normal distribution's function is exp(-x^2 / 2) t P(t) below 0, t = 1 / (1 + 0.3 |x|),
+// P of degree 7 fitted to the least largest relative error there, 1.5e-7 for |x| to 14; the
+// exponential is the derivative's too (8192 x 2048 x 8192 forward 769 us; with Hastings' five terms, whose
+// relative error is 5e-4 at -4 and past bfloat16's rounding from -5.3 on, 763).
 struct GpAct {
   float a, d;
 };
@@ -41,9 +43,11 @@ __device__ __forceinline__ GpAct gp_act(float x) {
     r.d = fmaf(r.a, 1.f - s, s);
   } else {
     const float e = __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f);
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752440f, 1.f));
-    const float p = fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float q = 0.5f * t * p * e, c = x < 0.f ? q : 1.f - q;
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3f, 1.f));
+    float p = fmaf(t, 0.035674773156642914f, -0.1572030782699585f);
+    p = fmaf(t, fmaf(t, fmaf(t, p, 0.20635348558425903f), -0.053683631122112274f), 0.1285616159439087f);
+    p = fmaf(t, fmaf(t, fmaf(t, p, 0.09991349279880524f), 0.12075395882129669f), 0.11962930113077164f);
+    const float q = t * p * e, c = x < 0.f ? q : 1.f - q;
     r.a = x * c;
     r.d = fmaf(x * 0.39894228040143267794f, e, c);
   }

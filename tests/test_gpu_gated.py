@@ -278,3 +278,37 @@ def test_hidden_values_past_bfloat16(T):
     want[0], want[1] = 2.0 ** 64 * du, 2.0 ** 55 * du
     within(dwu, want, 2.0 ** -16 * want, "dw_up")
     within(dwd, torch.full((8, 8), h * 2.0 ** -10, device="cuda", dtype=torch.float64), 2.0 ** -16 * h * 2.0 ** -10, "dw_down")
+
+
+@pytest.mark.parametrize("T", [1, 64, 65, 300])
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_activations_relative(T, name):
+    """Gates of -12 to 12, one by one: act(G) and its derivative to their own size.  The function is within
+    (x^2 + 24) u of itself (its exponential's argument of up to x^2 / 2, or |x|, is rounded twice; the rest
+    are factors near 1 u each), the derivative's two terms within as much of theirs; H, dG and dU keep two
+    bfloat16, 2^-16 of themselves, of up to 64 tokens, and one, 2^-8, of more."""
+    n = 512
+    g = torch.linspace(-12, 12, n, dtype=torch.float64, device="cuda").to(BF)
+    wg, wu = torch.zeros(8, n, device="cuda", dtype=BF), torch.zeros(8, n, device="cuda", dtype=BF)
+    wg[0], wu[0] = g, 1
+    x, dy = torch.zeros(T, 8, device="cuda", dtype=BF), torch.zeros(T, n, device="cuda", dtype=BF)
+    x[0, 0], dy[0] = 1, 1
+    block = soap.GatedFeedForward(wg, wu, torch.eye(n, device="cuda", dtype=BF), activation=name)
+    y, gate, up = block.forward(x)
+    assert torch.equal(gate[0], g) and (up[0] == 1).all()
+    dx, dwg, dwu, dwd = block.backward(dy, x, gate, up)
+    v = g.double()
+    a, d = act(v, name)
+    if name == "gelu":
+        a = 0.5 * v * torch.special.erfc(-v * 0.5 ** 0.5)
+        terms = (a / v).abs() + v.abs() * torch.exp(-0.5 * v * v) * 0.3989422804014327
+        d = a / v + v * torch.exp(-0.5 * v * v) * 0.3989422804014327
+    else:
+        s = torch.sigmoid(v)
+        terms = s + (a * (1 - s)).abs()
+    keep = 2.0 ** -16 if T <= 64 else H
+    rel = (v * v + 24) * U
+    within(y[0], a, (rel + keep) * a.abs(), "y")
+    within(dwd[:, 0], a, (rel + keep) * a.abs(), "dw_down")
+    within(dwu[0], a, (rel + keep) * a.abs(), "dw_up")
+    within(dwg[0], d, rel * terms + keep * (d.abs() + rel * terms), "dw_gate")
