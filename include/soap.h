@@ -461,11 +461,13 @@ int soap_mx4_gemm_k(int64_t groups, int64_t M, int64_t N, int64_t K, const int32
  *   (a cos t - b sin t, b cos t + a sin t),  t = position frequencies[i] of pair i,
  * pair i being the values i and i + rotary / 2, or 2 i and 2 i + 1 with
  * SOAP_HEAD_INTERLEAVED.  q_heads queries and k_heads keys a token (0 .. SOAP_HEAD_MAX_HEADS;
- * a side without heads is not touched); strides of tokens and heads are in elements, those of
- * a head 1, so that q and k may lie in one fused row and heads in front of tokens.  Weights
+ * a side without heads is not touched); strides of tokens and heads are in elements (below
+ * 2^31), those of a head 1, so that q and k may lie in one fused row and heads in front of tokens.  Weights
  * hold dim floats (NULL: ones), positions one int32 a token (NULL: 0, 1, ..), frequencies
- * rotary / 2 doubles; the angle is formed in fp64.  Inputs may repeat (stride 0); an output's
- * heads may not lie over each other, but between those of the other side.
+ * rotary / 2 doubles; the angle is formed in fp64.  Inputs may repeat (stride 0).  An output's
+ * heads lie behind each other within a token and tokens behind each other, or tokens within a head;
+ * they may lie between those of the other side: in rows of the same stride, the heads next to each
+ * other or (of the same stride too) in turn with them.
  * A head whose sum of squares passes fp32's range becomes zeros (NaN if it holds an infinity
  * or a NaN).
  * The backward pass takes the gradients of the outputs and the inputs again and gives, with

@@ -3,6 +3,7 @@
 // Everything is enqueued on the caller's stream; nothing here allocates.
 #include "soap.h"
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 
@@ -136,8 +137,21 @@ int check_strides(const char *name, int64_t tokens, int64_t heads, int64_t dim, 
   return SOAP_OK;
 }
 
-// Two sides whose tokens' rows may lie between each other's, as queries and keys of a fused row
-// do, but not over each other.
+// Whether a head of one side meets one of the other, heads being `width` bytes, d + v s + u step
+// apart with v in [first, last] and u in (-tokens, tokens).
+bool heads_meet(int64_t d, int64_t s, int64_t first, int64_t last, int64_t step, int64_t tokens, int64_t width) {
+  for (int64_t v = first; v <= last; ++v) {
+    const int64_t x = d + v * s, u = step ? -x / step : 0;   // the nearest u are this one and its neighbours
+    for (int64_t i = u - 1; i <= u + 1; ++i) {
+      const int64_t at = x + std::min(std::max(i, 1 - tokens), tokens - 1) * step;
+      if (at < width && -at < width) return true;
+    }
+  }
+  return false;
+}
+
+// Two sides whose heads may lie between each other's (as queries and keys of a fused row do, or of
+// rows in which they take turns), but not over each other.
 int check_sides(const char *an, const void *a, int64_t ah, int64_t at, int64_t ahead, const char *bn, const void *b,
                 int64_t bh, int64_t bt, int64_t bhead, int64_t tokens, int64_t dim, size_t e) {
   const int64_t as = (int64_t)head_span(tokens, ah, dim, at, ahead, e), bs = (int64_t)head_span(tokens, bh, dim, bt, bhead, e);
@@ -149,6 +163,10 @@ int check_sides(const char *an, const void *a, int64_t ah, int64_t at, int64_t a
     const int64_t ra = (int64_t)e * ((ah - 1) * ahead + dim), rb = (int64_t)e * ((bh - 1) * bhead + dim);
     const int64_t r = (d % step + step) % step;
     if (r >= ra && r + rb <= step) return SOAP_OK;
+  }
+  if ((at == bt || tokens == 1) && (ahead == bhead || ah == 1 || bh == 1)) {
+    const int64_t s = (int64_t)e * (ah == 1 ? bhead : ahead);
+    if (!heads_meet(d, s, 1 - ah, bh - 1, tokens == 1 ? 0 : step, tokens, (int64_t)e * dim)) return SOAP_OK;
   }
   return api_fail(SOAP_ERR_ALIAS, "%s overlaps %s", bn, an);
 }

@@ -1,6 +1,8 @@
 """Argument checks of the dense layer's entry points (no GPU): every refusal comes before
 anything is enqueued, with its documented status and a message; only fake pointers are passed, and
 only to calls that must fail.  The classes refuse host tensors and wrong shapes themselves."""
+import random
+
 import pytest
 import torch
 
@@ -95,6 +97,63 @@ def head_bwd(L, **o):
 ])
 def test_head_norm_backward_refuses(L, over, code):
     assert head_bwd(L, **over) == code
+
+
+def interleaved(at, ahead, bt, bhead, at_b, tokens=8, qh=4, kh=2):
+    """Strides for dq and dk in one buffer, dk `at_b` floats behind it."""
+    return dict(tokens=tokens, q_heads=qh, k_heads=kh, dq=P(8), dq_token=at, dq_head=ahead, dk=P(8, 4 * at_b),
+                dk_token=bt, dk_head=bhead, q_token=qh * 32, dq_out_token=qh * 32, k_token=kh * 32, dk_out_token=kh * 32)
+
+
+@pytest.mark.parametrize("over,code", [
+    # heads of both in turn in a token's row, and in heads in front of tokens
+    (interleaved(256, 64, 256, 64, 32), soap.SOAP_ERR_WORKSPACE),
+    (interleaved(256, 64, 256, 64, 32 + 2 * 64), soap.SOAP_ERR_WORKSPACE),
+    (interleaved(64, 512, 64, 512, 32), soap.SOAP_ERR_WORKSPACE),
+    (interleaved(32, 512, 32, 512, 256), soap.SOAP_ERR_WORKSPACE),
+    # one head between the other side's
+    (interleaved(256, 64, 256, 7, 32, kh=1), soap.SOAP_ERR_WORKSPACE),
+    (interleaved(256, 9, 256, 64, 32, qh=1), soap.SOAP_ERR_WORKSPACE),
+    # one token: its strides say nothing
+    (interleaved(256, 64, 99, 64, 32, tokens=1), soap.SOAP_ERR_WORKSPACE),
+    # a value over another's
+    (interleaved(256, 64, 256, 64, 31), soap.SOAP_ERR_ALIAS),
+    (interleaved(256, 64, 256, 64, 33), soap.SOAP_ERR_ALIAS),
+    (interleaved(64, 512, 64, 512, 33), soap.SOAP_ERR_ALIAS),
+    (interleaved(32, 512, 32, 512, 255), soap.SOAP_ERR_ALIAS),
+    (interleaved(32, 512, 32, 512, 257), soap.SOAP_ERR_ALIAS),
+    (interleaved(256, 64, 256, 7, 33, kh=1), soap.SOAP_ERR_ALIAS),
+    # in turn in the first token, not in the next ones
+    (interleaved(256, 64, 288, 64, 32), soap.SOAP_ERR_ALIAS),
+    # the last head of a token on the next token's first
+    (interleaved(256, 64, 256, 64, 32 + 192), soap.SOAP_ERR_WORKSPACE),
+    (interleaved(224, 64, 224, 64, 32 + 192), soap.SOAP_ERR_ALIAS),
+    (interleaved(256, 64, 256, 64, 32 + 193), soap.SOAP_ERR_ALIAS),
+])
+def test_heads_in_turn(L, over, code):
+    """Outputs between those of the other side are taken, as far as the workspace, which is too small."""
+    assert head_bwd(L, wsb=15, **over) == code
+
+
+def test_heads_in_turn_against_all_pairs(L):
+    """Layouts of equal strides at random against every pair of heads."""
+    rng, seen = random.Random(5), set()
+    for _ in range(3000):
+        tokens, qh, kh = rng.randint(1, 4), rng.randint(1, 3), rng.randint(1, 3)
+        head, token = rng.choice([(16, 16 * rng.randint(4, 9)), (16 * rng.randint(1, 3), 128), (16 * rng.randint(4, 12), 16 * rng.randint(1, 4))])
+        d = rng.choice([rng.randint(0, 700), 8 * rng.randint(0, 80)])
+        a = dict(interleaved(token, head, token, head, d, tokens, qh, kh), dim=8, rotary=8, q_head=8, k_head=8,
+                 dq_out_head=8, dk_out_head=8)
+        rows = lambda h, o: [o + i * token + j * head for i in range(tokens) for j in range(h)]  # noqa: E731
+        q, k = rows(qh, 0), rows(kh, d)
+        apart = lambda u, v: all(abs(x - y) >= 8 for x in u for y in v)  # noqa: E731
+        # a side's own heads: of a token, or tokens of a head, one behind the other
+        nested = lambda h: token >= (h - 1) * head + 8 or tokens == 1 or head >= (tokens - 1) * token + 8 or h == 1  # noqa: E731
+        if nested(qh) and nested(kh):
+            code = head_bwd(L, wsb=15, **a)
+            assert code == (soap.SOAP_ERR_WORKSPACE if apart(q, k) else soap.SOAP_ERR_ALIAS), (a, apart(q, k))
+            seen.add(code)
+    assert len(seen) == 2
 
 
 def gated_fwd(L, **o):

@@ -300,3 +300,25 @@ def test_built_in_a_graph():
         want = soap.HeadNorm(64, w).forward(q)[0]
         torch.cuda.synchronize()
         assert torch.equal(out, want), i
+
+
+def test_heads_in_turn():
+    """The C entry points with inputs and outputs of rows in which heads of queries and keys take turns,
+    and of one key's between the queries'."""
+    T, h, dim = 37, 3, 24
+    f = frequencies(dim)
+    norm = soap.HeadNorm(dim, frequencies=f, eps=EPS)
+    row, dy = randn(1, T, h, 3, dim), randn(2, T, h, 3, dim)
+    t, s = 3 * h * dim, 3 * dim
+    want = norm.forward(row[:, :, 0], row[:, :, 1])
+    dwant = norm.backward(dy[:, :, 0], dy[:, :, 1], row[:, :, 0], row[:, :, 1])
+    for kh in (h, 1):
+        out, dout = torch.full_like(row, 7.0), torch.full_like(row, 7.0)
+        soap.soap_head_norm_forward(T, h, kh, dim, dim, soap.SOAP_F32, 0, row, t, s, row[:, :, 1], t, s, None, None, EPS, None,
+                                    f, out, t, s, out[:, :, 1], t, s)
+        soap.soap_head_norm_backward(T, h, kh, dim, dim, soap.SOAP_F32, 0, dy, t, s, dy[:, :, 1], t, s, row, t, s,
+                                     row[:, :, 1], t, s, None, None, EPS, None, f, dout, t, s, dout[:, :, 1], t, s, None, None,
+                                     None, 0)
+        for o, w in ((out, want), (dout, dwant)):
+            assert torch.equal(o[:, :, 0], w[0]) and torch.equal(o[:, :kh, 1], w[1][:, :kh])
+            assert (o[:, kh:, 1] == 7).all() and (o[:, :, 2] == 7).all()
