@@ -340,6 +340,37 @@ def test_rows_past_32_bits():
     assert (loss[:-1] == loss[0]).all() and torch.equal(dz[0], dz[-2]) and torch.equal(dz[12345], dz[0])
 
 
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("rows,classes,dtype", [
+    (27000, 1000, torch.float32), (27000, 2000, torch.bfloat16), (9000, 3000, torch.float32), (9000, 6000, torch.bfloat16),
+    (1100, 24000, torch.float32), (1100, 48000, torch.bfloat16), (600, 50001, torch.float32), (600, 100001, torch.bfloat16),
+    (300, 100001, torch.float32), (300, 200001, torch.bfloat16), (520, 33000, torch.float32), (520, 66000, torch.bfloat16)])
+def test_loss_and_gradient_apart(rows, classes, dtype, tail):
+    """Loss and gradient by themselves of more than the caches hold, for each number of threads, and many
+    rows of the most threads."""
+    check(*make(rows, classes, 9, dtype, classes, tail=tail), tail=tail)
+
+
+def test_apart_past_32_bits():
+    """Loss and gradient by themselves of rows past 2^31 elements, with and without a tail: the last rows as they
+    are alone, to the rounding of their sums in another number of threads."""
+    rows, classes, last = 20000, 131072, 3
+    z = torch.zeros(rows, classes, device="cuda", dtype=torch.bfloat16)
+    z[-last:] = randn(1, last, classes)
+    index = torch.full((rows, 2), 5, device="cuda", dtype=torch.int32)
+    index[:, 1] = 77
+    t = torch.full((rows, 2), -2.0, device="cuda")
+    for tail in (False, True):
+        d = soap.Distillation(tail=tail)
+        loss, stats = d.forward(z, index, t)
+        dz = d.backward(z, index, t, stats)
+        want, bound, g, near, _ = reference(z[-last:], index[-last:], t[-last:], 1.0, tail)
+        within(loss[-last:], want, bound, "loss")
+        within(dz[-last:], g, near + 2.0 ** -8 * (g.abs() + near) + 1e-36, "dlogits")
+        assert (loss[:-last] == loss[0]).all() and torch.equal(dz[0], dz[-last - 1]) and torch.equal(dz[16384], dz[0])
+        del dz
+
+
 def test_most_rows():
     """As many rows as a call takes, in each of the three: the last ones as they are alone."""
     rows, last = 1 << 24, 1000

@@ -312,3 +312,25 @@ def test_activations_relative(T, name):
     within(dwd[:, 0], a, (rel + keep) * a.abs(), "dw_down")
     within(dwu[0], a, (rel + keep) * a.abs(), "dw_up")
     within(dwg[0], d, rel * terms + keep * (d.abs() + rel * terms), "dw_gate")
+
+
+@pytest.mark.parametrize("T", [16, 40])
+@pytest.mark.parametrize("m,n,p,name", [
+    (64, 8192, 4096, "silu"), (64, 4096, 8264, "gelu"), (2048, 8264, 64, "silu"), (2048, 8264, 64, "gelu"),
+    (64, 8264, 4096, "silu"), (64, 8264, 4096, "gelu"), (8264, 2048, 64, "silu")])
+def test_weights_past_the_caches(T, m, n, p, name):
+    """Few tokens with weights that are loaded past the caches, in every product, with and without parts
+    of k."""
+    check(*make(T, m, n, p, 15), name, BF)
+
+
+@pytest.mark.parametrize("T,m,n,p,name,dtype", [
+    (8, 64, 512, 2048, "gelu", BF), (77, 176, 8, 928, "gelu", torch.float32), (400, 1000, 2768, 1000, "silu", BF),
+    (400, 136, 13200, 8, "silu", torch.float32), (275, 328, 11608, 80, "silu", BF), (4491, 8, 8816, 152, "silu", BF),
+    (16427, 8, 80, 16, "gelu", BF), (18712, 136, 224, 16, "gelu", BF), (11019, 8, 1112, 8, "silu", BF),
+    (7081, 1344, 8, 32, "silu", BF), (17785, 32, 2280, 152, "silu", torch.float32), (17077, 2656, 72, 56, "silu", BF),
+    (16563, 8, 152, 16, "gelu", BF), (15566, 8, 568, 144, "gelu", torch.float32)])
+def test_plans(T, m, n, p, name, dtype):
+    """Tiles of either size, in parts and whole, more and fewer than compute units, of every product and
+    activation, with gradients stored through the caches and past them."""
+    check(*make(T, m, n, p, 16), name, dtype)

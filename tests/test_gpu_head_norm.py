@@ -111,6 +111,16 @@ def test_sizes(tokens, hq, hk, dim, rot, dtype, near):
           (1e-2 * randn(seed + 5, tokens, hk, dim)).to(dtype) if hk else None)
 
 
+@pytest.mark.parametrize("near", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens,hq,hk,dim", [
+    (50, 32, 32, 64), (50, 32, 32, 32), (50, 16, 16, 64), (20, 4, 4, 256), (20, 8, 8, 256), (30, 2, 2, 512)])
+def test_heads_side_by_side(tokens, hq, hk, dim, dtype, near):
+    """Heads that fill a wave's slots, and tokens that do, for each number of lanes."""
+    q, k, dq, dk = (0.1 + randn(i, tokens, h, dim).to(dtype) for i, h in ((1, hq), (2, hk), (3, hq), (4, hk)))
+    check(q, k, 1 + 0.2 * randn(5, dim), 1 + 0.2 * randn(6, dim), None, frequencies(dim), near, dq, dk)
+
+
 @pytest.mark.parametrize("tokens,hq,hk,dim,dtype", [
     (4001, 22, 14, 128, torch.float32), (8001, 20, 13, 128, torch.bfloat16), (2001, 20, 13, 256, torch.float32),
     (4001, 20, 13, 256, torch.bfloat16), (601, 40, 26, 512, torch.float32), (2001, 20, 13, 512, torch.bfloat16),
@@ -120,6 +130,12 @@ def test_more_than_caches_hold(tokens, hq, hk, dim, dtype):
     q, k, dq, dk = (0.1 + randn(i, tokens, h, dim).to(dtype) for i, h in ((1, hq), (2, hk), (3, hq), (4, hk)))
     wq, wk = 1 + 0.2 * randn(5, dim), 1 + 0.2 * randn(6, dim)
     check(q, k, wq, wk, None, frequencies(dim), False, dq, dk)
+
+
+def test_more_than_caches_hold_of_short_heads():
+    """The smallest halves of whole lines: 32 values of fp32."""
+    q, k, dq, dk = (0.1 + randn(i, 8001, 16, 64) for i in range(1, 5))
+    check(q, k, 1 + 0.2 * randn(5, 64), 1 + 0.2 * randn(6, 64), None, frequencies(64), False, dq, dk)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
