@@ -38,6 +38,7 @@ constexpr int GP_KB = 64;                        // k of a slab
 // Bytes of weights' gradients from which they are stored past the caches (bfloat16, 100 x 2048 x 8192:
 // 96.8 and 87.2 us, 777 x 1160 x 2744: 78.8 and 77.4, 1 x 512 x 1024: 24.0 and 27.7).
 constexpr int64_t GP_CACHED = 16 << 20;
+static_assert(GP_CACHED >= 4 * 256 * 128 * 128, "more than 256 tiles of 128 past the caches");
 constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows in LDS
 
 enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART, GP_BF16_FAR, GP_F32_FAR };
@@ -370,9 +371,13 @@ hipError_t gp_tiles(GpParams p, hipStream_t s) {
   const dim3 grid((unsigned)tiles, (unsigned)p.splits), block(GP_THREADS);
   // tiles that have a compute unit of their own may fill its LDS: more slabs on their way (128 x 4096
   // x 14336 forward 126 -> 101 us, 300 x 4096 x 8192 gradients 260 -> 237; two on one take 80 KB each)
-  if (NB == 2 && tiles * p.splits <= 256)
-    hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, NB == 2 ? 9 : 5>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 5>), grid, block, 0, s, p);
+  if constexpr (NB == 2 && EPI != GP_BF16_FAR && EPI != GP_F32_FAR) {   // these have more tiles
+    if (tiles * p.splits <= 256) {
+      hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 9>), grid, block, 0, s, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 5>), grid, block, 0, s, p);
   return hipGetLastError();
 }
 
