@@ -35,13 +35,15 @@ namespace soap {
 namespace {
 
 constexpr int GP_KB = 64;                        // k of a slab
-// Bytes of weights' gradients from which they are stored past the caches (bfloat16, 100 x 2048 x 8192:
-// 96.8 and 87.2 us, 777 x 1160 x 2744: 78.8 and 77.4, 1 x 512 x 1024: 24.0 and 27.7).
+// Bytes of weights' gradients from which they are stored past the caches, if they are bfloat16 (100 x 2048 x 8192:
+// 96.8 and 87.2 us, 777 x 1160 x 2744: 78.8 and 77.4, 1 x 512 x 1024: 24.0 and 27.7).  Not fp32, of which
+// a lane stores 16 bytes of every 32 at a time: past the caches 12 x 2048 x 8192 151 us, through them 93; 300 x
+// 4096 x 8192 473 and 260, 8192 x 2048 x 8192 1476 and 1433.
 constexpr int64_t GP_CACHED = 16 << 20;
-static_assert(GP_CACHED >= 4 * 256 * 128 * 128, "more than 256 tiles of 128 past the caches");
+static_assert(GP_CACHED >= 2 * 256 * 128 * 128, "more than 256 tiles of 128 past the caches");
 constexpr int GP_BLOCK = 64 * 128;               // bytes of a block of 64 rows in LDS
 
-enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART, GP_BF16_FAR, GP_F32_FAR };
+enum { GP_BF16, GP_F32, GP_GATED, GP_DGATED, GP_PART, GP_BF16_FAR };
 
 struct GpOther {               // product over the same k
   int M, N, tiles_m, tiles_n;
@@ -306,19 +308,13 @@ __global__ __launch_bounds__(GP_THREADS, NB == 4 || RING > 5 ? 1 : 2) void produ
             *reinterpret_cast<v4u *>(p.keep_gate + at) = og;
             *reinterpret_cast<v4u *>(p.keep_up + at) = ou;
           }
-        } else if constexpr (EPI == GP_F32 || EPI == GP_F32_FAR || EPI == GP_PART) {
+        } else if constexpr (EPI == GP_F32 || EPI == GP_PART) {
           float *o = EPI != GP_PART ? static_cast<float *>(p.C[0]) + at
                                    : static_cast<float *>(p.C[0]) +
                                          ((int64_t)blockIdx.y * (TWO ? 2 : 1) + second) * p.M * p.N + (int64_t)row * p.N + col;
           v4f *to = reinterpret_cast<v4f *>(o);
-          const v4f lo = {x[0], x[1], x[2], x[3]}, hi = {x[4], x[5], x[6], x[7]};
-          if constexpr (EPI == GP_F32_FAR) {
-            __builtin_nontemporal_store(lo, to);
-            __builtin_nontemporal_store(hi, to + 1);
-          } else {
-            to[0] = lo;
-            to[1] = hi;
-          }
+          to[0] = v4f{x[0], x[1], x[2], x[3]};
+          to[1] = v4f{x[4], x[5], x[6], x[7]};
         } else if constexpr (EPI == GP_BF16 || EPI == GP_BF16_FAR) {
           v4u o;
 #pragma unroll
@@ -371,7 +367,7 @@ hipError_t gp_tiles(GpParams p, hipStream_t s) {
   const dim3 grid((unsigned)tiles, (unsigned)p.splits), block(GP_THREADS);
   // tiles that have a compute unit of their own may fill its LDS: more slabs on their way (128 x 4096
   // x 14336 forward 126 -> 101 us, 300 x 4096 x 8192 gradients 260 -> 237; two on one take 80 KB each)
-  if constexpr (NB == 2 && EPI != GP_BF16_FAR && EPI != GP_F32_FAR) {   // these have more tiles
+  if constexpr (NB == 2 && EPI != GP_BF16_FAR) {   // these have more tiles
     if (tiles * p.splits <= 256) {
       hipLaunchKernelGGL((product_tiles<AK, BK, EPI, NB, ACT, TWO, 9>), grid, block, 0, s, p);
       return hipGetLastError();
@@ -439,7 +435,7 @@ hipError_t gp_launch(GpParams p, float *part, hipStream_t s) {
   } else if constexpr (EPI == GP_DGATED) {
     j[0].kind = GatedJoin::DGATED;
     j[0].out2 = static_cast<uint16_t *>(p.C[1]); j[0].hidden = p.hidden; j[0].gate = p.gate; j[0].up = p.up;
-  } else if constexpr (EPI == GP_F32 || EPI == GP_F32_FAR) {
+  } else if constexpr (EPI == GP_F32) {
     j[0].kind = GatedJoin::F32;
     j[0].out_f32 = static_cast<float *>(p.C[0]);
   }
@@ -580,9 +576,9 @@ hipError_t launch_gated_bwd(const GatedDesc &d, hipStream_t s) {
   grad(d.m, d.n, d.x, d.x, d.ldx, dg, halves[1], d.n, d.dw_gate);
   grad(d.m, d.n, d.x, d.x, d.ldx, du, halves[3], d.n, d.dw_up);
   grad(d.n, d.p, hidden, halves[5], d.n, d.dy, d.dy, d.lddy, d.dw_down);
-  if ((d.grad_bf16 ? 2 : 4) * d.n * (2 * d.m + d.p) > GP_CACHED)
-    return d.grad_bf16 ? gp_launch<false, false, GP_BF16_FAR>(p, part, s) : gp_launch<false, false, GP_F32_FAR>(p, part, s);
-  return d.grad_bf16 ? gp_launch<false, false, GP_BF16>(p, part, s) : gp_launch<false, false, GP_F32>(p, part, s);
+  if (!d.grad_bf16) return gp_launch<false, false, GP_F32>(p, part, s);
+  return 2 * d.n * (2 * d.m + d.p) > GP_CACHED ? gp_launch<false, false, GP_BF16_FAR>(p, part, s)
+                                               : gp_launch<false, false, GP_BF16>(p, part, s);
 }
 
 }  // namespace soap
