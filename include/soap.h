@@ -545,7 +545,9 @@ int soap_gated_backward(int64_t tokens, int64_t m, int64_t n, int64_t p, int act
  *   dlogits = dloss tau ((sum p + r) q - r q / q_rest)
  * with dloss one float a row (NULL: ones); a row whose dloss is 0 gets zeros, whatever its
  * logits.  soap_distill_forward_backward gives both in one pass over the logits.  Sums are
- * fp32; a NaN or +inf among the logits makes its row NaN. */
+ * fp32; a NaN or +inf among the logits makes its row NaN.  Logits that are all -inf have no q: their
+ * loss and gradient are NaN (with a tail the gradient at the listed classes, elsewhere 0), but for
+ * the zeros of empty lists and of a dloss of 0. */
 enum { SOAP_DISTILL_TAIL = 1u << 0, SOAP_DISTILL_SUMS = 1u << 2 };
 #define SOAP_DISTILL_MAX_CLASSES (1 << 18)
 #define SOAP_DISTILL_MAX_SLOTS 512

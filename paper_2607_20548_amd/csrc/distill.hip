@@ -254,7 +254,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
       }
       sum = ds_total(sum);
       l.twice = __ballot(twice) != 0;
-      l.logs = tail ? 0.f : logf((float)sum);
+      l.logs = tail || sum == 0.0 ? 0.f : logf((float)sum);   // p of 0 where there is nothing to divide
       // a list without a class weighs nothing, nor does one whose teacher has all of its at -inf
       l.any = tail ? __ballot(some) != 0 : sum != 0.0;
       l.rest = !tail || !l.any ? 0.f : (float)(sum == sum ? fmax(0.0, 1.0 - sum) : sum);
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
         const double logw = ds_log(whole.s);
 #pragma unroll 1
         for (int j = tid; j < p.slots; j += 64) {
-          if (cls[j] < 0 || !l.any) continue;
+          if (cls[j] < 0) continue;
           const float logp = ps[j] - l.logs, w = expf(logp);
           if (w != 0.f) part += (double)w * ((double)logp - ((double)zs[j] - base) * p.inv + logw);
         }

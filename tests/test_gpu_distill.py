@@ -298,6 +298,30 @@ def test_not_numbers():
 
 
 @pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_no_logit(dtype, tail):
+    """Rows whose logits are all -inf: NaN, but zeros for an empty list and a dloss of 0; the other rows'
+    bits are as without them."""
+    z, index, t = make(6, 999, 5, dtype, 19, tail=tail)
+    clean, dloss = z.clone(), torch.ones(6, device="cuda")
+    z[[1, 3, 4]] = -math.inf
+    index[3] = -1
+    dloss[4] = 0
+    d = soap.Distillation(tail=tail)
+    loss, dz = d.forward_backward(z, index, t, dloss)
+    alone, stats = d.forward(z, index, t)
+    want, dwant = d.forward_backward(clean, index, t, dloss)
+    assert loss[1].isnan() and loss[4].isnan() and loss[3] == 0 and torch.equal(loss.nan_to_num(9), alone.nan_to_num(9))
+    for g in (dz, d.backward(z, index, t, stats, dloss)):
+        listed = torch.zeros(999, dtype=torch.bool, device="cuda")
+        listed[index[1].long()] = True
+        assert g[1, listed].isnan().all() and (not g[1, ~listed].any() if tail else g[1].isnan().all())
+        assert not g[3].any() and not g[4].any()
+    for r in (0, 2, 5):
+        assert torch.equal(loss[r], want[r]) and torch.equal(dz[r], dwant[r])
+
+
+@pytest.mark.parametrize("tail", [False, True])
 def test_gradient_against_differences(tail):
     """<gradient, v> against the kernel's own losses half a step on either side: h^2 of the third
     derivative (below 8 h^2 tau^-1 for |v| <= 1) and the losses' rounding over h."""
