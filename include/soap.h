@@ -506,11 +506,12 @@ int soap_head_norm_backward(int64_t tokens, int64_t q_heads, int64_t k_heads, in
  * The backward pass gives, from dY, X and the kept G and U (H is computed again),
  *   dH = dY Wd^T,  dG = dH U act'(G),  dU = dH act(G)
  *   dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY
- * (each NULL where it is not wanted): dG, dU and H are rounded to bfloat16 as operands, dX too,
- * the weights' gradients are fp32 (what the steps read) or bfloat16 (grad_dtype).  Up to 64 tokens'
- * H, dG and dU keep 16 binary digits, in two bfloat16 (where the matrix that they meet holds an
- * infinity, their product with it may be NaN).  Without tokens the gradients are zeros.  The workspace's
- * size never shrinks as tokens, m, n or p grow. */
+ * (each NULL where it is not wanted): dG, dU and H are rounded to bfloat16 as operands (so that a
+ * bfloat16 result's error is sqrt 2 times that of its own rounding, Y's too), dX too, the weights'
+ * gradients are fp32 (what the steps read) or bfloat16 (grad_dtype).  Up to 64 tokens' H, dG and dU
+ * keep 16 binary digits, in two bfloat16 (where the matrix that they meet holds an infinity, their
+ * product with it may be NaN).  Without tokens the gradients are zeros.  The workspace's size never
+ * shrinks as tokens, m, n or p grow. */
 typedef enum { SOAP_ACT_SILU = 0, SOAP_ACT_GELU = 1 } soap_activation;
 #define SOAP_GATED_MAX_HIDDEN 65536
 #define SOAP_GATED_MAX_LD (1 << 21)

@@ -11,9 +11,9 @@
 // logit above -inf, r counts as 0.
 //
 // Bound by HBM: a row is read once, and once more where a gradient is written from a row that the
-// registers did not hold (both in one pass over 4096 x 131072 bfloat16 487 us, 4.4 TB/s; the
-// loss alone 179 us, 6.0 TB/s; the gradient alone of 999 x 50001 fp32, rows at every alignment, 91 us,
-// 4.4 TB/s).  One workgroup takes a row.  A thread keeps a running maximum and the
+// registers did not hold (both in one pass over 4096 x 131072 bfloat16 488 us, 4.4 TB/s; the
+// loss alone 168 us, 6.4 TB/s; the gradient alone of 999 x 50001 fp32, rows at every alignment, 89 us,
+// 4.5 TB/s).  One workgroup takes a row.  A thread keeps a running maximum and the
 // sum of the exponentials under it, and the workgroup joins these once.  Logits are taken from
 // their maximum before anything else, so that neither a large one's digits nor a row of the
 // type's lowest values are lost; a gradient by itself takes maxima and sums from the loss' pass
@@ -39,9 +39,11 @@ typedef uint32_t v4u_any __attribute__((ext_vector_type(4), aligned(2)));   // 1
 constexpr int64_t DS_FILL = 512;          // workgroups that fill the chip
 // Bytes of logits from which a call that reads them once loads past the caches (4096 x 131072 bfloat16
 // loss 202 us, past them 179; gradient of 4096 x 32000 120 and 112, of 1000 x 50257 54.0 and 54.7, of
-// 600 x 32000 18.7 and 22.1).  Gradients are always stored so (that of 4096 x 32000 before 131; loss
-// and gradient of 4096 x 131072 503 and 487, of 300 x 131072 73 and 61; of rows read twice, 4096 x 80000
-// fp32, 609 and 623: they are not).
+// 600 x 32000 18.7 and 22.1).  Gradients are always stored so (loss
+// and gradient of 4096 x 131072 through the caches 487, past them 480, of 300 x 131072 73 and 61; gradient alone of
+// 4096 x 131072 410 and 380, of 4096 x 40000 fp32 264 and 237, but of 200 MB and less, which the last cache
+// may hold, 999 x 50001 fp32 70 and 86, 4096 x 32000 90 and 99; of rows read twice, 4096 x 80000 fp32, 609 and
+// 623: they are not).
 constexpr size_t DS_CACHED = 100 << 20;
 constexpr float DS_LOG2E = 1.44269504088896340736f;
 
@@ -473,7 +475,8 @@ __global__ __launch_bounds__(NT) void distill_kernel(DsParams p) {
 // twice 640; 4096 x 65536 fp32 465,
 // read twice 502; 8192 x 50257 bfloat16 1024 x 8 424, 512 x 16 449; 8192 x 16000 256 x 8 141, 512 x 4
 // 177; 8192 x 2000 128 x 4 25, 512 x 2 34.  Longer rows are read twice, by 1024 threads (4096 x 80000
-// fp32 608; 512 757, 256 826).  Loss alone, bfloat16: workgroups side by side hide each other's
+// fp32 608; 512 757, 256 826).  32 units of 512 threads are as many as fit: 233 registers in bfloat16, in fp32
+// all 256 with 6 spilled (28 bytes a lane), and in both about 70 scalar ones kept in lanes of others.  Loss alone, bfloat16: workgroups side by side hide each other's
 // joins, few rows need their threads (4096 x 2000: 128 threads 10.9, 256 13.0, 1024 47; 4096 x 32000:
 // 256 53, 1024 75; 600 x 131072: 38 and 41; 64 x 131072: 22 and 14).  The gradient alone: 4096 x
 // 2000: 128 14.2, 256 16.2; 4096 x 8000: 128 41, 256 37, 512 44, 1024 75; 600 x 32000: 20, 18.5 and 24; 2048 x 131072: 249, 228 and 220;

@@ -6,7 +6,11 @@
 //
 // X is tokens x m, Wg and Wu m x n, Wd n x p.  H, dG and dU are rounded to bfloat16 once, as
 // the operands of the next product (of up to 64 tokens to two bfloat16, whose products are added);
-// act works on fp32 sums forward and on the kept (rounded) G and U backward.
+// act works on fp32 sums forward and on the kept (rounded) G and U backward.  That one rounding makes the
+// error of Y, dX and the weights' gradients sqrt 2 times that of their own rounding.  Two bfloat16 for more
+// tokens too would take it away, and double the matrix instructions behind them: 8192 x 2048 x 8192 forward 694
+// us and 884, backward 1349 and 2324, before the lower halves' own bytes; 300 x 4096 x 8192 93 and 117, 192 and
+// 288.  Up to 64 tokens the weights' loads hide them.
 //
 // Products of up to 64 tokens are product_few's; all others are one kernel's, product_tiles: C =
 // sum over k of A(x, k) B(y, k), its operands in memory either k-contiguous ([x][k]: X, H, dY,
@@ -17,11 +21,11 @@
 // k-contiguous blocks are read 16 bytes of a row at a time, x-contiguous ones by the transposing
 // reads, which give a lane four k of its own x.
 //
-// What bounds it, 8192 x 2048 x 8192: matrix instructions where sums are long (dX 410 us, 1340 TFLOP/s,
-// busy 0.79 of the cycles; the weights' gradients 625, 1320), and where an activation is behind
-// them, the outputs that all compute units write at the same time (H, G and U 490 to 540; dG, dU and
-// H from G and U 360, of which 246 without their bytes).  The whole: 703 to 711 forward (1165
-// TFLOP/s), 1380 to 1405 backward (1185).
+// What bounds it, 8192 x 2048 x 8192: matrix instructions where sums are long (dX 405 us, 1355 TFLOP/s,
+// busy 0.79 of the cycles; the weights' gradients 614, 1340), and where an activation is behind
+// them, the outputs that all compute units write at the same time (H, G and U 498; dG, dU and
+// H from G and U 368, of which 246 without their bytes).  The whole: 702 to 715 forward (1165
+// TFLOP/s), 1379 to 1400 backward (1185), with fp32 gradients of weights 1430.
 //
 // Operands past their ends read as zeros (buffer bounds; units past the end of k are sent
 // out of bounds), so that sizes need no multiple of a tile; m, n and p are multiples of 8

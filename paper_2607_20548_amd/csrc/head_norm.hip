@@ -18,7 +18,10 @@
 // rotation stays within a lane, and the 64 / LANES groups of a wave take different heads of
 // one token, whose angles are formed once for all of them, or where a token has few heads a
 // token each.  16384 tokens of 16 + 16 heads of 128 bfloat16: 50 us forward (5.4 TB/s), 89 backward
-// (4.5 TB/s, with 5 for the second kernel).
+// (4.5 TB/s, with 5 for the second kernel).  Away from such heads lanes idle (halves of 72 take 16
+// lanes of 9: 81 and 154, floor 58 and 87) or units are partial and go value by value (rotary 36 of 128: 150
+// and 321).  Backward, sums for both sides, a head and its gradient take 209 to 241 registers in bfloat16 (two
+// waves a SIMD; fp32 132 to 197, three or two), and 14 to 54 scalar ones are kept in lanes of others.
 //
 // dw: every workgroup walks over tokens and writes the sums over its own, a second kernel adds
 // these in a fixed order.
