@@ -1063,7 +1063,8 @@ class HeadNorm:
     or None (0, 1, ..).  The first `rotary` values of a head (default: all) are turned, pairs being
     its halves' values of one index or (interleaved) neighbours, by position * frequency:
     frequencies float64 [rotary / 2], by default base ** (-2 i / rotary), for which the constructor
-    waits for the current stream.  Results are contiguous and have no autograd graph."""
+    waits for the current stream (in a capture they are written by the graph's replays).  Results are
+    contiguous and have no autograd graph."""
 
     def __init__(self, dim: int, q_weight=None, k_weight=None, eps: float = 1e-6, rotary: Optional[int] = None,
                  base: float = 10000.0, frequencies=None, interleaved: bool = False):
